@@ -477,7 +477,8 @@ int8t_variant int8t_conv_selected_variant(int8t_op op, const int8t_conv_desc *de
  *            "absmax_batch_kernel", "quantize_batch_kernel", "quantize_act_kernel", "quantize_planar_kernel", "quantize_wgt_kernel",
  *            "deviation_finish_kernel", "igemm_kernel", "igemm_dma_kernel", "igemm_fused_kernel", "igemm_reduce_kernel",
  *            "band_kernel", "band_reg_kernel", "wgrad_kernel", "wgrad_lines_kernel", "wgrad_reduce_kernel", "s2d_repack_kernel",
- *            "conv_trio_kernel", "dw_conv_kernel" (every depthwise forward / backward-data variant),
+ *            "conv_trio_kernel", "quantize_rows_kernel", "quantize_cols_kernel" (both passes), "transpose_codes_kernel", "product_kernel",
+ *            "product_reduce_kernel", "cache_write_kernel", "cache_read_kernel", "attend_kernel", "attend_join_kernel", "dw_conv_kernel" (every depthwise forward / backward-data variant),
  *            "dw_wgrad_kernel" (every depthwise backward-weight variant), "dw_wgrad_reduce_kernel", "dw_trio_kernel", "infer_1x1_kernel");
  *            "conv_trio_kernel" and "dw_trio_kernel" are all the launches that several passes share: strided layers' and the one that
  *            quantizes depthwise tensors too;
@@ -516,6 +517,137 @@ int8t_status int8t_profile_mfma_ceiling(int random_operands, int lds_reads, int 
 
 /* Eq.7 on the host: max(exp(-alpha * d_c), beta).  The paper uses alpha = 20, beta = 0.1. */
 double int8t_dclr_scale(double d_c, double alpha, double beta);
+
+/*
+ * ---- Tokens: scales per token and output channel, a paged cache, attention over it ---------------------------------------
+ * The quantizer of Eq.1 / Eq.3 with c the maximum of a ROW (a token, an output channel) or a COLUMN in place of the tensor's: for the
+ * linear layers and the attention of transformers, whose tokens differ in size.  Floating tensors are of an int8t_dtype; a result is
+ * formed in fp32 and rounded once.  `pitch` arguments are in elements; rows themselves are contiguous.  Any alignment of an element is
+ * served; rows that start on 16 bytes are faster.  fp32 vectors (scales, factors, biases) and codes lie on 16 bytes.
+ * Codes of `rows` x `cols`: INT8T_ACT codes of dims {rows, cols, 1, 1}, i.e. [rows][cols rounded up to 16], zero beyond cols.
+ * Sums of products are exact: at most INT8T_MAX_REDUCTION products (16129 each at most) go into one int32.
+ */
+typedef enum { INT8T_F32 = 0, INT8T_BF16 = 1, INT8T_F16 = 2, INT8T_DTYPE_MAX_ENUM = 0x7fffffff } int8t_dtype;
+#define INT8T_MAX_REDUCTION 131072
+
+/*
+ * Codes with a scale for each row: v = x (times factor[col], rounded, where factor_dev is given), c = max|v| of the row,
+ * codes as int8t_quantize makes them of v with that c; the draw of an element goes by row * cols + col.
+ *   x_dev       rows x cols elements of `type`, rows `pitch` elements apart (pitch >= cols); rows * (cols rounded up to 16) < 2^31
+ *   factor_dev  NULL, or cols floats
+ *   q_dev       out: codes of rows x cols;   scale_dev  out: rows floats, c / 127
+ */
+int8t_status int8t_quantize_rows(const void *x_dev, int8t_dtype type, int rows, int cols, size_t pitch, const float *factor_dev,
+                                 int8t_round mode, uint64_t seed, int8_t *q_dev, float *scale_dev, void *stream);
+
+/*
+ * The same with a scale for each column, the codes transposed: for a reduction over the rows.
+ *   factor_dev  NULL, or rows floats
+ *   q_dev       out: codes of cols x rows;   scale_dev  out: cols floats
+ *   sum_dev     NULL, or out: cols floats, the columns' sums of x (without the factor)
+ *   ws_dev      int8t_quantize_cols_workspace_bytes(rows, cols) bytes, 16-byte aligned
+ */
+size_t int8t_quantize_cols_workspace_bytes(int rows, int cols);
+int8t_status int8t_quantize_cols(const void *x_dev, int8t_dtype type, int rows, int cols, size_t pitch, const float *factor_dev,
+                                 int8t_round mode, uint64_t seed, int8_t *q_dev, float *scale_dev, float *sum_dev,
+                                 void *ws_dev, size_t ws_bytes, void *stream);
+
+/* Codes of rows x cols to codes of cols x rows (both dimensions at most what a reduction may be, or the other way round). */
+int8t_status int8t_transpose_codes(const int8_t *q_dev, int rows, int cols, int8_t *qt_dev, void *stream);
+
+/*
+ * y[m][n] = (float)(sum_k a[m][k] b[n][k]) * (sa[m] * sb[n]) + bias[n]
+ *   a_dev, b_dev   codes of M x K and N x K, zero beyond K
+ *   sb_dev, bias_dev   NULL (ones; none), or N floats;   sa_dev  M floats
+ *   y_dev          out: M x N of `type`, rows `pitch` apart
+ *   ws_dev         NULL, or int8t_product_workspace_bytes(M, N, K) bytes, 16-byte aligned: products with few results split their
+ *                  reduction with it (the sums are integers: the result is the same)
+ */
+size_t int8t_product_workspace_bytes(int M, int N, int K);
+int8t_status int8t_product(const int8_t *a_dev, const float *sa_dev, const int8_t *b_dev, const float *sb_dev, int M, int N, int K,
+                           const float *bias_dev, void *y_dev, int8t_dtype type, size_t pitch, void *ws_dev, size_t ws_bytes,
+                           void *stream);
+
+/*
+ * A linear layer of M tokens, y = x W^T + b, with a scale for each token and each output channel.
+ *   forward   codes of x and W by rows, nearest;  y as int8t_product
+ *   backward  dx[m][k] = sg[m] sum_n gq[m][n] wq[n][k],   gq, sg = stochastic codes by rows of dy[m][n] * sw[n], draws of `seed`
+ *             dw[n][k] = sh[n] sum_m hq[m][n] xq[m][k],   hq, sh = stochastic codes by columns of dy[m][n] * sx[m], draws of
+ *                                                          `seed` with its highest bit flipped
+ *             db[n] = sum_m dy[m][n]
+ *             (the scale that changes along the summed axis is in the values before their codes are made)
+ * int8t_linear_fwd: w NULL takes the codes at wq, sw (laid out before) as they are; xq NULL keeps no codes of x (nobody's backward
+ * pass comes for them).  M may be 0 there.  int8t_linear_bwd: dx, dw, db NULL: not wanted (one of dx, dw at least); reads xq, sx,
+ * wq, sw of the forward pass.
+ */
+typedef struct int8t_linear_desc {
+    int M, K, N;
+    int8t_dtype type, wtype;       /* of x, y, dy, dx; of w, dw */
+} int8t_linear_desc;
+typedef struct int8t_linear_buffers {
+    const void *x, *w, *dy;
+    size_t x_pitch, w_pitch, y_pitch, dy_pitch;
+    int8_t *xq, *wq;
+    float *sx, *sw;
+    const float *bias;
+    void *y, *dx, *dw;             /* dx, dw: rows of K elements, dense */
+    float *db;
+    void *ws;
+    size_t ws_bytes;
+} int8t_linear_buffers;
+size_t int8t_linear_workspace_bytes(const int8t_linear_desc *desc, int backward);
+int8t_status int8t_linear_fwd(const int8t_linear_desc *desc, const int8t_linear_buffers *b, void *stream);
+int8t_status int8t_linear_bwd(const int8t_linear_desc *desc, const int8t_linear_buffers *b, uint64_t seed, void *stream);
+
+/*
+ * A paged cache of keys and values in 8 bits, a scale for each token and head.  Place `slot` is row slot % page_size of page
+ * slot / page_size.  dim: a multiple of 16, at most 256; pages * page_size < 2^31 (the cache itself may pass 4 GiB).
+ */
+typedef struct int8t_cache {
+    int8_t *kq, *vq;               /* [pages][heads][page_size][dim] */
+    float *ks, *vs;                /* [pages][heads][page_size] */
+    int pages, page_size, heads, dim;
+} int8t_cache;
+
+/*
+ * Writes `tokens` rows of every head to their slots, as Eq.1 codes with the row's own maximum (nearest).  A slot below 0 or beyond the
+ * last place: the token is left out.  No two tokens of a call share a slot.
+ *   k_dev, v_dev   element (t, h, d) at t * token_pitch + h * head_pitch + d
+ *   slots_dev      `tokens` 64-bit integers
+ */
+int8t_status int8t_cache_write(const int8t_cache *cache, const void *k_dev, const void *v_dev, int8t_dtype type, int tokens,
+                               size_t k_token_pitch, size_t k_head_pitch, size_t v_token_pitch, size_t v_head_pitch,
+                               const int64_t *slots_dev, void *stream);
+/* Reads back: [tokens][heads][dim] of `type`, code times scale; zeros for a slot outside the cache. */
+int8t_status int8t_cache_read(const int8t_cache *cache, const int64_t *slots_dev, int tokens, void *k_dev, void *v_dev,
+                              int8t_dtype type, void *stream);
+
+/*
+ * Attention of new tokens over the cache: token i of request b (of n = starts[b+1] - starts[b] tokens) sees the keys j < lengths[b],
+ * causal: j <= lengths[b] - n + i (its own key is in the cache already, and those of the tokens after it may be).  Query head
+ * h * group + g goes with head h of the cache.
+ *   out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale * q . k_j), sums in fp32;  zeros where a token sees nothing (its lse: -infinity)
+ *   q_dev        element (t, head, d) at t * q_token_pitch + head * q_head_pitch + d
+ *   starts_dev   requests + 1 ints, ascending from 0 to `tokens`;   lengths_dev  `requests` ints
+ *   table_dev    pages of a request in order: [requests][table_width], rows table_pitch apart; entries behind the last page that a length
+ *                needs are not used; keys on a page that is not in the cache are not seen
+ *   longest      no length is larger (a guide for the division of the work: the result does not depend on it); 0: unknown
+ *   out_dev      out: [tokens][heads * group][dim] of `type`, 16-byte aligned
+ *   lse_dev      NULL, or out: [tokens][heads * group] floats, the natural logarithm of sum_j p_j
+ *   ws_dev       int8t_cache_attend_workspace_bytes(cache, desc) bytes, 16-byte aligned; may be NULL where that is 0
+ * fp32 tensors are multiplied as two fp16 pieces of each q (scaled by a power of two) and p, 22 bits; codes are exact in fp16.
+ */
+typedef struct int8t_attend_desc {
+    int tokens, requests, group, table_width, longest;
+    int8t_dtype type;
+    int causal;
+    float scale;
+    size_t q_token_pitch, q_head_pitch, table_pitch;
+} int8t_attend_desc;
+size_t int8t_cache_attend_workspace_bytes(const int8t_cache *cache, const int8t_attend_desc *desc);
+int8t_status int8t_cache_attend(const int8t_cache *cache, const int8t_attend_desc *desc, const void *q_dev, const int *starts_dev,
+                                const int *lengths_dev, const int *table_dev, void *out_dev, float *lse_dev, void *ws_dev,
+                                size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

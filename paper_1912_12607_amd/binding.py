@@ -22,6 +22,9 @@ OP_QUANTIZE, OP_DSGC, OP_CONV_FWD, OP_CONV_BWD_DATA, OP_CONV_BWD_WEIGHT = range(
  VARIANT_WIDE_SQ128_DEEP, VARIANT_WIDE_128X64, VARIANT_WIDE_CELLS) = range(14)
 VARIANT_NAMES = ["auto", "band", "tile", "tile_split", "wide128", "wide256", "wgrad_fewer", "wgrad_more", "wgrad_images",
                  "wgrad_lines", "wide_sq128", "wide_sq128_deep", "wide_128x64", "wide_cells"]
+F32, BF16, F16 = 0, 1, 2
+DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+MAX_REDUCTION = 131072
 MAX_CANDIDATES = 64
 MAX_BATCH = 8
 
@@ -30,6 +33,9 @@ EXPORTS = ["int8t_status_string", "int8t_code_bytes", "int8t_unpack_codes", "int
            "int8t_quantize_batch", "int8t_quantize_batch_prepare", "int8t_dsgc_clip", "int8t_dsgc_clip_static", "int8t_dsgc_prepare", "int8t_dsgc_search", "int8t_conv_fwd", "int8t_conv_fwd_fused",
            "int8t_conv_bwd_data", "int8t_conv_bwd_weight", "int8t_conv_bwd_weight_fwd", "int8t_dclr_scale",
            "int8t_layer_step", "int8t_layer_step_form", "int8t_layer_backward", "int8t_layer_infer", "int8t_conv_variant_ok", "int8t_conv_select_variant", "int8t_conv_selected_variant",
+           "int8t_quantize_rows", "int8t_quantize_cols_workspace_bytes", "int8t_quantize_cols", "int8t_transpose_codes",
+           "int8t_product_workspace_bytes", "int8t_product", "int8t_linear_workspace_bytes", "int8t_linear_fwd", "int8t_linear_bwd",
+           "int8t_cache_write", "int8t_cache_read", "int8t_cache_attend_workspace_bytes", "int8t_cache_attend",
            "int8t_profile_start", "int8t_profile_start_sampled", "int8t_profile_stop", "int8t_profile_mfma_ceiling"]
 
 
@@ -56,6 +62,25 @@ class LayerBuffers(C.Structure):
                   "y", "dx", "dw", "y_acc", "dx_acc", "dw_acc", "ws_quant", "ws_dy", "ws_fwd", "ws_bwd_data", "ws_bwd_weight")]
                 + [(n + "_bytes", C.c_size_t) for n in ("ws_quant", "ws_dy", "ws_fwd", "ws_bwd_data", "ws_bwd_weight")]
                 + [("n_cand", C.c_int)])
+
+
+class LinearDesc(C.Structure):
+    _fields_ = [("M", C.c_int), ("K", C.c_int), ("N", C.c_int), ("type", C.c_int), ("wtype", C.c_int)]
+
+
+class LinearBuffers(C.Structure):
+    """int8t_linear_buffers: field names are the header's."""
+    _fields_ = ([(n, C.c_void_p) for n in ("x", "w", "dy")] + [(n, C.c_size_t) for n in ("x_pitch", "w_pitch", "y_pitch", "dy_pitch")]
+                + [(n, C.c_void_p) for n in ("xq", "wq", "sx", "sw", "bias", "y", "dx", "dw", "db", "ws")] + [("ws_bytes", C.c_size_t)])
+
+
+class Cache(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("kq", "vq", "ks", "vs")] + [(n, C.c_int) for n in ("pages", "page_size", "heads", "dim")])
+
+
+class AttendDesc(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("tokens", "requests", "group", "table_width", "longest", "type", "causal")]
+                + [("scale", C.c_float)] + [(n, C.c_size_t) for n in ("q_token_pitch", "q_head_pitch", "table_pitch")])
 
 
 class ConvDesc(C.Structure):
@@ -123,6 +148,32 @@ def _load():
     L.int8t_conv_select_variant.argtypes = [i32, dp, i32]
     L.int8t_conv_selected_variant.restype = i32
     L.int8t_conv_selected_variant.argtypes = [i32, dp]
+    L.int8t_quantize_rows.restype = i32
+    L.int8t_quantize_rows.argtypes = [vp, i32, i32, i32, sz, vp, i32, u64, vp, vp, vp]
+    L.int8t_quantize_cols_workspace_bytes.restype = sz
+    L.int8t_quantize_cols_workspace_bytes.argtypes = [i32, i32]
+    L.int8t_quantize_cols.restype = i32
+    L.int8t_quantize_cols.argtypes = [vp, i32, i32, i32, sz, vp, i32, u64, vp, vp, vp, vp, sz, vp]
+    L.int8t_transpose_codes.restype = i32
+    L.int8t_transpose_codes.argtypes = [vp, i32, i32, vp, vp]
+    L.int8t_product_workspace_bytes.restype = sz
+    L.int8t_product_workspace_bytes.argtypes = [i32, i32, i32]
+    L.int8t_product.restype = i32
+    L.int8t_product.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, i32, sz, vp, sz, vp]
+    L.int8t_linear_workspace_bytes.restype = sz
+    L.int8t_linear_workspace_bytes.argtypes = [C.POINTER(LinearDesc), i32]
+    L.int8t_linear_fwd.restype = i32
+    L.int8t_linear_fwd.argtypes = [C.POINTER(LinearDesc), C.POINTER(LinearBuffers), vp]
+    L.int8t_linear_bwd.restype = i32
+    L.int8t_linear_bwd.argtypes = [C.POINTER(LinearDesc), C.POINTER(LinearBuffers), u64, vp]
+    L.int8t_cache_write.restype = i32
+    L.int8t_cache_write.argtypes = [C.POINTER(Cache), vp, vp, i32, i32, sz, sz, sz, sz, vp, vp]
+    L.int8t_cache_read.restype = i32
+    L.int8t_cache_read.argtypes = [C.POINTER(Cache), vp, i32, vp, vp, i32, vp]
+    L.int8t_cache_attend_workspace_bytes.restype = sz
+    L.int8t_cache_attend_workspace_bytes.argtypes = [C.POINTER(Cache), C.POINTER(AttendDesc)]
+    L.int8t_cache_attend.restype = i32
+    L.int8t_cache_attend.argtypes = [C.POINTER(Cache), C.POINTER(AttendDesc), vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.int8t_dclr_scale.restype = C.c_double
     L.int8t_dclr_scale.argtypes = [C.c_double, C.c_double, C.c_double]
     L.int8t_profile_start.restype = i32
@@ -344,6 +395,61 @@ def int8t_conv_selected_variant(op: int, desc: ConvDesc) -> int:
     return int(lib.int8t_conv_selected_variant(op, C.byref(desc)))
 
 
+def int8t_quantize_rows(x, rows, cols, pitch, factor, mode, seed, q, scale, type=F32, stream=None):
+    _check(lib.int8t_quantize_rows(_ptr(x), type, rows, cols, pitch, _ptr(factor), mode, seed, _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def int8t_quantize_cols_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib.int8t_quantize_cols_workspace_bytes(rows, cols))
+
+
+def int8t_quantize_cols(x, rows, cols, pitch, factor, mode, seed, q, scale, sums=None, ws=None, type=F32, stream=None):
+    _check(lib.int8t_quantize_cols(_ptr(x), type, rows, cols, pitch, _ptr(factor), mode, seed, _ptr(q), _ptr(scale), _ptr(sums),
+                                   _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def int8t_transpose_codes(q, rows, cols, qt, stream=None):
+    _check(lib.int8t_transpose_codes(_ptr(q), rows, cols, _ptr(qt), _stream(stream)))
+
+
+def int8t_product_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib.int8t_product_workspace_bytes(M, N, K))
+
+
+def int8t_product(a, sa, b, sb, M, N, K, bias, y, pitch, type=F32, ws=None, stream=None):
+    _check(lib.int8t_product(_ptr(a), _ptr(sa), _ptr(b), _ptr(sb), M, N, K, _ptr(bias), _ptr(y), type, pitch, _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def int8t_linear_workspace_bytes(desc: LinearDesc, backward: int) -> int:
+    return int(lib.int8t_linear_workspace_bytes(C.byref(desc), backward))
+
+
+def int8t_linear_fwd(desc: LinearDesc, buffers: LinearBuffers, stream=None):
+    _check(lib.int8t_linear_fwd(C.byref(desc), C.byref(buffers), _stream(stream)))
+
+
+def int8t_linear_bwd(desc: LinearDesc, buffers: LinearBuffers, seed: int = 0, stream=None):
+    _check(lib.int8t_linear_bwd(C.byref(desc), C.byref(buffers), seed, _stream(stream)))
+
+
+def int8t_cache_write(cache: Cache, k, v, type, tokens, k_token_pitch, k_head_pitch, v_token_pitch, v_head_pitch, slots, stream=None):
+    _check(lib.int8t_cache_write(C.byref(cache), _ptr(k), _ptr(v), type, tokens, k_token_pitch, k_head_pitch, v_token_pitch, v_head_pitch, _ptr(slots),
+                                 _stream(stream)))
+
+
+def int8t_cache_read(cache: Cache, slots, tokens, k, v, type, stream=None):
+    _check(lib.int8t_cache_read(C.byref(cache), _ptr(slots), tokens, _ptr(k), _ptr(v), type, _stream(stream)))
+
+
+def int8t_cache_attend_workspace_bytes(cache: Cache, desc: AttendDesc) -> int:
+    return int(lib.int8t_cache_attend_workspace_bytes(C.byref(cache), C.byref(desc)))
+
+
+def int8t_cache_attend(cache: Cache, desc: AttendDesc, q, starts, lengths, table, out, lse=None, ws=None, stream=None):
+    _check(lib.int8t_cache_attend(C.byref(cache), C.byref(desc), _ptr(q), _ptr(starts), _ptr(lengths), _ptr(table), _ptr(out), _ptr(lse), _ptr(ws),
+                                  _nbytes(ws), _stream(stream)))
+
+
 def int8t_dclr_scale(d_c: float, alpha: float = 20.0, beta: float = 0.1) -> float:
     return float(lib.int8t_dclr_scale(d_c, alpha, beta))
 
@@ -358,10 +464,10 @@ def int8t_profile_start_sampled(kernel: str | None, every: int):
 
 def int8t_profile_stop() -> dict:
     """{kernel name: (launches, total milliseconds)} of the launches since int8t_profile_start."""
-    buf = (KernelTime * 32)()
+    buf = (KernelTime * 64)()
     n = C.c_int(0)
-    _check(lib.int8t_profile_stop(buf, 32, C.byref(n)))
-    return {buf[i].name.decode(): (int(buf[i].launches), float(buf[i].total_ms)) for i in range(min(n.value, 32))}
+    _check(lib.int8t_profile_stop(buf, 64, C.byref(n)))
+    return {buf[i].name.decode(): (int(buf[i].launches), float(buf[i].total_ms)) for i in range(min(n.value, 64))}
 
 
 def int8t_profile_mfma_ceiling(random_operands: bool, lds_reads: bool, iters: int = 20000, stream=None):

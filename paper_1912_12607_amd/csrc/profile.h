@@ -38,6 +38,15 @@ enum KernelId : int {
     KID_DW_TRIO,
     KID_INFER,
     KID_CONV_BAND_TRIO,
+    KID_TOKEN_ROWS,
+    KID_TOKEN_COLS,
+    KID_TOKEN_TRANSPOSE,
+    KID_TOKEN_PRODUCT,
+    KID_TOKEN_REDUCE,
+    KID_CACHE_WRITE,
+    KID_CACHE_READ,
+    KID_ATTEND,
+    KID_ATTEND_JOIN,
     KID_COUNT
 };
 

@@ -1,0 +1,283 @@
+// Codes of tokens: a scale for each row, or for each column with the codes transposed (Eq.1 / Eq.3 of the per-tensor quantizer, c the
+// maximum of the row or column), and the transposition of codes.
+#include "device_common.h"
+#include "tokens.h"
+
+namespace int8t {
+namespace {
+
+constexpr int kRowChunks = 4;       // groups of eight values that a lane holds
+
+inline int pad16(int v) { return (v + 15) & ~15; }
+
+// Keeps the computation of eight values in front of a change of the rounding mode.
+__device__ __forceinline__ void pin8(float v[8]) {
+    asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7]));
+}
+
+// Codes of eight neighbouring values.  STOCH: in the round-down mode, inv times 2^24 (see stoch_fixed()).
+template <bool STOCH>
+__device__ __forceinline__ uint2 codes8(const float v[8], float inv, uint32_t kx, uint32_t ka, uint32_t index, uint32_t step) {
+    int c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = quantize_one<STOCH>(v[i], inv, kx, ka, index + (uint32_t)i * step);
+    return make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
+}
+
+// One pass: a row's values are loaded once, stay in registers while their maximum is found, and leave as codes.  TPR lanes have a
+// row; rows beyond TPR * 32 values (LONG) are read a second time, from the caches.
+// Bound by memory: bytes read and written once.
+template <int TYPE, bool STOCH, int TPR, bool LONG>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quantize_rows_kernel(const RowsArgs a, const int wide, const uint32_t kx, const uint32_t ka) {
+    typedef typename ElemOf<TYPE>::type T;
+    constexpr int RPB = TPR < 256 ? 256 / TPR : 1, SPAN = TPR * 8 * kRowChunks;
+    const int t = (int)threadIdx.x % TPR;
+    const int row = (int)blockIdx.x * RPB + (int)threadIdx.x / TPR;
+    const bool live = row < a.rows;            // (all lanes stay for the reductions)
+    const int Kp = (a.cols + 15) & ~15;
+    const T* __restrict__ x = static_cast<const T*>(a.x) + (size_t)(live ? row : 0) * a.pitch;
+    const int cols = live ? a.cols : 0;
+    float v[kRowChunks][8];
+    auto fetch = [&](int base) {
+#pragma unroll
+        for (int u = 0; u < kRowChunks; ++u) {
+            const int c = base + (u * TPR + t) * 8;
+            load8<TYPE>(x + c, cols - c, wide, v[u]);
+        }
+        if (a.factor) {
+#pragma unroll
+            for (int u = 0; u < kRowChunks; ++u) {
+                const int c = base + (u * TPR + t) * 8;
+                float f[8];
+                load8<kF32>(a.factor + c, cols - c, true, f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[u][i] = __fmul_rn(v[u][i], f[i]);
+            }
+        }
+    };
+    float m = 0.0f;
+    for (int base = 0; base < (LONG ? a.cols : 1); base += SPAN) {
+        fetch(base);
+#pragma unroll
+        for (int u = 0; u < kRowChunks; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[u][i]));
+    }
+    m = wave_max(m);
+    if constexpr (TPR > 64) {
+        __shared__ float lds[TPR / 64];
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
+        __syncthreads();
+        m = lds[0];
+#pragma unroll
+        for (int i = 1; i < TPR / 64; ++i) m = fmaxf(m, lds[i]);
+    }
+    float inv = inv_scale_of(m), sc = scale_of(m);
+    if (live && t == 0) a.scale[row] = sc;
+    if (STOCH) inv = __fmul_rn(inv, kTwo24);
+    int8_t* __restrict__ q = a.q + (size_t)(live ? row : 0) * Kp;
+    for (int base = 0; base < (LONG ? a.cols : 1); base += SPAN) {
+        if (LONG) fetch(base);
+#pragma unroll
+        for (int u = 0; u < kRowChunks; ++u) pin8(v[u]);
+        if (STOCH) fp32_round_down_mode(inv, sc);
+#pragma unroll
+        for (int u = 0; u < kRowChunks; ++u) {
+            const int c = base + (u * TPR + t) * 8;
+            const uint2 o = codes8<STOCH>(v[u], inv, kx, ka, (uint32_t)row * (uint32_t)a.cols + (uint32_t)c, 1u);
+            if (live && c < Kp) *reinterpret_cast<uint2*>(q + c) = o;      // (values beyond the row are zero, and so are their codes)
+        }
+        if (STOCH) fp32_round_nearest_mode(inv);
+    }
+}
+
+template <int TYPE, bool STOCH>
+void rows_of(const RowsArgs& a, int wide, hipStream_t st) {
+    KernelTimer kt(KID_TOKEN_ROWS, st);
+    const uint32_t kx = seed_key_x(a.seed), ka = seed_key_a(a.seed);
+    // lanes of a row: as few as hold it, at least a wave
+    if (a.cols <= 64 * 8 * kRowChunks) launch_timed(kt, (quantize_rows_kernel<TYPE, STOCH, 64, false>), dim3((a.rows + 3) / 4), dim3(256), 0, st, a, wide, kx, ka);
+    else if (a.cols <= 256 * 8 * kRowChunks) launch_timed(kt, (quantize_rows_kernel<TYPE, STOCH, 256, false>), dim3(a.rows), dim3(256), 0, st, a, wide, kx, ka);
+    else if (a.cols <= 1024 * 8 * kRowChunks) launch_timed(kt, (quantize_rows_kernel<TYPE, STOCH, 1024, false>), dim3(a.rows), dim3(1024), 0, st, a, wide, kx, ka);
+    else launch_timed(kt, (quantize_rows_kernel<TYPE, STOCH, 1024, true>), dim3(a.rows), dim3(1024), 0, st, a, wide, kx, ka);
+}
+
+inline int wide_rows(const void* x, size_t pitch, int type) {
+    return (((uintptr_t)x | (pitch * (type == kF32 ? 4 : 2))) & 15) == 0;
+}
+
+// ---- scales of columns -----------------------------------------------------------------------
+// First pass: maxima of |x factor| and sums of x over a part of the rows, for 256 columns of a block: lane (c, r) has the columns
+// 8 c .. + 7 of every eighth row.
+template <int TYPE>
+__global__ __launch_bounds__(256) void cols_max_kernel(const ColsArgs a, const int wide) {
+    typedef typename ElemOf<TYPE>::type T;
+    __shared__ float lds[8][257];
+    const int cg = (int)threadIdx.x & 31, r0 = (int)threadIdx.x >> 5;
+    const int col = (int)blockIdx.x * 256 + cg * 8;
+    const int from = (int)((long long)a.rows * blockIdx.y / a.parts), to = (int)((long long)a.rows * (blockIdx.y + 1) / a.parts);
+    float m[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int r = from + r0; r < to; r += 8) {
+        float v[8];
+        load8<TYPE>(static_cast<const T*>(a.x) + (size_t)r * a.pitch + col, a.cols - col, wide, v);
+        const float f = a.factor ? a.factor[r] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            s[i] += v[i];
+            m[i] = fmaxf(m[i], fabsf(__fmul_rn(v[i], f)));
+        }
+    }
+    const int c = (int)blockIdx.x * 256 + (int)threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) lds[r0][cg * 8 + i] = m[i];
+    __syncthreads();
+    if (c < a.cols) {
+        float t = lds[0][threadIdx.x];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) t = fmaxf(t, lds[i][threadIdx.x]);
+        a.part_max[(size_t)blockIdx.y * a.cols + c] = t;
+    }
+    if (!a.sum) return;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) lds[r0][cg * 8 + i] = s[i];
+    __syncthreads();
+    if (c < a.cols) {
+        float t = lds[0][threadIdx.x];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) t += lds[i][threadIdx.x];
+        a.part_sum[(size_t)blockIdx.y * a.cols + c] = t;
+    }
+}
+
+// Second pass: codes of a tile of 128 rows x 64 columns, turned in LDS, leave in runs of 128 bytes along the rows.
+constexpr int CT_R = 128, CT_C = 64, CT_PITCH = CT_R + 16;
+__device__ __forceinline__ void tile_out(const int8_t* tile, int8_t* __restrict__ q, int row0, int col0, int rows_p, int cols) {
+    const int g = (int)threadIdx.x & 7;
+#pragma unroll
+    for (int u = 0; u < CT_C / 32; ++u) {
+        const int c = ((int)threadIdx.x >> 3) + 32 * u;
+        const int r = row0 + 16 * g;
+        if (col0 + c < cols && r < rows_p) *reinterpret_cast<uint4*>(q + (size_t)(col0 + c) * rows_p + r) = *reinterpret_cast<const uint4*>(tile + c * CT_PITCH + 16 * g);
+    }
+}
+template <int TYPE, bool STOCH>
+__global__ __launch_bounds__(256) void cols_codes_kernel(const ColsArgs a, const int wide, const uint32_t kx, const uint32_t ka) {
+    typedef typename ElemOf<TYPE>::type T;
+    __shared__ __attribute__((aligned(16))) int8_t tile[CT_C * CT_PITCH];
+    __shared__ __attribute__((aligned(16))) float invs[CT_C];
+    const int col0 = (int)blockIdx.x * CT_C, row0 = (int)blockIdx.y * CT_R;
+    if (threadIdx.x < CT_C) {
+        const int c = col0 + (int)threadIdx.x;
+        float m = 0.0f;
+        if (c < a.cols) {
+            for (int p = 0; p < a.parts; ++p) m = fmaxf(m, a.part_max[(size_t)p * a.cols + c]);
+            if (blockIdx.y == 0) {
+                a.scale[c] = scale_of(m);
+                if (a.sum) {
+                    double s = 0.0;
+                    for (int p = 0; p < a.parts; ++p) s += (double)a.part_sum[(size_t)p * a.cols + c];
+                    a.sum[c] = (float)s;
+                }
+            }
+        }
+        const float inv = inv_scale_of(m);
+        invs[threadIdx.x] = STOCH ? __fmul_rn(inv, kTwo24) : inv;
+    }
+    __syncthreads();
+    const int cg = (int)threadIdx.x & 7, r0 = (int)threadIdx.x >> 3;
+    const int col = col0 + cg * 8;
+    constexpr int NV = CT_R / 32;
+    float v[NV][8], inv[8];
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+        const int r = row0 + r0 + 32 * u;
+        load8<TYPE>(static_cast<const T*>(a.x) + (size_t)(r < a.rows ? r : 0) * a.pitch + col, r < a.rows ? a.cols - col : 0, wide, v[u]);
+        const float f = a.factor && r < a.rows ? a.factor[r] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] = __fmul_rn(v[u][i], f);
+        pin8(v[u]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) inv[i] = invs[cg * 8 + i];
+    float dummy = 0.0f;
+    if (STOCH) {
+        pin8(inv);
+        fp32_round_down_mode(inv[0], dummy);
+    }
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+        const int r = r0 + 32 * u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t index = (uint32_t)(row0 + r) * (uint32_t)a.cols + (uint32_t)(col + i);
+            tile[(cg * 8 + i) * CT_PITCH + r] = (int8_t)quantize_one<STOCH>(v[u][i], inv[i], kx, ka, index);
+        }
+    }
+    __syncthreads();
+    tile_out(tile, a.q, row0, col0, (a.rows + 15) & ~15, a.cols);
+}
+
+template <int TYPE>
+void cols_of(const ColsArgs& a, int wide, hipStream_t st) {
+    {
+        KernelTimer kt(KID_TOKEN_COLS, st);
+        launch_timed(kt, cols_max_kernel<TYPE>, dim3((a.cols + 255) / 256, a.parts), dim3(256), 0, st, a, wide);
+    }
+    KernelTimer kt(KID_TOKEN_COLS, st);
+    const dim3 grid((a.cols + CT_C - 1) / CT_C, (a.rows + CT_R - 1) / CT_R);
+    const uint32_t kx = seed_key_x(a.seed), ka = seed_key_a(a.seed);
+    if (a.stochastic) launch_timed(kt, (cols_codes_kernel<TYPE, true>), grid, dim3(256), 0, st, a, wide, kx, ka);
+    else launch_timed(kt, (cols_codes_kernel<TYPE, false>), grid, dim3(256), 0, st, a, wide, kx, ka);
+}
+
+// Codes [rows][pad16(cols)] -> [cols][pad16(rows)]
+__global__ __launch_bounds__(256) void transpose_codes_kernel(const int8_t* __restrict__ q, const int rows, const int cols, int8_t* __restrict__ qt) {
+    __shared__ __attribute__((aligned(16))) int8_t tile[CT_C * CT_PITCH];
+    const int col0 = (int)blockIdx.x * CT_C, row0 = (int)blockIdx.y * CT_R;
+    const int Kp = (cols + 15) & ~15;
+    const int g = (int)threadIdx.x & 3, r0 = (int)threadIdx.x >> 2;
+#pragma unroll
+    for (int u = 0; u < CT_R / 64; ++u) {
+        const int r = r0 + 64 * u, c = col0 + 16 * g;
+        uint4 t = make_uint4(0u, 0u, 0u, 0u);
+        if (row0 + r < rows && c < Kp) t = *reinterpret_cast<const uint4*>(q + (size_t)(row0 + r) * Kp + c);
+        const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) tile[(16 * g + i) * CT_PITCH + r] = (int8_t)(w[i >> 2] >> (8 * (i & 3)));
+    }
+    __syncthreads();
+    tile_out(tile, qt, row0, col0, (rows + 15) & ~15, cols);
+}
+
+}  // namespace
+
+hipError_t launch_quantize_rows(const RowsArgs& a, hipStream_t st) {
+    const int wide = wide_rows(a.x, a.pitch, a.type);
+#define LAUNCH(TY) a.stochastic ? rows_of<TY, true>(a, wide, st) : rows_of<TY, false>(a, wide, st)
+    if (a.type == kF32) LAUNCH(kF32);
+    else if (a.type == kBF16) LAUNCH(kBF16);
+    else LAUNCH(kF16);
+#undef LAUNCH
+    return hipGetLastError();
+}
+
+// parts of the rows in the first pass: blocks of 256 columns times parts fill the chip, a part has 32 rows at least
+int quantize_cols_parts(int rows, int cols) {
+    const int want = 1024 / ((cols + 255) / 256), most = (rows + 31) / 32;
+    return want < 1 ? 1 : want > 64 ? (most < 64 ? most : 64) : (most < want ? most : want);
+}
+hipError_t launch_quantize_cols(const ColsArgs& a, hipStream_t st) {
+    const int wide = wide_rows(a.x, a.pitch, a.type);
+    if (a.type == kF32) cols_of<kF32>(a, wide, st);
+    else if (a.type == kBF16) cols_of<kBF16>(a, wide, st);
+    else cols_of<kF16>(a, wide, st);
+    return hipGetLastError();
+}
+hipError_t launch_transpose_codes(const int8_t* q, int rows, int cols, int8_t* qt, hipStream_t st) {
+    KernelTimer kt(KID_TOKEN_TRANSPOSE, st);
+    launch_timed(kt, transpose_codes_kernel, dim3((cols + CT_C - 1) / CT_C, (rows + CT_R - 1) / CT_R), dim3(256), 0, st, q, rows, cols, qt);
+    return hipGetLastError();
+}
+
+}  // namespace int8t

@@ -1,0 +1,150 @@
+// Shared by the token operators (scales per token and output channel, paged cache, attention): element types, argument structs,
+// launchers.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kernels.h"
+#include "profile.h"
+
+namespace int8t {
+
+// Element types of the floating tensors (the values of int8t_dtype)
+constexpr int kF32 = 0, kBF16 = 1, kF16 = 2;
+
+typedef _Float16 tk_h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 tk_h8 __attribute__((ext_vector_type(8)));
+typedef float tk_f4 __attribute__((ext_vector_type(4)));
+typedef float tk_f16 __attribute__((ext_vector_type(16)));
+
+template <int TYPE> struct ElemOf;
+template <> struct ElemOf<kF32> { typedef float type; };
+template <> struct ElemOf<kBF16> { typedef __bf16 type; };
+template <> struct ElemOf<kF16> { typedef _Float16 type; };
+
+// Eight elements from p, of which the first `left` exist (left <= 0: none); the others are zero.  `wide`: p is 16-byte aligned
+// wherever left >= 8.
+template <int TYPE>
+__device__ __forceinline__ void load8(const typename ElemOf<TYPE>::type* __restrict__ p, int left, bool wide, float v[8]) {
+    typedef typename ElemOf<TYPE>::type T;
+    if (wide && left >= 8) {
+        if constexpr (TYPE == kF32) {
+            const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+            typedef T V8 __attribute__((ext_vector_type(8)));
+            const V8 a = *reinterpret_cast<const V8*>(p);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? (float)p[i] : 0.0f;
+    }
+}
+// Eight results, each rounded once (to nearest even) to the type
+template <int TYPE>
+__device__ __forceinline__ void store8(typename ElemOf<TYPE>::type* __restrict__ p, int left, bool wide, const float v[8]) {
+    typedef typename ElemOf<TYPE>::type T;
+    if (wide && left >= 8) {
+        if constexpr (TYPE == kF32) {
+            *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+            typedef T V8 __attribute__((ext_vector_type(8)));
+            V8 a;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = (T)v[i];
+            *reinterpret_cast<V8*>(p) = a;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) p[i] = (T)v[i];
+    }
+}
+
+// ---- token_quantize.hip ------------------------------------------------------------------------
+struct RowsArgs {            // codes of rows x cols values, a scale for each row
+    const void* x;
+    size_t pitch;            // elements between rows
+    int type, rows, cols;
+    const float* factor;     // cols, or null: values are multiplied first
+    int stochastic;
+    uint64_t seed;
+    int8_t* q;               // [rows][pad16(cols)]
+    float* scale;            // rows
+};
+hipError_t launch_quantize_rows(const RowsArgs& a, hipStream_t st);
+
+struct ColsArgs {            // ... a scale for each column, codes transposed
+    const void* x;
+    size_t pitch;
+    int type, rows, cols;
+    const float* factor;     // rows, or null
+    int stochastic;
+    uint64_t seed;
+    int8_t* q;               // [cols][pad16(rows)]
+    float* scale;            // cols
+    float* sum;              // cols, or null: sums of x (without the factor)
+    float *part_max, *part_sum;   // [parts][cols]
+    int parts;
+};
+int quantize_cols_parts(int rows, int cols);
+hipError_t launch_quantize_cols(const ColsArgs& a, hipStream_t st);
+hipError_t launch_transpose_codes(const int8_t* q, int rows, int cols, int8_t* qt, hipStream_t st);
+
+// ---- token_product.hip -------------------------------------------------------------------------
+struct ProductArgs {         // y[m][n] = (sum_k a[m][k] b[n][k]) * (sa[m] * sb[n]) + bias[n]
+    const int8_t *a, *b;     // [M][Kp], [N][Kp], Kp = pad16(K), the padding zero in one of them at least
+    const float *sa, *sb;    // sb null: ones
+    const float* bias;       // null: none
+    int M, N, Kp;
+    void* y;
+    size_t pitch;
+    int type;
+    int32_t* part;           // partial sums of a split reduction, or null
+    int splits;
+};
+size_t product_scratch(int M, int N, int Kp);
+hipError_t launch_product(ProductArgs a, size_t scratch_bytes, hipStream_t st);
+
+// ---- token_cache.hip ---------------------------------------------------------------------------
+struct CacheArgs {
+    int8_t *kq, *vq;         // [pages][heads][page_size][dim]
+    float *ks, *vs;          // [pages][heads][page_size]
+    int pages, page_size, heads, dim;
+    FastDiv by_page;
+    long long places;        // pages * page_size
+};
+struct CacheMoveArgs {       // tokens to (write) or from (read) their places
+    CacheArgs c;
+    void *k, *v;
+    size_t k_token, k_head, v_token, v_head;      // pitches, elements
+    const long long* slots;
+    int tokens, type;
+    int wide;                // 16-byte accesses
+};
+hipError_t launch_cache_write(const CacheMoveArgs& a, hipStream_t st);
+hipError_t launch_cache_read(const CacheMoveArgs& a, hipStream_t st);
+
+// ---- token_attend.hip --------------------------------------------------------------------------
+struct AttendArgs {
+    CacheArgs c;
+    const void* q;
+    size_t q_token, q_head;
+    const int *starts, *lengths, *table;
+    size_t table_pitch;
+    int tokens, requests, group, width, type, causal;
+    float scale;
+    void* out;               // [tokens][heads * group][dim]
+    float* lse;              // [tokens][heads * group], or null
+    int splits;
+    float *part_o, *part_ml; // [splits][tokens * heads * group][dim], [..][2]
+    int wide_q;
+};
+int attend_splits(const AttendArgs& a, int longest);
+hipError_t launch_attend(const AttendArgs& a, hipStream_t st);
+
+}  // namespace int8t
