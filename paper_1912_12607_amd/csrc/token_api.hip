@@ -126,7 +126,8 @@ AttendArgs attend_args(const int8t_cache* c, const int8t_attend_desc* d) {
     a.causal = d->causal;
     a.scale = d->scale;
     const int most = d->table_width * c->page_size;
-    a.splits = d->tokens && d->requests ? attend_splits(a, d->longest > 0 && d->longest < most ? d->longest : most) : 1;
+    a.splits = 1;
+    if (d->tokens && d->requests) attend_plan(&a, d->longest > 0 && d->longest < most ? d->longest : most);
     return a;
 }
 size_t attend_bytes(const AttendArgs& a) {

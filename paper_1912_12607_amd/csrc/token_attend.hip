@@ -1,70 +1,9 @@
 // Attention of new tokens over a paged cache in 8 bits:
 //   o_i = sum_j p_ij vs_j vq_j / sum_j p_ij,   p_ij = exp(scale ks_j (q_i . kq_j)),   j < length (causal: up to the token's own place).
-#include "device_common.h"
-#include "tokens.h"
+#include "token_attend.h"
 
 namespace int8t {
 namespace {
-
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kNone = -INFINITY;
-
-__device__ __forceinline__ tk_h2 as_h2(uint32_t w) { return __builtin_bit_cast(tk_h2, w); }
-__device__ __forceinline__ uint32_t as_u32(tk_h2 h) { return __builtin_bit_cast(uint32_t, h); }
-
-// Two codes as fp16, exactly: u = code + 128 placed in the low bits of 0x6400 is 1024 + u; minus 1152.  `w` holds codes xor 0x80, the
-// selector puts two of its bytes under 0x64.
-template <uint32_t SEL>
-__device__ __forceinline__ uint32_t codes_f16(uint32_t w) {
-    const tk_h2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-    return as_u32(as_h2(__builtin_amdgcn_perm(0x64646464u, w, SEL)) + off);
-}
-constexpr uint32_t kLowPair = 0x04010400u, kHighPair = 0x04030402u;
-
-// The request that owns tile `t` of `per` rows: request b's tiles start at floor(starts[b] * group / per) + b, which leaves each request
-// at least the tiles it needs.  Returns the last b with start <= t.
-__device__ __forceinline__ int tile_request(const AttendArgs& a, int t, int per) {
-    int lo = 0, hi = a.requests - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        const long long s = (long long)a.starts[mid] * a.group / per + mid;
-        if (s <= t) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
-}
-
-// What a block knows of its request: rows (token, head of the group) and keys
-struct Request {
-    int token0, tokens;      // first token of q, how many (within q)
-    int length;              // keys
-    int new_tokens;          // (as the starts say: the causal limit goes by it)
-    const int* pages;
-};
-__device__ __forceinline__ Request request_of(const AttendArgs& a, int b) {
-    Request r;
-    const int s0 = a.starts[b], s1 = a.starts[b + 1];
-    r.new_tokens = s1 - s0;
-    r.token0 = s0 < 0 ? 0 : s0;
-    const int end = s1 < a.tokens ? s1 : a.tokens;
-    r.tokens = end > r.token0 && s0 >= 0 ? end - r.token0 : 0;
-    const long long most = (long long)a.width * a.c.page_size;
-    const int len = a.lengths[b];
-    r.length = len < 0 ? 0 : (long long)len < most ? len : (int)most;
-    r.pages = a.table + (size_t)b * a.table_pitch;
-    return r;
-}
-
-// Where key j of a request lies (its row of the cache's codes and scales); false: nowhere -- beyond `end`, or on a page that there is not.
-__device__ __forceinline__ bool key_place(const AttendArgs& a, const Request& r, int head, int j, int end, size_t* place) {
-    *place = 0;
-    if (j >= end) return false;
-    const int p = div_by(j, a.c.by_page);
-    const int id = r.pages[p];
-    if ((unsigned)id >= (unsigned)a.c.pages) return false;
-    *place = ((size_t)id * a.c.heads + head) * a.c.page_size + (j - p * a.c.page_size);
-    return true;
-}
 
 // ------------------------------------------------------------------------------------------------
 // Sixteen rows (tokens times heads of a group, in order) of one request and one head of the cache per block; the request's keys are dealt
@@ -100,7 +39,6 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttendArgs a) {
     const int last_token = min(r0 + 15, nrows - 1) / a.group;
     const int end = max(0, a.causal ? min(rq.length, rq.length - rq.new_tokens + last_token + 1) : rq.length);
 
-    // q: scaled by a power of two that brings the row's largest into [2^14, 2^15), which fp16 holds with room below
     tk_h8 qf[PARTS][2 * KL];
     float qscale;
     {
@@ -116,17 +54,20 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttendArgs a) {
         }
         m = fmaxf(m, __shfl_xor(m, 16, kWave));
         m = fmaxf(m, __shfl_xor(m, 32, kWave));
-        const int e = max((int)((__float_as_uint(m) >> 23) & 255u), 30);         // (biased)
-        const float up = __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 254) << 23);
-        qscale = __uint_as_float((uint32_t)max(e - 14, 1) << 23) * (a.scale * kLog2e);
+        float back;
+        const float up = row_scale(m, &back);
+        qscale = back * (a.scale * kLog2e);
 #pragma unroll
         for (int i = 0; i < 2 * KL; ++i)
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const float t = v[i][u] * up;
-                const _Float16 h = (_Float16)t;
-                qf[0][i][u] = h;
-                if (PARTS == 2) qf[PARTS - 1][i][u] = (_Float16)(t - (float)h);
+                _Float16 first = (_Float16)t, rest;
+                if (PARTS == 2) {
+                    two_pieces(t, &first, &rest);
+                    qf[PARTS - 1][i][u] = rest;
+                }
+                qf[0][i][u] = first;
             }
     }
 
@@ -219,10 +160,13 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttendArgs a) {
         for (int u = 0; u < 8; ++u) {
             const float p = __builtin_amdgcn_exp2f(x[u] - base);
             l += p;
-            const float t = p * (vs[u] * inv_ref);
-            const _Float16 h = (_Float16)t;
-            pf[0][u] = h;
-            if (PARTS == 2) pf[PARTS - 1][u] = (_Float16)(t - (float)h);
+            const float w = p * (vs[u] * inv_ref);
+            _Float16 first = (_Float16)w, rest;
+            if (PARTS == 2) {
+                two_pieces(w, &first, &rest);
+                pf[PARTS - 1][u] = rest;
+            }
+            pf[0][u] = first;
         }
         // values: pairs of keys interleaved, two bytes of a dim at a time under 0x64
 #pragma unroll
@@ -331,8 +275,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
 
 template <int TYPE>
 hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
-    const dim3 grid((unsigned)((long long)a.tokens * a.group / 16 + a.requests), (unsigned)a.c.heads, (unsigned)a.splits);
-    {
+    if (a.rows > 16) {
+        const hipError_t e = launch_attend_chunk(a, st);
+        if (e != hipSuccess) return e;
+    } else {
+        const dim3 grid((unsigned)((long long)a.tokens * a.group / 16 + a.requests), (unsigned)a.c.heads, (unsigned)a.splits);
         KernelTimer kt(KID_ATTEND, st);
         if (a.c.dim <= 64) launch_timed(kt, (attend_rows_kernel<TYPE, 64>), grid, dim3(256), 0, st, a);
         else if (a.c.dim <= 128) launch_timed(kt, (attend_rows_kernel<TYPE, 128>), grid, dim3(256), 0, st, a);
@@ -348,14 +295,18 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Shares of the keys: enough blocks to fill the chip, at least 256 keys (64 a wave) in a share where all requests are as long as the longest
-int attend_splits(const AttendArgs& a, int longest) {
-    const long long tiles = ((long long)a.tokens * a.group / 16 + a.requests) * a.c.heads;
-    long long s = (1024 + tiles - 1) / tiles;
+// Rows of a block by the average of a request, and shares of the keys: enough blocks to fill the chip, and at least 256 keys in a share where
+// all requests are as long as the longest
+void attend_plan(AttendArgs* a, int longest) {
+    const long long rows = (long long)a->tokens * a->group, each = rows / a->requests;
+    a->rows = each <= 32 ? 16 : each < 256 || a->c.dim > 128 ? 128 : 256;
+    const long long tiles = (rows / a->rows + a->requests) * a->c.heads;
+    const long long fill = a->rows == 16 ? 1024 : a->rows == 128 ? 512 : 256;
+    long long s = fill / (tiles > 0 ? tiles : 1);
     const long long most = (longest + 255) / 256;
     if (s > most) s = most;
     if (s > 64) s = 64;
-    return s < 1 ? 1 : (int)s;
+    a->splits = s < 1 ? 1 : (int)s;
 }
 
 hipError_t launch_attend(const AttendArgs& a, hipStream_t st) {

@@ -129,7 +129,7 @@ struct CacheMoveArgs {       // tokens to (write) or from (read) their places
 hipError_t launch_cache_write(const CacheMoveArgs& a, hipStream_t st);
 hipError_t launch_cache_read(const CacheMoveArgs& a, hipStream_t st);
 
-// ---- token_attend.hip --------------------------------------------------------------------------
+// ---- token_attend.hip, token_attend_chunk.hip --------------------------------------------------------------------------
 struct AttendArgs {
     CacheArgs c;
     const void* q;
@@ -140,11 +140,13 @@ struct AttendArgs {
     float scale;
     void* out;               // [tokens][heads * group][dim]
     float* lse;              // [tokens][heads * group], or null
+    int rows;                // rows of a block: attend_plan()
     int splits;
     float *part_o, *part_ml; // [splits][tokens * heads * group][dim], [..][2]
     int wide_q;
 };
-int attend_splits(const AttendArgs& a, int longest);
+void attend_plan(AttendArgs* a, int longest);       // rows, splits
+hipError_t launch_attend_chunk(const AttendArgs& a, hipStream_t st);      // (blocks of 128 or 256 rows; does not join)
 hipError_t launch_attend(const AttendArgs& a, hipStream_t st);
 
 }  // namespace int8t
