@@ -73,6 +73,21 @@ __device__ __forceinline__ float row_scale(float m, float* back) {
     return __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 254) << 23);
 }
 
+// The power of two that p carries: p times a value scale is held in fp16, and 2^up times the largest scale seen so far lies between 2^14 and
+// 2^15, so that it fits, with room below (p may pass 1 by a factor below 2).
+struct ValueUnit {
+    float up = 0.0f, ref = -1.0f;            // ref: the largest scale that up allows
+    // `largest`, of all of the wave's rows: the change of up
+    __device__ __forceinline__ float raise(float largest) {
+        if (!(largest > ref)) return 0.0f;
+        const int e = max((int)((__float_as_uint(largest) >> 23) & 255u), 27);
+        const float before = up;
+        up = (float)(14 + 127 - e);
+        ref = __uint_as_float(((uint32_t)(e + 1) << 23) - 1u);
+        return up - before;
+    }
+};
+
 // w in two fp16 pieces.  The product that w is must be rounded to fp32 before it is split: left to itself the compiler forms the first
 // piece from the unrounded product and the rest from the rounded one, which differ by a step of the first now and then.
 __device__ __forceinline__ void two_pieces(float w, _Float16* first, _Float16* rest) {

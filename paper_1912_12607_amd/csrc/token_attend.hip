@@ -6,16 +6,19 @@ namespace int8t {
 namespace {
 
 // ------------------------------------------------------------------------------------------------
-// Sixteen rows (tokens times heads of a group, in order) of one request and one head of the cache per block; the request's keys are dealt
-// to `splits` blocks and in each to four waves, which run on their own, 32 keys at a time, and join their sums in LDS.
+// Sixteen rows (tokens times heads of a group, in order) of one request and one head of the cache per block.  The request's keys are dealt
+// out in shares of `share` to blocks and in each to eight waves, which run on their own, 32 keys at a time, the next 32 on their way
+// meanwhile, and join their sums in LDS.
 //   scores   S^T[key][row] = K Q^T (16 x 16 x 32 products): a lane loads 16 bytes of a key, codes become fp16 exactly;
 //   softmax  a lane's eight scores belong to one row; running maximum shared by a row's four lanes, raised when some lane needs it;
 //   values   O^T[dim][row] = V^T P^T: S^T's layout is P^T's operand layout if the keys of a 32 are numbered (lane group, tile, i), so
 //            nothing is exchanged; a lane loads DIM / 16 bytes of eight keys and turns them in registers.
-// PARTS = 2 (fp32): q and p in two fp16 pieces each.
+// PARTS = 2 (fp32): q and p in two fp16 pieces each.  UNI: the page size is a multiple of 16, whole tiles of 16 keys lie on a page and their
+// address is scalar.  Bound by memory: codes and scales read once.
 // ------------------------------------------------------------------------------------------------
-template <int TYPE, int DIM>
-__global__ __launch_bounds__(256) void attend_rows_kernel(const AttendArgs a) {
+constexpr int RW = 8;            // waves of a block
+template <int TYPE, int DIM, bool UNI>
+__global__ __launch_bounds__(64 * RW) void attend_rows_kernel(const AttendArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int PARTS = TYPE == kF32 ? 2 : 1, KL = DIM / 64, CB = DIM / 16;      // 16-byte loads of a key; bytes of a value row per lane
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -29,15 +32,87 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttendArgs a) {
     const long long tile = (long long)blockIdx.x - ((long long)a.starts[b] * a.group / 16 + b);
     if (tile < 0 || tile * 16 >= nrows) return;
     const int r0 = (int)tile * 16;
+    const int heads = a.c.heads * a.group;
+
+    // the block's keys: of those that its last row sees
+    const int last_token = min(r0 + 15, nrows - 1) / a.group;
+    const int seen_end = max(0, a.causal ? min(rq.length, rq.length - rq.new_tokens + last_token + 1) : rq.length);
+    const int from = (int)min((long long)split * a.share, (long long)seen_end), end = split + 1 == a.splits ? seen_end : min(from + a.share, seen_end);
+    if (a.splits > 1 && from >= end && !(split == 0)) {              // nothing here: the joining pass looks at m alone
+        if ((int)threadIdx.x < 16 && r0 + (int)threadIdx.x < nrows) {
+            const int r = r0 + (int)threadIdx.x, t = r / a.group;
+            a.part_ml[2 * ((size_t)split * a.tokens * heads + (size_t)(rq.token0 + t) * heads + head * a.group + (r - t * a.group))] = kNone;
+        }
+        return;
+    }
 
     // this lane's row
     const int row = r0 + n16;
     const bool have = row < nrows;
     const int token = (have ? row : r0) / a.group, gh = (have ? row : r0) - token * a.group;
     const int limit = !have ? 0 : a.causal ? min(rq.length, rq.length - rq.new_tokens + token + 1) : rq.length;
-    // the block's keys: those that its last row sees
-    const int last_token = min(r0 + 15, nrows - 1) / a.group;
-    const int end = max(0, a.causal ? min(rq.length, rq.length - rq.new_tokens + last_token + 1) : rq.length);
+
+    // this wave's keys: whole 32s of the block's share
+    const int steps = (end - from + 31) >> 5;
+    const int s_from = steps * wave / RW, s_to = steps * (wave + 1) / RW;
+
+    // ---- loader
+    uint4 kw[2][KL];                     // keys of the scores' operand: 16 t + n16
+    uint32_t vw[8][CB / 4];              // slot u = 4 t + i is key 16 t + 4 kg + i, of this lane's scores and values
+    float ks[8], vs[8];
+    uint32_t okl;                        // bit u: the slot's key is in the cache
+    int ids[2];
+    const int kd = kg * 16, vd = n16 * CB < D ? n16 * CB : 0;                      // (beyond D: q is zero there, and nothing is stored)
+    auto page_ids = [&](int s) __attribute__((always_inline)) {
+        if (!UNI) return;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int j = from + s * 32 + 16 * t;
+            ids[t] = j < end ? rq.pages[div_by(j, a.c.by_page)] : -1;
+        }
+    };
+    auto fetch = [&](int s) __attribute__((always_inline)) {
+        const int j0 = from + s * 32;
+        okl = 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            if (UNI) {
+                const int j = j0 + 16 * t;
+                const bool ok = (unsigned)ids[t] < (unsigned)a.c.pages;
+                const int id = __builtin_amdgcn_readfirstlane(ok ? ids[t] : 0), in = ok ? j - div_by(j, a.c.by_page) * a.c.page_size : 0;
+                const size_t place = ((size_t)id * a.c.heads + head) * a.c.page_size + in;
+                const int8_t *kq = a.c.kq + place * D, *vq = a.c.vq + place * D;
+#pragma unroll
+                for (int i = 0; i < KL; ++i) kw[t][i] = *reinterpret_cast<const uint4*>(kq + n16 * D + (i * 64 + kd < D ? i * 64 + kd : 0));
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < CB / 4; ++c) vw[4 * t + i][c] = *reinterpret_cast<const uint32_t*>(vq + (4 * kg + i) * D + vd + 4 * c);
+                const float4 k4 = *reinterpret_cast<const float4*>(a.c.ks + place + 4 * kg), v4 = *reinterpret_cast<const float4*>(a.c.vs + place + 4 * kg);
+                ks[4 * t] = k4.x; ks[4 * t + 1] = k4.y; ks[4 * t + 2] = k4.z; ks[4 * t + 3] = k4.w;
+                vs[4 * t] = v4.x; vs[4 * t + 1] = v4.y; vs[4 * t + 2] = v4.z; vs[4 * t + 3] = v4.w;
+                if (ok) okl |= 15u << (4 * t);
+            } else {
+                size_t place;
+                key_place(a, rq, head, j0 + 16 * t + n16, end, &place);
+#pragma unroll
+                for (int i = 0; i < KL; ++i) kw[t][i] = *reinterpret_cast<const uint4*>(a.c.kq + place * D + (i * 64 + kd < D ? i * 64 + kd : 0));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (key_place(a, rq, head, j0 + 16 * t + 4 * kg + i, end, &place)) okl |= 1u << (4 * t + i);
+                    ks[4 * t + i] = a.c.ks[place];
+                    vs[4 * t + i] = a.c.vs[place];
+#pragma unroll
+                    for (int c = 0; c < CB / 4; ++c) vw[4 * t + i][c] = *reinterpret_cast<const uint32_t*>(a.c.vq + place * D + vd + 4 * c);
+                }
+            }
+        }
+    };
+    if (s_from < s_to) {
+        page_ids(s_from);
+        fetch(s_from);
+        page_ids(s_from + 1);
+    }
 
     tk_h8 qf[PARTS][2 * KL];
     float qscale;
@@ -71,48 +146,15 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttendArgs a) {
             }
     }
 
-    // this wave's keys: whole 32s of the block's share
-    const int steps = (end + 31) >> 5;
-    const int s_from = (int)((long long)steps * split / a.splits), s_to = (int)((long long)steps * (split + 1) / a.splits);
-    const int w_from = s_from + (int)((long long)(s_to - s_from) * wave / 4), w_to = s_from + (int)((long long)(s_to - s_from) * (wave + 1) / 4);
-
-    float m = kNone, l = 0.0f, ref = 0.0f, inv_ref = 0.0f;      // maximum; sum of this lane's p; largest value scale so far, 2^15 / it
+    ValueUnit unit;
+    float m = kNone, l = 0.0f;                   // maximum that p goes by; sum of this lane's p (times 2^up)
     tk_f4 o[CB];
 #pragma unroll
     for (int c = 0; c < CB; ++c) o[c] = tk_f4{0.f, 0.f, 0.f, 0.f};
 
-    for (int s = w_from; s < w_to; ++s) {
-        const int j0 = s * 32;
-        // keys of the scores' operand: 16 t + n16
-        uint4 kw[2][KL];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            size_t place;
-            key_place(a, rq, head, j0 + 16 * t + n16, end, &place);
-#pragma unroll
-            for (int i = 0; i < KL; ++i) {
-                const int d = i * 64 + kg * 16;
-                kw[t][i] = *reinterpret_cast<const uint4*>(a.c.kq + place * D + (d < D ? d : 0));      // (beyond D: q is zero there)
-            }
-        }
-        // keys of this lane's scores and values: slot u = 4 t + i is key 16 t + 4 kg + i
-        uint32_t vw[8][CB / 4];
-        float ks[8], vs[8];
-        bool seen[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int j = j0 + 16 * (u >> 2) + 4 * kg + (u & 3);
-            size_t place;
-            const bool ok = key_place(a, rq, head, j, end, &place);
-            seen[u] = ok && j < limit;
-            ks[u] = a.c.ks[place];
-            const float s0 = a.c.vs[place];
-            vs[u] = ok ? s0 : 0.0f;
-            const int d = n16 * CB;
-            const uint32_t* p = reinterpret_cast<const uint32_t*>(a.c.vq + place * D + (d < D ? d : 0));
-#pragma unroll
-            for (int c = 0; c < CB / 4; ++c) vw[u][c] = p[c];
-        }
+    for (int s = s_from; s < s_to; ++s) {
+        const int j0 = from + s * 32;
+        // this step's operands leave the loader's registers as fp16 (scores: at once; values: as they are), then the next step's are requested
         tk_f4 sc[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -130,37 +172,50 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttendArgs a) {
                 }
             }
         }
+        uint32_t vc[8][CB / 4];
+        float kc[8], vsc[8];
+        bool seen[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int j = j0 + 16 * (u >> 2) + 4 * kg + (u & 3);
+            const bool in = ((okl >> u) & 1u) != 0 && j < end;
+            seen[u] = in && j < limit;
+            kc[u] = ks[u] * qscale;
+            vsc[u] = in ? vs[u] : 0.0f;
+#pragma unroll
+            for (int c = 0; c < CB / 4; ++c) vc[u][c] = vw[u][c] ^ 0x80808080u;
+        }
+        if (s + 1 < s_to) {
+            fetch(s + 1);
+            page_ids(s + 2);
+        }
         float x[8], top = kNone, vmax = 0.0f;
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const float t = sc[u >> 2][u & 3] * (ks[u] * qscale);
+            const float t = sc[u >> 2][u & 3] * kc[u];
             x[u] = seen[u] ? t : kNone;
             top = fmaxf(top, x[u]);
-            vmax = fmaxf(vmax, vs[u]);
+            vmax = fmaxf(vmax, vsc[u]);
         }
-        if (__any(top > m || vmax > ref)) {
+        if (__any(top > m + 0.99f || vmax > unit.ref)) {
             top = fmaxf(top, __shfl_xor(top, 16, kWave));
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
-            const float m1 = fmaxf(m, top);
-            vmax = fmaxf(wave_max(vmax), fmaxf(ref, 1e-30f));
-            const float keep = m == kNone ? 0.0f : __builtin_amdgcn_exp2f(m - m1);
-            l *= keep;
-            const float by = keep * (ref / vmax);
+            const float m1 = fmaxf(m, top), grown = unit.raise(wave_max(vmax));
+            const float by = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - m1) + grown);
+            l *= by;
 #pragma unroll
             for (int c = 0; c < CB; ++c)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o[c][r] *= by;
             m = m1;
-            ref = vmax;
-            inv_ref = 32768.0f / vmax;
         }
-        const float base = m == kNone ? 0.0f : m;
+        const float base = m == kNone ? 0.0f : unit.up - m;
         tk_h8 pf[PARTS];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const float p = __builtin_amdgcn_exp2f(x[u] - base);
+            const float p = __builtin_amdgcn_exp2f(x[u] + base);
             l += p;
-            const float w = p * (vs[u] * inv_ref);
+            const float w = p * vsc[u];
             _Float16 first = (_Float16)w, rest;
             if (PARTS == 2) {
                 two_pieces(w, &first, &rest);
@@ -174,8 +229,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttendArgs a) {
             uint32_t f[4][4];        // [byte of the word][pair of keys]
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const uint32_t x0 = vw[2 * u][c4] ^ 0x80808080u, x1 = vw[2 * u + 1][c4] ^ 0x80808080u;
-                const uint32_t lo = __builtin_amdgcn_perm(x1, x0, 0x05010400u), hi = __builtin_amdgcn_perm(x1, x0, 0x07030602u);
+                const uint32_t lo = __builtin_amdgcn_perm(vc[2 * u + 1][c4], vc[2 * u][c4], 0x05010400u), hi = __builtin_amdgcn_perm(vc[2 * u + 1][c4], vc[2 * u][c4], 0x07030602u);
                 f[0][u] = codes_f16<kLowPair>(lo);
                 f[1][u] = codes_f16<kHighPair>(lo);
                 f[2][u] = codes_f16<kLowPair>(hi);
@@ -191,53 +245,79 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttendArgs a) {
     }
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
-    const float unit = ref * (1.0f / 32768.0f);
+    const float down = __builtin_amdgcn_exp2f(-unit.up);
 
-    // the four waves' sums, in LDS: [wave][row][DIM + 1], in units of the values
-    __shared__ float sm[4][16], sl[4][16];
-    __shared__ float so[4][16][DIM + 4];
+    // the waves' sums, in LDS, the first half's dims and then the others: [wave][row][DIM / 2 + 4]
+    constexpr int HD = DIM / 2;
+    __shared__ float sm[RW][16], sl[RW][16];
+    __shared__ float so[RW][16][HD + 4];
     if (kg == 0) {
         sm[wave][n16] = m;
-        sl[wave][n16] = l;
+        sl[wave][n16] = l * down;
     }
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) so[wave][n16][CB * (4 * kg + r) + c] = o[c][r] * unit;
-    __syncthreads();
-    // 16 lanes per row
-    const int jr = (int)threadIdx.x >> 4, jl = (int)threadIdx.x & 15;
-    if (r0 + jr >= nrows) return;
-    const float mm = fmaxf(fmaxf(sm[0][jr], sm[1][jr]), fmaxf(sm[2][jr], sm[3][jr]));
-    float w[4], total = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        w[i] = sm[i][jr] == kNone ? 0.0f : __builtin_amdgcn_exp2f(sm[i][jr] - mm);
-        total += w[i] * sl[i][jr];
-    }
+    // 32 lanes per row
+    const int jr = (int)threadIdx.x >> 5, jl = (int)threadIdx.x & 31;
     const int jt = (r0 + jr) / a.group, jg = (r0 + jr) - jt * a.group;
-    const int heads = a.c.heads * a.group;
+    const bool write = r0 + jr < nrows;
     const size_t out_row = (size_t)(rq.token0 + jt) * heads + head * a.group + jg;
     const bool whole = a.splits == 1;
-    const float by = !whole ? 1.0f : total > 0.0f ? 1.0f / total : 0.0f;
     const size_t part_row = (size_t)split * a.tokens * heads + out_row;
-    if (jl == 0) {
-        if (whole) {
-            if (a.lse) a.lse[out_row] = total > 0.0f ? (mm + __log2f(total)) * (1.0f / kLog2e) : kNone;
-        } else {
-            a.part_ml[2 * part_row] = mm;
-            a.part_ml[2 * part_row + 1] = total;
+    float w[RW], by = 1.0f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        // dim CB (4 kg + r) + c is in the first half where kg < 2
+        if (h) __syncthreads();
+        if ((kg >> 1) == h) {
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) so[wave][n16][CB * (4 * (kg & 1) + r) + c] = o[c][r] * down;
         }
-    }
+        __syncthreads();
+        if (h == 0) {
+            float mm = sm[0][jr], total = 0.0f;
 #pragma unroll
-    for (int d = jl * 8; d < DIM; d += 128) {
-        if (d >= D) break;
-        float v[8];
+            for (int i = 1; i < RW; ++i) mm = fmaxf(mm, sm[i][jr]);
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            v[u] = (w[0] * so[0][jr][d + u] + w[1] * so[1][jr][d + u] + w[2] * so[2][jr][d + u] + w[3] * so[3][jr][d + u]) * by;
-        if (whole) store8<TYPE>(static_cast<T*>(a.out) + out_row * D + d, 8, true, v);
-        else store8<kF32>(a.part_o + part_row * D + d, 8, true, v);
+            for (int i = 0; i < RW; ++i) {
+                w[i] = sm[i][jr] == kNone ? 0.0f : __builtin_amdgcn_exp2f(sm[i][jr] - mm);
+                total += w[i] * sl[i][jr];
+            }
+            if (whole) by = total > 0.0f ? 1.0f / total : 0.0f;
+            if (write && jl == 0) {
+                if (whole) {
+                    if (a.lse) a.lse[out_row] = total > 0.0f ? (mm + __log2f(total)) * (1.0f / kLog2e) : kNone;
+                } else {
+                    a.part_ml[2 * part_row] = mm;
+                    a.part_ml[2 * part_row + 1] = total;
+                }
+            }
+        }
+        constexpr int PER = HD / 32 < 2 ? 2 : HD / 32;           // dims per lane (HD 32: half of the lanes)
+        const int d = jl * PER;
+        if (write && d < HD && h * HD + d < D) {
+            float v[PER];
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+                v[u] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < RW; ++i) v[u] += w[i] * so[i][jr][d + u];
+                v[u] *= by;
+            }
+            if (whole) {
+                typedef T V __attribute__((ext_vector_type(PER)));
+                V r;
+#pragma unroll
+                for (int u = 0; u < PER; ++u) r[u] = (T)v[u];
+                *reinterpret_cast<V*>(static_cast<T*>(a.out) + out_row * D + h * HD + d) = r;
+            } else {
+                typedef float V __attribute__((ext_vector_type(PER)));
+                V r;
+#pragma unroll
+                for (int u = 0; u < PER; ++u) r[u] = v[u];
+                *reinterpret_cast<V*>(a.part_o + part_row * D + h * HD + d) = r;
+            }
+        }
     }
 }
 
@@ -273,17 +353,23 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     }
 }
 
+template <int TYPE, bool UNI>
+void rows_of(const AttendArgs& a, hipStream_t st) {
+    const dim3 grid((unsigned)((long long)a.tokens * a.group / 16 + a.requests), (unsigned)a.c.heads, (unsigned)a.splits);
+    KernelTimer kt(KID_ATTEND, st);
+    if (a.c.dim <= 64) launch_timed(kt, (attend_rows_kernel<TYPE, 64, UNI>), grid, dim3(64 * RW), 0, st, a);
+    else if (a.c.dim <= 128) launch_timed(kt, (attend_rows_kernel<TYPE, 128, UNI>), grid, dim3(64 * RW), 0, st, a);
+    else launch_timed(kt, (attend_rows_kernel<TYPE, 256, UNI>), grid, dim3(64 * RW), 0, st, a);
+}
+
 template <int TYPE>
 hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
     if (a.rows > 16) {
         const hipError_t e = launch_attend_chunk(a, st);
         if (e != hipSuccess) return e;
     } else {
-        const dim3 grid((unsigned)((long long)a.tokens * a.group / 16 + a.requests), (unsigned)a.c.heads, (unsigned)a.splits);
-        KernelTimer kt(KID_ATTEND, st);
-        if (a.c.dim <= 64) launch_timed(kt, (attend_rows_kernel<TYPE, 64>), grid, dim3(256), 0, st, a);
-        else if (a.c.dim <= 128) launch_timed(kt, (attend_rows_kernel<TYPE, 128>), grid, dim3(256), 0, st, a);
-        else launch_timed(kt, (attend_rows_kernel<TYPE, 256>), grid, dim3(256), 0, st, a);
+        if (a.c.page_size % 16 == 0) rows_of<TYPE, true>(a, st);
+        else rows_of<TYPE, false>(a, st);
     }
     if (a.splits > 1) {
         const size_t rows = (size_t)a.tokens * a.c.heads * a.group;
@@ -295,14 +381,24 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Rows of a block by the average of a request, and shares of the keys: enough blocks to fill the chip, and at least 256 keys in a share where
-// all requests are as long as the longest
+// Rows of a block by the average of a request; shares of the keys.
 void attend_plan(AttendArgs* a, int longest) {
     const long long rows = (long long)a->tokens * a->group, each = rows / a->requests;
     a->rows = each <= 32 ? 16 : each < 256 || a->c.dim > 128 ? 128 : 256;
     const long long tiles = (rows / a->rows + a->requests) * a->c.heads;
-    const long long fill = a->rows == 16 ? 1024 : a->rows == 128 ? 512 : 256;
-    long long s = fill / (tiles > 0 ? tiles : 1);
+    if (a->rows == 16) {
+        // Shares of a fixed number of keys, so that long requests among short ones have more blocks: 1024, or down to 512 (two steps of a wave)
+        // where that fills the chip
+        a->share = tiles * ((longest + 1023) / 1024) >= 512 ? 1024 : 512;
+        a->splits = (longest + a->share - 1) / a->share;
+        if (a->splits > 256) {
+            a->splits = 256;
+            a->share = ((longest + 255) / 256 + 31) & ~31;
+        }
+        if (a->splits < 1) a->splits = 1;
+        return;
+    }
+    long long s = (a->rows == 128 ? 512 : 256) / (tiles > 0 ? tiles : 1);
     const long long most = (longest + 255) / 256;
     if (s > most) s = most;
     if (s > 64) s = 64;

@@ -10,6 +10,8 @@
 //            of V (rows of keys, as they came) delivers: p never leaves its lane.
 // Bound by the vector units: 9 to 10 operations per score, of which the exponential counts for four, against 256 multiply-adds of the
 // matrix units (DIM 128).
+#include <type_traits>
+
 #include "token_attend.h"
 
 namespace int8t {
@@ -26,9 +28,12 @@ __device__ __forceinline__ int k_slot(int key, int g) { return DIM == 64 ? key *
 template <int DIM>
 __device__ __forceinline__ int v_slot(int key, int g) { return DIM == 64 ? key * 8 + (g ^ ((key & 2) << 1)) : key * (DIM / 8) + (g ^ ((key & 3) << 2)); }
 
-constexpr int chunk_lds(int DIM) { return 2 * (2 * TK * DIM * 2 + 3 * TK * 4); }
+// Tiles in LDS: two of keys; three of values where they fit (a tile's values are multiplied a step after its keys), three sets of scales.
+constexpr int value_tiles(int DIM) { return DIM == 256 ? 2 : 3; }
+constexpr int chunk_lds(int DIM) { return (2 + value_tiles(DIM)) * TK * DIM * 2 + 3 * 3 * TK * 4; }
 
-template <int TYPE, int DIM, int NW>
+// UNI: the keys whose pieces a wave loads at a time lie on one page (its size is a multiple of 1024 / DIM): addresses are scalar.
+template <int TYPE, int DIM, int NW, bool UNI>
 __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kernel(const AttendArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int PARTS = TYPE == kF32 ? 2 : 1, NT = 64 * NW, ROWS = 32 * NW;
@@ -37,9 +42,11 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
     constexpr bool APART = CH < NT;                            // keys' and values' pieces to different threads
     constexpr int NP = APART ? 1 : CH / NT;                    // pieces of either tensor per thread
     extern __shared__ __attribute__((aligned(1024))) uint4 lds[];
+    constexpr int VT = value_tiles(DIM), TILE = TK * DIM / 8;
+    constexpr bool TURNS = NW == 8;                            // two waves on each SIMD that take turns, see below
     uint4* const sk = lds;                                     // [2][TK][DIM] fp16
-    uint4* const sv = lds + 2 * TK * DIM / 8;
-    float* const sc = reinterpret_cast<float*>(lds + 4 * TK * DIM / 8);      // [2][3][TK]: key scales, value scales, 0 or -infinity
+    uint4* const sv = lds + 2 * TILE;                          // [VT][TK][DIM]
+    float* const sc = reinterpret_cast<float*>(lds + (2 + VT) * TILE);      // [3][3][TK]: key scales, value scales, 0 or -infinity
 
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, half = lane >> 5;
@@ -99,53 +106,80 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
             }
     }
 
-    // ---- loader: this thread's pieces, piece p is 16 dims of a key
+    // ---- loader: this thread's pieces, piece p is 16 dims of a key; a wave's are those of KW neighbouring keys
+    constexpr int KW = 1024 / DIM;
     const bool loads_k = !APART || tid < CH, loads_v = !APART || (tid >= CH && tid < 2 * CH);
     const int pt = APART ? tid % CH : tid;
     uint4 rk[NP], rv[NP];
     float rks[NP], rvs[NP];
     bool rok[NP];
     int ids[NP];
-    auto key_of = [&](int p) { return (pt + p * NT) / (DIM / 16); };
-    auto page_ids = [&](int t) {                               // pages of tile t's keys
+    const int d16 = (pt % (DIM / 16)) * 16, dc = d16 < D ? d16 : 0;              // (beyond D: q is zero there, and nothing is stored)
+    const int key0 = pt / (DIM / 16), wkey0 = __builtin_amdgcn_readfirstlane(key0);
+    auto key_of = [&](int p) __attribute__((always_inline)) { return key0 + p * (NT / (DIM / 16)); };
+    auto page_ids = [&](int t) __attribute__((always_inline)) {                               // pages of tile t's keys
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            const int j = t * TK + key_of(p);
+            const int j = t * TK + (UNI ? wkey0 + p * (NT / (DIM / 16)) : key_of(p));
             ids[p] = j < end ? rq.pages[div_by(j, a.c.by_page)] : -1;
         }
     };
-    auto fetch = [&](int t) {
+    auto fetch = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            const int j = t * TK + key_of(p), d = ((pt + p * NT) % (DIM / 16)) * 16;
-            rok[p] = (unsigned)ids[p] < (unsigned)a.c.pages;
-            const size_t place = rok[p] ? ((size_t)ids[p] * a.c.heads + head) * a.c.page_size + (j - div_by(j, a.c.by_page) * a.c.page_size) : 0;
-            const size_t at = place * D + (d < D ? d : 0);      // (beyond D: q is zero there, and nothing is stored)
+            const int j = t * TK + key_of(p);
+            bool ok = (unsigned)ids[p] < (unsigned)a.c.pages;
+            size_t place;
+            const int8_t *kq = a.c.kq, *vq = a.c.vq;
+            const float *ks = a.c.ks, *vs = a.c.vs;
+            uint32_t code_at, scale_at;                        // from there on
+            if (UNI) {
+                const int id = __builtin_amdgcn_readfirstlane(ok ? ids[p] : 0);
+                const int jw = t * TK + wkey0 + p * (NT / (DIM / 16)), in = jw - div_by(jw, a.c.by_page) * a.c.page_size;
+                place = ((size_t)id * a.c.heads + head) * a.c.page_size + (ok ? in : 0);
+                const size_t base = place * D;
+                kq += base;
+                vq += base;
+                ks += place;
+                vs += place;
+                code_at = (uint32_t)((key0 - wkey0) * D + dc);
+                scale_at = (uint32_t)(key0 - wkey0);
+                ok = ok && j < end;
+            } else {
+                place = ok ? ((size_t)ids[p] * a.c.heads + head) * a.c.page_size + (j - div_by(j, a.c.by_page) * a.c.page_size) : 0;
+                kq += place * D;
+                vq += place * D;
+                ks += place;
+                vs += place;
+                code_at = (uint32_t)dc;
+                scale_at = 0;
+            }
+            rok[p] = ok;
             if (loads_k) {
-                rk[p] = *reinterpret_cast<const uint4*>(a.c.kq + at);
-                rks[p] = a.c.ks[place];
+                rk[p] = *reinterpret_cast<const uint4*>(kq + code_at);
+                rks[p] = ks[scale_at];
             }
             if (loads_v) {
-                rv[p] = *reinterpret_cast<const uint4*>(a.c.vq + at);
-                rvs[p] = a.c.vs[place];
+                rv[p] = *reinterpret_cast<const uint4*>(vq + code_at);
+                rvs[p] = vs[scale_at];
             }
         }
     };
-    auto expand = [](const uint4& c, uint4* lo, uint4* hi) {
+    auto expand = [](const uint4& c, uint4* lo, uint4* hi) __attribute__((always_inline)) {
         const uint32_t w[4] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u, c.z ^ 0x80808080u, c.w ^ 0x80808080u};
         *lo = make_uint4(codes_f16<kLowPair>(w[0]), codes_f16<kHighPair>(w[0]), codes_f16<kLowPair>(w[1]), codes_f16<kHighPair>(w[1]));
         *hi = make_uint4(codes_f16<kLowPair>(w[2]), codes_f16<kHighPair>(w[2]), codes_f16<kLowPair>(w[3]), codes_f16<kHighPair>(w[3]));
     };
-    auto stage = [&](int buf) {
+    auto stage = [&](int kslot, int vslot, int sslot) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            const int key = key_of(p), g = ((pt + p * NT) % (DIM / 16)) * 2;
+            const int key = key_of(p), g = d16 >> 3;
             uint4 lo, hi;
-            float* const s = sc + buf * 3 * TK;
+            float* const s = sc + sslot * 3 * TK;
             if (loads_k) {
                 expand(rk[p], &lo, &hi);
-                sk[buf * (TK * DIM / 8) + k_slot<DIM>(key, g)] = lo;
-                sk[buf * (TK * DIM / 8) + k_slot<DIM>(key, g + 1)] = hi;
+                sk[kslot * TILE + k_slot<DIM>(key, g)] = lo;
+                sk[kslot * TILE + k_slot<DIM>(key, g + 1)] = hi;
                 if (g == 0) {
                     s[key] = rok[p] ? rks[p] : 0.0f;
                     s[2 * TK + key] = rok[p] ? 0.0f : kNone;
@@ -153,50 +187,74 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
             }
             if (loads_v) {
                 expand(rv[p], &lo, &hi);
-                sv[buf * (TK * DIM / 8) + v_slot<DIM>(key, g)] = lo;
-                sv[buf * (TK * DIM / 8) + v_slot<DIM>(key, g + 1)] = hi;
+                sv[vslot * TILE + v_slot<DIM>(key, g)] = lo;
+                sv[vslot * TILE + v_slot<DIM>(key, g + 1)] = hi;
                 if (g == 0) s[TK + key] = rok[p] ? rvs[p] : 0.0f;
             }
         }
     };
 
-    float m = kNone, l = 0.0f, ref = 0.0f, unit = 0.0f;       // maximum (times qscale); sum of this lane's p; largest value scale so far, 2^15 / it
+    ValueUnit unit;
+    float m = kNone, l = 0.0f;                   // maximum (times qscale) that p goes by; sum of this lane's p (times 2^up)
     tk_f16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[d][v] = 0.0f;
 
-    if (t_from < t_to) {
-        page_ids(t_from);
-        fetch(t_from);
-        page_ids(t_from + 1);
-        stage(t_from & 1);
-        fetch(t_from + 1);
-        page_ids(t_from + 2);
-    }
-    for (int t = t_from; t < t_to; ++t) {
-        const int buf = t & 1;
-        __syncthreads();                          // the tile is in LDS; the other buffer has been read by all
-        if (t + 1 < t_to) {
-            stage(buf ^ 1);
-            fetch(t + 2);
-            page_ids(t + 3);
+    // What is the same for every tile: where a lane finds its operands.  Values: slot 8 half + i of a product of 16 keys is key 4 half + i
+    // (i < 4) or 8 + 4 half + i - 4; a group of 16 lanes reads four keys by 16 dims: lane j points at key j / 4, dims 4 (j % 4) .. + 3, and gets
+    // dim j of the four.
+    const int vg = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), vkey = 4 * half + ((lane & 15) >> 2);
+    const auto keys_at = [&](int kslot, int kt, int i) __attribute__((always_inline)) { return __builtin_bit_cast(tk_h8, sk[kslot * TILE + k_slot<DIM>(kt * 32 + n32, 2 * i + half)]); };
+    const auto values_at = [&](uint32_t tv, int kt, int u, int d) __attribute__((always_inline)) {
+        typedef short tc_s8 __attribute__((ext_vector_type(8)));
+        const uint32_t at = tv + 16 * v_slot<DIM>(vkey, d * 4 + vg), row = (kt * 32 + u * 16) * DIM * 2;
+        const tc_s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tc_lds)(uintptr_t)(at + row));
+        const tc_s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tc_lds)(uintptr_t)(at + row + 8 * DIM * 2));
+        return __builtin_bit_cast(tk_h8, tc_s8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    };
+    tk_f16 x[2];                 // scores of a tile
+    tk_h8 pf[2][PARTS][2];       // p of the tile before
+    // values of the tile before
+    const auto add_values = [&](int vslot) __attribute__((always_inline)) {
+        const uint32_t tv = (uint32_t)(size_t)(sv + vslot * TILE) + 8 * (lane & 1);
+        tk_h8 vf[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) vf[d] = values_at(tv, 0, 0, d);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ku = 0; ku < 4; ++ku) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[d], pf[ku >> 1][p][ku & 1], o[d], 0, 0, 0);
+                if (ku < 3) vf[d] = values_at(tv, (ku + 1) >> 1, (ku + 1) & 1, d);
+            }
         }
-        const float* const s = sc + buf * 3 * TK;
-        // scores
-        tk_f16 x[2];
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // scores.  A half tile's operands are requested together, ahead of its products: read one by one, each product would wait for LDS.
+    const auto scores = [&](int kslot) __attribute__((always_inline)) {
+        tk_h8 kf[QS];
+#pragma unroll
+        for (int i = 0; i < QS; ++i) kf[i] = keys_at(kslot, 0, i);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) x[kt][v] = 0.0f;
 #pragma unroll
             for (int i = 0; i < QS; ++i) {
-                const tk_h8 kf = __builtin_bit_cast(tk_h8, sk[buf * (TK * DIM / 8) + k_slot<DIM>(kt * 32 + n32, 2 * i + half)]);
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p) x[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[p][i], x[kt], 0, 0, 0);
+                for (int p = 0; p < PARTS; ++p) x[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[i], qf[p][i], x[kt], 0, 0, 0);
+                if (kt == 0) kf[i] = keys_at(kslot, 1, i);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto softmax = [&](int t, int sslot) __attribute__((always_inline)) {
+        const float* const s = sc + sslot * 3 * TK;
         // times the keys' scales; the tile's last keys and those behind a row's own
         const bool masked = (t + 1) * TK > all || __any(s[2 * TK + lane] != 0.0f);
         float top = kNone;
@@ -209,6 +267,7 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
                 for (int i = 0; i < 4; ++i) x[kt][4 * q + i] *= ks[i];
             }
         if (masked) {
+            const int left = limit - t * TK - 4 * half;
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -216,7 +275,7 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
                     const tk_f4 none = *reinterpret_cast<const tk_f4*>(s + 2 * TK + kt * 32 + 8 * q + 4 * half);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (none[i] != 0.0f || t * TK + kt * 32 + 8 * q + 4 * half + i >= limit) x[kt][4 * q + i] = kNone;
+                        if (none[i] != 0.0f || kt * 32 + 8 * q + i >= left) x[kt][4 * q + i] = kNone;
                 }
         }
 #pragma unroll
@@ -224,25 +283,21 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
 #pragma unroll
             for (int v = 0; v < 16; ++v) top = fmaxf(top, x[kt][v]);
         top = fmaxf(top, __shfl_xor(top, 32, kWave)) * qscale;
-        const float vmax = wave_max(s[TK + lane]);
-        if (vmax > ref || __any(top > m)) {
-            const float m1 = fmaxf(m, top), ref1 = fmaxf(fmaxf(vmax, ref), 1e-30f);
-            const float keep = m == kNone ? 0.0f : __builtin_amdgcn_exp2f(m - m1);
-            const float by = keep * (ref / ref1);
-            l *= keep;
+        // (half of the raised maxima are within the factor of 2 that p may pass 1 by)
+        const float vsl = s[TK + lane];
+        if (__any(vsl > unit.ref || top > m + 0.99f)) {
+            const float m1 = fmaxf(m, top), grown = unit.raise(wave_max(vsl));
+            const float by = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - m1) + grown);
+            l *= by;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) o[d][v] *= by;
             m = m1;
-            ref = ref1;
-            unit = 32768.0f / ref1;
         }
-        // p, times the values' scales in units of 2^-15 of the largest
-        const float base = m == kNone ? 0.0f : -m;
+        const float base = m == kNone ? 0.0f : unit.up - m;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            tk_h8 pf[PARTS][2];
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const tk_f4 vs = *reinterpret_cast<const tk_f4*>(s + TK + kt * 32 + 8 * q + 4 * half);
@@ -250,43 +305,67 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
                 for (int i = 0; i < 4; ++i) {
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kt][4 * q + i], qscale, base));
                     l += p;
-                    const float w = p * (vs[i] * unit);
+                    const float w = p * vs[i];
                     _Float16 first = (_Float16)w, rest;
                     if (PARTS == 2) {
                         two_pieces(w, &first, &rest);
-                        pf[PARTS - 1][q >> 1][4 * (q & 1) + i] = rest;
+                        pf[kt][PARTS - 1][q >> 1][4 * (q & 1) + i] = rest;
                     }
-                    pf[0][q >> 1][4 * (q & 1) + i] = first;
+                    pf[kt][0][q >> 1][4 * (q & 1) + i] = first;
                 }
             }
-            // values: 16 keys at a time; slot 8 half + i of the product is key 4 half + i (i < 4) or 8 + 4 half + i - 4
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    // a group of 16 lanes reads four keys by 16 dims: lane j points at key j / 4, dims 4 (j % 4) .. + 3, and gets dim j of the four
-                    const int g4 = (lane >> 4) & 1, j = lane & 15;
-                    const int key = kt * 32 + u * 16 + 4 * half + (j >> 2), gran = d * 4 + g4 * 2 + ((j & 3) >> 1);
-                    const uint4* const at = sv + buf * (TK * DIM / 8);
-                    const uintptr_t p0 = (uintptr_t)(uint32_t)(size_t)(at + v_slot<DIM>(key, gran)) + 8 * (j & 1);
-                    const uintptr_t p1 = (uintptr_t)(uint32_t)(size_t)(at + v_slot<DIM>(key + 8, gran)) + 8 * (j & 1);
-                    const tc_s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tc_lds)p0), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tc_lds)p1);
-                    typedef short tc_s8 __attribute__((ext_vector_type(8)));
-                    const tk_h8 vf = __builtin_bit_cast(tk_h8, tc_s8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
-#pragma unroll
-                    for (int p = 0; p < PARTS; ++p) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[p][u], o[d], 0, 0, 0);
-                }
+    };
+
+    // Steps: products (scores of tile t, values of tile t - 1) and tile t + 1 to LDS, then the softmax of tile t.  With eight waves the two of a
+    // SIMD take turns, a barrier between: in turn 2 t the first has the products of tile t, in turn 2 t + 1 the second, each its softmax in
+    // the turn after.  Tile t + 1 is written in turns 2 t and 2 t + 1 and read from turn 2 t + 2 on; in its place were keys of tile t - 1, last read in
+    // turn 2 t - 1, values of tile t - 2, last read in that turn too, scales of tile t - 2, last read in turn 2 t - 2.
+    const auto turn = []() __attribute__((always_inline)) { __syncthreads(); };
+    if (t_from < t_to) {
+        page_ids(t_from);
+        fetch(t_from);
+        page_ids(t_from + 1);
+        stage(0, 0, 0);
+        fetch(t_from + 1);
+        page_ids(t_from + 2);
+        turn();
+        if (TURNS && wave >= 4) turn();
+        int vcur = 0, vnext = 1 % VT, vlast = 0, scur = 0, snext = 1;
+        const auto step = [&](const auto slot, int t) __attribute__((always_inline)) {
+            constexpr int K = decltype(slot)::value;
+            scores(K);
+            if (t > t_from) add_values(vlast);
+            if (VT == 2) turn();                     // (the values' other tile is free from here on)
+            if (t + 1 < t_to) {
+                stage(K ^ 1, vnext, snext);
+                fetch(t + 2);
+                page_ids(t + 3);
+            }
+            if (TURNS) turn();
+            softmax(t, scur);
+            turn();
+            vlast = vcur;
+            vcur = vnext;
+            vnext = vnext + 1 == VT ? 0 : vnext + 1;
+            scur = snext;
+            snext = snext + 1 == 3 ? 0 : snext + 1;
+        };
+        for (int t = t_from; t < t_to; t += 2) {
+            step(std::integral_constant<int, 0>(), t);
+            if (t + 1 < t_to) step(std::integral_constant<int, 1>(), t + 1);
         }
+        add_values(vlast);
+        if (TURNS && wave < 4) turn();
     }
 
     l += __shfl_xor(l, 32, kWave);
     if (!have) return;
     const int heads = a.c.heads * a.group;
     const size_t out_row = (size_t)(rq.token0 + token) * heads + head * a.group + gh;
-    const float out_unit = ref * (1.0f / 32768.0f);
+    const float down = __builtin_amdgcn_exp2f(-unit.up);
     if (a.splits == 1) {
-        const float by = l > 0.0f ? out_unit / l : 0.0f;
-        if (a.lse && half == 0) a.lse[out_row] = l > 0.0f ? (m + __log2f(l)) * (1.0f / kLog2e) : kNone;
+        const float by = l > 0.0f ? 1.0f / l : 0.0f;
+        if (a.lse && half == 0) a.lse[out_row] = l > 0.0f ? (m + __log2f(l * down)) * (1.0f / kLog2e) : kNone;
         T* const out = static_cast<T*>(a.out) + out_row * D;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -305,7 +384,7 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
         const size_t part_row = (size_t)split * a.tokens * heads + out_row;
         if (half == 0) {
             a.part_ml[2 * part_row] = m;
-            a.part_ml[2 * part_row + 1] = l;
+            a.part_ml[2 * part_row + 1] = l * down;
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -314,20 +393,24 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
                 const int at = 32 * d + 8 * q + 4 * half;
                 if (at < D)
                     *reinterpret_cast<float4*>(a.part_o + part_row * D + at) =
-                        make_float4(o[d][4 * q] * out_unit, o[d][4 * q + 1] * out_unit, o[d][4 * q + 2] * out_unit, o[d][4 * q + 3] * out_unit);
+                        make_float4(o[d][4 * q] * down, o[d][4 * q + 1] * down, o[d][4 * q + 2] * down, o[d][4 * q + 3] * down);
             }
     }
 }
 
-template <int TYPE, int DIM, int NW>
-hipError_t chunk_of(const AttendArgs& a, hipStream_t st) {
+template <int TYPE, int DIM, int NW, bool UNI>
+hipError_t chunk_pages(const AttendArgs& a, hipStream_t st) {
     static std::atomic<unsigned long long> done{0};
-    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&attend_chunk_kernel<TYPE, DIM, NW>), chunk_lds(DIM), done);
+    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&attend_chunk_kernel<TYPE, DIM, NW, UNI>), chunk_lds(DIM), done);
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)((long long)a.tokens * a.group / (32 * NW) + a.requests), (unsigned)a.c.heads, (unsigned)a.splits);
     KernelTimer kt(KID_ATTEND, st);
-    launch_timed(kt, (attend_chunk_kernel<TYPE, DIM, NW>), grid, dim3(64 * NW), chunk_lds(DIM), st, a);
+    launch_timed(kt, (attend_chunk_kernel<TYPE, DIM, NW, UNI>), grid, dim3(64 * NW), chunk_lds(DIM), st, a);
     return hipGetLastError();
+}
+template <int TYPE, int DIM, int NW>
+hipError_t chunk_of(const AttendArgs& a, hipStream_t st) {
+    return a.c.page_size % (1024 / DIM) == 0 ? chunk_pages<TYPE, DIM, NW, true>(a, st) : chunk_pages<TYPE, DIM, NW, false>(a, st);
 }
 template <int TYPE>
 hipError_t chunk_type(const AttendArgs& a, hipStream_t st) {

@@ -141,7 +141,8 @@ struct AttendArgs {
     void* out;               // [tokens][heads * group][dim]
     float* lse;              // [tokens][heads * group], or null
     int rows;                // rows of a block: attend_plan()
-    int splits;
+    int splits;              // blocks per row tile; blocks of 16 rows: the last one has what is left
+    int share;               // keys of one, blocks of 16 rows (a multiple of 32)
     float *part_o, *part_ml; // [splits][tokens * heads * group][dim], [..][2]
     int wide_q;
 };

@@ -473,6 +473,37 @@ def test_attend_rows_that_see_nothing(dtype, new):
     assert not got[:new - 11].any() and not got[new:2 * new].any()
 
 
+@pytest.mark.parametrize("dtype,heads,group,dim,page,new,lengths", [
+    (BF16, 2, 4, 128, 64, [1024, 700], [4096, 3001]), (F16, 2, 2, 64, 16, [900, 1500], [2500, 1500]), (F32, 1, 4, 128, 24, [600, 64], [2100, 3000]),
+    (BF16, 1, 8, 256, 32, [300, 90], [3000, 1111]), (F16, 1, 16, 128, 16, [1] * 40, list(range(7, 6000, 150)))])
+def test_attend_of_many_tiles(dtype, heads, group, dim, page, new, lengths):
+    """Hundreds of tiles of keys and several blocks, against 64 bits on the GPU; bounds as in check_attend(), the keys' spread from its definition."""
+    cache, table = make_cache(lengths, heads, dim, page, poison=False)
+    q = queries(sum(new), heads * group, dim, dtype)
+    t = torch.zeros(len(new), max(map(len, table)), dtype=torch.int32)
+    for b, row in enumerate(table):
+        t[b, :len(row)] = torch.tensor(row)
+    starts = starts_of(new)
+    args = [torch.tensor(v, dtype=torch.int32, device=DEV) for v in (starts, lengths)]
+    got = cache.attend(q, args[0], args[1], t.to(DEV), longest=max(lengths)).double()
+    e_p, e_out = {F32: (2.0**-20, 2.0**-22), BF16: (2.0**-10.9, 2.0**-8), F16: (2.0**-10.9, 2.0**-10.9)}[dtype]
+    for b, (n, L) in enumerate(zip(new, lengths)):
+        ids = torch.tensor(table[b], device=DEV)
+        k, v = ((c[ids].double() * s[ids].double()[..., None]).transpose(0, 1).reshape(heads, -1, dim)[:, :L] for c, s in ((cache.kq, cache.ks), (cache.vq, cache.vs)))
+        rows = q[starts[b]:starts[b + 1]].double().view(n, heads, group, dim)
+        last = L - n + torch.arange(n, device=DEV)
+        for h in range(heads):
+            for g in range(group):
+                a = rows[:, h, g] @ k[h].t() / math.sqrt(dim)
+                size = (rows[:, h, g].abs() @ k[h].abs().t()).amax(1) / math.sqrt(dim)
+                a = a.masked_fill(torch.arange(L, device=DEV) > last[:, None], -math.inf)
+                p = torch.softmax(a, 1)
+                want, absolute = p @ v[h], p @ v[h].abs()
+                bound = (2 * (2.0**-18 * size[:, None] + 2.0**-20) + e_p) * absolute + e_out * want.abs() + L * 127 * 2.0**-40 * cache.vs.max().double() + 2.0**-25
+                off = (got[starts[b]:starts[b + 1], h * group + g] - want).abs() / bound
+                assert float(off.max()) <= 1, (b, h, g, float(off.max()))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attend_long_context(dtype):
     lengths = [16001, 3, 8000]
