@@ -478,7 +478,7 @@ int8t_variant int8t_conv_selected_variant(int8t_op op, const int8t_conv_desc *de
  *            "deviation_finish_kernel", "igemm_kernel", "igemm_dma_kernel", "igemm_fused_kernel", "igemm_reduce_kernel",
  *            "band_kernel", "band_reg_kernel", "wgrad_kernel", "wgrad_lines_kernel", "wgrad_reduce_kernel", "s2d_repack_kernel",
  *            "conv_trio_kernel", "quantize_rows_kernel", "quantize_cols_kernel" (both passes), "transpose_codes_kernel", "product_kernel",
- *            "product_reduce_kernel", "cache_write_kernel", "cache_read_kernel", "attend_kernel", "attend_join_kernel", "dw_conv_kernel" (every depthwise forward / backward-data variant),
+ *            "product_reduce_kernel", "few_tokens_kernel", "cache_write_kernel", "cache_read_kernel", "attend_kernel", "attend_join_kernel", "dw_conv_kernel" (every depthwise forward / backward-data variant),
  *            "dw_wgrad_kernel" (every depthwise backward-weight variant), "dw_wgrad_reduce_kernel", "dw_trio_kernel", "infer_1x1_kernel");
  *            "conv_trio_kernel" and "dw_trio_kernel" are all the launches that several passes share: strided layers' and the one that
  *            quantizes depthwise tensors too;
@@ -578,7 +578,7 @@ int8t_status int8t_product(const int8_t *a_dev, const float *sa_dev, const int8_
  *             (the scale that changes along the summed axis is in the values before their codes are made)
  * int8t_linear_fwd: w NULL takes the codes at wq, sw (laid out before) as they are; xq NULL keeps no codes of x (nobody's backward
  * pass comes for them).  M may be 0 there.  int8t_linear_bwd: dx, dw, db NULL: not wanted (one of dx, dw at least); reads xq, sx,
- * wq, sw of the forward pass.
+ * wq, sw of the forward pass.  ws: int8t_linear_workspace_bytes() bytes, 16-byte aligned; may be NULL where that is 0.
  */
 typedef struct int8t_linear_desc {
     int M, K, N;
@@ -595,7 +595,8 @@ typedef struct int8t_linear_buffers {
     void *ws;
     size_t ws_bytes;
 } int8t_linear_buffers;
-size_t int8t_linear_workspace_bytes(const int8t_linear_desc *desc, int backward);
+/* direction: 0 forward, 1 backward, 2 forward that keeps no codes of x and takes those of W as they are */
+size_t int8t_linear_workspace_bytes(const int8t_linear_desc *desc, int direction);
 int8t_status int8t_linear_fwd(const int8t_linear_desc *desc, const int8t_linear_buffers *b, void *stream);
 int8t_status int8t_linear_bwd(const int8t_linear_desc *desc, const int8t_linear_buffers *b, uint64_t seed, void *stream);
 

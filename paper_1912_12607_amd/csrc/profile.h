@@ -43,6 +43,7 @@ enum KernelId : int {
     KID_TOKEN_TRANSPOSE,
     KID_TOKEN_PRODUCT,
     KID_TOKEN_REDUCE,
+    KID_TOKEN_FEW,
     KID_CACHE_WRITE,
     KID_CACHE_READ,
     KID_ATTEND,

@@ -57,9 +57,11 @@ struct FwdScratch {
     void* product;
     size_t product_bytes, bytes;
 };
-FwdScratch fwd_scratch(const int8t_linear_desc* d, void* ws) {
+// served: no codes of x are kept, those of W are there
+FwdScratch fwd_scratch(const int8t_linear_desc* d, bool served, void* ws) {
     Carve c{static_cast<unsigned char*>(ws)};
     FwdScratch s{};
+    if (served && few_tokens(d->M, pad16(d->K))) return s;
     s.xq = c.take<int8_t>(code_bytes(d->M, d->K));
     s.sx = c.take<float>((size_t)d->M * 4);
     s.product_bytes = product_scratch(d->M, d->N, pad16(d->K));
@@ -187,9 +189,9 @@ extern "C" int8t_status int8t_product(const int8_t* a_dev, const float* sa_dev, 
     return launched(launch_product(a, ws_dev ? ws_bytes : 0, (hipStream_t)stream));
 }
 
-extern "C" size_t int8t_linear_workspace_bytes(const int8t_linear_desc* d, int backward) {
-    if (linear_ok(d, backward != 0) != INT8T_OK) return 0;
-    return backward ? bwd_scratch(d, nullptr).bytes : fwd_scratch(d, nullptr).bytes;
+extern "C" size_t int8t_linear_workspace_bytes(const int8t_linear_desc* d, int direction) {
+    if (direction < 0 || direction > 2 || linear_ok(d, direction == 1) != INT8T_OK) return 0;
+    return direction == 1 ? bwd_scratch(d, nullptr).bytes : fwd_scratch(d, direction == 2, nullptr).bytes;
 }
 
 extern "C" int8t_status int8t_linear_fwd(const int8t_linear_desc* d, const int8t_linear_buffers* b, void* stream) {
@@ -198,9 +200,10 @@ extern "C" int8t_status int8t_linear_fwd(const int8t_linear_desc* d, const int8t
     if (!b || !b->wq || !b->sw) return INT8T_ERR_NULL;
     if (b->w && b->w_pitch < (size_t)d->K) return INT8T_ERR_SHAPE;
     if (!aligned16(b->wq) || !aligned16(b->sw) || !aligned(b->w, bytes_of(d->wtype)) || !aligned(b->bias, 4)) return INT8T_ERR_ARG;
-    const FwdScratch s = fwd_scratch(d, b->ws);
+    const bool served = !b->w && !b->xq;
+    const FwdScratch s = fwd_scratch(d, served, b->ws);
     if (d->M > 0) {
-        if (!b->x || !b->y || !b->ws || (!b->xq != !b->sx)) return INT8T_ERR_NULL;
+        if (!b->x || !b->y || (!b->ws && s.bytes > 0) || (!b->xq != !b->sx)) return INT8T_ERR_NULL;
         if (b->x_pitch < (size_t)d->K || b->y_pitch < (size_t)d->N) return INT8T_ERR_SHAPE;
         if (!aligned(b->x, bytes_of(d->type)) || !aligned(b->y, bytes_of(d->type)) || !aligned16(b->xq) || !aligned16(b->sx) || !aligned16(b->ws)) return INT8T_ERR_ARG;
         if (b->ws_bytes < s.bytes) return INT8T_ERR_WORKSPACE;
@@ -212,6 +215,10 @@ extern "C" int8t_status int8t_linear_fwd(const int8t_linear_desc* d, const int8t
         if (e != hipSuccess) return INT8T_ERR_RUNTIME;
     }
     if (d->M == 0) return INT8T_OK;
+    if (served && few_tokens(d->M, pad16(d->K))) {
+        const int wide = (((uintptr_t)b->x | b->x_pitch * bytes_of(d->type)) & 15) == 0;
+        return launched(launch_few_tokens(FewArgs{b->x, b->x_pitch, d->type, d->M, d->K, pad16(d->K), d->N, wide, b->wq, b->sw, b->bias, b->y, b->y_pitch}, st));
+    }
     const RowsArgs x{b->x, b->x_pitch, d->type, d->M, d->K, nullptr, 0, 0, b->xq ? b->xq : s.xq, b->sx ? b->sx : s.sx};
     hipError_t e = launch_quantize_rows(x, st);
     if (e != hipSuccess) return INT8T_ERR_RUNTIME;

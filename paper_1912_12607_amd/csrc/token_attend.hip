@@ -7,7 +7,7 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------
 // Sixteen rows (tokens times heads of a group, in order) of one request and one head of the cache per block.  The request's keys are dealt
-// out in shares of `share` to blocks and in each to eight waves, which run on their own, 32 keys at a time, the next 32 on their way
+// out in shares of `share` to blocks and in each to RW waves, which run on their own, 32 keys at a time, the next 32 on their way
 // meanwhile, and join their sums in LDS.
 //   scores   S^T[key][row] = K Q^T (16 x 16 x 32 products): a lane loads 16 bytes of a key, codes become fp16 exactly;
 //   softmax  a lane's eight scores belong to one row; running maximum shared by a row's four lanes, raised when some lane needs it;
@@ -16,9 +16,9 @@ namespace {
 // PARTS = 2 (fp32): q and p in two fp16 pieces each.  UNI: the page size is a multiple of 16, whole tiles of 16 keys lie on a page and their
 // address is scalar.  Bound by memory: codes and scales read once.
 // ------------------------------------------------------------------------------------------------
-constexpr int RW = 8;            // waves of a block
-template <int TYPE, int DIM, bool UNI>
-__global__ __launch_bounds__(64 * RW) void attend_rows_kernel(const AttendArgs a) {
+// RW waves: four (two blocks on a compute unit, one at work while the other starts or ends), or eight where there are few blocks.
+template <int TYPE, int DIM, bool UNI, int RW>
+__global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int PARTS = TYPE == kF32 ? 2 : 1, KL = DIM / 64, CB = DIM / 16;      // 16-byte loads of a key; bytes of a value row per lane
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -255,8 +255,8 @@ __global__ __launch_bounds__(64 * RW) void attend_rows_kernel(const AttendArgs a
         sm[wave][n16] = m;
         sl[wave][n16] = l * down;
     }
-    // 32 lanes per row
-    const int jr = (int)threadIdx.x >> 5, jl = (int)threadIdx.x & 31;
+    constexpr int LR = 4 * RW;                   // lanes per row
+    const int jr = (int)threadIdx.x / LR, jl = (int)threadIdx.x % LR;
     const int jt = (r0 + jr) / a.group, jg = (r0 + jr) - jt * a.group;
     const bool write = r0 + jr < nrows;
     const size_t out_row = (size_t)(rq.token0 + jt) * heads + head * a.group + jg;
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(64 * RW) void attend_rows_kernel(const AttendArgs a
                 }
             }
         }
-        constexpr int PER = HD / 32 < 2 ? 2 : HD / 32;           // dims per lane (HD 32: half of the lanes)
+        constexpr int PER = HD / LR < 2 ? 2 : HD / LR;           // dims per lane
         const int d = jl * PER;
         if (write && d < HD && h * HD + d < D) {
             float v[PER];
@@ -353,13 +353,13 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     }
 }
 
-template <int TYPE, bool UNI>
+template <int TYPE, bool UNI, int RW>
 void rows_of(const AttendArgs& a, hipStream_t st) {
     const dim3 grid((unsigned)((long long)a.tokens * a.group / 16 + a.requests), (unsigned)a.c.heads, (unsigned)a.splits);
     KernelTimer kt(KID_ATTEND, st);
-    if (a.c.dim <= 64) launch_timed(kt, (attend_rows_kernel<TYPE, 64, UNI>), grid, dim3(64 * RW), 0, st, a);
-    else if (a.c.dim <= 128) launch_timed(kt, (attend_rows_kernel<TYPE, 128, UNI>), grid, dim3(64 * RW), 0, st, a);
-    else launch_timed(kt, (attend_rows_kernel<TYPE, 256, UNI>), grid, dim3(64 * RW), 0, st, a);
+    if (a.c.dim <= 64) launch_timed(kt, (attend_rows_kernel<TYPE, 64, UNI, RW>), grid, dim3(64 * RW), 0, st, a);
+    else if (a.c.dim <= 128) launch_timed(kt, (attend_rows_kernel<TYPE, 128, UNI, RW>), grid, dim3(64 * RW), 0, st, a);
+    else launch_timed(kt, (attend_rows_kernel<TYPE, 256, UNI, RW>), grid, dim3(64 * RW), 0, st, a);
 }
 
 template <int TYPE>
@@ -368,8 +368,9 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
         const hipError_t e = launch_attend_chunk(a, st);
         if (e != hipSuccess) return e;
     } else {
-        if (a.c.page_size % 16 == 0) rows_of<TYPE, true>(a, st);
-        else rows_of<TYPE, false>(a, st);
+        const bool uni = a.c.page_size % 16 == 0;
+        if (a.waves == 8) uni ? rows_of<TYPE, true, 8>(a, st) : rows_of<TYPE, false, 8>(a, st);
+        else uni ? rows_of<TYPE, true, 4>(a, st) : rows_of<TYPE, false, 4>(a, st);
     }
     if (a.splits > 1) {
         const size_t rows = (size_t)a.tokens * a.c.heads * a.group;
@@ -387,10 +388,11 @@ void attend_plan(AttendArgs* a, int longest) {
     a->rows = each <= 32 ? 16 : each < 256 || a->c.dim > 128 ? 128 : 256;
     const long long tiles = (rows / a->rows + a->requests) * a->c.heads;
     if (a->rows == 16) {
-        // Shares of a fixed number of keys, so that long requests among short ones have more blocks: 1024, or down to 512 (two steps of a wave)
-        // where that fills the chip
-        a->share = tiles * ((longest + 1023) / 1024) >= 512 ? 1024 : 512;
+        // Shares of a fixed number of keys, so that long requests among short ones have more blocks: 2048, or down to 1024 where that brings
+        // more blocks to the chip
+        a->share = tiles * ((longest + 2047) / 2048) >= 512 ? 2048 : 1024;
         a->splits = (longest + a->share - 1) / a->share;
+        a->waves = tiles * a->splits <= 256 ? 8 : 4;
         if (a->splits > 256) {
             a->splits = 256;
             a->share = ((longest + 255) / 256 + 31) & ~31;

@@ -8,6 +8,7 @@ namespace {
 
 typedef int tp_v4i __attribute__((ext_vector_type(4)));
 typedef int tp_v16i __attribute__((ext_vector_type(16)));
+constexpr int kFewLds = 140 * 1024;      // codes of few tokens
 
 // Output tile of WM x WN waves, each MI x NJ products of 32 x 32; stages of 128 reduction bytes, two of them in LDS: while one is
 // multiplied, the next is on its way (buffer loads into LDS, rows beyond the operand and bytes beyond the reduction read as zeros).
@@ -107,6 +108,109 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     }
 }
 
+// ------------------------------------------------------------------------------------------------
+// Few tokens (at most 16) through weights that are laid out: one launch, codes of the tokens included.  Every block makes them for itself
+// in LDS -- the tokens are small and come from the caches -- and multiplies them with 16 channels at a time: a wave has an eighth of the
+// reduction, loads its 16 bytes of 16 weight rows per lane straight into the products' operand (16 x 16 x 64), and the eight sums meet in
+// LDS.  The first channels' weights are on their way while the codes are made.  Bound by reading the weights once.
+// ------------------------------------------------------------------------------------------------
+constexpr int FW = 8;            // waves
+constexpr int FL = 8;            // weight loads of a lane in flight: 512 reduction bytes of a wave
+__host__ __device__ constexpr int few_pitch(int Kp) { return ((Kp + 255) & ~255) + 16; }       // rows of codes 16 bytes apart modulo the banks
+template <int TYPE>
+__global__ __launch_bounds__(64 * FW) void few_tokens_kernel(const FewArgs a) {
+    typedef typename ElemOf<TYPE>::type T;
+    extern __shared__ __attribute__((aligned(1024))) int8_t codes[];      // [M][few_pitch]
+    __shared__ float part[FW][16], scales[16];
+    __shared__ __attribute__((aligned(16))) int sums[FW][4][64];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n16 = lane & 15, kg = lane >> 4;
+    const int pitch = few_pitch(a.Kp);
+    // this wave's part of the reduction: whole 64s
+    const int chunks = (a.Kp + 63) >> 6, c_from = chunks * wave / FW, c_to = chunks * (wave + 1) / FW;
+    const int tiles = (a.N + 15) >> 4;
+
+    uint4 w[FL];
+    auto fetch = [&](int tile, int c0) __attribute__((always_inline)) {
+        const int n = tile * 16 + n16;
+        const int8_t* const row = a.wq + (size_t)(n < a.N ? n : a.N - 1) * a.Kp;
+#pragma unroll
+        for (int i = 0; i < FL; ++i) {
+            const int k = (c0 + i) * 64 + kg * 16;
+            w[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (c0 + i < c_to && k < a.Kp) w[i] = *reinterpret_cast<const uint4*>(row + k);
+        }
+    };
+    int tile = (int)blockIdx.x;
+    fetch(tile, c_from);
+
+    // maxima, scales, codes of the tokens: a thread has eight neighbouring values of every row
+    const T* const x = static_cast<const T*>(a.x);
+    for (int m = 0; m < a.M; ++m) {
+        float top = 0.0f;
+        for (int c = tid * 8; c < a.K; c += 64 * FW * 8) {
+            float v[8];
+            load8<TYPE>(x + (size_t)m * a.x_pitch + c, a.K - c, a.wide, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[i]));
+        }
+        top = wave_max(top);
+        if (lane == 0) part[wave][m] = top;
+    }
+    __syncthreads();
+    for (int m = 0; m < a.M; ++m) {
+        float top = part[0][m];
+#pragma unroll
+        for (int i = 1; i < FW; ++i) top = fmaxf(top, part[i][m]);
+        const float inv = inv_scale_of(top);
+        if (tid == 0) scales[m] = scale_of(top);
+        for (int c = tid * 8; c < a.Kp; c += 64 * FW * 8) {
+            float v[8];
+            load8<TYPE>(x + (size_t)m * a.x_pitch + c, a.K - c, a.wide, v);
+            int q[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = quantize_one<false>(v[i], inv, 0u, 0u, 0u);
+            *reinterpret_cast<uint2*>(codes + m * pitch + c) = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+        }
+    }
+    __syncthreads();
+
+    const int8_t* const mine = codes + (n16 < a.M ? n16 : 0) * pitch + kg * 16;      // (columns of tokens that there are not: not stored)
+    for (;;) {
+        tp_v4i acc = {0, 0, 0, 0};
+        for (int c0 = c_from; c0 < c_to; c0 += FL) {
+            if (c0 > c_from) fetch(tile, c0);
+#pragma unroll
+            for (int i = 0; i < FL; ++i) {
+                // (beyond the wave's part, and beyond the row, the weights are zero: any codes will do there)
+                const int k = c0 + i < c_to ? (c0 + i) * 64 : 0;
+                const uint4 t = *reinterpret_cast<const uint4*>(mine + k);
+                acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(tp_v4i{(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w}, tp_v4i{(int)t.x, (int)t.y, (int)t.z, (int)t.w}, acc, 0, 0, 0);
+            }
+        }
+        const int next = tile + (int)gridDim.x;
+        if (next < tiles) fetch(next, c_from);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[wave][r][lane] = acc[r];
+        __syncthreads();
+        if (tid < 256) {
+            // channel 4 (lane / 16) + r of token lane % 16: neighbouring threads take neighbouring channels
+            const int n = tile * 16 + (tid & 15), m = tid >> 4, at = ((tid & 15) >> 2) * 16 + m, r = tid & 3;
+            int s = 0;
+#pragma unroll
+            for (int i = 0; i < FW; ++i) s += sums[i][r][at];
+            if (n < a.N && m < a.M) {
+                float v = __fmul_rn((float)s, __fmul_rn(scales[m], a.sw[n]));
+                if (a.bias) v = __fadd_rn(v, a.bias[n]);
+                static_cast<T*>(a.y)[(size_t)m * a.y_pitch + n] = (T)v;
+            }
+        }
+        if (next >= tiles) break;
+        tile = next;
+        __syncthreads();
+    }
+}
+
 template <int TYPE, int WM, int WN, int MI, int NJ>
 hipError_t product_of(const ProductArgs& a, hipStream_t st) {
     constexpr int BM = WM * MI * 32, BN = WN * NJ * 32, LDS = 2 * (BM + BN) * 128;
@@ -124,7 +228,25 @@ hipError_t product_type(const ProductArgs& a, hipStream_t st) {
     return product_of<TYPE, 2, 2, 2, 2>(a, st);
 }
 
+template <int TYPE>
+hipError_t few_of(const FewArgs& a, hipStream_t st) {
+    static std::atomic<unsigned long long> done{0};
+    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&few_tokens_kernel<TYPE>), kFewLds, done);
+    if (e != hipSuccess) return e;
+    const int tiles = (a.N + 15) / 16;
+    KernelTimer kt(KID_TOKEN_FEW, st);
+    launch_timed(kt, few_tokens_kernel<TYPE>, dim3(tiles < 512 ? tiles : 512), dim3(64 * FW), (size_t)a.M * few_pitch(a.Kp), st, a);
+    return hipGetLastError();
+}
+
 }  // namespace
+
+bool few_tokens(int M, int Kp) { return M <= 16 && M * few_pitch(Kp) <= kFewLds; }
+hipError_t launch_few_tokens(const FewArgs& a, hipStream_t st) {
+    if (a.type == kF32) return few_of<kF32>(a, st);
+    if (a.type == kBF16) return few_of<kBF16>(a, st);
+    return few_of<kF16>(a, st);
+}
 
 size_t product_scratch(int M, int N, int Kp) {
     (void)M; (void)N; (void)Kp;

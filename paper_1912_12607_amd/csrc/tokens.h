@@ -107,6 +107,17 @@ struct ProductArgs {         // y[m][n] = (sum_k a[m][k] b[n][k]) * (sa[m] * sb[
     int32_t* part;           // partial sums of a split reduction, or null
     int splits;
 };
+struct FewArgs {             // the same from x itself, codes made on the way: few_tokens(M, Kp)
+    const void* x;
+    size_t x_pitch;
+    int type, M, K, Kp, N, wide;
+    const int8_t* wq;
+    const float *sw, *bias;
+    void* y;
+    size_t y_pitch;
+};
+bool few_tokens(int M, int Kp);
+hipError_t launch_few_tokens(const FewArgs& a, hipStream_t st);
 size_t product_scratch(int M, int N, int Kp);
 hipError_t launch_product(ProductArgs a, size_t scratch_bytes, hipStream_t st);
 
@@ -140,7 +151,7 @@ struct AttendArgs {
     float scale;
     void* out;               // [tokens][heads * group][dim]
     float* lse;              // [tokens][heads * group], or null
-    int rows;                // rows of a block: attend_plan()
+    int rows, waves;         // of a block (waves: blocks of 16 rows): attend_plan()
     int splits;              // blocks per row tile; blocks of 16 rows: the last one has what is left
     int share;               // keys of one, blocks of 16 rows (a multiple of 32)
     float *part_o, *part_ml; // [splits][tokens * heads * group][dim], [..][2]
