@@ -123,6 +123,7 @@ AttendArgs attend_args(const int8t_cache* c, const int8t_attend_desc* d) {
     a.tokens = d->tokens;
     a.requests = d->requests;
     a.group = d->group;
+    a.by_group = fast_div((unsigned)d->group);
     a.width = d->table_width;
     a.type = d->type;
     a.causal = d->causal;

@@ -73,6 +73,13 @@ __device__ __forceinline__ float row_scale(float m, float* back) {
     return __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 254) << 23);
 }
 
+// The scores' factor, kept positive (maxima are taken before it): a negative scale goes into q through *up, and for none q becomes zero.
+__device__ __forceinline__ float score_scale(float scale, float back, float* up) {
+    if (scale < 0.0f) *up = -*up;
+    if (scale == 0.0f) *up = 0.0f;
+    return fmaxf(back * (fabsf(scale) * kLog2e), 1e-37f);
+}
+
 // The power of two that p carries: p times a value scale is held in fp16, and 2^up times the largest scale seen so far lies between 2^14 and
 // 2^15, so that it fits, with room below (p may pass 1 by a factor below 2).
 struct ValueUnit {

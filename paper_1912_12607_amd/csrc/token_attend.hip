@@ -35,12 +35,14 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
     const int heads = a.c.heads * a.group;
 
     // the block's keys: of those that its last row sees
-    const int last_token = min(r0 + 15, nrows - 1) / a.group;
-    const int seen_end = max(0, a.causal ? min(rq.length, rq.length - rq.new_tokens + last_token + 1) : rq.length);
+    const int last_token = div_by(min(r0 + 15, nrows - 1), a.by_group);
+    const int behind = rq.length - rq.new_tokens;               // keys before the new tokens
+    const int seen_end = max(0, a.causal ? min(rq.length, behind + last_token + 1) : rq.length);
+    const int all = max(0, a.causal ? min(rq.length, behind + div_by(r0, a.by_group) + 1) : rq.length);      // keys that all of its rows see
     const int from = (int)min((long long)split * a.share, (long long)seen_end), end = split + 1 == a.splits ? seen_end : min(from + a.share, seen_end);
     if (a.splits > 1 && from >= end && !(split == 0)) {              // nothing here: the joining pass looks at m alone
         if ((int)threadIdx.x < 16 && r0 + (int)threadIdx.x < nrows) {
-            const int r = r0 + (int)threadIdx.x, t = r / a.group;
+            const int r = r0 + (int)threadIdx.x, t = div_by(r, a.by_group);
             a.part_ml[2 * ((size_t)split * a.tokens * heads + (size_t)(rq.token0 + t) * heads + head * a.group + (r - t * a.group))] = kNone;
         }
         return;
@@ -49,20 +51,23 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
     // this lane's row
     const int row = r0 + n16;
     const bool have = row < nrows;
-    const int token = (have ? row : r0) / a.group, gh = (have ? row : r0) - token * a.group;
-    const int limit = !have ? 0 : a.causal ? min(rq.length, rq.length - rq.new_tokens + token + 1) : rq.length;
+    const int token = div_by(have ? row : r0, a.by_group), gh = (have ? row : r0) - token * a.group;
+    const int limit = !have ? 0 : a.causal ? min(rq.length, behind + token + 1) : rq.length;
 
     // this wave's keys: whole 32s of the block's share
     const int steps = (end - from + 31) >> 5;
     const int s_from = steps * wave / RW, s_to = steps * (wave + 1) / RW;
 
-    // ---- loader
+    // ---- loader: a step's codes and scales as they are
     uint4 kw[2][KL];                     // keys of the scores' operand: 16 t + n16
     uint32_t vw[8][CB / 4];              // slot u = 4 t + i is key 16 t + 4 kg + i, of this lane's scores and values
     float ks[8], vs[8];
-    uint32_t okl;                        // bit u: the slot's key is in the cache
+    uint32_t okl;                        // bit u: the slot's key is in the cache, and before `end`
     int ids[2];
-    const int kd = kg * 16, vd = n16 * CB < D ? n16 * CB : 0;                      // (beyond D: q is zero there, and nothing is stored)
+    uint32_t k_at[KL];                   // (beyond D: q is zero there, and nothing is stored)
+#pragma unroll
+    for (int i = 0; i < KL; ++i) k_at[i] = (uint32_t)(i * 64 + kg * 16 < D ? i * 64 + kg * 16 : 0);
+    const uint32_t v_at = (uint32_t)(n16 * CB < D ? n16 * CB : 0), key_row = (uint32_t)(n16 * D), value_row = (uint32_t)(4 * kg * D) + v_at;
     auto page_ids = [&](int s) __attribute__((always_inline)) {
         if (!UNI) return;
 #pragma unroll
@@ -83,27 +88,27 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
                 const size_t place = ((size_t)id * a.c.heads + head) * a.c.page_size + in;
                 const int8_t *kq = a.c.kq + place * D, *vq = a.c.vq + place * D;
 #pragma unroll
-                for (int i = 0; i < KL; ++i) kw[t][i] = *reinterpret_cast<const uint4*>(kq + n16 * D + (i * 64 + kd < D ? i * 64 + kd : 0));
+                for (int i = 0; i < KL; ++i) kw[t][i] = *reinterpret_cast<const uint4*>(kq + (key_row + k_at[i]));
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int c = 0; c < CB / 4; ++c) vw[4 * t + i][c] = *reinterpret_cast<const uint32_t*>(vq + (4 * kg + i) * D + vd + 4 * c);
-                const float4 k4 = *reinterpret_cast<const float4*>(a.c.ks + place + 4 * kg), v4 = *reinterpret_cast<const float4*>(a.c.vs + place + 4 * kg);
+                    for (int c = 0; c < CB / 4; ++c) vw[4 * t + i][c] = reinterpret_cast<const uint32_t*>(vq + (value_row + (uint32_t)(i * D)))[c];
+                const float4 k4 = *reinterpret_cast<const float4*>(a.c.ks + place + 4u * kg), v4 = *reinterpret_cast<const float4*>(a.c.vs + place + 4u * kg);
                 ks[4 * t] = k4.x; ks[4 * t + 1] = k4.y; ks[4 * t + 2] = k4.z; ks[4 * t + 3] = k4.w;
                 vs[4 * t] = v4.x; vs[4 * t + 1] = v4.y; vs[4 * t + 2] = v4.z; vs[4 * t + 3] = v4.w;
-                if (ok) okl |= 15u << (4 * t);
+                if (ok) okl |= (j + 16 <= end ? 15u : (1u << min(4, max(0, end - j - 4 * kg))) - 1u) << (4 * t);
             } else {
                 size_t place;
                 key_place(a, rq, head, j0 + 16 * t + n16, end, &place);
 #pragma unroll
-                for (int i = 0; i < KL; ++i) kw[t][i] = *reinterpret_cast<const uint4*>(a.c.kq + place * D + (i * 64 + kd < D ? i * 64 + kd : 0));
+                for (int i = 0; i < KL; ++i) kw[t][i] = *reinterpret_cast<const uint4*>(a.c.kq + place * D + k_at[i]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (key_place(a, rq, head, j0 + 16 * t + 4 * kg + i, end, &place)) okl |= 1u << (4 * t + i);
                     ks[4 * t + i] = a.c.ks[place];
                     vs[4 * t + i] = a.c.vs[place];
 #pragma unroll
-                    for (int c = 0; c < CB / 4; ++c) vw[4 * t + i][c] = *reinterpret_cast<const uint32_t*>(a.c.vq + place * D + vd + 4 * c);
+                    for (int c = 0; c < CB / 4; ++c) vw[4 * t + i][c] = reinterpret_cast<const uint32_t*>(a.c.vq + place * D + v_at)[c];
                 }
             }
         }
@@ -130,8 +135,8 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
         m = fmaxf(m, __shfl_xor(m, 16, kWave));
         m = fmaxf(m, __shfl_xor(m, 32, kWave));
         float back;
-        const float up = row_scale(m, &back);
-        qscale = back * (a.scale * kLog2e);
+        float up = row_scale(m, &back);
+        qscale = score_scale(a.scale, back, &up);
 #pragma unroll
         for (int i = 0; i < 2 * KL; ++i)
 #pragma unroll
@@ -174,14 +179,11 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
         }
         uint32_t vc[8][CB / 4];
         float kc[8], vsc[8];
-        bool seen[8];
+        const uint32_t in = okl;
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const int j = j0 + 16 * (u >> 2) + 4 * kg + (u & 3);
-            const bool in = ((okl >> u) & 1u) != 0 && j < end;
-            seen[u] = in && j < limit;
-            kc[u] = ks[u] * qscale;
-            vsc[u] = in ? vs[u] : 0.0f;
+            kc[u] = ks[u];
+            vsc[u] = vs[u];
 #pragma unroll
             for (int c = 0; c < CB / 4; ++c) vc[u][c] = vw[u][c] ^ 0x80808080u;
         }
@@ -189,14 +191,24 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
             fetch(s + 1);
             page_ids(s + 2);
         }
-        float x[8], top = kNone, vmax = 0.0f;
+        float x[8], top = kNone;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = sc[u >> 2][u & 3] * kc[u];
+        if (j0 + 32 > all || __any(in != 255u)) {            // some keys are not there, or not for all rows
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const bool there = ((in >> u) & 1u) != 0;
+                vsc[u] = there ? vsc[u] : 0.0f;
+                x[u] = there && j0 + 16 * (u >> 2) + 4 * kg + (u & 3) < limit ? x[u] : kNone;
+            }
+        }
+        float vmax = vsc[0];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const float t = sc[u >> 2][u & 3] * kc[u];
-            x[u] = seen[u] ? t : kNone;
             top = fmaxf(top, x[u]);
             vmax = fmaxf(vmax, vsc[u]);
         }
+        top *= qscale;
         if (__any(top > m + 0.99f || vmax > unit.ref)) {
             top = fmaxf(top, __shfl_xor(top, 16, kWave));
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
@@ -213,7 +225,7 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
         tk_h8 pf[PARTS];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const float p = __builtin_amdgcn_exp2f(x[u] + base);
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u], qscale, base));
             l += p;
             const float w = p * vsc[u];
             _Float16 first = (_Float16)w, rest;
@@ -257,7 +269,7 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
     }
     constexpr int LR = 4 * RW;                   // lanes per row
     const int jr = (int)threadIdx.x / LR, jl = (int)threadIdx.x % LR;
-    const int jt = (r0 + jr) / a.group, jg = (r0 + jr) - jt * a.group;
+    const int jt = div_by(r0 + jr, a.by_group), jg = (r0 + jr) - jt * a.group;
     const bool write = r0 + jr < nrows;
     const size_t out_row = (size_t)(rq.token0 + jt) * heads + head * a.group + jg;
     const bool whole = a.splits == 1;
@@ -321,33 +333,45 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
     }
 }
 
-// Joins the shares of a row: 16 lanes each.
+// Joins the shares of a row: 16 lanes each, which look at 16 shares' maxima and sums at a time.
 template <int TYPE>
 __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     const size_t rows = (size_t)a.tokens * a.c.heads * a.group;
     const size_t row = (size_t)blockIdx.x * 16 + ((int)threadIdx.x >> 4);
     const int l = (int)threadIdx.x & 15, D = a.c.dim;
-    if (row >= rows) return;
-    float m = kNone;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * rows + row)]);
-    float total = 0.0f;
-    for (int s = 0; s < a.splits; ++s) {
-        const float ms = a.part_ml[2 * (s * rows + row)];
-        if (ms != kNone) total += __builtin_amdgcn_exp2f(ms - m) * a.part_ml[2 * (s * rows + row) + 1];
+    const bool have = row < rows;                       // (all lanes stay for the exchanges)
+    const size_t r = have ? row : 0;
+    float m = kNone, total = 0.0f;
+    for (int s = l; s < a.splits; s += 16) {
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (s * rows + r));
+        if (ml.x == kNone) continue;
+        const float m1 = fmaxf(m, ml.x);
+        total = total * __builtin_amdgcn_exp2f(m - m1) + __builtin_amdgcn_exp2f(ml.x - m1) * ml.y;      // (m = -infinity: total is 0)
+        m = m1;
     }
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) {
+        const float m2 = __shfl_xor(m, o, kWave), t2 = __shfl_xor(total, o, kWave), m1 = fmaxf(m, m2);
+        if (m1 != kNone) total = total * __builtin_amdgcn_exp2f(m - m1) + t2 * __builtin_amdgcn_exp2f(m2 - m1);
+        m = m1;
+    }
+    if (!have) return;
     const float by = total > 0.0f ? 1.0f / total : 0.0f;
     if (l == 0 && a.lse) a.lse[row] = total > 0.0f ? (m + __log2f(total)) * (1.0f / kLog2e) : kNone;
     for (int d = l * 8; d < D; d += 128) {
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
         for (int s = 0; s < a.splits; ++s) {
             const float ms = a.part_ml[2 * (s * rows + row)];
-            if (ms == kNone) continue;
-            const float w = __builtin_amdgcn_exp2f(ms - m) * by;
+            // (a share of which nothing was seen may have written no sums: they are read -- the memory is there -- and not used)
             float p[8];
             load8<kF32>(a.part_o + (s * rows + row) * D + d, 8, true, p);
+            const float w = __builtin_amdgcn_exp2f(ms - m) * by;
+            if (ms != kNone) {
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] += w * p[u];
+                for (int u = 0; u < 8; ++u) v[u] += w * p[u];
+            }
         }
         store8<TYPE>(static_cast<T*>(a.out) + row * D + d, 8, true, v);
     }

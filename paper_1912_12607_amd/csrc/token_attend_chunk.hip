@@ -61,13 +61,13 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
     const int r0 = (int)tile * ROWS;
     const int row = r0 + 32 * wave + n32;
     const bool have = row < nrows;
-    const int token = (have ? row : r0) / a.group, gh = (have ? row : r0) - token * a.group;
+    const int token = div_by(have ? row : r0, a.by_group), gh = (have ? row : r0) - token * a.group;
     const int behind = rq.length - rq.new_tokens;               // keys before the new tokens
     const int limit = !have ? 0 : a.causal ? min(rq.length, behind + token + 1) : rq.length;
     // keys that the block's last row sees, and those that all of its rows see
-    const int last_token = min(r0 + ROWS - 1, nrows - 1) / a.group;
+    const int last_token = div_by(min(r0 + ROWS - 1, nrows - 1), a.by_group);
     const int end = max(0, a.causal ? min(rq.length, behind + last_token + 1) : rq.length);
-    const int all = max(0, a.causal ? min(rq.length, behind + r0 / a.group + 1) : rq.length);
+    const int all = max(0, a.causal ? min(rq.length, behind + div_by(r0, a.by_group) + 1) : rq.length);
     const int tiles = (end + TK - 1) / TK;
     const int t_from = (int)((long long)tiles * split / a.splits), t_to = (int)((long long)tiles * (split + 1) / a.splits);
 
@@ -88,10 +88,7 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
         m = fmaxf(m, __shfl_xor(m, 32, kWave));
         float back;
         float up = row_scale(m, &back);
-        // the scores' factor is kept positive (the maximum is taken before it): a negative scale goes into q, and for none q is zero
-        qscale = fmaxf(back * (fabsf(a.scale) * kLog2e), 1e-37f);
-        if (a.scale < 0.0f) up = -up;
-        if (a.scale == 0.0f) up = 0.0f;
+        qscale = score_scale(a.scale, back, &up);
 #pragma unroll
         for (int i = 0; i < QS; ++i)
 #pragma unroll

@@ -117,11 +117,12 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
 constexpr int FW = 8;            // waves
 constexpr int FL = 8;            // weight loads of a lane in flight: 512 reduction bytes of a wave
 __host__ __device__ constexpr int few_pitch(int Kp) { return ((Kp + 255) & ~255) + 16; }       // rows of codes 16 bytes apart modulo the banks
-template <int TYPE>
+// RM: tokens whose values are loaded together (more at a time gain nothing: 9 tokens 2048 -> 1000 with all at once 12.9 us, code to fetch).
+template <int TYPE, int RM>
 __global__ __launch_bounds__(64 * FW) void few_tokens_kernel(const FewArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     extern __shared__ __attribute__((aligned(1024))) int8_t codes[];      // [M][few_pitch]
-    __shared__ float part[FW][16], scales[16];
+    __shared__ float part[FW][16], scales[16], invs[16];
     __shared__ __attribute__((aligned(16))) int sums[FW][4][64];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, kg = lane >> 4;
@@ -146,24 +147,37 @@ __global__ __launch_bounds__(64 * FW) void few_tokens_kernel(const FewArgs a) {
 
     // maxima, scales, codes of the tokens: a thread has eight neighbouring values of every row
     const T* const x = static_cast<const T*>(a.x);
-    for (int m = 0; m < a.M; ++m) {
-        float top = 0.0f;
-        for (int c = tid * 8; c < a.K; c += 64 * FW * 8) {
-            float v[8];
-            load8<TYPE>(x + (size_t)m * a.x_pitch + c, a.K - c, a.wide, v);
+    for (int m0 = 0; m0 < a.M; m0 += RM) {
+        float top[RM];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[i]));
+        for (int m = 0; m < RM; ++m) top[m] = 0.0f;
+        for (int c = tid * 8; c < a.K; c += 64 * FW * 8) {
+#pragma unroll
+            for (int m = 0; m < RM; ++m) {
+                float v[8];
+                load8<TYPE>(x + (size_t)(m0 + m < a.M ? m0 + m : m0) * a.x_pitch + c, a.K - c, a.wide, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top[m] = fmaxf(top[m], fabsf(v[i]));
+            }
         }
-        top = wave_max(top);
-        if (lane == 0) part[wave][m] = top;
+#pragma unroll
+        for (int m = 0; m < RM; ++m) {
+            top[m] = wave_max(top[m]);
+            if (lane == 0) part[wave][(m0 + m) & 15] = top[m];          // (those beyond M: another's value, not used)
+        }
     }
     __syncthreads();
-    for (int m = 0; m < a.M; ++m) {
-        float top = part[0][m];
+    if (tid < a.M) {
+        float top = part[0][tid];
 #pragma unroll
-        for (int i = 1; i < FW; ++i) top = fmaxf(top, part[i][m]);
-        const float inv = inv_scale_of(top);
-        if (tid == 0) scales[m] = scale_of(top);
+        for (int i = 1; i < FW; ++i) top = fmaxf(top, part[i][tid]);
+        scales[tid] = scale_of(top);
+        invs[tid] = inv_scale_of(top);
+    }
+    __syncthreads();
+#pragma unroll RM
+    for (int m = 0; m < a.M; ++m) {
+        const float inv = invs[m];
         for (int c = tid * 8; c < a.Kp; c += 64 * FW * 8) {
             float v[8];
             load8<TYPE>(x + (size_t)m * a.x_pitch + c, a.K - c, a.wide, v);
@@ -228,14 +242,14 @@ hipError_t product_type(const ProductArgs& a, hipStream_t st) {
     return product_of<TYPE, 2, 2, 2, 2>(a, st);
 }
 
-template <int TYPE>
+template <int TYPE, int RM>
 hipError_t few_of(const FewArgs& a, hipStream_t st) {
     static std::atomic<unsigned long long> done{0};
-    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&few_tokens_kernel<TYPE>), kFewLds, done);
+    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&few_tokens_kernel<TYPE, RM>), kFewLds, done);
     if (e != hipSuccess) return e;
     const int tiles = (a.N + 15) / 16;
     KernelTimer kt(KID_TOKEN_FEW, st);
-    launch_timed(kt, few_tokens_kernel<TYPE>, dim3(tiles < 512 ? tiles : 512), dim3(64 * FW), (size_t)a.M * few_pitch(a.Kp), st, a);
+    launch_timed(kt, (few_tokens_kernel<TYPE, RM>), dim3(tiles < 512 ? tiles : 512), dim3(64 * FW), (size_t)a.M * few_pitch(a.Kp), st, a);
     return hipGetLastError();
 }
 
@@ -243,9 +257,11 @@ hipError_t few_of(const FewArgs& a, hipStream_t st) {
 
 bool few_tokens(int M, int Kp) { return M <= 16 && M * few_pitch(Kp) <= kFewLds; }
 hipError_t launch_few_tokens(const FewArgs& a, hipStream_t st) {
-    if (a.type == kF32) return few_of<kF32>(a, st);
-    if (a.type == kBF16) return few_of<kBF16>(a, st);
-    return few_of<kF16>(a, st);
+#define LAUNCH(TY) return a.M == 1 ? few_of<TY, 1>(a, st) : few_of<TY, 4>(a, st)
+    if (a.type == kF32) LAUNCH(kF32);
+    if (a.type == kBF16) LAUNCH(kBF16);
+    LAUNCH(kF16);
+#undef LAUNCH
 }
 
 size_t product_scratch(int M, int N, int Kp) {
