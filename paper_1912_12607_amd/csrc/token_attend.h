@@ -80,6 +80,21 @@ __device__ __forceinline__ float score_scale(float scale, float back, float* up)
     return fmaxf(back * (fabsf(scale) * kLog2e), 1e-37f);
 }
 
+// Exchanges between the halves of a wave and between neighbouring rows of 16 lanes, in registers: both sides of a pair get both values.
+struct Pair { float a, b; };
+__device__ __forceinline__ Pair halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return Pair{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ Pair rows16(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return Pair{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ float halves_max(float x) { const Pair p = halves(x); return fmaxf(p.a, p.b); }
+__device__ __forceinline__ float halves_sum(float x) { const Pair p = halves(x); return p.a + p.b; }
+__device__ __forceinline__ float rows16_max(float x) { const Pair p = rows16(x); return fmaxf(p.a, p.b); }
+__device__ __forceinline__ float rows16_sum(float x) { const Pair p = rows16(x); return p.a + p.b; }
+
 // The power of two that p carries: p times a value scale is held in fp16, and 2^up times the largest scale seen so far lies between 2^14 and
 // 2^15, so that it fits, with room below (p may pass 1 by a factor below 2).
 struct ValueUnit {

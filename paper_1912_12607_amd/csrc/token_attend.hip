@@ -21,6 +21,7 @@ template <int TYPE, int DIM, bool UNI, int RW>
 __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int PARTS = TYPE == kF32 ? 2 : 1, KL = DIM / 64, CB = DIM / 16;      // 16-byte loads of a key; bytes of a value row per lane
+    extern __shared__ __attribute__((aligned(1024))) float lds[];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n16 = lane & 15, kg = lane >> 4;
     const int head = (int)blockIdx.y, split = (int)blockIdx.z;
@@ -113,12 +114,7 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
             }
         }
     };
-    if (s_from < s_to) {
-        page_ids(s_from);
-        fetch(s_from);
-        page_ids(s_from + 1);
-    }
-
+    // q is requested first: its place is known before the keys' pages are
     tk_h8 qf[PARTS][2 * KL];
     float qscale;
     {
@@ -129,11 +125,17 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
         for (int i = 0; i < 2 * KL; ++i) {
             const int d = (i >> 1) * 64 + kg * 16 + (i & 1) * 8;
             load8<TYPE>(qp + d, D - d, a.wide_q, v[i]);
+        }
+        if (s_from < s_to) {
+            page_ids(s_from);
+            fetch(s_from);
+            page_ids(s_from + 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * KL; ++i)
 #pragma unroll
             for (int u = 0; u < 8; ++u) m = fmaxf(m, fabsf(v[i][u]));
-        }
-        m = fmaxf(m, __shfl_xor(m, 16, kWave));
-        m = fmaxf(m, __shfl_xor(m, 32, kWave));
+        m = halves_max(rows16_max(m));
         float back;
         float up = row_scale(m, &back);
         qscale = score_scale(a.scale, back, &up);
@@ -210,8 +212,7 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
         }
         top *= qscale;
         if (__any(top > m + 0.99f || vmax > unit.ref)) {
-            top = fmaxf(top, __shfl_xor(top, 16, kWave));
-            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            top = halves_max(rows16_max(top));
             const float m1 = fmaxf(m, top), grown = unit.raise(wave_max(vmax));
             const float by = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - m1) + grown);
             l *= by;
@@ -255,81 +256,72 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
             }
         }
     }
-    l += __shfl_xor(l, 16, kWave);
-    l += __shfl_xor(l, 32, kWave);
+    l = halves_sum(rows16_sum(l));
     const float down = __builtin_amdgcn_exp2f(-unit.up);
 
-    // the waves' sums, in LDS, the first half's dims and then the others: [wave][row][DIM / 2 + 4]
-    constexpr int HD = DIM / 2;
-    __shared__ float sm[RW][16], sl[RW][16];
-    __shared__ float so[RW][16][HD + 4];
+    // the waves' sums, in LDS: [wave][row][DIM + 4], in units of the values.  A lane has CB neighbouring dims of its row for each r.
+    float* const sm = lds;
+    float* const sl = sm + 16 * RW;
+    float* const so = sl + 16 * RW;
+    constexpr int PITCH = DIM + 4;
     if (kg == 0) {
-        sm[wave][n16] = m;
-        sl[wave][n16] = l * down;
+        sm[wave * 16 + n16] = m;
+        sl[wave * 16 + n16] = l * down;
     }
-    constexpr int LR = 4 * RW;                   // lanes per row
+    if (have) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < CB; c += 4)
+                *reinterpret_cast<float4*>(so + (wave * 16 + n16) * PITCH + CB * (4 * kg + r) + c) =
+                    make_float4(o[c][r] * down, o[c + 1][r] * down, o[c + 2][r] * down, o[c + 3][r] * down);
+    }
+    __syncthreads();
+    constexpr int LR = 4 * RW, PER = DIM / LR < 4 ? 4 : DIM / LR;      // lanes per row; dims of a lane
     const int jr = (int)threadIdx.x / LR, jl = (int)threadIdx.x % LR;
+    if (r0 + jr >= nrows) return;
+    float mm = sm[jr], total = 0.0f, w[RW];
+#pragma unroll
+    for (int i = 1; i < RW; ++i) mm = fmaxf(mm, sm[16 * i + jr]);
+#pragma unroll
+    for (int i = 0; i < RW; ++i) {
+        const float mi = sm[16 * i + jr];
+        w[i] = mi == kNone ? 0.0f : __builtin_amdgcn_exp2f(mi - mm);
+        total += w[i] * sl[16 * i + jr];
+    }
     const int jt = div_by(r0 + jr, a.by_group), jg = (r0 + jr) - jt * a.group;
-    const bool write = r0 + jr < nrows;
     const size_t out_row = (size_t)(rq.token0 + jt) * heads + head * a.group + jg;
     const bool whole = a.splits == 1;
     const size_t part_row = (size_t)split * a.tokens * heads + out_row;
-    float w[RW], by = 1.0f;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        // dim CB (4 kg + r) + c is in the first half where kg < 2
-        if (h) __syncthreads();
-        if ((kg >> 1) == h) {
-#pragma unroll
-            for (int c = 0; c < CB; ++c)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) so[wave][n16][CB * (4 * (kg & 1) + r) + c] = o[c][r] * down;
+    const float by = !whole ? 1.0f : total > 0.0f ? 1.0f / total : 0.0f;
+    if (jl == 0) {
+        if (whole) {
+            if (a.lse) a.lse[out_row] = total > 0.0f ? (mm + __log2f(total)) * (1.0f / kLog2e) : kNone;
+        } else {
+            a.part_ml[2 * part_row] = mm;
+            a.part_ml[2 * part_row + 1] = total;
         }
-        __syncthreads();
-        if (h == 0) {
-            float mm = sm[0][jr], total = 0.0f;
+    }
 #pragma unroll
-            for (int i = 1; i < RW; ++i) mm = fmaxf(mm, sm[i][jr]);
+    for (int c = 0; c < PER; c += 4) {
+        const int d = jl * PER + c;
+        if (d >= D) break;
+        tk_f4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < RW; ++i) {
-                w[i] = sm[i][jr] == kNone ? 0.0f : __builtin_amdgcn_exp2f(sm[i][jr] - mm);
-                total += w[i] * sl[i][jr];
-            }
-            if (whole) by = total > 0.0f ? 1.0f / total : 0.0f;
-            if (write && jl == 0) {
-                if (whole) {
-                    if (a.lse) a.lse[out_row] = total > 0.0f ? (mm + __log2f(total)) * (1.0f / kLog2e) : kNone;
-                } else {
-                    a.part_ml[2 * part_row] = mm;
-                    a.part_ml[2 * part_row + 1] = total;
-                }
-            }
+        for (int i = 0; i < RW; ++i) {
+            const tk_f4 t = *reinterpret_cast<const tk_f4*>(so + (16 * i + jr) * PITCH + d);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] += w[i] * t[u];
         }
-        constexpr int PER = HD / LR < 2 ? 2 : HD / LR;           // dims per lane
-        const int d = jl * PER;
-        if (write && d < HD && h * HD + d < D) {
-            float v[PER];
+        typedef T V __attribute__((ext_vector_type(4)));
+        V r;
 #pragma unroll
-            for (int u = 0; u < PER; ++u) {
-                v[u] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < RW; ++i) v[u] += w[i] * so[i][jr][d + u];
-                v[u] *= by;
-            }
-            if (whole) {
-                typedef T V __attribute__((ext_vector_type(PER)));
-                V r;
-#pragma unroll
-                for (int u = 0; u < PER; ++u) r[u] = (T)v[u];
-                *reinterpret_cast<V*>(static_cast<T*>(a.out) + out_row * D + h * HD + d) = r;
-            } else {
-                typedef float V __attribute__((ext_vector_type(PER)));
-                V r;
-#pragma unroll
-                for (int u = 0; u < PER; ++u) r[u] = v[u];
-                *reinterpret_cast<V*>(a.part_o + part_row * D + h * HD + d) = r;
-            }
+        for (int u = 0; u < 4; ++u) {
+            v[u] *= by;
+            r[u] = (T)v[u];
         }
+        if (whole) *reinterpret_cast<V*>(static_cast<T*>(a.out) + out_row * D + d) = r;
+        else *reinterpret_cast<tk_f4*>(a.part_o + part_row * D + d) = v;
     }
 }
 
@@ -377,13 +369,20 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     }
 }
 
-template <int TYPE, bool UNI, int RW>
-void rows_of(const AttendArgs& a, hipStream_t st) {
+template <int TYPE, int DIM, bool UNI, int RW>
+hipError_t rows_dim(const AttendArgs& a, hipStream_t st) {
+    constexpr int LDS = RW * 16 * (DIM + 4 + 2) * 4;
+    static std::atomic<unsigned long long> done{0};
+    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&attend_rows_kernel<TYPE, DIM, UNI, RW>), LDS, done);
+    if (e != hipSuccess) return e;
     const dim3 grid((unsigned)((long long)a.tokens * a.group / 16 + a.requests), (unsigned)a.c.heads, (unsigned)a.splits);
     KernelTimer kt(KID_ATTEND, st);
-    if (a.c.dim <= 64) launch_timed(kt, (attend_rows_kernel<TYPE, 64, UNI, RW>), grid, dim3(64 * RW), 0, st, a);
-    else if (a.c.dim <= 128) launch_timed(kt, (attend_rows_kernel<TYPE, 128, UNI, RW>), grid, dim3(64 * RW), 0, st, a);
-    else launch_timed(kt, (attend_rows_kernel<TYPE, 256, UNI, RW>), grid, dim3(64 * RW), 0, st, a);
+    launch_timed(kt, (attend_rows_kernel<TYPE, DIM, UNI, RW>), grid, dim3(64 * RW), LDS, st, a);
+    return hipGetLastError();
+}
+template <int TYPE, bool UNI, int RW>
+hipError_t rows_of(const AttendArgs& a, hipStream_t st) {
+    return a.c.dim <= 64 ? rows_dim<TYPE, 64, UNI, RW>(a, st) : a.c.dim <= 128 ? rows_dim<TYPE, 128, UNI, RW>(a, st) : rows_dim<TYPE, 256, UNI, RW>(a, st);
 }
 
 template <int TYPE>
@@ -393,8 +392,9 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
         if (e != hipSuccess) return e;
     } else {
         const bool uni = a.c.page_size % 16 == 0;
-        if (a.waves == 8) uni ? rows_of<TYPE, true, 8>(a, st) : rows_of<TYPE, false, 8>(a, st);
-        else uni ? rows_of<TYPE, true, 4>(a, st) : rows_of<TYPE, false, 4>(a, st);
+        const hipError_t e = a.waves == 8 ? (uni ? rows_of<TYPE, true, 8>(a, st) : rows_of<TYPE, false, 8>(a, st))
+                                          : (uni ? rows_of<TYPE, true, 4>(a, st) : rows_of<TYPE, false, 4>(a, st));
+        if (e != hipSuccess) return e;
     }
     if (a.splits > 1) {
         const size_t rows = (size_t)a.tokens * a.c.heads * a.group;

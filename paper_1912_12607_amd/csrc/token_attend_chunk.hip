@@ -85,7 +85,7 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
 #pragma unroll
             for (int u = 0; u < 8; ++u) m = fmaxf(m, fabsf(v[i][u]));
         }
-        m = fmaxf(m, __shfl_xor(m, 32, kWave));
+        m = halves_max(m);
         float back;
         float up = row_scale(m, &back);
         qscale = score_scale(a.scale, back, &up);
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int v = 0; v < 16; ++v) top = fmaxf(top, x[kt][v]);
-        top = fmaxf(top, __shfl_xor(top, 32, kWave)) * qscale;
+        top = halves_max(top) * qscale;
         // (half of the raised maxima are within the factor of 2 that p may pass 1 by)
         const float vsl = s[TK + lane];
         if (__any(vsl > unit.ref || top > m + 0.99f)) {
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
         if (TURNS && wave < 4) turn();
     }
 
-    l += __shfl_xor(l, 32, kWave);
+    l = halves_sum(l);
     if (!have) return;
     const int heads = a.c.heads * a.group;
     const size_t out_row = (size_t)(rq.token0 + token) * heads + head * a.group + gh;
