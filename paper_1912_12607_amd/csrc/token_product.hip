@@ -1,4 +1,6 @@
 // Products of 8-bit codes with a scale for each row of either operand:  y[m][n] = (float)(sum_k a[m][k] b[n][k]) * (sa[m] sb[n]) + bias[n].
+#include <type_traits>
+
 #include "device_common.h"
 #include "lds_dma.h"
 #include "tokens.h"
@@ -19,6 +21,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     constexpr int NLA = BM * KG / 64 / NW, NLB = BN * KG / 64 / NW, NL = NLA + NLB;
     static_assert((NW & 1) == 0, "the swizzle below needs an even wave count");
     extern __shared__ __attribute__((aligned(1024))) uint4 ring[];
+    __shared__ __attribute__((aligned(16))) float cscale[2 * BN];       // scales and biases of the tile's columns
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
 
@@ -42,16 +45,19 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     const uint32_t voff = (uint32_t)(8 * wave + lrow) * (uint32_t)a.Kp + (uint32_t)gran * 16u;
     const uint32_t vstep = (uint32_t)(8 * NW) * (uint32_t)a.Kp;
     const int nsteps = (a.Kp + 127) >> 7;
-    auto issue = [&](int buf, int step) {
+    auto load = [&](int buf, int step, int u) __attribute__((always_inline)) {      // the u-th of this wave's NL loads of a stage
         const uint32_t boff = (uint32_t)buf * (STAGE * 16u);
         const uint32_t past = step * 128 + gran * 16 < a.Kp ? 0u : IGD_OOB;      // beyond the reduction
         const uint32_t k = (uint32_t)__builtin_amdgcn_readfirstlane(step * 128);
-#pragma unroll
-        for (int i = 0; i < NLA; ++i) igd_load_lds(ra, lds_a + boff + (uint32_t)i * (NW * 1024), (voff + (uint32_t)i * vstep) | past, k);
-#pragma unroll
-        for (int i = 0; i < NLB; ++i) igd_load_lds(rb, lds_b + boff + (uint32_t)i * (NW * 1024), (voff + (uint32_t)i * vstep) | past, k);
+        if (u < NLA) igd_load_lds(ra, lds_a + boff + (uint32_t)u * (NW * 1024), (voff + (uint32_t)u * vstep) | past, k);
+        else igd_load_lds(rb, lds_b + boff + (uint32_t)(u - NLA) * (NW * 1024), (voff + (uint32_t)(u - NLA) * vstep) | past, k);
     };
 
+    for (int c = (int)threadIdx.x; c < BN; c += 64 * NW) {
+        const bool in = c < cols;
+        cscale[c] = in && a.sb ? a.sb[col0 + c] : 1.0f;
+        cscale[BN + c] = in && a.bias ? a.bias[col0 + c] : 0.0f;
+    }
     tp_v16i acc[MI][NJ];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -60,51 +66,118 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
 
-    issue(0, 0);
-    for (int step = 0; step < nsteps; ++step) {
-        igd_wait_vmcnt<0>();
-        __syncthreads();         // the stage is in LDS, and the one before it has been read by all
-        if (step + 1 < nsteps) issue((step + 1) & 1, step + 1);
-        const uint4* __restrict__ sA = ring + (step & 1) * STAGE;
+    // Operands of 32 reduction bytes are read while the 32 before them are multiplied, across the stages too: before a stage's last
+    // products every wave has all of the stage's operands in registers, so behind the barrier that stands there the next stage can be
+    // read and this one's place filled again.
+    tp_v4i fa[2][MI], fb[2][NJ];
+    const auto read = [&](int buf, int kk) __attribute__((always_inline)) {
+        const uint4* __restrict__ sA = ring + buf * STAGE;
         const uint4* __restrict__ sB = sA + BM * KG;
+        const int g = kk * 2 + (lane >> 5);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const uint4 t = sA[igd_slot<KG>((wm * MI + i) * 32 + (lane & 31), g)];
+            fa[kk & 1][i] = tp_v4i{(int)t.x, (int)t.y, (int)t.z, (int)t.w};
+        }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const uint4 t = sB[igd_slot<KG>((wn * NJ + j) * 32 + (lane & 31), g)];
+            fb[kk & 1][j] = tp_v4i{(int)t.x, (int)t.y, (int)t.z, (int)t.w};
+        }
+    };
+    const auto turn = []() __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+#pragma unroll
+    for (int u = 0; u < NL; ++u) load(0, 0, u);
+    constexpr int NQ = MI * NJ * 3 / NL > 0 ? MI * NJ * 3 / NL : 1;
+    static_assert((NL - 1) * NQ < MI * NJ * 4, "all loads of a stage are issued before it is waited for");
+    turn();
+#pragma unroll
+    for (int u = 0; u < NL; ++u)
+        if (u * NQ < MI * NJ && nsteps > 1) load(1, 1, u);
+    read(0, 0);
+    // The loads of a stage are dealt out between the products from the barrier on that frees their place, NQ products to a load, so that they
+    // are under way a step before they are waited for: all at once they keep the waves from their products until the last has been taken.
+    const auto stage = [&](const auto slot, int step) __attribute__((always_inline)) {
+        constexpr int BUF = decltype(slot)::value;
 #pragma unroll
         for (int kk = 0; kk < KG / 2; ++kk) {
-            const int g = kk * 2 + (lane >> 5);
-            tp_v4i fa[MI], fb[NJ];
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const uint4 t = sA[igd_slot<KG>((wm * MI + i) * 32 + (lane & 31), g)];
-                fa[i] = tp_v4i{(int)t.x, (int)t.y, (int)t.z, (int)t.w};
+            // at the last group the loads of the stage after the next begin, into this stage's place; they go on through the next stage's first two
+            if (kk + 1 < KG / 2) {
+                read(BUF, kk + 1);
+            } else if (step + 1 < nsteps) {
+                turn();
+                read(BUF ^ 1, 0);
             }
+            const bool last = kk + 1 == KG / 2;
+            const int into = last ? BUF : BUF ^ 1, which = last ? step + 2 : step + 1;
+            const int done = last ? 0 : (kk + 1) * MI * NJ;                      // products since the barrier
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const uint4 t = sB[igd_slot<KG>((wn * NJ + j) * 32 + (lane & 31), g)];
-                fb[j] = tp_v4i{(int)t.x, (int)t.y, (int)t.z, (int)t.w};
+            for (int q = 0; q < MI * NJ; ++q) {
+                const int i = q / NJ, j = q % NJ;
+                if ((done + q) % NQ == 0 && (done + q) / NQ < NL && which < nsteps) load(into, which, (done + q) / NQ);
+                acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[kk & 1][j], fa[kk & 1][i], acc[i][j], 0, 0, 0);
             }
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[i], fb[j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    for (int step = 0; step < nsteps; step += 2) {
+        stage(std::integral_constant<int, 0>(), step);
+        if (step + 1 < nsteps) stage(std::integral_constant<int, 1>(), step + 1);
     }
 
+    // Results: a lane has four neighbouring columns of a row at a time (the products' rows are b's).  They go through LDS, 32 rows of the
+    // wave at a time in a place of its own, and leave in pieces of 16 bytes, whole cache lines of a row together.
+    __syncthreads();                 // the ring has been read by all
+    constexpr int CW = NJ * 32, ES = (int)sizeof(T), RP = CW * ES + 16, VE = 16 / ES, LPR = CW / VE, RPI = 64 / LPR;
+    static_assert(NW * 32 * RP <= 2 * STAGE * 16, "the staged rows fit the ring");
+    unsigned char* const stg = reinterpret_cast<unsigned char*>(ring) + wave * 32 * RP;
+    const int n0 = col0 + wn * CW;
+    const bool wide = ((uintptr_t)a.y & 15) == 0 && (a.pitch * ES & 15) == 0;
     T* const y = static_cast<T*>(a.y);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-        const int n = col0 + (wn * NJ + j) * 32 + (lane & 31);
-        if (n >= a.N) continue;
-        const float sb = a.sb ? a.sb[n] : 1.0f, bias = a.bias ? a.bias[n] : 0.0f;
+    for (int i = 0; i < MI; ++i) {
+        const int m0 = row0 + (wm * MI + i) * 32;
+        const int m = m0 + (lane & 31);
+        const float sa = a.sa[m < a.M ? m : a.M - 1];
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int m = row0 + (wm * MI + i) * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
-                if (m < a.M) {
-                    float r = __fmul_rn((float)acc[i][j][v], __fmul_rn(a.sa[m], sb));
-                    if (a.bias) r = __fadd_rn(r, bias);
-                    y[(size_t)m * a.pitch + n] = (T)r;
+            for (int q = 0; q < 4; ++q) {
+                const int c = j * 32 + 8 * q + 4 * (lane >> 5);
+                typedef T V4 __attribute__((ext_vector_type(4)));
+                V4 o;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float sb = cscale[wn * CW + c + u];
+                    float r = __fmul_rn((float)acc[i][j][4 * q + u], __fmul_rn(sa, sb));
+                    if (a.bias) r = __fadd_rn(r, cscale[BN + wn * CW + c + u]);
+                    o[u] = (T)r;
                 }
+                *reinterpret_cast<V4*>(stg + (lane & 31) * RP + c * ES) = o;
             }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the wave's own place: no other wave reads or writes it)
+        const int pc = lane % LPR * VE, pr = lane / LPR;
+#pragma unroll
+        for (int p = 0; p < 32 / RPI; ++p) {
+            const int r = m0 + p * RPI + pr, n = n0 + pc;
+            typedef T VE_ __attribute__((ext_vector_type(VE)));
+            const VE_ t = *reinterpret_cast<const VE_*>(stg + (p * RPI + pr) * RP + pc * ES);
+            if (r >= a.M) continue;
+            T* const to = y + (size_t)r * a.pitch + n;
+            if (wide && n + VE <= a.N) {
+                *reinterpret_cast<VE_*>(to) = t;
+            } else {
+#pragma unroll
+                for (int u = 0; u < VE; ++u)
+                    if (n + u < a.N) to[u] = t[u];
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 }
 
@@ -239,7 +312,7 @@ hipError_t product_of(const ProductArgs& a, hipStream_t st) {
 
 template <int TYPE>
 hipError_t product_type(const ProductArgs& a, hipStream_t st) {
-    return product_of<TYPE, 2, 2, 2, 2>(a, st);
+    return product_of<TYPE, 2, 4, 4, 2>(a, st);
 }
 
 template <int TYPE, int RM>
