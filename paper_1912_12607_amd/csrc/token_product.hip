@@ -12,9 +12,10 @@ typedef int tp_v4i __attribute__((ext_vector_type(4)));
 typedef int tp_v16i __attribute__((ext_vector_type(16)));
 constexpr int kFewLds = 140 * 1024;      // codes of few tokens
 
-// Output tile of WM x WN waves, each MI x NJ products of 32 x 32; stages of 128 reduction bytes, two of them in LDS: while one is
-// multiplied, the next is on its way (buffer loads into LDS, rows beyond the operand and bytes beyond the reduction read as zeros).
-template <int TYPE, int WM, int WN, int MI, int NJ>
+// Output tile of WM x WN waves, each MI x NJ products of 32 x 32; stages of 128 reduction bytes, NS of them in LDS: while one is
+// multiplied, the next ones are on their way (buffer loads into LDS, rows beyond the operand and bytes beyond the reduction read as zeros).
+// SPLIT: the block has a share of the reduction and leaves its sums for product_reduce_kernel.
+template <int TYPE, int WM, int WN, int MI, int NJ, int NS, bool SPLIT>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs a, const int mtiles, const int ntiles) {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int KG = 8, NW = WM * WN, BM = WM * MI * 32, BN = WN * NJ * 32, STAGE = (BM + BN) * KG;
@@ -25,13 +26,18 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
 
-    // Workgroup b runs on XCD b % 8: an XCD takes a run of tiles, eight tiles of rows by one of columns at a time, so that the operands
-    // that its tiles share meet in its L2.
-    const int total = mtiles * ntiles, per = (total + 7) >> 3;
-    const int tile = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+    // Workgroup b runs on XCD b % 8: an XCD takes a run of tiles, four tiles of rows by one of columns at a time, so that the operands
+    // that its tiles share meet in its L2 (eight by one: 16384 tokens 4096 -> 4096 294 us instead of 285).  SPLIT: the shares of a tile's reduction
+    // are tiles of their own.
+    const int total = mtiles * ntiles * (SPLIT ? a.splits : 1), per = (total + 7) >> 3;
+    int tile = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3), share = 0;
     if (((int)blockIdx.x >> 3) >= per || tile >= total) return;
-    const int group = tile / (8 * ntiles), first = group * 8, height = mtiles - first < 8 ? mtiles - first : 8;
-    const int in = tile - group * 8 * ntiles;
+    if (SPLIT) {
+        share = tile / (mtiles * ntiles);
+        tile -= share * (mtiles * ntiles);
+    }
+    const int group = tile / (4 * ntiles), first = group * 4, height = mtiles - first < 4 ? mtiles - first : 4;
+    const int in = tile - group * 4 * ntiles;
     const int row0 = (first + in % height) * BM, col0 = (in / height) * BN;
 
     const int rows = a.M - row0 < BM ? a.M - row0 : BM, cols = a.N - col0 < BN ? a.N - col0 : BN;
@@ -44,11 +50,13 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     const int gran = (lane & 7) ^ (((lrow >> 1) & 3) | ((wave & 1) << 2));
     const uint32_t voff = (uint32_t)(8 * wave + lrow) * (uint32_t)a.Kp + (uint32_t)gran * 16u;
     const uint32_t vstep = (uint32_t)(8 * NW) * (uint32_t)a.Kp;
-    const int nsteps = (a.Kp + 127) >> 7;
+    const int all_steps = (a.Kp + 127) >> 7;
+    const int first_step = SPLIT ? all_steps * share / a.splits : 0, nsteps = SPLIT ? all_steps * (share + 1) / a.splits - first_step : all_steps;
     auto load = [&](int buf, int step, int u) __attribute__((always_inline)) {      // the u-th of this wave's NL loads of a stage
         const uint32_t boff = (uint32_t)buf * (STAGE * 16u);
-        const uint32_t past = step * 128 + gran * 16 < a.Kp ? 0u : IGD_OOB;      // beyond the reduction
-        const uint32_t k = (uint32_t)__builtin_amdgcn_readfirstlane(step * 128);
+        const int at = (first_step + step) * 128;
+        const uint32_t past = at + gran * 16 < a.Kp ? 0u : IGD_OOB;      // beyond the reduction
+        const uint32_t k = (uint32_t)__builtin_amdgcn_readfirstlane(at);
         if (u < NLA) igd_load_lds(ra, lds_a + boff + (uint32_t)u * (NW * 1024), (voff + (uint32_t)u * vstep) | past, k);
         else igd_load_lds(rb, lds_b + boff + (uint32_t)(u - NLA) * (NW * 1024), (voff + (uint32_t)(u - NLA) * vstep) | past, k);
     };
@@ -85,39 +93,45 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
             fb[kk & 1][j] = tp_v4i{(int)t.x, (int)t.y, (int)t.z, (int)t.w};
         }
     };
-    const auto turn = []() __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    // (more: the loads of the NS - 2 stages behind the next one are still under way)
+    const auto turn = [&](bool more) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (NS > 2 && more) igd_wait_vmcnt<NS == 2 ? 0 : (NS - 2) * NL>();
+        else igd_wait_vmcnt<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    // The loads of a stage are dealt out between the products from the barrier on that frees their place, NQ products to a load, so that they
+    // are under way at least a step before they are waited for: all at once they keep the waves from their products until the last has been taken.
+    constexpr int NQ = MI * NJ * 3 / NL > 0 ? MI * NJ * 3 / NL : 1, NP = MI * NJ;
+    static_assert((NL - 1) * NQ < NP * 4, "all loads of a stage are issued before the next barrier");
 #pragma unroll
-    for (int u = 0; u < NL; ++u) load(0, 0, u);
-    constexpr int NQ = MI * NJ * 3 / NL > 0 ? MI * NJ * 3 / NL : 1;
-    static_assert((NL - 1) * NQ < MI * NJ * 4, "all loads of a stage are issued before it is waited for");
-    turn();
+    for (int p = 0; p < NS - 1; ++p)
+#pragma unroll
+        for (int u = 0; u < NL; ++u)
+            if (p < nsteps) load(p, p, u);
+    turn(nsteps >= NS);
 #pragma unroll
     for (int u = 0; u < NL; ++u)
-        if (u * NQ < MI * NJ && nsteps > 1) load(1, 1, u);
+        if (u * NQ < NP && NS - 1 < nsteps) load(NS - 1, NS - 1, u);
     read(0, 0);
-    // The loads of a stage are dealt out between the products from the barrier on that frees their place, NQ products to a load, so that they
-    // are under way a step before they are waited for: all at once they keep the waves from their products until the last has been taken.
     const auto stage = [&](const auto slot, int step) __attribute__((always_inline)) {
         constexpr int BUF = decltype(slot)::value;
 #pragma unroll
         for (int kk = 0; kk < KG / 2; ++kk) {
-            // at the last group the loads of the stage after the next begin, into this stage's place; they go on through the next stage's first two
-            if (kk + 1 < KG / 2) {
+            // from the last group on the loads of NS stages ahead go into this stage's place; they go on through the next stage's other groups
+            const bool last = kk + 1 == KG / 2;
+            if (!last) {
                 read(BUF, kk + 1);
             } else if (step + 1 < nsteps) {
-                turn();
-                read(BUF ^ 1, 0);
+                turn(step + NS - 1 < nsteps);
+                read((BUF + 1) % NS, 0);
             }
-            const bool last = kk + 1 == KG / 2;
-            const int into = last ? BUF : BUF ^ 1, which = last ? step + 2 : step + 1;
-            const int done = last ? 0 : (kk + 1) * MI * NJ;                      // products since the barrier
+            const int into = last ? BUF : (BUF + NS - 1) % NS, which = last ? step + NS : step + NS - 1;
+            const int done = last ? 0 : (kk + 1) * NP;                      // products since the barrier
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int q = 0; q < MI * NJ; ++q) {
+            for (int q = 0; q < NP; ++q) {
                 const int i = q / NJ, j = q % NJ;
                 if ((done + q) % NQ == 0 && (done + q) / NQ < NL && which < nsteps) load(into, which, (done + q) / NQ);
                 acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[kk & 1][j], fa[kk & 1][i], acc[i][j], 0, 0, 0);
@@ -125,16 +139,41 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    for (int step = 0; step < nsteps; step += 2) {
+    for (int step = 0; step < nsteps; step += NS) {
         stage(std::integral_constant<int, 0>(), step);
         if (step + 1 < nsteps) stage(std::integral_constant<int, 1>(), step + 1);
+        if constexpr (NS > 2) {
+            if (step + 2 < nsteps) stage(std::integral_constant<int, 2 % NS>(), step + 2);
+        }
+        if constexpr (NS > 3) {
+            if (step + 3 < nsteps) stage(std::integral_constant<int, 3 % NS>(), step + 3);
+        }
+    }
+
+    if constexpr (SPLIT) {
+        // [share][row][column], columns padded to four
+        const int np = (a.N + 3) & ~3;
+        int32_t* const part = a.part + (size_t)share * a.M * np;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const int m = row0 + (wm * MI + i) * 32 + (lane & 31);
+            if (m >= a.M) continue;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = col0 + (wn * NJ + j) * 32 + 8 * q + 4 * (lane >> 5);
+                    if (n < a.N) *reinterpret_cast<int4*>(part + (size_t)m * np + n) = make_int4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                }
+        }
+        return;
     }
 
     // Results: a lane has four neighbouring columns of a row at a time (the products' rows are b's).  They go through LDS, 32 rows of the
     // wave at a time in a place of its own, and leave in pieces of 16 bytes, whole cache lines of a row together.
     __syncthreads();                 // the ring has been read by all
     constexpr int CW = NJ * 32, ES = (int)sizeof(T), RP = CW * ES + 16, VE = 16 / ES, LPR = CW / VE, RPI = 64 / LPR;
-    static_assert(NW * 32 * RP <= 2 * STAGE * 16, "the staged rows fit the ring");
+    static_assert(NW * 32 * RP <= NS * STAGE * 16, "the staged rows fit the ring");
     unsigned char* const stg = reinterpret_cast<unsigned char*>(ring) + wave * 32 * RP;
     const int n0 = col0 + wn * CW;
     const bool wide = ((uintptr_t)a.y & 15) == 0 && (a.pitch * ES & 15) == 0;
@@ -298,21 +337,88 @@ __global__ __launch_bounds__(64 * FW) void few_tokens_kernel(const FewArgs a) {
     }
 }
 
-template <int TYPE, int WM, int WN, int MI, int NJ>
-hipError_t product_of(const ProductArgs& a, hipStream_t st) {
-    constexpr int BM = WM * MI * 32, BN = WN * NJ * 32, LDS = 2 * (BM + BN) * 128;
+// Sums of the shares, scales, bias: four neighbouring results a lane
+template <int TYPE>
+__global__ __launch_bounds__(256) void product_reduce_kernel(const ProductArgs a) {
+    typedef typename ElemOf<TYPE>::type T;
+    const int np = (a.N + 3) & ~3, quads = np >> 2;
+    const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= (size_t)a.M * quads) return;
+    const int m = (int)(at / quads), n = (int)(at - (size_t)m * quads) * 4;
+    int4 s = make_int4(0, 0, 0, 0);
+    for (int p = 0; p < a.splits; ++p) {
+        const int4 t = *reinterpret_cast<const int4*>(a.part + ((size_t)p * a.M + m) * np + n);
+        s.x += t.x;
+        s.y += t.y;
+        s.z += t.z;
+        s.w += t.w;
+    }
+    const int v[4] = {s.x, s.y, s.z, s.w};
+    const float sa = a.sa[m];
+    T* const y = static_cast<T*>(a.y) + (size_t)m * a.pitch;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        if (n + u < a.N) {
+            float r = __fmul_rn((float)v[u], __fmul_rn(sa, a.sb ? a.sb[n + u] : 1.0f));
+            if (a.bias) r = __fadd_rn(r, a.bias[n + u]);
+            y[n + u] = (T)r;
+        }
+}
+
+template <int TYPE, int WM, int WN, int MI, int NJ, int NS, bool SPLIT>
+hipError_t product_split(const ProductArgs& a, hipStream_t st) {
+    constexpr int BM = WM * MI * 32, BN = WN * NJ * 32, LDS = NS * (BM + BN) * 128;
     static std::atomic<unsigned long long> done{0};
-    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&product_kernel<TYPE, WM, WN, MI, NJ>), LDS, done);
+    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&product_kernel<TYPE, WM, WN, MI, NJ, NS, SPLIT>), LDS, done);
     if (e != hipSuccess) return e;
     const int mt = (a.M + BM - 1) / BM, nt = (a.N + BN - 1) / BN;
-    KernelTimer kt(KID_TOKEN_PRODUCT, st);
-    launch_timed(kt, (product_kernel<TYPE, WM, WN, MI, NJ>), dim3((unsigned)((((size_t)mt * nt + 7) / 8) * 8)), dim3(64 * WM * WN), LDS, st, a, mt, nt);
+    {
+        KernelTimer kt(KID_TOKEN_PRODUCT, st);
+        launch_timed(kt, (product_kernel<TYPE, WM, WN, MI, NJ, NS, SPLIT>), dim3((unsigned)((((size_t)mt * nt * (SPLIT ? a.splits : 1) + 7) / 8) * 8)), dim3(64 * WM * WN), LDS, st,
+                     a, mt, nt);
+    }
+    if (SPLIT) {
+        KernelTimer kt(KID_TOKEN_REDUCE, st);
+        launch_timed(kt, product_reduce_kernel<TYPE>, dim3((unsigned)(((size_t)a.M * ((a.N + 3) / 4) + 255) / 256)), dim3(256), 0, st, a);
+    }
     return hipGetLastError();
+}
+template <int TYPE, int WM, int WN, int MI, int NJ, int NS>
+hipError_t product_of(const ProductArgs& a, hipStream_t st) {
+    return a.splits > 1 ? product_split<TYPE, WM, WN, MI, NJ, NS, true>(a, st) : product_split<TYPE, WM, WN, MI, NJ, NS, false>(a, st);
+}
+
+// Tiles and shares of the reduction by an estimate, us: rounds of blocks times stages of 128 reduction bytes, plus what a block and the
+// joining pass cost.  occ: blocks on a compute unit; busy: of its matrix units per stage; least: a stage of a block alone.
+struct ProductPlan {
+    int tile, splits;          // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+};
+ProductPlan product_plan(int M, int N, int Kp, bool scratch) {
+    static const struct { int bm, occ; double busy, least, fixed; } kTiles[3] = {{256, 1, 1.5, 1.5, 6.0}, {128, 2, 0.42, 0.5, 3.0}, {64, 4, 0.16, 0.3, 2.0}};
+    const int steps = (Kp + 127) >> 7;
+    ProductPlan best{0, 1};
+    double least = 1e30;
+    for (int t = 0; t < 3; ++t) {
+        const long long tiles = (long long)((M + kTiles[t].bm - 1) / kTiles[t].bm) * ((N + kTiles[t].bm - 1) / kTiles[t].bm);
+        for (int s = 1; s <= (scratch ? 16 : 1) && s <= steps; s *= 2) {
+            const long long blocks = tiles * s, slots = 256ll * kTiles[t].occ;
+            if (s > 1 && (tiles * s > 1024 || (size_t)M * N * s > (1u << 26))) break;
+            const double together = blocks >= slots ? kTiles[t].occ : (double)((blocks + 255) / 256);
+            const double stage = together * kTiles[t].busy > kTiles[t].least ? together * kTiles[t].busy : kTiles[t].least;
+            double us = (double)((blocks + slots - 1) / slots) * ((steps + s - 1) / s * stage + kTiles[t].fixed);
+            if (s > 1) us += 3.5 + 8e-6 * (double)s * M * N / 4;
+            if (us < least) {
+                least = us;
+                best = ProductPlan{t, s};
+            }
+        }
+    }
+    return best;
 }
 
 template <int TYPE>
-hipError_t product_type(const ProductArgs& a, hipStream_t st) {
-    return product_of<TYPE, 2, 4, 4, 2>(a, st);
+hipError_t product_type(const ProductArgs& a, int tile, hipStream_t st) {
+    return tile == 0 ? product_of<TYPE, 2, 4, 4, 2, 2>(a, st) : tile == 1 ? product_of<TYPE, 2, 2, 2, 2, 2>(a, st) : product_of<TYPE, 2, 2, 1, 1, 4>(a, st);
 }
 
 template <int TYPE, int RM>
@@ -338,14 +444,16 @@ hipError_t launch_few_tokens(const FewArgs& a, hipStream_t st) {
 }
 
 size_t product_scratch(int M, int N, int Kp) {
-    (void)M; (void)N; (void)Kp;
-    return 0;
+    const ProductPlan p = product_plan(M, N, Kp, true);
+    return p.splits > 1 ? (size_t)p.splits * M * ((N + 3) & ~3) * sizeof(int32_t) : 0;
 }
 hipError_t launch_product(ProductArgs a, size_t scratch_bytes, hipStream_t st) {
-    (void)scratch_bytes;
-    if (a.type == kF32) return product_type<kF32>(a, st);
-    if (a.type == kBF16) return product_type<kBF16>(a, st);
-    return product_type<kF16>(a, st);
+    const size_t need = product_scratch(a.M, a.N, a.Kp);
+    const ProductPlan p = product_plan(a.M, a.N, a.Kp, need > 0 && a.part && scratch_bytes >= need);
+    a.splits = p.splits;
+    if (a.type == kF32) return product_type<kF32>(a, p.tile, st);
+    if (a.type == kBF16) return product_type<kBF16>(a, p.tile, st);
+    return product_type<kF16>(a, p.tile, st);
 }
 
 }  // namespace int8t
