@@ -10,8 +10,6 @@
 //            of V (rows of keys, as they came) delivers: p never leaves its lane.
 // Bound by the vector units: 9 to 10 operations per score, of which the exponential counts for four, against 256 multiply-adds of the
 // matrix units (DIM 128).
-#include <type_traits>
-
 #include "token_attend.h"
 
 namespace int8t {
@@ -28,13 +26,15 @@ __device__ __forceinline__ int k_slot(int key, int g) { return DIM == 64 ? key *
 template <int DIM>
 __device__ __forceinline__ int v_slot(int key, int g) { return DIM == 64 ? key * 8 + (g ^ ((key & 2) << 1)) : key * (DIM / 8) + (g ^ ((key & 3) << 2)); }
 
-// Tiles in LDS: two of keys; three of values where they fit (a tile's values are multiplied a step after its keys), three sets of scales.
-constexpr int value_tiles(int DIM) { return DIM == 256 ? 2 : 3; }
-constexpr int chunk_lds(int DIM) { return (2 + value_tiles(DIM)) * TK * DIM * 2 + 3 * 3 * TK * 4; }
+// Tiles in LDS of keys, of values (multiplied a step after their keys) and of scales, see the steps below; and how far ahead tiles are written.
+constexpr bool takes_turns(int NW) { return NW == 8; }
+constexpr int key_tiles(int NW) { return takes_turns(NW) ? 3 : 2; }
+constexpr int value_tiles(int DIM, int NW) { return takes_turns(NW) ? 4 : DIM == 256 ? 2 : 3; }
+constexpr int chunk_lds(int DIM, int NW) { return (key_tiles(NW) + value_tiles(DIM, NW)) * TK * DIM * 2 + 3 * 3 * TK * 4; }
 
 // UNI: the keys whose pieces a wave loads at a time lie on one page (its size is a multiple of 1024 / DIM): addresses are scalar.
 template <int TYPE, int DIM, int NW, bool UNI>
-__global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && TYPE == kF32)) ? 1 : 2) void attend_chunk_kernel(const AttendArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int PARTS = TYPE == kF32 ? 2 : 1, NT = 64 * NW, ROWS = 32 * NW;
     constexpr int QS = DIM / 16, DT = DIM / 32;                // steps of the scores' products; tiles of dims
@@ -42,11 +42,11 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
     constexpr bool APART = CH < NT;                            // keys' and values' pieces to different threads
     constexpr int NP = APART ? 1 : CH / NT;                    // pieces of either tensor per thread
     extern __shared__ __attribute__((aligned(1024))) uint4 lds[];
-    constexpr int VT = value_tiles(DIM), TILE = TK * DIM / 8;
-    constexpr bool TURNS = NW == 8;                            // two waves on each SIMD that take turns, see below
-    uint4* const sk = lds;                                     // [2][TK][DIM] fp16
-    uint4* const sv = lds + 2 * TILE;                          // [VT][TK][DIM]
-    float* const sc = reinterpret_cast<float*>(lds + (2 + VT) * TILE);      // [3][3][TK]: key scales, value scales, 0 or -infinity
+    constexpr bool TURNS = takes_turns(NW);                    // two waves on each SIMD that take turns, see below
+    constexpr int KT = key_tiles(NW), VT = value_tiles(DIM, NW), TILE = TK * DIM / 8, AHEAD = TURNS ? 2 : 1;
+    uint4* const sk = lds;                                     // [KT][TK][DIM] fp16
+    uint4* const sv = lds + KT * TILE;                         // [VT][TK][DIM]
+    float* const sc = reinterpret_cast<float*>(lds + (KT + VT) * TILE);      // [3][3][TK]: key scales, value scales, 0 or -infinity
 
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, half = lane >> 5;
@@ -110,55 +110,38 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
     uint4 rk[NP], rv[NP];
     float rks[NP], rvs[NP];
     bool rok[NP];
-    int ids[NP];
+    int ids[NP], ins[NP];                                      // pages, and places on them, of the keys that are loaded next
     const int d16 = (pt % (DIM / 16)) * 16, dc = d16 < D ? d16 : 0;              // (beyond D: q is zero there, and nothing is stored)
     const int key0 = pt / (DIM / 16), wkey0 = __builtin_amdgcn_readfirstlane(key0);
     auto key_of = [&](int p) __attribute__((always_inline)) { return key0 + p * (NT / (DIM / 16)); };
-    auto page_ids = [&](int t) __attribute__((always_inline)) {                               // pages of tile t's keys
+    auto page_ids = [&](int t) __attribute__((always_inline)) {                               // of tile t's keys
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            const int j = t * TK + (UNI ? wkey0 + p * (NT / (DIM / 16)) : key_of(p));
-            ids[p] = j < end ? rq.pages[div_by(j, a.c.by_page)] : -1;
+            const int j = t * TK + (UNI ? wkey0 + p * (NT / (DIM / 16)) : key_of(p)), page = div_by(j, a.c.by_page);
+            ids[p] = j < end ? rq.pages[page] : -1;
+            ins[p] = j - page * a.c.page_size;
         }
     };
+    const size_t page_rows = (size_t)a.c.heads * a.c.page_size, head_rows = (size_t)head * a.c.page_size;
+    const uint32_t code_at = UNI ? (uint32_t)((key0 - wkey0) * D + dc) : (uint32_t)dc, scale_at = UNI ? (uint32_t)(key0 - wkey0) : 0u;      // from a wave's (a key's) place on
     auto fetch = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            const int j = t * TK + key_of(p);
-            bool ok = (unsigned)ids[p] < (unsigned)a.c.pages;
-            size_t place;
-            const int8_t *kq = a.c.kq, *vq = a.c.vq;
-            const float *ks = a.c.ks, *vs = a.c.vs;
-            uint32_t code_at, scale_at;                        // from there on
+            const bool ok = (unsigned)ids[p] < (unsigned)a.c.pages;
+            int id = ok ? ids[p] : 0, in = ok ? ins[p] : 0;
             if (UNI) {
-                const int id = __builtin_amdgcn_readfirstlane(ok ? ids[p] : 0);
-                const int jw = t * TK + wkey0 + p * (NT / (DIM / 16)), in = jw - div_by(jw, a.c.by_page) * a.c.page_size;
-                place = ((size_t)id * a.c.heads + head) * a.c.page_size + (ok ? in : 0);
-                const size_t base = place * D;
-                kq += base;
-                vq += base;
-                ks += place;
-                vs += place;
-                code_at = (uint32_t)((key0 - wkey0) * D + dc);
-                scale_at = (uint32_t)(key0 - wkey0);
-                ok = ok && j < end;
-            } else {
-                place = ok ? ((size_t)ids[p] * a.c.heads + head) * a.c.page_size + (j - div_by(j, a.c.by_page) * a.c.page_size) : 0;
-                kq += place * D;
-                vq += place * D;
-                ks += place;
-                vs += place;
-                code_at = (uint32_t)dc;
-                scale_at = 0;
+                id = __builtin_amdgcn_readfirstlane(id);
+                in = __builtin_amdgcn_readfirstlane(in);
             }
-            rok[p] = ok;
+            const size_t place = (size_t)id * page_rows + (head_rows + in), codes = place * D;
+            rok[p] = ok && t * TK + key_of(p) < end;
             if (loads_k) {
-                rk[p] = *reinterpret_cast<const uint4*>(kq + code_at);
-                rks[p] = ks[scale_at];
+                rk[p] = *reinterpret_cast<const uint4*>(a.c.kq + codes + code_at);
+                rks[p] = (a.c.ks + place)[scale_at];
             }
             if (loads_v) {
-                rv[p] = *reinterpret_cast<const uint4*>(vq + code_at);
-                rvs[p] = vs[scale_at];
+                rv[p] = *reinterpret_cast<const uint4*>(a.c.vq + codes + code_at);
+                rvs[p] = (a.c.vs + place)[scale_at];
             }
         }
     };
@@ -214,12 +197,13 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
     tk_f16 x[2];                 // scores of a tile
     tk_h8 pf[2][PARTS][2];       // p of the tile before
     // values of the tile before
-    const auto add_values = [&](int vslot) __attribute__((always_inline)) {
-        const uint32_t tv = (uint32_t)(size_t)(sv + vslot * TILE) + 8 * (lane & 1);
-        tk_h8 vf[DT];
+    tk_h8 vf[DT];
+    const auto first_values = [&](int vslot) __attribute__((always_inline)) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) vf[d] = values_at(tv, 0, 0, d);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int d = 0; d < DT; ++d) vf[d] = values_at((uint32_t)(size_t)(sv + vslot * TILE) + 8 * (lane & 1), 0, 0, d);
+    };
+    const auto add_values = [&](int vslot) __attribute__((always_inline)) {      // (the first operands are there)
+        const uint32_t tv = (uint32_t)(size_t)(sv + vslot * TILE) + 8 * (lane & 1);
 #pragma unroll
         for (int ku = 0; ku < 4; ++ku) {
 #pragma unroll
@@ -231,8 +215,9 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    // scores.  A half tile's operands are requested together, ahead of its products: read one by one, each product would wait for LDS.
-    const auto scores = [&](int kslot) __attribute__((always_inline)) {
+    // scores.  A half tile's operands are requested together, ahead of its products: read one by one, each product would wait for LDS.  The
+    // values' first ones follow (fp32: there are no registers for them yet).
+    const auto scores = [&](int kslot, int vslot) __attribute__((always_inline)) {
         tk_h8 kf[QS];
 #pragma unroll
         for (int i = 0; i < QS; ++i) kf[i] = keys_at(kslot, 0, i);
@@ -247,8 +232,9 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
                 for (int p = 0; p < PARTS; ++p) x[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[i], qf[p][i], x[kt], 0, 0, 0);
                 if (kt == 0) kf[i] = keys_at(kslot, 1, i);
             }
+            if (kt == 0 && PARTS == 1) first_values(vslot);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
     };
     const auto softmax = [&](int t, int sslot) __attribute__((always_inline)) {
         const float* const s = sc + sslot * 3 * TK;
@@ -313,44 +299,48 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
             }
     };
 
-    // Steps: products (scores of tile t, values of tile t - 1) and tile t + 1 to LDS, then the softmax of tile t.  With eight waves the two of a
-    // SIMD take turns, a barrier between: in turn 2 t the first has the products of tile t, in turn 2 t + 1 the second, each its softmax in
-    // the turn after.  Tile t + 1 is written in turns 2 t and 2 t + 1 and read from turn 2 t + 2 on; in its place were keys of tile t - 1, last read in
-    // turn 2 t - 1, values of tile t - 2, last read in that turn too, scales of tile t - 2, last read in turn 2 t - 2.
+    // Steps: products (scores of tile t, values of tile t - 1), then arithmetic (softmax of tile t, tile t + AHEAD to LDS).  With eight waves the
+    // two of a SIMD take turns, a barrier between: the first has the products of tile t in turn 2 t and its arithmetic in turn 2 t + 1, the
+    // second in turns 2 t + 1 and 2 t + 2.  Tile t + 2 is then written in turns 2 t + 1 and 2 t + 2 and read from turn 2 t + 4 on; in its place
+    // were (three tiles of keys, four of values, three of scales) the keys of tile t - 1, last read in turn 2 t - 1, the values of
+    // tile t - 2, last read in turn 2 t - 1, the scales of tile t - 1, last read in turn 2 t.  With four waves there is one barrier a step (two
+    // where only two tiles of values fit): tile t + 1 takes the place of keys of tile t - 1 and values of tile t - 2, last read before it.
     const auto turn = []() __attribute__((always_inline)) { __syncthreads(); };
     if (t_from < t_to) {
-        page_ids(t_from);
-        fetch(t_from);
-        page_ids(t_from + 1);
-        stage(0, 0, 0);
-        fetch(t_from + 1);
-        page_ids(t_from + 2);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            page_ids(t_from + i);
+            fetch(t_from + i);
+            stage(i, i, i);
+        }
+        page_ids(t_from + AHEAD);
         turn();
         if (TURNS && wave >= 4) turn();
-        int vcur = 0, vnext = 1 % VT, vlast = 0, scur = 0, snext = 1;
-        const auto step = [&](const auto slot, int t) __attribute__((always_inline)) {
-            constexpr int K = decltype(slot)::value;
-            scores(K);
-            if (t > t_from) add_values(vlast);
-            if (VT == 2) turn();                     // (the values' other tile is free from here on)
-            if (t + 1 < t_to) {
-                stage(K ^ 1, vnext, snext);
-                fetch(t + 2);
-                page_ids(t + 3);
+        int kcur = 0, knext = AHEAD % KT, vlast = 0, vcur = 0, vnext = AHEAD % VT, scur = 0, snext = AHEAD % 3;
+        const auto after = [](int slot, int n) { return slot + 1 == n ? 0 : slot + 1; };
+        for (int t = t_from; t < t_to; ++t) {
+            if (t + AHEAD < t_to) {
+                fetch(t + AHEAD);
+                page_ids(t + AHEAD + 1);
             }
-            if (TURNS) turn();
+            scores(kcur, vlast);
+            if (t > t_from) {
+                if (PARTS == 2) first_values(vlast);
+                add_values(vlast);
+            }
+            if (TURNS || VT == 2) turn();
             softmax(t, scur);
+            if (t + AHEAD < t_to) stage(knext, vnext, snext);
             turn();
             vlast = vcur;
-            vcur = vnext;
-            vnext = vnext + 1 == VT ? 0 : vnext + 1;
-            scur = snext;
-            snext = snext + 1 == 3 ? 0 : snext + 1;
-        };
-        for (int t = t_from; t < t_to; t += 2) {
-            step(std::integral_constant<int, 0>(), t);
-            if (t + 1 < t_to) step(std::integral_constant<int, 1>(), t + 1);
+            kcur = after(kcur, KT);
+            knext = after(knext, KT);
+            vcur = after(vcur, VT);
+            vnext = after(vnext, VT);
+            scur = after(scur, 3);
+            snext = after(snext, 3);
         }
+        first_values(vlast);
         add_values(vlast);
         if (TURNS && wave < 4) turn();
     }
@@ -398,11 +388,11 @@ __global__ __launch_bounds__(64 * NW, DIM == 256 ? 1 : 2) void attend_chunk_kern
 template <int TYPE, int DIM, int NW, bool UNI>
 hipError_t chunk_pages(const AttendArgs& a, hipStream_t st) {
     static std::atomic<unsigned long long> done{0};
-    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&attend_chunk_kernel<TYPE, DIM, NW, UNI>), chunk_lds(DIM), done);
+    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&attend_chunk_kernel<TYPE, DIM, NW, UNI>), chunk_lds(DIM, NW), done);
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)((long long)a.tokens * a.group / (32 * NW) + a.requests), (unsigned)a.c.heads, (unsigned)a.splits);
     KernelTimer kt(KID_ATTEND, st);
-    launch_timed(kt, (attend_chunk_kernel<TYPE, DIM, NW, UNI>), grid, dim3(64 * NW), chunk_lds(DIM), st, a);
+    launch_timed(kt, (attend_chunk_kernel<TYPE, DIM, NW, UNI>), grid, dim3(64 * NW), chunk_lds(DIM, NW), st, a);
     return hipGetLastError();
 }
 template <int TYPE, int DIM, int NW>
