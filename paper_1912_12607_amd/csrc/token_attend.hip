@@ -406,10 +406,23 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Rows of a block by the average of a request; shares of the keys.
+// Rows of a block and shares of the keys.  Blocks of 16 rows stream the cache; the larger ones of token_attend_chunk.hip multiply it, from so many
+// rows of a request on average that they are faster (us with 16 rows / with more, 8 heads, pages of 64 tokens, 16 and 8 requests over
+// 2048 keys with 64 rows each, 16 with 128, 4 over 1024 with 256, 1 over 8192 with 512 and 2048, 2 over 4096 with 4096):
+//   dim  64 bf16 (128 rows)  34/45 25/29  52/49  20/25  46/41  146/103  271/146     (256 rows: 69 34 71 29 48 103 241)
+//   dim  64 fp32 (128 rows)  39/55 27/33  60/62  23/29  54/50  177/132  309/184     (256 rows: 86 41 88 33 56 126 301)
+//   dim 128 bf16 (256 rows)  61/86 40/42  94/89  30/34  70/55  254/131  442/297     (128 rows: 101 54 110 43 82 242 345)
+//   dim 128 fp32 (128 rows)  65/126 42/65 100/138 34/52 89/104 302/306  521/436     (256 rows: 317 146 327 72 177 549 1232)
+//   dim 256 bf16 (128 rows)  152/173 91/90 238/188 74/67 170/144 602/419 1078/600
+//   dim 256 fp32 (128 rows)  240/320 138/157 378/383 116/112 268/255 973/785 1924/1125
+// Shares of the keys of larger blocks: up to a block for each compute unit (two blocks of 128 rows), of 1024 keys at least (dim 128, bf16: 128 tokens of 32 heads
+// over 8192 keys in 1, 2, 4, 8, 16 shares: 310, 170, 97, 63, 77; 4 x 128 tokens over 2048 keys: 89, 61, 72, 77, 76).
 void attend_plan(AttendArgs* a, int longest) {
     const long long rows = (long long)a->tokens * a->group, each = rows / a->requests;
-    a->rows = each <= 32 ? 16 : each < 256 || a->c.dim > 128 ? 128 : 256;
+    const bool fp32 = a->type == kF32;
+    const int dim = a->c.dim <= 64 ? 64 : a->c.dim <= 128 ? 128 : 256;
+    const int many = dim == 64 ? (fp32 ? 384 : 128) : dim == 128 ? (fp32 ? 2048 : 128) : fp32 ? 256 : 128;
+    a->rows = each < many ? 16 : dim == 128 && !fp32 ? 256 : 128;
     const long long tiles = (rows / a->rows + a->requests) * a->c.heads;
     if (a->rows == 16) {
         // Shares of a fixed number of keys, so that long requests among short ones have more blocks: 2048, or down to 1024 where that brings
@@ -424,10 +437,9 @@ void attend_plan(AttendArgs* a, int longest) {
         if (a->splits < 1) a->splits = 1;
         return;
     }
-    long long s = (a->rows == 128 ? 512 : 256) / (tiles > 0 ? tiles : 1);
-    const long long most = (longest + 255) / 256;
-    if (s > most) s = most;
-    if (s > 64) s = 64;
+    const long long blocks = (each + a->rows - 1) / a->rows * a->requests * a->c.heads;
+    long long s = (a->rows == 128 ? 512 : 256) / blocks;
+    if (s > longest / 1024) s = longest / 1024;
     a->splits = s < 1 ? 1 : (int)s;
 }
 

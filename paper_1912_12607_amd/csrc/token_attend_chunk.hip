@@ -39,8 +39,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
     constexpr int PARTS = TYPE == kF32 ? 2 : 1, NT = 64 * NW, ROWS = 32 * NW;
     constexpr int QS = DIM / 16, DT = DIM / 32;                // steps of the scores' products; tiles of dims
     constexpr int CH = 4 * DIM;                                // 16-byte pieces of a tile of codes
-    constexpr bool APART = CH < NT;                            // keys' and values' pieces to different threads
-    constexpr int NP = APART ? 1 : CH / NT;                    // pieces of either tensor per thread
+    constexpr int NP = CH / NT;                                // pieces of either tensor per thread
+    static_assert(CH % NT == 0, "whole rounds of pieces");
     extern __shared__ __attribute__((aligned(1024))) uint4 lds[];
     constexpr bool TURNS = takes_turns(NW);                    // two waves on each SIMD that take turns, see below
     constexpr int KT = key_tiles(NW), VT = value_tiles(DIM, NW), TILE = TK * DIM / 8, AHEAD = TURNS ? 2 : 1;
@@ -105,14 +105,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
 
     // ---- loader: this thread's pieces, piece p is 16 dims of a key; a wave's are those of KW neighbouring keys
     constexpr int KW = 1024 / DIM;
-    const bool loads_k = !APART || tid < CH, loads_v = !APART || (tid >= CH && tid < 2 * CH);
-    const int pt = APART ? tid % CH : tid;
     uint4 rk[NP], rv[NP];
     float rks[NP], rvs[NP];
     bool rok[NP];
     int ids[NP], ins[NP];                                      // pages, and places on them, of the keys that are loaded next
-    const int d16 = (pt % (DIM / 16)) * 16, dc = d16 < D ? d16 : 0;              // (beyond D: q is zero there, and nothing is stored)
-    const int key0 = pt / (DIM / 16), wkey0 = __builtin_amdgcn_readfirstlane(key0);
+    const int d16 = (tid % (DIM / 16)) * 16, dc = d16 < D ? d16 : 0;              // (beyond D: q is zero there, and nothing is stored)
+    const int key0 = tid / (DIM / 16), wkey0 = __builtin_amdgcn_readfirstlane(key0);
     auto key_of = [&](int p) __attribute__((always_inline)) { return key0 + p * (NT / (DIM / 16)); };
     auto page_ids = [&](int t) __attribute__((always_inline)) {                               // of tile t's keys
 #pragma unroll
@@ -135,14 +133,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
             }
             const size_t place = (size_t)id * page_rows + (head_rows + in), codes = place * D;
             rok[p] = ok && t * TK + key_of(p) < end;
-            if (loads_k) {
-                rk[p] = *reinterpret_cast<const uint4*>(a.c.kq + codes + code_at);
-                rks[p] = (a.c.ks + place)[scale_at];
-            }
-            if (loads_v) {
-                rv[p] = *reinterpret_cast<const uint4*>(a.c.vq + codes + code_at);
-                rvs[p] = (a.c.vs + place)[scale_at];
-            }
+            rk[p] = *reinterpret_cast<const uint4*>(a.c.kq + codes + code_at);
+            rks[p] = (a.c.ks + place)[scale_at];
+            rv[p] = *reinterpret_cast<const uint4*>(a.c.vq + codes + code_at);
+            rvs[p] = (a.c.vs + place)[scale_at];
         }
     };
     auto expand = [](const uint4& c, uint4* lo, uint4* hi) __attribute__((always_inline)) {
@@ -156,20 +150,16 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
             const int key = key_of(p), g = d16 >> 3;
             uint4 lo, hi;
             float* const s = sc + sslot * 3 * TK;
-            if (loads_k) {
-                expand(rk[p], &lo, &hi);
-                sk[kslot * TILE + k_slot<DIM>(key, g)] = lo;
-                sk[kslot * TILE + k_slot<DIM>(key, g + 1)] = hi;
-                if (g == 0) {
-                    s[key] = rok[p] ? rks[p] : 0.0f;
-                    s[2 * TK + key] = rok[p] ? 0.0f : kNone;
-                }
-            }
-            if (loads_v) {
-                expand(rv[p], &lo, &hi);
-                sv[vslot * TILE + v_slot<DIM>(key, g)] = lo;
-                sv[vslot * TILE + v_slot<DIM>(key, g + 1)] = hi;
-                if (g == 0) s[TK + key] = rok[p] ? rvs[p] : 0.0f;
+            expand(rk[p], &lo, &hi);
+            sk[kslot * TILE + k_slot<DIM>(key, g)] = lo;
+            sk[kslot * TILE + k_slot<DIM>(key, g + 1)] = hi;
+            expand(rv[p], &lo, &hi);
+            sv[vslot * TILE + v_slot<DIM>(key, g)] = lo;
+            sv[vslot * TILE + v_slot<DIM>(key, g + 1)] = hi;
+            if (g == 0) {
+                s[key] = rok[p] ? rks[p] : 0.0f;
+                s[TK + key] = rok[p] ? rvs[p] : 0.0f;
+                s[2 * TK + key] = rok[p] ? 0.0f : kNone;
             }
         }
     };
@@ -404,9 +394,8 @@ hipError_t chunk_of(const AttendArgs& a, hipStream_t st) {
 }
 template <int TYPE>
 hipError_t chunk_type(const AttendArgs& a, hipStream_t st) {
-    const bool many = a.rows == 256;
-    if (a.c.dim <= 64) return many ? chunk_of<TYPE, 64, 8>(a, st) : chunk_of<TYPE, 64, 4>(a, st);
-    if (a.c.dim <= 128) return many ? chunk_of<TYPE, 128, 8>(a, st) : chunk_of<TYPE, 128, 4>(a, st);
+    if (a.c.dim <= 64) return chunk_of<TYPE, 64, 4>(a, st);
+    if (a.c.dim <= 128) return chunk_of<TYPE, 128, TYPE == kF32 ? 4 : 8>(a, st);
     return chunk_of<TYPE, 256, 4>(a, st);
 }
 

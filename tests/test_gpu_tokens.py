@@ -504,6 +504,46 @@ def test_attend_of_many_tiles(dtype, heads, group, dim, page, new, lengths):
                 assert float(off.max()) <= 1, (b, h, g, float(off.max()))
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,heads,group,dim,page,new,lengths", [
+    (BF16, 2, 4, 128, 7, [40, 33, 90], [41, 500, 1300]), (F16, 1, 8, 96, 24, [17, 70], [300, 129]), (F32, 1, 4, 128, 24, [700, 600], [700, 1500]),
+    (F32, 1, 4, 112, 32, [513, 700], [2000, 611]), (F32, 2, 4, 64, 7, [130, 90], [130, 400]), (BF16, 1, 3, 48, 24, [90, 50], [77, 301]),
+    (F32, 1, 8, 256, 5, [60, 40], [200, 65]), (F16, 1, 3, 144, 16, [80, 55], [1000, 55])])
+def test_attend_of_larger_blocks(dtype, causal, heads, group, dim, page, new, lengths):
+    """Enough rows of a request for blocks of 128 or 256 rows, ragged; pages that end inside a tile and dims that end inside a block's."""
+    cache, table = make_cache(lengths, heads, dim, page)
+    q = queries(sum(new), heads * group, dim, dtype)
+    t = torch.full((len(new), max(map(len, table))), 0x7FFFFFF0, dtype=torch.int32)
+    for b, row in enumerate(table):
+        t[b, :len(row)] = torch.tensor(row)
+    starts = starts_of(new)
+    args = [torch.tensor(v, dtype=torch.int32, device=DEV) for v in (starts, lengths)]
+    got, glse = cache.attend(q, args[0], args[1], t.to(DEV), causal=causal, return_lse=True)
+    got, glse = got.double(), glse.double()
+    e_p, e_out = {F32: (2.0**-20, 2.0**-22), BF16: (2.0**-10.9, 2.0**-8), F16: (2.0**-10.9, 2.0**-10.9)}[dtype]
+    for b, (n, L) in enumerate(zip(new, lengths)):
+        ids = torch.tensor(table[b], device=DEV)
+        k, v = ((c[ids].double() * s[ids].double()[..., None]).transpose(0, 1).reshape(heads, -1, dim)[:, :L] for c, s in ((cache.kq, cache.ks), (cache.vq, cache.vs)))
+        largest = float(torch.where(torch.isfinite(cache.vs), cache.vs, torch.zeros_like(cache.vs)).max())
+        rows = q[starts[b]:starts[b + 1]].double().view(n, heads, group, dim)
+        seen = torch.arange(L, device=DEV) <= (L - n + torch.arange(n, device=DEV))[:, None] if causal else torch.ones(n, L, dtype=torch.bool, device=DEV)
+        none = ~seen.any(1)
+        for h in range(heads):
+            for g in range(group):
+                at = slice(starts[b], starts[b + 1]), h * group + g
+                a = rows[:, h, g] @ k[h].t() / math.sqrt(dim)
+                size = (rows[:, h, g].abs() @ k[h].abs().t()).amax(1) / math.sqrt(dim)
+                a = a.masked_fill(~seen, -math.inf)
+                p = torch.nan_to_num(torch.softmax(a, 1))
+                want, absolute = p @ v[h], p @ v[h].abs()
+                ds = 2.0**-18 * size + 2.0**-20
+                bound = (2 * ds[:, None] + e_p) * absolute + e_out * want.abs() + L * 127 * 2.0**-40 * largest + 2.0**-25
+                assert float(((got[at] - want).abs() / bound).max()) <= 1, (b, h, g)
+                assert not got[at][none].any() and bool((glse[at][none] == -math.inf).all())
+                lse = torch.logsumexp(a[~none], 1)
+                assert bool(((glse[at][~none] - lse).abs() <= 2 * ds[~none] + 2.0**-20 * lse.abs() + 2.0**-18).all())
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attend_long_context(dtype):
     lengths = [16001, 3, 8000]
