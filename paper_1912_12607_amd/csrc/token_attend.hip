@@ -69,6 +69,7 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
 #pragma unroll
     for (int i = 0; i < KL; ++i) k_at[i] = (uint32_t)(i * 64 + kg * 16 < D ? i * 64 + kg * 16 : 0);
     const uint32_t v_at = (uint32_t)(n16 * CB < D ? n16 * CB : 0), key_row = (uint32_t)(n16 * D), value_row = (uint32_t)(4 * kg * D) + v_at;
+    const bool quads = a.c.page_size % 4 == 0;
     auto page_ids = [&](int s) __attribute__((always_inline)) {
         if (!UNI) return;
 #pragma unroll
@@ -103,9 +104,23 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
                 key_place(a, rq, head, j0 + 16 * t + n16, end, &place);
 #pragma unroll
                 for (int i = 0; i < KL; ++i) kw[t][i] = *reinterpret_cast<const uint4*>(a.c.kq + place * D + k_at[i]);
+                const int j = j0 + 16 * t + 4 * kg;
+                if (quads) {                     // four neighbouring keys lie on a page: one look at the table for them
+                    const bool ok = key_place(a, rq, head, j, end, &place);
+                    if (ok) okl |= ((1u << min(4, end - j)) - 1u) << (4 * t);
+                    const float4 k4 = *reinterpret_cast<const float4*>(a.c.ks + place), v4 = *reinterpret_cast<const float4*>(a.c.vs + place);
+                    ks[4 * t] = k4.x; ks[4 * t + 1] = k4.y; ks[4 * t + 2] = k4.z; ks[4 * t + 3] = k4.w;
+                    vs[4 * t] = v4.x; vs[4 * t + 1] = v4.y; vs[4 * t + 2] = v4.z; vs[4 * t + 3] = v4.w;
+                    const int8_t* const vq = a.c.vq + place * D + v_at;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int c = 0; c < CB / 4; ++c) vw[4 * t + i][c] = reinterpret_cast<const uint32_t*>(vq + i * D)[c];
+                    continue;
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (key_place(a, rq, head, j0 + 16 * t + 4 * kg + i, end, &place)) okl |= 1u << (4 * t + i);
+                    if (key_place(a, rq, head, j + i, end, &place)) okl |= 1u << (4 * t + i);
                     ks[4 * t + i] = a.c.ks[place];
                     vs[4 * t + i] = a.c.vs[place];
 #pragma unroll
@@ -415,13 +430,20 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
 //   dim 128 fp32 (128 rows)  65/126 42/65 100/138 34/52 89/104 302/306  521/436     (256 rows: 317 146 327 72 177 549 1232)
 //   dim 256 bf16 (128 rows)  152/173 91/90 238/188 74/67 170/144 602/419 1078/600
 //   dim 256 fp32 (128 rows)  240/320 138/157 378/383 116/112 268/255 973/785 1924/1125
+//   pages of 24 tokens, dim 64 bf16  53/50 29/38  82/52  28/34  62/52  350/148      (the second with 32 rows each; the sixth as the seventh above)
+//   pages of 24 tokens, dim 128 fp32 101/125 41/65 153/136 54/63 115/133 756/443
+//   pages of 7 tokens,  dim 64 bf16  83/48 46/38  147/51 44/34  95/53  585/150
 // Shares of the keys of larger blocks: up to a block for each compute unit (two blocks of 128 rows), of 1024 keys at least (dim 128, bf16: 128 tokens of 32 heads
-// over 8192 keys in 1, 2, 4, 8, 16 shares: 310, 170, 97, 63, 77; 4 x 128 tokens over 2048 keys: 89, 61, 72, 77, 76).
+// over 8192 keys in 1, 2, 4, 8, 16 shares: 310, 170, 97, 63, 77; 4 x 128 tokens over 2048 keys: 89, 61, 72, 77, 76), of 256 where blocks have 128
+// rows (9 requests of 1 to 131 tokens over 0 to 1500 keys, 12 heads, dim 64, fp32, shares of 1024, 512, 256: 56, 38, 30).
 void attend_plan(AttendArgs* a, int longest) {
     const long long rows = (long long)a->tokens * a->group, each = rows / a->requests;
     const bool fp32 = a->type == kF32;
     const int dim = a->c.dim <= 64 ? 64 : a->c.dim <= 128 ? 128 : 256;
-    const int many = dim == 64 ? (fp32 ? 384 : 128) : dim == 128 ? (fp32 ? 2048 : 128) : fp32 ? 256 : 128;
+    int many = dim == 64 ? (fp32 ? 384 : 128) : dim == 128 ? (fp32 ? 2048 : 128) : fp32 ? 256 : 128;
+    // smaller ones look a table up for four keys at a time, or for each: they look less often
+    if (a->c.page_size % 4 != 0) many = 48;
+    else if (a->c.page_size % 16 != 0) many = many > 1024 ? 1024 : dim == 64 ? 64 : 128;
     a->rows = each < many ? 16 : dim == 128 && !fp32 ? 256 : 128;
     const long long tiles = (rows / a->rows + a->requests) * a->c.heads;
     if (a->rows == 16) {
@@ -439,7 +461,8 @@ void attend_plan(AttendArgs* a, int longest) {
     }
     const long long blocks = (each + a->rows - 1) / a->rows * a->requests * a->c.heads;
     long long s = (a->rows == 128 ? 512 : 256) / blocks;
-    if (s > longest / 1024) s = longest / 1024;
+    const int least = a->rows == 128 ? 256 : 1024;
+    if (s > longest / least) s = longest / least;
     a->splits = s < 1 ? 1 : (int)s;
 }
 
