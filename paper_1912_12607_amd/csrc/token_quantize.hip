@@ -6,8 +6,6 @@
 namespace int8t {
 namespace {
 
-constexpr int kRowChunks = 4;       // groups of eight values that a lane holds
-
 inline int pad16(int v) { return (v + 15) & ~15; }
 
 // Keeps the computation of eight values in front of a change of the rounding mode.
@@ -27,26 +25,26 @@ __device__ __forceinline__ uint2 codes8(const float v[8], float inv, uint32_t kx
 // One pass: a row's values are loaded once, stay in registers while their maximum is found, and leave as codes.  TPR lanes have a
 // row; rows beyond TPR * 32 values (LONG) are read a second time, from the caches.
 // Bound by memory: bytes read and written once.
-template <int TYPE, bool STOCH, int TPR, bool LONG>
+template <int TYPE, bool STOCH, int TPR, int CH, bool LONG>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quantize_rows_kernel(const RowsArgs a, const int wide, const uint32_t kx, const uint32_t ka) {
     typedef typename ElemOf<TYPE>::type T;
-    constexpr int RPB = TPR < 256 ? 256 / TPR : 1, SPAN = TPR * 8 * kRowChunks;
+    constexpr int RPB = TPR < 256 ? 256 / TPR : 1, SPAN = TPR * 8 * CH;
     const int t = (int)threadIdx.x % TPR;
     const int row = (int)blockIdx.x * RPB + (int)threadIdx.x / TPR;
     const bool live = row < a.rows;            // (all lanes stay for the reductions)
     const int Kp = (a.cols + 15) & ~15;
     const T* __restrict__ x = static_cast<const T*>(a.x) + (size_t)(live ? row : 0) * a.pitch;
     const int cols = live ? a.cols : 0;
-    float v[kRowChunks][8];
+    float v[CH][8];
     auto fetch = [&](int base) {
 #pragma unroll
-        for (int u = 0; u < kRowChunks; ++u) {
+        for (int u = 0; u < CH; ++u) {
             const int c = base + (u * TPR + t) * 8;
             load8<TYPE>(x + c, cols - c, wide, v[u]);
         }
         if (a.factor) {
 #pragma unroll
-            for (int u = 0; u < kRowChunks; ++u) {
+            for (int u = 0; u < CH; ++u) {
                 const int c = base + (u * TPR + t) * 8;
                 float f[8];
                 load8<kF32>(a.factor + c, cols - c, true, f);
@@ -59,7 +57,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quantize_rows_kernel(co
     for (int base = 0; base < (LONG ? a.cols : 1); base += SPAN) {
         fetch(base);
 #pragma unroll
-        for (int u = 0; u < kRowChunks; ++u)
+        for (int u = 0; u < CH; ++u)
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[u][i]));
     }
@@ -79,10 +77,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quantize_rows_kernel(co
     for (int base = 0; base < (LONG ? a.cols : 1); base += SPAN) {
         if (LONG) fetch(base);
 #pragma unroll
-        for (int u = 0; u < kRowChunks; ++u) pin8(v[u]);
+        for (int u = 0; u < CH; ++u) pin8(v[u]);
         if (STOCH) fp32_round_down_mode(inv, sc);
 #pragma unroll
-        for (int u = 0; u < kRowChunks; ++u) {
+        for (int u = 0; u < CH; ++u) {
             const int c = base + (u * TPR + t) * 8;
             const uint2 o = codes8<STOCH>(v[u], inv, kx, ka, (uint32_t)row * (uint32_t)a.cols + (uint32_t)c, 1u);
             if (live && c < Kp) *reinterpret_cast<uint2*>(q + c) = o;      // (values beyond the row are zero, and so are their codes)
@@ -96,10 +94,17 @@ void rows_of(const RowsArgs& a, int wide, hipStream_t st) {
     KernelTimer kt(KID_TOKEN_ROWS, st);
     const uint32_t kx = seed_key_x(a.seed), ka = seed_key_a(a.seed);
     // lanes of a row: as few as hold it, at least a wave
-    if (a.cols <= 64 * 8 * kRowChunks) launch_timed(kt, (quantize_rows_kernel<TYPE, STOCH, 64, false>), dim3((a.rows + 3) / 4), dim3(256), 0, st, a, wide, kx, ka);
-    else if (a.cols <= 256 * 8 * kRowChunks) launch_timed(kt, (quantize_rows_kernel<TYPE, STOCH, 256, false>), dim3(a.rows), dim3(256), 0, st, a, wide, kx, ka);
-    else if (a.cols <= 1024 * 8 * kRowChunks) launch_timed(kt, (quantize_rows_kernel<TYPE, STOCH, 1024, false>), dim3(a.rows), dim3(1024), 0, st, a, wide, kx, ka);
-    else launch_timed(kt, (quantize_rows_kernel<TYPE, STOCH, 1024, true>), dim3(a.rows), dim3(1024), 0, st, a, wide, kx, ka);
+#define LAUNCH(TPRv, CHv, LONGv) launch_timed(kt, (quantize_rows_kernel<TYPE, STOCH, TPRv, CHv, LONGv>), dim3(TPRv < 256 ? (a.rows + 256 / TPRv - 1) / (256 / TPRv) : a.rows), \
+                                              dim3(TPRv < 256 ? 256 : TPRv), 0, st, a, wide, kx, ka)
+    if (a.cols <= 512) LAUNCH(64, 1, false);
+    else if (a.cols <= 1024) LAUNCH(64, 2, false);
+    else if (a.cols <= 2048) LAUNCH(64, 4, false);
+    else if (a.cols <= 4096) LAUNCH(256, 2, false);
+    else if (a.cols <= 8192) LAUNCH(256, 4, false);
+    else if (a.cols <= 16384) LAUNCH(1024, 2, false);
+    else if (a.cols <= 32768) LAUNCH(1024, 4, false);
+    else LAUNCH(1024, 4, true);
+#undef LAUNCH
 }
 
 inline int wide_rows(const void* x, size_t pitch, int type) {
@@ -150,50 +155,63 @@ __global__ __launch_bounds__(256) void cols_max_kernel(const ColsArgs a, const i
     }
 }
 
-// Second pass: codes of a tile of 128 rows x 64 columns, turned in LDS, leave in runs of 128 bytes along the rows.
-constexpr int CT_R = 128, CT_C = 64, CT_PITCH = CT_R + 16;
-__device__ __forceinline__ void tile_out(const int8_t* tile, int8_t* __restrict__ q, int row0, int col0, int rows_p, int cols) {
+// Tiles of 128 rows, turned in LDS: the codes of four neighbouring rows of a column are one word, 32 words a column, and leave in runs of 128
+// bytes along the rows.  A lane has four rows of eight or sixteen columns; words 8, 16, 24 are exchanged by the column so that a wave's lanes
+// use all banks.
+constexpr int CT_R = 128, CT_PITCH = CT_R + 16;
+__device__ __forceinline__ int tile_word(int c, int w) { return c * (CT_PITCH / 4) + (w ^ (((c >> 4) & 3) << 3)); }
+template <int COLS>
+__device__ __forceinline__ void tile_out(const uint32_t* tile, int8_t* __restrict__ q, int row0, int col0, int rows_p, int cols) {
     const int g = (int)threadIdx.x & 7;
 #pragma unroll
-    for (int u = 0; u < CT_C / 32; ++u) {
+    for (int u = 0; u < COLS / 32; ++u) {
         const int c = ((int)threadIdx.x >> 3) + 32 * u;
         const int r = row0 + 16 * g;
-        if (col0 + c < cols && r < rows_p) *reinterpret_cast<uint4*>(q + (size_t)(col0 + c) * rows_p + r) = *reinterpret_cast<const uint4*>(tile + c * CT_PITCH + 16 * g);
+        if (col0 + c < cols && r < rows_p) *reinterpret_cast<uint4*>(q + (size_t)(col0 + c) * rows_p + r) = *reinterpret_cast<const uint4*>(tile + tile_word(c, 4 * g));
     }
 }
+// Second pass: codes of a tile of 128 rows x 64 columns
+constexpr int CT_C = 64;
 template <int TYPE, bool STOCH>
 __global__ __launch_bounds__(256) void cols_codes_kernel(const ColsArgs a, const int wide, const uint32_t kx, const uint32_t ka) {
     typedef typename ElemOf<TYPE>::type T;
-    __shared__ __attribute__((aligned(16))) int8_t tile[CT_C * CT_PITCH];
+    __shared__ __attribute__((aligned(16))) uint32_t tile[CT_C * CT_PITCH / 4];
     __shared__ __attribute__((aligned(16))) float invs[CT_C];
     const int col0 = (int)blockIdx.x * CT_C, row0 = (int)blockIdx.y * CT_R;
+    // the parts' maxima: four lanes a column
+    __shared__ float tops[4][CT_C];
+    {
+        const int c = (int)threadIdx.x & (CT_C - 1), p0 = (int)threadIdx.x / CT_C;
+        const float* const part = a.part_max + (col0 + c < a.cols ? col0 + c : 0);
+        float m = 0.0f;
+#pragma unroll 8
+        for (int p = p0; p < a.parts; p += 4) m = fmaxf(m, part[(size_t)p * a.cols]);
+        tops[p0][c] = m;
+    }
+    __syncthreads();
     if (threadIdx.x < CT_C) {
         const int c = col0 + (int)threadIdx.x;
-        float m = 0.0f;
-        if (c < a.cols) {
-            for (int p = 0; p < a.parts; ++p) m = fmaxf(m, a.part_max[(size_t)p * a.cols + c]);
-            if (blockIdx.y == 0) {
-                a.scale[c] = scale_of(m);
-                if (a.sum) {
-                    double s = 0.0;
-                    for (int p = 0; p < a.parts; ++p) s += (double)a.part_sum[(size_t)p * a.cols + c];
-                    a.sum[c] = (float)s;
-                }
+        const float m = fmaxf(fmaxf(tops[0][threadIdx.x], tops[1][threadIdx.x]), fmaxf(tops[2][threadIdx.x], tops[3][threadIdx.x]));
+        if (blockIdx.y == 0 && c < a.cols) {
+            a.scale[c] = scale_of(m);
+            if (a.sum) {
+                double s = 0.0;
+                for (int p = 0; p < a.parts; ++p) s += (double)a.part_sum[(size_t)p * a.cols + c];
+                a.sum[c] = (float)s;
             }
         }
         const float inv = inv_scale_of(m);
         invs[threadIdx.x] = STOCH ? __fmul_rn(inv, kTwo24) : inv;
     }
     __syncthreads();
-    const int cg = (int)threadIdx.x & 7, r0 = (int)threadIdx.x >> 3;
-    const int col = col0 + cg * 8;
-    constexpr int NV = CT_R / 32;
-    float v[NV][8], inv[8];
+    const int cg = (int)threadIdx.x & 7, rq = (int)threadIdx.x >> 3;
+    const int col = col0 + cg * 8, row = row0 + 4 * rq;
+    float v[4][8], inv[8];
 #pragma unroll
-    for (int u = 0; u < NV; ++u) {
-        const int r = row0 + r0 + 32 * u;
-        load8<TYPE>(static_cast<const T*>(a.x) + (size_t)(r < a.rows ? r : 0) * a.pitch + col, r < a.rows ? a.cols - col : 0, wide, v[u]);
-        const float f = a.factor && r < a.rows ? a.factor[r] : 1.0f;
+    for (int u = 0; u < 4; ++u) {
+        const bool in = row + u < a.rows;
+        load8<TYPE>(static_cast<const T*>(a.x) + (size_t)(in ? row + u : 0) * a.pitch + col, in ? a.cols - col : 0, wide, v[u]);
+        const float f = a.factor && in ? a.factor[row + u] : 1.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[u][i] = __fmul_rn(v[u][i], f);
         pin8(v[u]);
@@ -206,16 +224,15 @@ __global__ __launch_bounds__(256) void cols_codes_kernel(const ColsArgs a, const
         fp32_round_down_mode(inv[0], dummy);
     }
 #pragma unroll
-    for (int u = 0; u < NV; ++u) {
-        const int r = r0 + 32 * u;
+    for (int i = 0; i < 8; ++i) {
+        int c[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t index = (uint32_t)(row0 + r) * (uint32_t)a.cols + (uint32_t)(col + i);
-            tile[(cg * 8 + i) * CT_PITCH + r] = (int8_t)quantize_one<STOCH>(v[u][i], inv[i], kx, ka, index);
-        }
+        for (int u = 0; u < 4; ++u)
+            c[u] = quantize_one<STOCH>(v[u][i], inv[i], kx, ka, (uint32_t)(row + u) * (uint32_t)a.cols + (uint32_t)(col + i));
+        tile[tile_word(cg * 8 + i, rq)] = pack4(c[0], c[1], c[2], c[3]);
     }
     __syncthreads();
-    tile_out(tile, a.q, row0, col0, (a.rows + 15) & ~15, a.cols);
+    tile_out<CT_C>(tile, a.q, row0, col0, (a.rows + 15) & ~15, a.cols);
 }
 
 template <int TYPE>
@@ -231,23 +248,31 @@ void cols_of(const ColsArgs& a, int wide, hipStream_t st) {
     else launch_timed(kt, (cols_codes_kernel<TYPE, false>), grid, dim3(256), 0, st, a, wide, kx, ka);
 }
 
-// Codes [rows][pad16(cols)] -> [cols][pad16(rows)]
+// Codes [rows][pad16(cols)] -> [cols][pad16(rows)], tiles of 128 x 128
+constexpr int TT_C = 128;
 __global__ __launch_bounds__(256) void transpose_codes_kernel(const int8_t* __restrict__ q, const int rows, const int cols, int8_t* __restrict__ qt) {
-    __shared__ __attribute__((aligned(16))) int8_t tile[CT_C * CT_PITCH];
-    const int col0 = (int)blockIdx.x * CT_C, row0 = (int)blockIdx.y * CT_R;
+    __shared__ __attribute__((aligned(16))) uint32_t tile[TT_C * CT_PITCH / 4];
+    const int col0 = (int)blockIdx.x * TT_C, row0 = (int)blockIdx.y * CT_R;
     const int Kp = (cols + 15) & ~15;
-    const int g = (int)threadIdx.x & 3, r0 = (int)threadIdx.x >> 2;
+    const int g = (int)threadIdx.x & 7, rq = (int)threadIdx.x >> 3;
+    const int c = col0 + 16 * g, row = row0 + 4 * rq;
+    uint4 t[4];
 #pragma unroll
-    for (int u = 0; u < CT_R / 64; ++u) {
-        const int r = r0 + 64 * u, c = col0 + 16 * g;
-        uint4 t = make_uint4(0u, 0u, 0u, 0u);
-        if (row0 + r < rows && c < Kp) t = *reinterpret_cast<const uint4*>(q + (size_t)(row0 + r) * Kp + c);
-        const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+    for (int u = 0; u < 4; ++u) {
+        t[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (row + u < rows && c < Kp) t[u] = *reinterpret_cast<const uint4*>(q + (size_t)(row + u) * Kp + c);
+    }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) tile[(16 * g + i) * CT_PITCH + r] = (int8_t)(w[i >> 2] >> (8 * (i & 3)));
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t d[4] = {w == 0 ? t[0].x : w == 1 ? t[0].y : w == 2 ? t[0].z : t[0].w, w == 0 ? t[1].x : w == 1 ? t[1].y : w == 2 ? t[1].z : t[1].w,
+                               w == 0 ? t[2].x : w == 1 ? t[2].y : w == 2 ? t[2].z : t[2].w, w == 0 ? t[3].x : w == 1 ? t[3].y : w == 2 ? t[3].z : t[3].w};
+        uint32_t o[4];
+        transpose4x4_bytes(d, o);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tile[tile_word(16 * g + 4 * w + i, rq)] = o[i];
     }
     __syncthreads();
-    tile_out(tile, qt, row0, col0, (rows + 15) & ~15, cols);
+    tile_out<TT_C>(tile, qt, row0, col0, (rows + 15) & ~15, cols);
 }
 
 }  // namespace
@@ -276,7 +301,7 @@ hipError_t launch_quantize_cols(const ColsArgs& a, hipStream_t st) {
 }
 hipError_t launch_transpose_codes(const int8_t* q, int rows, int cols, int8_t* qt, hipStream_t st) {
     KernelTimer kt(KID_TOKEN_TRANSPOSE, st);
-    launch_timed(kt, transpose_codes_kernel, dim3((cols + CT_C - 1) / CT_C, (rows + CT_R - 1) / CT_R), dim3(256), 0, st, q, rows, cols, qt);
+    launch_timed(kt, transpose_codes_kernel, dim3((cols + TT_C - 1) / TT_C, (rows + CT_R - 1) / CT_R), dim3(256), 0, st, q, rows, cols, qt);
     return hipGetLastError();
 }
 
