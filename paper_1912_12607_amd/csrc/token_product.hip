@@ -12,7 +12,7 @@ typedef int tp_v4i __attribute__((ext_vector_type(4)));
 typedef int tp_v16i __attribute__((ext_vector_type(16)));
 constexpr int kFewLds = 140 * 1024;      // codes of few tokens
 
-// Output tile of WM x WN waves, each MI x NJ products of 32 x 32; stages of 128 reduction bytes, NS of them in LDS: while one is
+// Output tile of WM x WN waves, each MI x NJ products of 32 x 32; stages of 128 reduction bytes (whole lines; half as many: 7 % slower), NS of them in LDS: while one is
 // multiplied, the next ones are on their way (buffer loads into LDS, rows beyond the operand and bytes beyond the reduction read as zeros).
 // SPLIT: the block has a share of the reduction and leaves its sums for product_reduce_kernel.
 template <int TYPE, int WM, int WN, int MI, int NJ, int NS, bool SPLIT>
@@ -45,16 +45,17 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     const lds_dma_v4i rb = igd_rsrc(a.b + (size_t)col0 * a.Kp, (uint32_t)cols * (uint32_t)a.Kp);
     const uint32_t lds_a = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(size_t)(ring + 64 * wave));
     const uint32_t lds_b = lds_a + BM * KG * 16;
-    // load i of this wave covers 8 tile rows from 8 (wave + NW i); the lane's granule is the inverse of igd_slot<8>()
-    const int lrow = lane >> 3;
+    // load i of this wave covers RL tile rows from RL (wave + NW i); the lane's granule is the inverse of igd_slot<KG>()
+    constexpr int RL = 64 / KG;
+    const int lrow = lane / KG;
     const int gran = (lane & 7) ^ (((lrow >> 1) & 3) | ((wave & 1) << 2));
-    const uint32_t voff = (uint32_t)(8 * wave + lrow) * (uint32_t)a.Kp + (uint32_t)gran * 16u;
-    const uint32_t vstep = (uint32_t)(8 * NW) * (uint32_t)a.Kp;
-    const int all_steps = (a.Kp + 127) >> 7;
+    const uint32_t voff = (uint32_t)(RL * wave + lrow) * (uint32_t)a.Kp + (uint32_t)gran * 16u;
+    const uint32_t vstep = (uint32_t)(RL * NW) * (uint32_t)a.Kp;
+    const int all_steps = (a.Kp + KG * 16 - 1) / (KG * 16);
     const int first_step = SPLIT ? all_steps * share / a.splits : 0, nsteps = SPLIT ? all_steps * (share + 1) / a.splits - first_step : all_steps;
     auto load = [&](int buf, int step, int u) __attribute__((always_inline)) {      // the u-th of this wave's NL loads of a stage
         const uint32_t boff = (uint32_t)buf * (STAGE * 16u);
-        const int at = (first_step + step) * 128;
+        const int at = (first_step + step) * (KG * 16);
         const uint32_t past = at + gran * 16 < a.Kp ? 0u : IGD_OOB;      // beyond the reduction
         const uint32_t k = (uint32_t)__builtin_amdgcn_readfirstlane(at);
         if (u < NLA) igd_load_lds(ra, lds_a + boff + (uint32_t)u * (NW * 1024), (voff + (uint32_t)u * vstep) | past, k);
@@ -103,8 +104,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     };
     // The loads of a stage are dealt out between the products from the barrier on that frees their place, NQ products to a load, so that they
     // are under way at least a step before they are waited for: all at once they keep the waves from their products until the last has been taken.
-    constexpr int NQ = MI * NJ * 3 / NL > 0 ? MI * NJ * 3 / NL : 1, NP = MI * NJ;
-    static_assert((NL - 1) * NQ < NP * 4, "all loads of a stage are issued before the next barrier");
+    constexpr int NP = MI * NJ, NQ = NP * (NS > 2 ? KG / 2 : KG / 2 - 1) / NL > 0 ? NP * (NS > 2 ? KG / 2 : KG / 2 - 1) / NL : 1;
+    static_assert((NL - 1) * NQ < NP * (KG / 2), "all loads of a stage are issued before the next barrier");
 #pragma unroll
     for (int p = 0; p < NS - 1; ++p)
 #pragma unroll
@@ -389,16 +390,18 @@ hipError_t product_of(const ProductArgs& a, hipStream_t st) {
 }
 
 // Tiles and shares of the reduction by an estimate, us: rounds of blocks times stages of 128 reduction bytes, plus what a block and the
-// joining pass cost.  occ: blocks on a compute unit; busy: of its matrix units per stage; least: a stage of a block alone.
+// joining pass cost.  occ: blocks on a compute unit; busy: of its matrix units per stage; least: a stage of a block alone.  (Measured, one share,
+// bf16 results, tiles of 256, 128 with two and three stages in LDS, 64: 16384 x 4096 -> 4096 250, 320, 369, -; 1001 x 4096 -> 16384 64, 83, 95, 113;
+// 1001 x 4096 -> 4096 48, 31, 25, 29; 512 x 4096 -> 4096 -, 28, 22, 17; 128 x 4096 -> 4096 -, 23, 21, 10.)
 struct ProductPlan {
-    int tile, splits;          // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+    int tile, splits;          // 0: 256 x 256, 1: 128 x 128, 2: the same with three stages, 3: 64 x 64 with four
 };
 ProductPlan product_plan(int M, int N, int Kp, bool scratch) {
-    static const struct { int bm, occ; double busy, least, fixed; } kTiles[3] = {{256, 1, 1.5, 1.5, 6.0}, {128, 2, 0.42, 0.5, 3.0}, {64, 4, 0.16, 0.3, 2.0}};
+    static const struct { int bm, occ; double busy, least, fixed; } kTiles[4] = {{256, 1, 1.63, 1.63, 10.0}, {128, 2, 0.57, 0.85, 4.0}, {128, 1, 0.66, 0.66, 4.5}, {64, 4, 0.22, 0.26, 2.5}};
     const int steps = (Kp + 127) >> 7;
     ProductPlan best{0, 1};
     double least = 1e30;
-    for (int t = 0; t < 3; ++t) {
+    for (int t = 0; t < 4; ++t) {
         const long long tiles = (long long)((M + kTiles[t].bm - 1) / kTiles[t].bm) * ((N + kTiles[t].bm - 1) / kTiles[t].bm);
         for (int s = 1; s <= (scratch ? 16 : 1) && s <= steps; s *= 2) {
             const long long blocks = tiles * s, slots = 256ll * kTiles[t].occ;
@@ -418,7 +421,8 @@ ProductPlan product_plan(int M, int N, int Kp, bool scratch) {
 
 template <int TYPE>
 hipError_t product_type(const ProductArgs& a, int tile, hipStream_t st) {
-    return tile == 0 ? product_of<TYPE, 2, 4, 4, 2, 2>(a, st) : tile == 1 ? product_of<TYPE, 2, 2, 2, 2, 2>(a, st) : product_of<TYPE, 2, 2, 1, 1, 4>(a, st);
+    return tile == 0 ? product_of<TYPE, 2, 4, 4, 2, 2>(a, st) : tile == 1 ? product_of<TYPE, 2, 2, 2, 2, 2>(a, st)
+           : tile == 2 ? product_of<TYPE, 2, 2, 2, 2, 3>(a, st) : product_of<TYPE, 2, 2, 1, 1, 4>(a, st);
 }
 
 template <int TYPE, int RM>
