@@ -210,18 +210,16 @@ extern "C" int8t_status int8t_linear_fwd(const int8t_linear_desc* d, const int8t
         if (b->ws_bytes < s.bytes) return INT8T_ERR_WORKSPACE;
     }
     const hipStream_t st = (hipStream_t)stream;
-    if (b->w) {
-        const RowsArgs w{b->w, b->w_pitch, d->wtype, d->N, d->K, nullptr, 0, 0, b->wq, b->sw};
-        const hipError_t e = launch_quantize_rows(w, st);
-        if (e != hipSuccess) return INT8T_ERR_RUNTIME;
-    }
-    if (d->M == 0) return INT8T_OK;
+    const RowsArgs w{b->w, b->w_pitch, d->wtype, d->N, d->K, nullptr, 0, 0, b->wq, b->sw};
+    if (d->M == 0) return b->w ? launched(launch_quantize_rows(w, st)) : INT8T_OK;
     if (served && few_tokens(d->M, pad16(d->K))) {
         const int wide = (((uintptr_t)b->x | b->x_pitch * bytes_of(d->type)) & 15) == 0;
         return launched(launch_few_tokens(FewArgs{b->x, b->x_pitch, d->type, d->M, d->K, pad16(d->K), d->N, wide, b->wq, b->sw, b->bias, b->y, b->y_pitch}, st));
     }
     const RowsArgs x{b->x, b->x_pitch, d->type, d->M, d->K, nullptr, 0, 0, b->xq ? b->xq : s.xq, b->sx ? b->sx : s.sx};
-    hipError_t e = launch_quantize_rows(x, st);
+    const bool together = b->w && d->wtype == d->type;
+    hipError_t e = b->w && !together ? launch_quantize_rows(w, st) : hipSuccess;
+    if (e == hipSuccess) e = launch_quantize_rows(x, st, together ? &w : nullptr);
     if (e != hipSuccess) return INT8T_ERR_RUNTIME;
     ProductArgs a{};
     a.a = x.q; a.sa = x.scale; a.b = b->wq; a.sb = b->sw; a.bias = b->bias;
@@ -242,29 +240,30 @@ extern "C" int8t_status int8t_linear_bwd(const int8t_linear_desc* d, const int8t
     const BwdScratch s = bwd_scratch(d, b->ws);
     if (b->ws_bytes < s.bytes) return INT8T_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
+    const RowsArgs g{b->dy, b->dy_pitch, d->type, d->M, d->N, b->sw, 1, seed, s.gq, s.sg};
+    const ColsArgs h = cols_args(b->dy, d->type, d->M, d->N, b->dy_pitch, b->sx, 1, seed ^ (1ull << 63), s.hq, s.sh, b->db, s.cols);
+    ProductArgs px{}, pw{};
+    px.part = pw.part = static_cast<int32_t*>(s.product);
+    px.a = s.gq; px.sa = s.sg; px.b = s.wqt;
+    px.M = d->M; px.N = d->K; px.Kp = pad16(d->N); px.y = b->dx; px.pitch = (size_t)d->K; px.type = d->type;
+    pw.a = s.hq; pw.sa = s.sh; pw.b = s.xqt;
+    pw.M = d->N; pw.N = d->K; pw.Kp = pad16(d->M); pw.y = b->dw; pw.pitch = (size_t)d->K; pw.type = d->wtype;
     hipError_t e = hipSuccess;
-    ProductArgs a{};
-    a.part = static_cast<int32_t*>(s.product);
+    if (b->dx && b->dw && gradient_together(d->N)) {
+        e = launch_quantize_gradient(g, h, Transpose{b->wq, d->N, d->K, s.wqt}, Transpose{b->xq, d->M, d->K, s.xqt}, st);
+        if (e == hipSuccess) e = launch_products(px, pw, s.product_bytes, st);
+        return launched(e);
+    }
     if (b->dx) {
-        const RowsArgs g{b->dy, b->dy_pitch, d->type, d->M, d->N, b->sw, 1, seed, s.gq, s.sg};
         e = launch_quantize_rows(g, st);
         if (e == hipSuccess) e = launch_transpose_codes(b->wq, d->N, d->K, s.wqt, st);
-        if (e != hipSuccess) return INT8T_ERR_RUNTIME;
-        a.a = s.gq; a.sa = s.sg; a.b = s.wqt;
-        a.M = d->M; a.N = d->K; a.Kp = pad16(d->N); a.y = b->dx; a.pitch = (size_t)d->K; a.type = d->type;
-        e = launch_product(a, s.product_bytes, st);
+        if (e == hipSuccess) e = launch_product(px, s.product_bytes, st);
         if (e != hipSuccess) return INT8T_ERR_RUNTIME;
     }
-    if (b->dw || b->db) {
-        e = launch_quantize_cols(cols_args(b->dy, d->type, d->M, d->N, b->dy_pitch, b->sx, 1, seed ^ (1ull << 63), s.hq, s.sh, b->db, s.cols), st);
-        if (e != hipSuccess) return INT8T_ERR_RUNTIME;
-    }
-    if (b->dw) {
+    if (b->dw || b->db) e = launch_quantize_cols(h, st);
+    if (b->dw && e == hipSuccess) {
         e = launch_transpose_codes(b->xq, d->M, d->K, s.xqt, st);
-        if (e != hipSuccess) return INT8T_ERR_RUNTIME;
-        a.a = s.hq; a.sa = s.sh; a.b = s.xqt;
-        a.M = d->N; a.N = d->K; a.Kp = pad16(d->M); a.y = b->dw; a.pitch = (size_t)d->K; a.type = d->wtype;
-        e = launch_product(a, s.product_bytes, st);
+        if (e == hipSuccess) e = launch_product(pw, s.product_bytes, st);
     }
     return launched(e);
 }

@@ -16,7 +16,7 @@ constexpr int kFewLds = 140 * 1024;      // codes of few tokens
 // multiplied, the next ones are on their way (buffer loads into LDS, rows beyond the operand and bytes beyond the reduction read as zeros).
 // SPLIT: the block has a share of the reduction and leaves its sums for product_reduce_kernel.
 template <int TYPE, int WM, int WN, int MI, int NJ, int NS, bool SPLIT>
-__global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs a, const int mtiles, const int ntiles) {
+__device__ __forceinline__ void product_body(const ProductArgs& a, const int mtiles, const int ntiles, const int block) {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int KG = 8, NW = WM * WN, BM = WM * MI * 32, BN = WN * NJ * 32, STAGE = (BM + BN) * KG;
     constexpr int NLA = BM * KG / 64 / NW, NLB = BN * KG / 64 / NW, NL = NLA + NLB;
@@ -30,8 +30,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     // that its tiles share meet in its L2 (eight by one: 16384 tokens 4096 -> 4096 294 us instead of 285).  SPLIT: the shares of a tile's reduction
     // are tiles of their own.
     const int total = mtiles * ntiles * (SPLIT ? a.splits : 1), per = (total + 7) >> 3;
-    int tile = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3), share = 0;
-    if (((int)blockIdx.x >> 3) >= per || tile >= total) return;
+    int tile = (block & 7) * per + (block >> 3), share = 0;
+    if ((block >> 3) >= per || tile >= total) return;
     if (SPLIT) {
         share = tile / (mtiles * ntiles);
         tile -= share * (mtiles * ntiles);
@@ -221,6 +221,15 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     }
 }
 
+// One product, or two whose blocks from `first` (a multiple of eight) on have the second one's tiles.
+template <int TYPE, int WM, int WN, int MI, int NJ, int NS, bool SPLIT>
+__global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs a, const ProductArgs b, const int first) {
+    constexpr int BM = WM * MI * 32, BN = WN * NJ * 32;
+    const bool second = (int)blockIdx.x >= first;
+    const ProductArgs p = second ? b : a;
+    product_body<TYPE, WM, WN, MI, NJ, NS, SPLIT>(p, (p.M + BM - 1) / BM, (p.N + BN - 1) / BN, (int)blockIdx.x - (second ? first : 0));
+}
+
 // ------------------------------------------------------------------------------------------------
 // Few tokens (at most 16) through weights that are laid out: one launch, codes of the tokens included.  Every block makes them for itself
 // in LDS -- the tokens are small and come from the caches -- and multiplies them with 16 channels at a time: a wave has an eighth of the
@@ -367,16 +376,18 @@ __global__ __launch_bounds__(256) void product_reduce_kernel(const ProductArgs a
 }
 
 template <int TYPE, int WM, int WN, int MI, int NJ, int NS, bool SPLIT>
-hipError_t product_split(const ProductArgs& a, hipStream_t st) {
+hipError_t product_split(const ProductArgs& a, const ProductArgs* b, hipStream_t st) {
     constexpr int BM = WM * MI * 32, BN = WN * NJ * 32, LDS = NS * (BM + BN) * 128;
     static std::atomic<unsigned long long> done{0};
     const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&product_kernel<TYPE, WM, WN, MI, NJ, NS, SPLIT>), LDS, done);
     if (e != hipSuccess) return e;
-    const int mt = (a.M + BM - 1) / BM, nt = (a.N + BN - 1) / BN;
+    const auto blocks = [](const ProductArgs& p) {
+        return (unsigned)((((size_t)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * (SPLIT ? p.splits : 1) + 7) / 8) * 8);
+    };
+    const unsigned first = blocks(a);
     {
         KernelTimer kt(KID_TOKEN_PRODUCT, st);
-        launch_timed(kt, (product_kernel<TYPE, WM, WN, MI, NJ, NS, SPLIT>), dim3((unsigned)((((size_t)mt * nt * (SPLIT ? a.splits : 1) + 7) / 8) * 8)), dim3(64 * WM * WN), LDS, st,
-                     a, mt, nt);
+        launch_timed(kt, (product_kernel<TYPE, WM, WN, MI, NJ, NS, SPLIT>), dim3(first + (b ? blocks(*b) : 0u)), dim3(64 * WM * WN), LDS, st, a, b ? *b : a, (int)first);
     }
     if (SPLIT) {
         KernelTimer kt(KID_TOKEN_REDUCE, st);
@@ -385,8 +396,8 @@ hipError_t product_split(const ProductArgs& a, hipStream_t st) {
     return hipGetLastError();
 }
 template <int TYPE, int WM, int WN, int MI, int NJ, int NS>
-hipError_t product_of(const ProductArgs& a, hipStream_t st) {
-    return a.splits > 1 ? product_split<TYPE, WM, WN, MI, NJ, NS, true>(a, st) : product_split<TYPE, WM, WN, MI, NJ, NS, false>(a, st);
+hipError_t product_of(const ProductArgs& a, const ProductArgs* b, hipStream_t st) {
+    return a.splits > 1 ? product_split<TYPE, WM, WN, MI, NJ, NS, true>(a, nullptr, st) : product_split<TYPE, WM, WN, MI, NJ, NS, false>(a, b, st);
 }
 
 // Tiles and shares of the reduction by an estimate, us: rounds of blocks times stages of 128 reduction bytes, plus what a block and the
@@ -420,9 +431,21 @@ ProductPlan product_plan(int M, int N, int Kp, bool scratch) {
 }
 
 template <int TYPE>
-hipError_t product_type(const ProductArgs& a, int tile, hipStream_t st) {
-    return tile == 0 ? product_of<TYPE, 2, 4, 4, 2, 2>(a, st) : tile == 1 ? product_of<TYPE, 2, 2, 2, 2, 2>(a, st)
-           : tile == 2 ? product_of<TYPE, 2, 2, 2, 2, 3>(a, st) : product_of<TYPE, 2, 2, 1, 1, 4>(a, st);
+hipError_t product_type(const ProductArgs& a, const ProductArgs* b, int tile, hipStream_t st) {
+    return tile == 0 ? product_of<TYPE, 2, 4, 4, 2, 2>(a, b, st) : tile == 1 ? product_of<TYPE, 2, 2, 2, 2, 2>(a, b, st)
+           : tile == 2 ? product_of<TYPE, 2, 2, 2, 2, 3>(a, b, st) : product_of<TYPE, 2, 2, 1, 1, 4>(a, b, st);
+}
+hipError_t product_launch(const ProductArgs& a, const ProductArgs* b, int tile, hipStream_t st) {
+    if (a.type == kF32) return product_type<kF32>(a, b, tile, st);
+    if (a.type == kBF16) return product_type<kBF16>(a, b, tile, st);
+    return product_type<kF16>(a, b, tile, st);
+}
+// the plan of a product, with shares only where their scratch is there
+int planned(ProductArgs* a, size_t scratch_bytes) {
+    const size_t need = product_scratch(a->M, a->N, a->Kp);
+    const ProductPlan p = product_plan(a->M, a->N, a->Kp, need > 0 && a->part && scratch_bytes >= need);
+    a->splits = p.splits;
+    return p.tile;
 }
 
 template <int TYPE, int RM>
@@ -452,12 +475,14 @@ size_t product_scratch(int M, int N, int Kp) {
     return p.splits > 1 ? (size_t)p.splits * M * ((N + 3) & ~3) * sizeof(int32_t) : 0;
 }
 hipError_t launch_product(ProductArgs a, size_t scratch_bytes, hipStream_t st) {
-    const size_t need = product_scratch(a.M, a.N, a.Kp);
-    const ProductPlan p = product_plan(a.M, a.N, a.Kp, need > 0 && a.part && scratch_bytes >= need);
-    a.splits = p.splits;
-    if (a.type == kF32) return product_type<kF32>(a, p.tile, st);
-    if (a.type == kBF16) return product_type<kBF16>(a, p.tile, st);
-    return product_type<kF16>(a, p.tile, st);
+    const int tile = planned(&a, scratch_bytes);
+    return product_launch(a, nullptr, tile, st);
+}
+hipError_t launch_products(ProductArgs a, ProductArgs b, size_t scratch_bytes, hipStream_t st) {
+    const int ta = planned(&a, scratch_bytes), tb = planned(&b, scratch_bytes);
+    if (ta == tb && a.type == b.type && a.splits == 1 && b.splits == 1) return product_launch(a, &b, ta, st);
+    const hipError_t e = product_launch(a, nullptr, ta, st);
+    return e != hipSuccess ? e : product_launch(b, nullptr, tb, st);
 }
 
 }  // namespace int8t

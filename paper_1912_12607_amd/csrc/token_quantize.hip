@@ -1,5 +1,7 @@
 // Codes of tokens: a scale for each row, or for each column with the codes transposed (Eq.1 / Eq.3 of the per-tensor quantizer, c the
 // maximum of the row or column), and the transposition of codes.
+#include <type_traits>
+
 #include "device_common.h"
 #include "tokens.h"
 
@@ -26,11 +28,11 @@ __device__ __forceinline__ uint2 codes8(const float v[8], float inv, uint32_t kx
 // row; rows beyond TPR * 32 values (LONG) are read a second time, from the caches.
 // Bound by memory: bytes read and written once.
 template <int TYPE, bool STOCH, int TPR, int CH, bool LONG>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quantize_rows_kernel(const RowsArgs a, const int wide, const uint32_t kx, const uint32_t ka) {
+__device__ __forceinline__ void rows_body(const RowsArgs& a, const int block, const int wide, const uint32_t kx, const uint32_t ka) {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int RPB = TPR < 256 ? 256 / TPR : 1, SPAN = TPR * 8 * CH;
     const int t = (int)threadIdx.x % TPR;
-    const int row = (int)blockIdx.x * RPB + (int)threadIdx.x / TPR;
+    const int row = block * RPB + (int)threadIdx.x / TPR;
     const bool live = row < a.rows;            // (all lanes stay for the reductions)
     const int Kp = (a.cols + 15) & ~15;
     const T* __restrict__ x = static_cast<const T*>(a.x) + (size_t)(live ? row : 0) * a.pitch;
@@ -89,22 +91,40 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quantize_rows_kernel(co
     }
 }
 
+// Two matrices of as many columns in one launch (tokens and weights; a launch more costs small layers as much as either): blocks from `first` on
+// have the second's rows.
+template <int TYPE, bool STOCH, int TPR, int CH, bool LONG>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quantize_rows_kernel(const RowsArgs a, const RowsArgs b, const int first, const int wide, const uint32_t kx,
+                                                                              const uint32_t ka) {
+    if ((int)blockIdx.x < first) rows_body<TYPE, STOCH, TPR, CH, LONG>(a, (int)blockIdx.x, wide, kx, ka);
+    else rows_body<TYPE, STOCH, TPR, CH, LONG>(b, (int)blockIdx.x - first, wide, kx, ka);
+}
+
+inline int row_blocks(int rows, int tpr) { return tpr < 256 ? (rows + 256 / tpr - 1) / (256 / tpr) : rows; }
+
+// Calls f(lanes of a row, chunks of eight values a lane, whether a row is longer): as few lanes as hold a row, at least a wave.
+template <typename F>
+void for_row_length(int cols, F f) {
+    if (cols <= 512) f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>(), std::false_type());
+    else if (cols <= 1024) f(std::integral_constant<int, 64>(), std::integral_constant<int, 2>(), std::false_type());
+    else if (cols <= 2048) f(std::integral_constant<int, 64>(), std::integral_constant<int, 4>(), std::false_type());
+    else if (cols <= 4096) f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>(), std::false_type());
+    else if (cols <= 8192) f(std::integral_constant<int, 256>(), std::integral_constant<int, 4>(), std::false_type());
+    else if (cols <= 16384) f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>(), std::false_type());
+    else if (cols <= 32768) f(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>(), std::false_type());
+    else f(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>(), std::true_type());
+}
+
 template <int TYPE, bool STOCH>
-void rows_of(const RowsArgs& a, int wide, hipStream_t st) {
+void rows_of(const RowsArgs& a, const RowsArgs* b, int wide, hipStream_t st) {
     KernelTimer kt(KID_TOKEN_ROWS, st);
     const uint32_t kx = seed_key_x(a.seed), ka = seed_key_a(a.seed);
-    // lanes of a row: as few as hold it, at least a wave
-#define LAUNCH(TPRv, CHv, LONGv) launch_timed(kt, (quantize_rows_kernel<TYPE, STOCH, TPRv, CHv, LONGv>), dim3(TPRv < 256 ? (a.rows + 256 / TPRv - 1) / (256 / TPRv) : a.rows), \
-                                              dim3(TPRv < 256 ? 256 : TPRv), 0, st, a, wide, kx, ka)
-    if (a.cols <= 512) LAUNCH(64, 1, false);
-    else if (a.cols <= 1024) LAUNCH(64, 2, false);
-    else if (a.cols <= 2048) LAUNCH(64, 4, false);
-    else if (a.cols <= 4096) LAUNCH(256, 2, false);
-    else if (a.cols <= 8192) LAUNCH(256, 4, false);
-    else if (a.cols <= 16384) LAUNCH(1024, 2, false);
-    else if (a.cols <= 32768) LAUNCH(1024, 4, false);
-    else LAUNCH(1024, 4, true);
-#undef LAUNCH
+    for_row_length(a.cols, [&](auto tpr, auto ch, auto more) {
+        constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
+        const int first = row_blocks(a.rows, TPR);
+        launch_timed(kt, (quantize_rows_kernel<TYPE, STOCH, TPR, CH, decltype(more)::value>), dim3(first + (b ? row_blocks(b->rows, TPR) : 0)), dim3(TPR < 256 ? 256 : TPR), 0,
+                     st, a, b ? *b : a, first, wide, kx, ka);
+    });
 }
 
 inline int wide_rows(const void* x, size_t pitch, int type) {
@@ -115,12 +135,12 @@ inline int wide_rows(const void* x, size_t pitch, int type) {
 // First pass: maxima of |x factor| and sums of x over a part of the rows, for 256 columns of a block: lane (c, r) has the columns
 // 8 c .. + 7 of every eighth row.
 template <int TYPE>
-__global__ __launch_bounds__(256) void cols_max_kernel(const ColsArgs a, const int wide) {
+__device__ __forceinline__ void cols_max_body(const ColsArgs& a, const int bx, const int part, const int wide) {
     typedef typename ElemOf<TYPE>::type T;
     __shared__ float lds[8][257];
     const int cg = (int)threadIdx.x & 31, r0 = (int)threadIdx.x >> 5;
-    const int col = (int)blockIdx.x * 256 + cg * 8;
-    const int from = (int)((long long)a.rows * blockIdx.y / a.parts), to = (int)((long long)a.rows * (blockIdx.y + 1) / a.parts);
+    const int col = bx * 256 + cg * 8;
+    const int from = (int)((long long)a.rows * part / a.parts), to = (int)((long long)a.rows * (part + 1) / a.parts);
     float m[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int r = from + r0; r < to; r += 8) {
         float v[8];
@@ -132,7 +152,7 @@ __global__ __launch_bounds__(256) void cols_max_kernel(const ColsArgs a, const i
             m[i] = fmaxf(m[i], fabsf(__fmul_rn(v[i], f)));
         }
     }
-    const int c = (int)blockIdx.x * 256 + (int)threadIdx.x;
+    const int c = bx * 256 + (int)threadIdx.x;
 #pragma unroll
     for (int i = 0; i < 8; ++i) lds[r0][cg * 8 + i] = m[i];
     __syncthreads();
@@ -140,7 +160,7 @@ __global__ __launch_bounds__(256) void cols_max_kernel(const ColsArgs a, const i
         float t = lds[0][threadIdx.x];
 #pragma unroll
         for (int i = 1; i < 8; ++i) t = fmaxf(t, lds[i][threadIdx.x]);
-        a.part_max[(size_t)blockIdx.y * a.cols + c] = t;
+        a.part_max[(size_t)part * a.cols + c] = t;
     }
     if (!a.sum) return;
     __syncthreads();
@@ -151,8 +171,13 @@ __global__ __launch_bounds__(256) void cols_max_kernel(const ColsArgs a, const i
         float t = lds[0][threadIdx.x];
 #pragma unroll
         for (int i = 1; i < 8; ++i) t += lds[i][threadIdx.x];
-        a.part_sum[(size_t)blockIdx.y * a.cols + c] = t;
+        a.part_sum[(size_t)part * a.cols + c] = t;
     }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(256) void cols_max_kernel(const ColsArgs a, const int wide) {
+    cols_max_body<TYPE>(a, (int)blockIdx.x, (int)blockIdx.y, wide);
 }
 
 // Tiles of 128 rows, turned in LDS: the codes of four neighbouring rows of a column are one word, 32 words a column, and leave in runs of 128
@@ -173,11 +198,10 @@ __device__ __forceinline__ void tile_out(const uint32_t* tile, int8_t* __restric
 // Second pass: codes of a tile of 128 rows x 64 columns
 constexpr int CT_C = 64;
 template <int TYPE, bool STOCH>
-__global__ __launch_bounds__(256) void cols_codes_kernel(const ColsArgs a, const int wide, const uint32_t kx, const uint32_t ka) {
+__device__ __forceinline__ void cols_codes_body(uint32_t* const tile, const ColsArgs& a, const int bx, const int by, const int wide, const uint32_t kx, const uint32_t ka) {
     typedef typename ElemOf<TYPE>::type T;
-    __shared__ __attribute__((aligned(16))) uint32_t tile[CT_C * CT_PITCH / 4];
     __shared__ __attribute__((aligned(16))) float invs[CT_C];
-    const int col0 = (int)blockIdx.x * CT_C, row0 = (int)blockIdx.y * CT_R;
+    const int col0 = bx * CT_C, row0 = by * CT_R;
     // the parts' maxima: four lanes a column
     __shared__ float tops[4][CT_C];
     {
@@ -192,7 +216,7 @@ __global__ __launch_bounds__(256) void cols_codes_kernel(const ColsArgs a, const
     if (threadIdx.x < CT_C) {
         const int c = col0 + (int)threadIdx.x;
         const float m = fmaxf(fmaxf(tops[0][threadIdx.x], tops[1][threadIdx.x]), fmaxf(tops[2][threadIdx.x], tops[3][threadIdx.x]));
-        if (blockIdx.y == 0 && c < a.cols) {
+        if (by == 0 && c < a.cols) {
             a.scale[c] = scale_of(m);
             if (a.sum) {
                 double s = 0.0;
@@ -235,6 +259,12 @@ __global__ __launch_bounds__(256) void cols_codes_kernel(const ColsArgs a, const
     tile_out<CT_C>(tile, a.q, row0, col0, (a.rows + 15) & ~15, a.cols);
 }
 
+template <int TYPE, bool STOCH>
+__global__ __launch_bounds__(256) void cols_codes_kernel(const ColsArgs a, const int wide, const uint32_t kx, const uint32_t ka) {
+    __shared__ __attribute__((aligned(16))) uint32_t tile[CT_C * CT_PITCH / 4];
+    cols_codes_body<TYPE, STOCH>(tile, a, (int)blockIdx.x, (int)blockIdx.y, wide, kx, ka);
+}
+
 template <int TYPE>
 void cols_of(const ColsArgs& a, int wide, hipStream_t st) {
     {
@@ -250,9 +280,9 @@ void cols_of(const ColsArgs& a, int wide, hipStream_t st) {
 
 // Codes [rows][pad16(cols)] -> [cols][pad16(rows)], tiles of 128 x 128
 constexpr int TT_C = 128;
-__global__ __launch_bounds__(256) void transpose_codes_kernel(const int8_t* __restrict__ q, const int rows, const int cols, int8_t* __restrict__ qt) {
-    __shared__ __attribute__((aligned(16))) uint32_t tile[TT_C * CT_PITCH / 4];
-    const int col0 = (int)blockIdx.x * TT_C, row0 = (int)blockIdx.y * CT_R;
+__device__ __forceinline__ void transpose_body(uint32_t* const tile, const int8_t* __restrict__ q, const int rows, const int cols, int8_t* __restrict__ qt, const int bx,
+                                               const int by) {
+    const int col0 = bx * TT_C, row0 = by * CT_R;
     const int Kp = (cols + 15) & ~15;
     const int g = (int)threadIdx.x & 7, rq = (int)threadIdx.x >> 3;
     const int c = col0 + 16 * g, row = row0 + 4 * rq;
@@ -274,12 +304,60 @@ __global__ __launch_bounds__(256) void transpose_codes_kernel(const int8_t* __re
     __syncthreads();
     tile_out<TT_C>(tile, qt, row0, col0, (rows + 15) & ~15, cols);
 }
+__global__ __launch_bounds__(256) void transpose_codes_kernel(const int8_t* __restrict__ q, const int rows, const int cols, int8_t* __restrict__ qt) {
+    __shared__ __attribute__((aligned(16))) uint32_t tile[TT_C * CT_PITCH / 4];
+    transpose_body(tile, q, rows, cols, qt, (int)blockIdx.x, (int)blockIdx.y);
+}
+
+// ---- a gradient's codes for both products, in two launches -------------------------------------
+// First: codes of its rows (bound by the draws) beside the maxima of its columns (bound by memory); then: codes of its columns (draws) beside the
+// transposition of the other operands' codes (memory).  Blocks of either kind take turns in proportion to their numbers: of n + m blocks, those where
+// floor((i + 1) n / (n + m)) steps up have the first kind.
+__device__ __forceinline__ bool take_turn(int i, int n, int all, int* at) {
+    const int before = (int)((long long)i * n / all), after = (int)((long long)(i + 1) * n / all);
+    *at = after > before ? before : i - before;
+    return after > before;
+}
+template <int TYPE, int TPR, int CH>
+__global__ __launch_bounds__(256) void gradient_first_kernel(const RowsArgs r, const ColsArgs c, const int rblocks, const int cx, const int wide, const uint32_t kx,
+                                                             const uint32_t ka) {
+    int at;
+    if (take_turn((int)blockIdx.x, rblocks, (int)gridDim.x, &at)) rows_body<TYPE, true, TPR, CH, false>(r, at, wide, kx, ka);
+    else cols_max_body<TYPE>(c, at % cx, at / cx, wide);
+}
+template <int TYPE>
+__global__ __launch_bounds__(256) void gradient_second_kernel(const ColsArgs c, const int cx, const int cblocks, const Transpose w, const int wx, const int wblocks,
+                                                              const Transpose x, const int xx, const int wide, const uint32_t kx, const uint32_t ka) {
+    __shared__ __attribute__((aligned(16))) uint32_t tile[TT_C * CT_PITCH / 4];
+    int at;
+    if (take_turn((int)blockIdx.x, cblocks, (int)gridDim.x, &at)) cols_codes_body<TYPE, true>(tile, c, at % cx, at / cx, wide, kx, ka);
+    else if (at < wblocks) transpose_body(tile, w.q, w.rows, w.cols, w.qt, at % wx, at / wx);
+    else transpose_body(tile, x.q, x.rows, x.cols, x.qt, (at - wblocks) % xx, (at - wblocks) / xx);
+}
+inline int over(int n, int d) { return (n + d - 1) / d; }
+template <int TYPE>
+void gradient_of(const RowsArgs& r, const ColsArgs& c, const Transpose& w, const Transpose& x, int wide, hipStream_t st) {
+    const int maxima = over(c.cols, 256);
+    for_row_length(r.cols, [&](auto tpr, auto ch, auto) {
+        if constexpr (decltype(tpr)::value <= 256) {
+            KernelTimer kt(KID_TOKEN_ROWS, st);
+            const int rblocks = row_blocks(r.rows, decltype(tpr)::value);
+            launch_timed(kt, (gradient_first_kernel<TYPE, decltype(tpr)::value, decltype(ch)::value>), dim3(rblocks + maxima * c.parts), dim3(256), 0, st, r, c, rblocks, maxima,
+                         wide, seed_key_x(r.seed), seed_key_a(r.seed));
+        }
+    });
+    KernelTimer kt(KID_TOKEN_COLS, st);
+    const int cx = over(c.cols, CT_C), cblocks = cx * over(c.rows, CT_R);
+    const int wx = over(w.cols, TT_C), wblocks = wx * over(w.rows, CT_R), xx = over(x.cols, TT_C), xblocks = xx * over(x.rows, CT_R);
+    launch_timed(kt, gradient_second_kernel<TYPE>, dim3(cblocks + wblocks + xblocks), dim3(256), 0, st, c, cx, cblocks, w, wx, wblocks, x, xx, wide, seed_key_x(c.seed),
+                 seed_key_a(c.seed));
+}
 
 }  // namespace
 
-hipError_t launch_quantize_rows(const RowsArgs& a, hipStream_t st) {
-    const int wide = wide_rows(a.x, a.pitch, a.type);
-#define LAUNCH(TY) a.stochastic ? rows_of<TY, true>(a, wide, st) : rows_of<TY, false>(a, wide, st)
+hipError_t launch_quantize_rows(const RowsArgs& a, hipStream_t st, const RowsArgs* b) {
+    const int wide = wide_rows(a.x, a.pitch, a.type) && (!b || wide_rows(b->x, b->pitch, b->type));
+#define LAUNCH(TY) a.stochastic ? rows_of<TY, true>(a, b, wide, st) : rows_of<TY, false>(a, b, wide, st)
     if (a.type == kF32) LAUNCH(kF32);
     else if (a.type == kBF16) LAUNCH(kBF16);
     else LAUNCH(kF16);
@@ -297,6 +375,14 @@ hipError_t launch_quantize_cols(const ColsArgs& a, hipStream_t st) {
     if (a.type == kF32) cols_of<kF32>(a, wide, st);
     else if (a.type == kBF16) cols_of<kBF16>(a, wide, st);
     else cols_of<kF16>(a, wide, st);
+    return hipGetLastError();
+}
+bool gradient_together(int cols) { return cols <= 8192; }
+hipError_t launch_quantize_gradient(const RowsArgs& r, const ColsArgs& c, const Transpose& w, const Transpose& x, hipStream_t st) {
+    const int wide = wide_rows(r.x, r.pitch, r.type);
+    if (r.type == kF32) gradient_of<kF32>(r, c, w, x, wide, st);
+    else if (r.type == kBF16) gradient_of<kBF16>(r, c, w, x, wide, st);
+    else gradient_of<kF16>(r, c, w, x, wide, st);
     return hipGetLastError();
 }
 hipError_t launch_transpose_codes(const int8_t* q, int rows, int cols, int8_t* qt, hipStream_t st) {

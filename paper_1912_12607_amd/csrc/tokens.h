@@ -76,7 +76,8 @@ struct RowsArgs {            // codes of rows x cols values, a scale for each ro
     int8_t* q;               // [rows][pad16(cols)]
     float* scale;            // rows
 };
-hipError_t launch_quantize_rows(const RowsArgs& a, hipStream_t st);
+// with b (as many columns, the same type and rounding to nearest in both): two matrices in one launch
+hipError_t launch_quantize_rows(const RowsArgs& a, hipStream_t st, const RowsArgs* b = nullptr);
 
 struct ColsArgs {            // ... a scale for each column, codes transposed
     const void* x;
@@ -94,6 +95,15 @@ struct ColsArgs {            // ... a scale for each column, codes transposed
 int quantize_cols_parts(int rows, int cols);
 hipError_t launch_quantize_cols(const ColsArgs& a, hipStream_t st);
 hipError_t launch_transpose_codes(const int8_t* q, int rows, int cols, int8_t* qt, hipStream_t st);
+struct Transpose {
+    const int8_t* q;
+    int rows, cols;
+    int8_t* qt;
+};
+// A gradient's codes by rows and by columns, stochastic, and two transpositions, in two launches: where gradient_together(its columns), a block of
+// 256 lanes holding a row at least.
+bool gradient_together(int cols);
+hipError_t launch_quantize_gradient(const RowsArgs& r, const ColsArgs& c, const Transpose& w, const Transpose& x, hipStream_t st);
 
 // ---- token_product.hip -------------------------------------------------------------------------
 struct ProductArgs {         // y[m][n] = (sum_k a[m][k] b[n][k]) * (sa[m] * sb[n]) + bias[n]
@@ -120,6 +130,8 @@ bool few_tokens(int M, int Kp);
 hipError_t launch_few_tokens(const FewArgs& a, hipStream_t st);
 size_t product_scratch(int M, int N, int Kp);
 hipError_t launch_product(ProductArgs a, size_t scratch_bytes, hipStream_t st);
+// Two products, in one launch where both take the same tiles whole.  They share the scratch.
+hipError_t launch_products(ProductArgs a, ProductArgs b, size_t scratch_bytes, hipStream_t st);
 
 // ---- token_cache.hip ---------------------------------------------------------------------------
 struct CacheArgs {

@@ -220,6 +220,13 @@ def test_linear_and_gradients(M, K, N, dtype, wtype):
     assert np.all(np.abs(db.cpu().numpy() - g64.sum(0)) <= (M + 8) * 2.0**-24 * np.abs(g64).sum(0) + 1e-30)
 
 
+# outputs of each length that the gradient's rows are dealt out by, together with its columns up to 8192 and apart beyond
+@pytest.mark.parametrize("M,K,N", [(40, 33, 600), (9, 200, 1504), (35, 17, 3001), (130, 48, 8192), (20, 40, 8200), (300, 300, 9001)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_of_wide_outputs(M, K, N, dtype):
+    test_linear_and_gradients(M, K, N, dtype, dtype)
+
+
 def test_gradients_against_differences():
     """Differences of the loss <g, x W^T + b> in 64 bits against the gradients.  dx = sum_n q'[n] wq[n] with q' within one step sg of
     g sw and wq within half a step of w / sw:  |error| <= sum_n sg |wq| + |g sw| / 2; likewise dw over the tokens (|xq| instead)."""
