@@ -12,6 +12,7 @@ stream and the autograd graph.  CUDA(ROCm) tensors in fp32, bf16 or fp16.
 """
 from __future__ import annotations
 
+import functools
 import zlib
 
 import torch
@@ -62,6 +63,19 @@ def _call(index: int, func, *args):
         raise B.Int8tError(status)
 
 
+@functools.lru_cache(maxsize=1024)
+def _plan(M: int, K: int, N: int, kind: int, wkind: int):
+    """What calls of these sizes have in common: the descriptor, scratch bytes of its directions (forward, backward, served), and where the
+    backward pass's codes and scales (of x, of W) lie in one piece of memory, and its size."""
+    desc = B.LinearDesc(M, K, N, kind, wkind)
+    need = tuple(B.lib.int8t_linear_workspace_bytes(desc, i) for i in range(3))
+    at, places = 0, []
+    for n in (M * _pad16(K), N * _pad16(K), 4 * M, 4 * N):
+        places.append(at)
+        at += (n + 255) & ~255
+    return desc, need, tuple(places), at
+
+
 class ServedLinear:
     """A linear layer in use: weights as codes with a scale for each output channel, laid out once; each token gets its scale when it
     arrives.  y = x W^T + b in x's type; no gradients.
@@ -105,10 +119,9 @@ class ServedLinear:
         if y.numel() == 0:
             return y
         rows, pitch = _rows(x, self.in_features)
-        desc = B.LinearDesc(rows.shape[0], self.in_features, self.out_features, kind, kind)
+        desc, (_, _, need), _, _ = _plan(rows.shape[0], self.in_features, self.out_features, kind, kind)
         b = B.LinearBuffers.from_buffer_copy(self._b)
         b.x, b.x_pitch, b.y = rows.data_ptr(), pitch, y.data_ptr()
-        need = B.lib.int8t_linear_workspace_bytes(desc, 2)
         if need:
             ws = torch.empty(need, dtype=torch.uint8, device=x.device)
             b.ws, b.ws_bytes = ws.data_ptr(), need
@@ -129,27 +142,22 @@ class _LinearFn(torch.autograd.Function):
         (rows, pitch), (wr, w_pitch) = _rows(x, K), _rows(w, K)
         M = rows.shape[0]
         y = torch.empty(shape[:-1] + (N,), dtype=x.dtype, device=dev)
-        desc = B.LinearDesc(M, K, N, kind, wkind)
         # codes and scales of x and W, in one piece of memory: the backward pass reads them
-        sizes = (M * _pad16(K), N * _pad16(K), 4 * M, 4 * N)
-        kept = torch.empty(sum((n + 255) & ~255 for n in sizes), dtype=torch.uint8, device=dev)
-        at, places = kept.data_ptr(), []
-        for n in sizes:
-            places.append(at)
-            at += (n + 255) & ~255
+        desc, (need, later, _), places, size = _plan(M, K, N, kind, wkind)
+        kept = torch.empty(size, dtype=torch.uint8, device=dev)
+        at = kept.data_ptr()
         b = B.LinearBuffers()
-        b.xq, b.wq, b.sx, b.sw = places
+        b.xq, b.wq, b.sx, b.sw = at, at + places[1], at + places[2], at + places[3]
         if M:
             b.x, b.x_pitch, b.w, b.w_pitch, b.y, b.y_pitch = rows.data_ptr(), pitch, wr.data_ptr(), w_pitch, y.data_ptr(), N
             if bias is not None:
                 b.bias = bias.data_ptr()
-            need = B.lib.int8t_linear_workspace_bytes(desc, 0)
             if need:
                 ws = torch.empty(need, dtype=torch.uint8, device=dev)
                 b.ws, b.ws_bytes = ws.data_ptr(), need
             _call(index, B.lib.int8t_linear_fwd, desc, b)
         ctx.save_for_backward(kept)
-        ctx.desc, ctx.places, ctx.seed, ctx.x_shape, ctx.w_dtype = desc, places, seed, shape, w.dtype
+        ctx.desc, ctx.need, ctx.places, ctx.seed, ctx.x_shape, ctx.w_dtype = desc, later, places, seed, shape, w.dtype
         return y
 
     @staticmethod
@@ -171,7 +179,8 @@ class _LinearFn(torch.autograd.Function):
                 return None, None, db, None
         kept, = ctx.saved_tensors
         b = B.LinearBuffers()
-        b.xq, b.wq, b.sx, b.sw = ctx.places
+        at, places = kept.data_ptr(), ctx.places
+        b.xq, b.wq, b.sx, b.sw = at, at + places[1], at + places[2], at + places[3]
         b.dy, b.dy_pitch = g.data_ptr(), pitch
         if want_x:
             b.dx = dx.data_ptr()
@@ -182,7 +191,7 @@ class _LinearFn(torch.autograd.Function):
             if want_b:
                 db = torch.empty(N, dtype=torch.float32, device=dev)
                 b.db = db.data_ptr()
-        need = B.lib.int8t_linear_workspace_bytes(desc, 1)
+        need = ctx.need
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
         b.ws, b.ws_bytes = ws.data_ptr(), need
         _call(dy.get_device(), B.lib.int8t_linear_bwd, desc, b, ctx.seed)
