@@ -10,7 +10,7 @@ namespace {
 
 typedef int tp_v4i __attribute__((ext_vector_type(4)));
 typedef int tp_v16i __attribute__((ext_vector_type(16)));
-constexpr int kFewLds = 140 * 1024;      // codes of few tokens
+constexpr int kFewCodes = 32768;         // of few tokens, see few_tokens()
 
 // Output tile of WM x WN waves, each MI x NJ products of 32 x 32; stages of 128 reduction bytes (whole lines; half as many: 7 % slower), NS of them in LDS: while one is
 // multiplied, the next ones are on their way (buffer loads into LDS, rows beyond the operand and bytes beyond the reduction read as zeros).
@@ -238,17 +238,19 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
 // in LDS -- the tokens are small and come from the caches -- and multiplies them with 16 channels at a time: a wave has an eighth of the
 // reduction, loads its 16 bytes of 16 weight rows per lane straight into the products' operand (16 x 16 x 64), and the eight sums meet in
 // LDS.  The first channels' weights are on their way while the codes are made.  Bound by reading the weights once, behind the codes: 1 token through
-// 4096 x 4096 5.9 us (16.8 MB; 3.3 at a copy's rate), 9 through 1000 x 2048 10.2 (latency: values, maxima, codes, products one after the other).
+// 4096 x 4096 5.9 us (16.8 MB; 3.3 at a copy's rate), 9 through 1000 x 2048 7 (latency: values, maxima, codes, products one after the other).
 // ------------------------------------------------------------------------------------------------
 constexpr int FW = 8;            // waves
 constexpr int FL = 8;            // weight loads of a lane in flight: 512 reduction bytes of a wave
 __host__ __device__ constexpr int few_pitch(int Kp) { return ((Kp + 255) & ~255) + 16; }       // rows of codes 16 bytes apart modulo the banks
-// RM: tokens whose values are loaded together (more at a time gain nothing: 9 tokens 2048 -> 1000 with all at once 12.9 us, code to fetch).
-template <int TYPE, int RM>
-__global__ __launch_bounds__(64 * FW) void few_tokens_kernel(const FewArgs a) {
+// Codes: WPR waves have a token, or ROWS of them (the second eight after the first), whose values stay in registers while their maximum is found where
+// they are at most 512 WPR CH (beyond, they are read again).  One token by all eight waves, up to four by two each, others by a wave each, with no wait for
+// one another.
+template <int TYPE, int WPR, int ROWS, int CH>
+__global__ __launch_bounds__(64 * FW, 4) void few_tokens_kernel(const FewArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     extern __shared__ __attribute__((aligned(1024))) int8_t codes[];      // [M][few_pitch]
-    __shared__ float part[FW][16], scales[16], invs[16];
+    __shared__ float part[FW], scales[16];
     __shared__ __attribute__((aligned(16))) int sums[FW][4][64];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, kg = lane >> 4;
@@ -271,46 +273,60 @@ __global__ __launch_bounds__(64 * FW) void few_tokens_kernel(const FewArgs a) {
     int tile = (int)blockIdx.x;
     fetch(tile, c_from);
 
-    // maxima, scales, codes of the tokens: a thread has eight neighbouring values of every row
-    const T* const x = static_cast<const T*>(a.x);
-    for (int m0 = 0; m0 < a.M; m0 += RM) {
-        float top[RM];
+    // maxima, scales, codes of the tokens
+    {
+        constexpr int SPAN = 512 * WPR * CH;
+        const T* const x = static_cast<const T*>(a.x);
+        const int m0 = wave / WPR, t8 = (tid - m0 * 64 * WPR) * 8;
+        float v[ROWS][CH][8], top[ROWS];
+        const auto values = [&](int base) __attribute__((always_inline)) {
 #pragma unroll
-        for (int m = 0; m < RM; ++m) top[m] = 0.0f;
-        for (int c = tid * 8; c < a.K; c += 64 * FW * 8) {
+            for (int r = 0; r < ROWS; ++r) {
+                const int m = m0 + FW / WPR * r;
 #pragma unroll
-            for (int m = 0; m < RM; ++m) {
-                float v[8];
-                load8<TYPE>(x + (size_t)(m0 + m < a.M ? m0 + m : m0) * a.x_pitch + c, a.K - c, a.wide, v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top[m] = fmaxf(top[m], fabsf(v[i]));
+                for (int u = 0; u < CH; ++u) {
+                    const int c = base + u * 512 * WPR + t8;
+                    load8<TYPE>(x + (size_t)(m < a.M ? m : 0) * a.x_pitch + c, m < a.M ? a.K - c : 0, a.wide, v[r][u]);
+                }
             }
+        };
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) top[r] = 0.0f;
+        for (int base = 0; base < a.K; base += SPAN) {
+            values(base);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                for (int u = 0; u < CH; ++u)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) top[r] = fmaxf(top[r], fabsf(v[r][u][i]));
         }
 #pragma unroll
-        for (int m = 0; m < RM; ++m) {
-            top[m] = wave_max(top[m]);
-            if (lane == 0) part[wave][(m0 + m) & 15] = top[m];          // (those beyond M: another's value, not used)
+        for (int r = 0; r < ROWS; ++r) top[r] = wave_max(top[r]);
+        if (WPR > 1) {
+            if (lane == 0) part[wave] = top[0];
+            __syncthreads();
+            top[0] = part[m0 * WPR];
+#pragma unroll
+            for (int i = 1; i < WPR; ++i) top[0] = fmaxf(top[0], part[m0 * WPR + i]);
         }
-    }
-    __syncthreads();
-    if (tid < a.M) {
-        float top = part[0][tid];
+        for (int base = 0; base < a.Kp; base += SPAN) {
+            if (a.K > SPAN) values(base);
 #pragma unroll
-        for (int i = 1; i < FW; ++i) top = fmaxf(top, part[i][tid]);
-        scales[tid] = scale_of(top);
-        invs[tid] = inv_scale_of(top);
-    }
-    __syncthreads();
-#pragma unroll RM
-    for (int m = 0; m < a.M; ++m) {
-        const float inv = invs[m];
-        for (int c = tid * 8; c < a.Kp; c += 64 * FW * 8) {
-            float v[8];
-            load8<TYPE>(x + (size_t)m * a.x_pitch + c, a.K - c, a.wide, v);
-            int q[8];
+            for (int r = 0; r < ROWS; ++r) {
+                const int m = m0 + FW / WPR * r;
+                const float inv = inv_scale_of(top[r]);
+                if (m >= a.M) continue;
+                if (t8 == 0 && base == 0) scales[m] = scale_of(top[r]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = quantize_one<false>(v[i], inv, 0u, 0u, 0u);
-            *reinterpret_cast<uint2*>(codes + m * pitch + c) = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+                for (int u = 0; u < CH; ++u) {
+                    const int c = base + u * 512 * WPR + t8;
+                    int q[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q[i] = quantize_one<false>(v[r][u][i], inv, 0u, 0u, 0u);
+                    if (c < a.Kp) *reinterpret_cast<uint2*>(codes + m * pitch + c) = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+                }
+            }
         }
     }
     __syncthreads();
@@ -452,22 +468,22 @@ int planned(ProductArgs* a, size_t scratch_bytes) {
     return p.tile;
 }
 
-template <int TYPE, int RM>
+template <int TYPE, int WPR, int ROWS, int CH>
 hipError_t few_of(const FewArgs& a, hipStream_t st) {
-    static std::atomic<unsigned long long> done{0};
-    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&few_tokens_kernel<TYPE, RM>), kFewLds, done);
-    if (e != hipSuccess) return e;
+    static_assert(kFewCodes + 16 * (255 + 16) + 12 * 1024 <= 64 * 1024, "the codes fit what a launch may ask for");
     const int tiles = (a.N + 15) / 16;
     KernelTimer kt(KID_TOKEN_FEW, st);
-    launch_timed(kt, (few_tokens_kernel<TYPE, RM>), dim3(tiles < 512 ? tiles : 512), dim3(64 * FW), (size_t)a.M * few_pitch(a.Kp), st, a);
+    launch_timed(kt, (few_tokens_kernel<TYPE, WPR, ROWS, CH>), dim3(tiles < 512 ? tiles : 512), dim3(64 * FW), (size_t)a.M * few_pitch(a.Kp), st, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-bool few_tokens(int M, int Kp) { return M <= 16 && M * few_pitch(Kp) <= kFewLds; }
+// Up to so many codes it is cheaper that every block makes them for itself than a launch more (us, one launch / two: 8 x 4096 -> 4096 10.6/14.6,
+// 4 x 8192 -> 1000 14.0/15.6, 16 x 2048 -> 4096 9.3/11.3; 16 x 4096 -> 1000 13.3/14.2, -> 4096 16.8/13.8, -> 16384 31/19, 8 x 8192 -> 8192 30/22).
+bool few_tokens(int M, int Kp) { return M <= 16 && M * (long long)Kp <= kFewCodes; }
 hipError_t launch_few_tokens(const FewArgs& a, hipStream_t st) {
-#define LAUNCH(TY) return a.M == 1 ? few_of<TY, 1>(a, st) : few_of<TY, 4>(a, st)
+#define LAUNCH(TY) return a.M == 1 ? few_of<TY, FW, 1, 2>(a, st) : a.M <= FW / 2 ? few_of<TY, 2, 1, 4>(a, st) : a.M <= FW ? few_of<TY, 1, 1, 8>(a, st) : few_of<TY, 1, 2, 4>(a, st)
     if (a.type == kF32) LAUNCH(kF32);
     if (a.type == kBF16) LAUNCH(kBF16);
     LAUNCH(kF16);

@@ -195,6 +195,13 @@ def test_served_linear(M, K, N, dtype, bias):
     same(layer(x.to(DEV).t().contiguous().t()), want, dtype)
 
 
+# few tokens: by eight waves, two or one each or two rows of a wave, rows longer than stay in registers, and just too many codes for one launch
+@pytest.mark.parametrize("M,K,N", [(1, 9000, 33), (1, 33000, 20), (3, 8200, 40), (4, 20, 17), (7, 4600, 72), (8, 4096, 16), (9, 3600, 40), (13, 2040, 50), (16, 2048, 8200), (16, 2064, 24)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_served_few_tokens(M, K, N, dtype):
+    test_served_linear(M, K, N, dtype, True)
+
+
 def _train(x, w, b, g, seed, device=DEV):
     x, w = (t.to(device).requires_grad_(True) for t in (x, w))
     b = None if b is None else torch.from_numpy(b).to(device).requires_grad_(True)
