@@ -111,6 +111,7 @@ int8t_status attend_ok(const int8t_cache* c, const int8t_attend_desc* d) {
     if (d->tokens < 0 || d->requests < 0 || d->group <= 0 || d->table_width < 0 || d->longest < 0) return INT8T_ERR_SHAPE;
     if ((unsigned long long)d->tokens * (unsigned long long)c->heads * (unsigned long long)d->group > 0x7fffffffull) return INT8T_ERR_SHAPE;
     if ((unsigned long long)d->tokens * (unsigned long long)d->group / 16 + (unsigned long long)d->requests > 0x7fffffull) return INT8T_ERR_SHAPE;
+    if (((unsigned long long)d->tokens * (unsigned long long)d->group / 16 + (unsigned long long)d->requests) * (unsigned long long)c->heads > 0x7fffffffull) return INT8T_ERR_SHAPE;
     if ((long long)d->table_width * c->page_size > 0x7fffffffll || d->table_pitch < (size_t)d->table_width) return INT8T_ERR_SHAPE;
     return INT8T_OK;
 }
@@ -124,6 +125,7 @@ AttendArgs attend_args(const int8t_cache* c, const int8t_attend_desc* d) {
     a.requests = d->requests;
     a.group = d->group;
     a.by_group = fast_div((unsigned)d->group);
+    a.by_heads = fast_div((unsigned)c->heads);
     a.width = d->table_width;
     a.type = d->type;
     a.causal = d->causal;

@@ -25,13 +25,16 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
     extern __shared__ __attribute__((aligned(1024))) float lds[];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n16 = lane & 15, kg = lane >> 4;
-    const int head = (int)blockIdx.y, split = (int)blockIdx.z;
+    // Heads first: an XCD has as few heads' keys in its L2 as can be, and blocks without rows, a few for each request, lie together.  (Tiles first: 16
+    // requests of 16 tokens over 2048 keys, 8 heads of 256, 152 us, not 84; the next token of 64 requests over 4096 keys, 8 of 128, 121, not 107.)
+    const int place = (int)(blockIdx.y * gridDim.x + blockIdx.x), group_of = div_by(place, a.by_heads);
+    const int head = place - group_of * a.c.heads, split = (int)blockIdx.z, block = (int)gridDim.x - 1 - group_of;
     const int D = a.c.dim;
 
-    const int b = tile_request(a, (int)blockIdx.x, 16);
+    const int b = tile_request(a, block, 16);
     const Request rq = request_of(a, b);
     const int nrows = rq.tokens * a.group;
-    const long long tile = (long long)blockIdx.x - ((long long)a.starts[b] * a.group / 16 + b);
+    const long long tile = (long long)block - ((long long)a.starts[b] * a.group / 16 + b);
     if (tile < 0 || tile * 16 >= nrows) return;
     const int r0 = (int)tile * 16;
     const int heads = a.c.heads * a.group;
@@ -423,17 +426,20 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
 }  // namespace
 
 // Rows of a block and shares of the keys.  Blocks of 16 rows stream the cache; the larger ones of token_attend_chunk.hip multiply it, from so many
-// rows of a request on average that they are faster (us with 16 rows / with more, 8 heads, pages of 64 tokens, 16 and 8 requests over
-// 2048 keys with 64 rows each, 16 with 128, 4 over 1024 with 256, 1 over 8192 with 512 and 2048, 2 over 4096 with 4096):
-//   dim  64 bf16 (128 rows)  34/45 25/29  52/49  20/25  46/41  146/103  271/146     (256 rows: 69 34 71 29 48 103 241)
-//   dim  64 fp32 (128 rows)  39/55 27/33  60/62  23/29  54/50  177/132  309/184     (256 rows: 86 41 88 33 56 126 301)
-//   dim 128 bf16 (256 rows)  61/86 40/42  94/89  30/34  70/55  254/131  442/297     (128 rows: 101 54 110 43 82 242 345)
-//   dim 128 fp32 (128 rows)  65/126 42/65 100/138 34/52 89/104 302/306  521/436     (256 rows: 317 146 327 72 177 549 1232)
-//   dim 256 bf16 (128 rows)  152/173 91/90 238/188 74/67 170/144 602/419 1078/600
-//   dim 256 fp32 (128 rows)  240/320 138/157 378/383 116/112 268/255 973/785 1924/1125
-//   pages of 24 tokens, dim 64 bf16  53/50 29/38  82/52  28/34  62/52  350/148      (the second with 32 rows each; the sixth as the seventh above)
-//   pages of 24 tokens, dim 128 fp32 101/125 41/65 153/136 54/63 115/133 756/443
-//   pages of 7 tokens,  dim 64 bf16  83/48 46/38  147/51 44/34  95/53  585/150
+// rows of a request on average that they are faster (us with 16 rows / with 128, dim 128 in bf16: 256; all keys seen; rows of a request, requests, heads, keys:
+//                       32, 9, 12, 1500   66, 9, 12, 1500  100, 9, 12, 1500  128, 16, 8, 2048  264, 8, 8, 2048  256, 4, 8, 2048  400, 4, 8, 3000  2048, 1, 8, 8192
+//   pages of 16, dim 64 bf16    22/36             28/39            33/31             46/54             52/50            24/25            56/44           142/85
+//                dim 64 fp32    23/41             31/44            38/35             49/64             59/60            27/29            63/54           167/107
+//               dim 128 bf16    27/65             41/66            51/67             69/102            79/59            27/54            89/77           245/104
+//               dim 128 fp32    30/81             47/87            59/67             78/148            96/131           31/54           106/108          283/241
+//               dim 256 bf16    56/114           111/121          121/92            160/205           198/178           55/75           202/147          589/327
+//               dim 256 fp32    81/199           175/212          189/162           247/368           325/320           78/124          311/258          944/597
+//   pages of 24, dim 64 bf16    30/36             38/40            41/32             56/55             65/51            27/26            65/46           176/89
+//               dim 128 bf16    37/65             49/66            71/67             94/101           102/61            38/55           102/77           278/104
+//               dim 128 fp32    40/82             74/88            83/67            107/148           131/132           37/54           139/108          372/240
+//   pages of 7,  dim 64 bf16    46/37             61/40            63/31             87/55            104/51            37/27            98/46           283/90
+//               dim 128 bf16    55/65             74/67           121/67            160/102           160/63            49/56           155/78           412/106
+//               dim 256 bf16    72/116           156/122          163/93            216/204           268/180           68/75           258/147          719/328).
 // Shares of the keys of larger blocks: up to a block for each compute unit (two blocks of 128 rows), of 1024 keys at least (dim 128, bf16: 128 tokens of 32 heads
 // over 8192 keys in 1, 2, 4, 8, 16 shares: 310, 170, 97, 63, 77; 4 x 128 tokens over 2048 keys: 89, 61, 72, 77, 76), of 256 where blocks have 128
 // rows (9 requests of 1 to 131 tokens over 0 to 1500 keys, 12 heads, dim 64, fp32, shares of 1024, 512, 256: 56, 38, 30).
@@ -441,10 +447,10 @@ void attend_plan(AttendArgs* a, int longest) {
     const long long rows = (long long)a->tokens * a->group, each = rows / a->requests;
     const bool fp32 = a->type == kF32;
     const int dim = a->c.dim <= 64 ? 64 : a->c.dim <= 128 ? 128 : 256;
-    int many = dim == 64 ? (fp32 ? 384 : 128) : dim == 128 ? (fp32 ? 2048 : 128) : fp32 ? 256 : 128;
+    int many = dim == 128 && fp32 ? 1024 : 384;
     // smaller ones look a table up for four keys at a time, or for each: they look less often
-    if (a->c.page_size % 4 != 0) many = 48;
-    else if (a->c.page_size % 16 != 0) many = many > 1024 ? 1024 : dim == 64 ? 64 : 128;
+    if (a->c.page_size % 4 != 0) many = dim == 64 ? 24 : 64;
+    else if (a->c.page_size % 16 != 0) many = dim == 64 ? 64 : dim == 128 && !fp32 ? 192 : 384;
     a->rows = each < many ? 16 : dim == 128 && !fp32 ? 256 : 128;
     const long long tiles = (rows / a->rows + a->requests) * a->c.heads;
     if (a->rows == 16) {

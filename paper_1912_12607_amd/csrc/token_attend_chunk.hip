@@ -53,8 +53,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
     const int n32 = lane & 31, half = lane >> 5;
     // Heads first, so that an XCD has as few heads' keys in its L2 as can be, and each request's last rows, which see the most keys, before its others, so that
     // the chip runs out of short blocks (tiles first, in order: 650 us for two chunks of 2048 tokens over 8192 keys, not 597).
-    const unsigned long long place = (unsigned long long)blockIdx.y * gridDim.x + blockIdx.x;
-    const int head = (int)(place % gridDim.y), split = (int)blockIdx.z, block = (int)gridDim.x - 1 - (int)(place / gridDim.y);
+    const int place = (int)(blockIdx.y * gridDim.x + blockIdx.x), group_of = div_by(place, a.by_heads);
+    const int head = place - group_of * a.c.heads, split = (int)blockIdx.z, block = (int)gridDim.x - 1 - group_of;
     const int D = a.c.dim;
 
     const int b = tile_request(a, block, ROWS);

@@ -160,7 +160,7 @@ struct AttendArgs {
     const int *starts, *lengths, *table;
     size_t table_pitch;
     int tokens, requests, group, width, type, causal;
-    FastDiv by_group;
+    FastDiv by_group, by_heads;
     float scale;
     void* out;               // [tokens][heads * group][dim]
     float* lse;              // [tokens][heads * group], or null
