@@ -300,7 +300,7 @@ class PagedCache:
         """Attention of new tokens, (tokens, query heads, dim), over the pages of their requests: request b's are
         starts[b] .. starts[b + 1] - 1 and see the first lengths[b] keys of pages table[b], causal: each up to its own place (the last
         new token sees all).  Query heads are a multiple of the cache's; head h goes with h // group.  `longest`: no length is larger
-        (divides the work; the result does not depend on it).  int32 starts (requests + 1), lengths (requests), table (requests, width).
+        (a guide for the division of the work, by which sums are ordered).  int32 starts (requests + 1), lengths (requests), table (requests, width).
         A token that sees nothing gets zeros (logarithm of its sum: -inf).  No gradients."""
         kind = B.DTYPES.get(q.dtype)
         shape, index = q.shape, self._index

@@ -152,6 +152,13 @@ def test_attend_arguments():
     assert go(tokens=0, q=None) == 0
 
 
+def test_attend_of_too_many_blocks():
+    c = cache(heads=65535, dim=16, page_size=1)
+    d = B.AttendDesc(4, 1 << 20, 1, 8, 0, 0, 1, 0.125, 16, 16, 8)
+    assert call("int8t_cache_attend", C.byref(c), C.byref(d), FAKE, FAKE, FAKE, FAKE, FAKE, None, FAKE, BIG, None) == SHAPE
+    assert call("int8t_cache_attend_workspace_bytes", C.byref(c), C.byref(d)) == 0
+
+
 def test_host_tensors_are_refused():
     x, w = torch.zeros(2, 32), torch.zeros(4, 32)
     with pytest.raises(RuntimeError, match="device"):
