@@ -9,8 +9,8 @@
 //   values   O^T[dim][row] = V^T P^T: the scores' layout is P^T's operand layout with the keys in the order that the transposing LDS read
 //            of V (rows of keys, as they came) delivers: p never leaves its lane.
 // Bound by vector and matrix units together: a score costs 9 to 10 vector operations, of which the exponential counts for four, and 256 multiply-adds
-// (DIM 128), and what one wave's softmax takes the other's products give back only in part.  Two chunks of 2048 tokens over 8192 keys, 32 heads of 128 on 8, bf16:
-// 640 us (478 GFLOP: 0.75 PFLOP/s; a large library product in fp16 1.18).  Nine fp32 requests of up to 131 tokens over up to 1500 keys, 12 heads of 64: 25 us.
+// (DIM 128), and arithmetic of one wave and products of another overlap by half only (fma 295 us, products 322, together 466).  Two chunks of 2048 tokens over 8192 keys, 32 heads of 128 on 8, bf16:
+// 585 to 608 us (478 GFLOP: 0.8 PFLOP/s; a large library product in fp16 1.18).  Nine fp32 requests of up to 131 tokens over up to 1500 keys, 12 heads of 64: 25 us.
 #include "token_attend.h"
 
 namespace int8t {
