@@ -454,9 +454,13 @@ void attend_plan(AttendArgs* a, int longest) {
     a->rows = each < many ? 16 : dim == 128 && !fp32 ? 256 : 128;
     const long long tiles = (rows / a->rows + a->requests) * a->c.heads;
     if (a->rows == 16) {
-        // Shares of a fixed number of keys, so that long requests among short ones have more blocks: 2048, or down to 1024 where that brings
-        // more blocks to the chip
-        a->share = tiles * ((longest + 2047) / 2048) >= 512 ? 2048 : 1024;
+        // Shares of a fixed number of keys, so that long requests among short ones have more blocks: 2048, or 1024 where those are too few (below 128), or
+        // too many for one block of eight waves on each compute unit and too few for two of four (us, shares of 1024 / 2048: single tokens of 1 request over
+        // 2048 keys 16/19, over 8192 19/24, over 32768 39/33, 4 requests over 8192 29/25, 16 over 2000 25/20, 8 over 1 to 8192 29/30, 64 over 4096 113/107;
+        // 20 tokens of 9 over 1 to 4000 27/31).  Eight waves where blocks are few (4 requests over 8192, four / eight waves: 29/25, 16 50/55, 64 over 4096
+        // 107/116).
+        const long long blocks = tiles * ((longest + 2047) / 2048);
+        a->share = blocks >= 512 || (blocks >= 128 && blocks <= 256) ? 2048 : 1024;
         a->splits = (longest + a->share - 1) / a->share;
         a->waves = tiles * a->splits <= 256 ? 8 : 4;
         if (a->splits > 256) {
