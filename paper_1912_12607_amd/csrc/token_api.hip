@@ -17,6 +17,8 @@ inline size_t bytes_of(int8t_dtype t) { return t == INT8T_F32 ? 4 : 2; }
 inline bool codes_ok(int rows, int cols) {
     return rows > 0 && cols > 0 && cols <= 0x7ffffff0 && (unsigned long long)rows * (unsigned long long)pad16(cols) < (1ull << 31);
 }
+// ... of rows: long ones are passed kLongSpan values at a time, counted in an int
+inline bool rows_ok(int rows, int cols) { return codes_ok(rows, cols) && cols <= 0x7fffffff - kLongSpan + 1; }
 inline size_t code_bytes(int rows, int cols) { return align256((size_t)rows * pad16(cols)); }
 inline int8t_status launched(hipError_t e) { return e == hipSuccess ? INT8T_OK : INT8T_ERR_RUNTIME; }
 
@@ -146,7 +148,7 @@ size_t attend_bytes(const AttendArgs& a) {
 extern "C" int8t_status int8t_quantize_rows(const void* x_dev, int8t_dtype type, int rows, int cols, size_t pitch, const float* factor_dev, int8t_round mode,
                                             uint64_t seed, int8_t* q_dev, float* scale_dev, void* stream) {
     if (!x_dev || !q_dev || !scale_dev) return INT8T_ERR_NULL;
-    if (!codes_ok(rows, cols) || pitch < (size_t)cols) return INT8T_ERR_SHAPE;
+    if (!rows_ok(rows, cols) || pitch < (size_t)cols) return INT8T_ERR_SHAPE;
     if (!type_ok(type) || (mode != INT8T_ROUND_NEAREST_EVEN && mode != INT8T_ROUND_STOCHASTIC)) return INT8T_ERR_ARG;
     if (!aligned(x_dev, bytes_of(type)) || !aligned16(factor_dev) || !aligned16(q_dev) || !aligned16(scale_dev)) return INT8T_ERR_ARG;
     const RowsArgs a{x_dev, pitch, type, rows, cols, factor_dev, mode == INT8T_ROUND_STOCHASTIC, seed, q_dev, scale_dev};

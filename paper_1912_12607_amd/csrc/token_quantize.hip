@@ -32,6 +32,7 @@ template <int TYPE, bool STOCH, int TPR, int CH, bool LONG>
 __device__ __forceinline__ void rows_body(const RowsArgs& a, const int block, const int wide, const uint32_t kx, const uint32_t ka) {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int RPB = TPR < 256 ? 256 / TPR : 1, SPAN = TPR * 8 * CH;
+    static_assert(!LONG || SPAN == kLongSpan, "the step that the limit of columns goes by");
     const int t = (int)threadIdx.x % TPR;
     const int row = block * RPB + (int)threadIdx.x / TPR;
     const bool live = row < a.rows;            // (all lanes stay for the reductions)

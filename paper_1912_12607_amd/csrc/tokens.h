@@ -76,6 +76,7 @@ struct RowsArgs {            // codes of rows x cols values, a scale for each ro
     int8_t* q;               // [rows][pad16(cols)]
     float* scale;            // rows
 };
+constexpr int kLongSpan = 32768;         // values of a row that a block holds; longer rows are passed in steps of so many: at most 2^31 - kLongSpan columns
 // with b (as many columns, the same type and rounding to nearest in both): two matrices in one launch
 hipError_t launch_quantize_rows(const RowsArgs& a, hipStream_t st, const RowsArgs* b = nullptr);
 
