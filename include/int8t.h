@@ -534,7 +534,7 @@ typedef enum { INT8T_F32 = 0, INT8T_BF16 = 1, INT8T_F16 = 2, INT8T_DTYPE_MAX_ENU
  * Codes with a scale for each row: v = x (times factor[col], rounded, where factor_dev is given), c = max|v| of the row,
  * codes as int8t_quantize makes them of v with that c; the draw of an element goes by row * cols + col.
  *   x_dev       rows x cols elements of `type`, rows `pitch` elements apart (pitch >= cols); rows * (cols rounded up to 16) < 2^31,
- *               cols at most 2^31 - 2^15
+ *               cols at most 2^31 - 2^15, rows at most 2^26 - 4 (so do linear layers' tokens and weights)
  *   factor_dev  NULL, or cols floats
  *   q_dev       out: codes of rows x cols;   scale_dev  out: rows floats, c / 127
  */

@@ -18,7 +18,7 @@ inline bool codes_ok(int rows, int cols) {
     return rows > 0 && cols > 0 && cols <= 0x7ffffff0 && (unsigned long long)rows * (unsigned long long)pad16(cols) < (1ull << 31);
 }
 // ... of rows: long ones are passed kLongSpan values at a time, counted in an int
-inline bool rows_ok(int rows, int cols) { return codes_ok(rows, cols) && cols <= 0x7fffffff - kLongSpan + 1; }
+inline bool rows_ok(int rows, int cols) { return codes_ok(rows, cols) && cols <= 0x7fffffff - kLongSpan + 1 && rows <= kMostRows; }
 inline size_t code_bytes(int rows, int cols) { return align256((size_t)rows * pad16(cols)); }
 inline int8t_status launched(hipError_t e) { return e == hipSuccess ? INT8T_OK : INT8T_ERR_RUNTIME; }
 
@@ -183,7 +183,7 @@ extern "C" size_t int8t_product_workspace_bytes(int M, int N, int K) {
 extern "C" int8t_status int8t_product(const int8_t* a_dev, const float* sa_dev, const int8_t* b_dev, const float* sb_dev, int M, int N, int K,
                                       const float* bias_dev, void* y_dev, int8t_dtype type, size_t pitch, void* ws_dev, size_t ws_bytes, void* stream) {
     if (!a_dev || !sa_dev || !b_dev || !y_dev) return INT8T_ERR_NULL;
-    if (!codes_ok(M, K) || !codes_ok(N, K) || K > INT8T_MAX_REDUCTION || pitch < (size_t)N) return INT8T_ERR_SHAPE;
+    if (!codes_ok(M, K) || !codes_ok(N, K) || K > INT8T_MAX_REDUCTION || pitch < (size_t)N || !product_fits(M, N, pad16(K))) return INT8T_ERR_SHAPE;
     if (!type_ok(type) || !aligned16(a_dev) || !aligned16(b_dev) || !aligned(sa_dev, 4) || !aligned(sb_dev, 4) || !aligned(bias_dev, 4) ||
         !aligned(y_dev, bytes_of(type)) || !aligned16(ws_dev))
         return INT8T_ERR_ARG;
@@ -214,14 +214,16 @@ extern "C" int8t_status int8t_linear_fwd(const int8t_linear_desc* d, const int8t
         if (b->ws_bytes < s.bytes) return INT8T_ERR_WORKSPACE;
     }
     const hipStream_t st = (hipStream_t)stream;
+    const bool few = served && few_tokens(d->M, pad16(d->K));
+    if ((b->w && d->N > kMostRows) || (!few && d->M > kMostRows)) return INT8T_ERR_SHAPE;
     const RowsArgs w{b->w, b->w_pitch, d->wtype, d->N, d->K, nullptr, 0, 0, b->wq, b->sw};
     if (d->M == 0) return b->w ? launched(launch_quantize_rows(w, st)) : INT8T_OK;
-    if (served && few_tokens(d->M, pad16(d->K))) {
+    if (few) {
         const int wide = (((uintptr_t)b->x | b->x_pitch * bytes_of(d->type)) & 15) == 0;
         return launched(launch_few_tokens(FewArgs{b->x, b->x_pitch, d->type, d->M, d->K, pad16(d->K), d->N, wide, b->wq, b->sw, b->bias, b->y, b->y_pitch}, st));
     }
     const RowsArgs x{b->x, b->x_pitch, d->type, d->M, d->K, nullptr, 0, 0, b->xq ? b->xq : s.xq, b->sx ? b->sx : s.sx};
-    const bool together = b->w && d->wtype == d->type;
+    const bool together = b->w && d->wtype == d->type && (long long)d->M + d->N <= kMostRows;
     hipError_t e = b->w && !together ? launch_quantize_rows(w, st) : hipSuccess;
     if (e == hipSuccess) e = launch_quantize_rows(x, st, together ? &w : nullptr);
     if (e != hipSuccess) return INT8T_ERR_RUNTIME;

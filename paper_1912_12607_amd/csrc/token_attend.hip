@@ -349,7 +349,7 @@ template <int TYPE>
 __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     const size_t rows = (size_t)a.tokens * a.c.heads * a.group;
-    const size_t row = (size_t)blockIdx.x * 16 + ((int)threadIdx.x >> 4);
+    const size_t row = ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * 16 + ((int)threadIdx.x >> 4);      // (y: a launch has fewer than 2^32 threads a dimension)
     const int l = (int)threadIdx.x & 15, D = a.c.dim;
     const bool have = row < rows;                       // (all lanes stay for the exchanges)
     const size_t r = have ? row : 0;
@@ -417,8 +417,9 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
     }
     if (a.splits > 1) {
         const size_t rows = (size_t)a.tokens * a.c.heads * a.group;
+        const size_t blocks = (rows + 15) / 16, x = blocks < (1u << 22) ? blocks : (1u << 22);
         KernelTimer kt(KID_ATTEND_JOIN, st);
-        launch_timed(kt, attend_join_kernel<TYPE>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, a);
+        launch_timed(kt, attend_join_kernel<TYPE>, dim3((unsigned)x, (unsigned)((blocks + x - 1) / x)), dim3(256), 0, st, a);
     }
     return hipGetLastError();
 }

@@ -16,14 +16,14 @@ __device__ __forceinline__ bool place_of(const CacheArgs& c, long long slot, siz
     return true;
 }
 
-// LANES neighbouring lanes have a row of up to 8 LANES values; a block has 256 / LANES rows, keys in blocks with z = 0 and values in
-// those with y = 1.  Bound by memory: 16384 tokens of 8 heads of 128 values, fp16, are written in 24.5 us and read back in 20.3 (102 MB each way: 4.2 and
+// LANES neighbouring lanes have a row of up to 8 LANES values; a block has 256 / LANES rows, keys in blocks with y = 0 and values in
+// those with y = 1 (z: a launch has fewer than 2^32 threads a dimension, and there may be more rows than that).  Bound by memory: 16384 tokens of 8 heads of 128 values, fp16, are written in 24.5 us and read back in 20.3 (102 MB each way: 4.2 and
 // 5.0 TB/s, a large copy 5.1; writes leave scattered lines of 128 bytes and single scales); 64 tokens take the 3 us of a launch.
 template <int TYPE, int LANES>
 __global__ __launch_bounds__(256) void cache_write_kernel(const CacheMoveArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     const int l = (int)threadIdx.x % LANES;
-    const long long row = (long long)blockIdx.x * (256 / LANES) + (int)threadIdx.x / LANES;
+    const long long row = ((long long)blockIdx.z * gridDim.x + blockIdx.x) * (256 / LANES) + (int)threadIdx.x / LANES;
     const long long token = row / a.c.heads;
     const int head = (int)(row - token * a.c.heads);
     const bool values = blockIdx.y != 0;
@@ -57,7 +57,7 @@ template <int TYPE, int LANES>
 __global__ __launch_bounds__(256) void cache_read_kernel(const CacheMoveArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     const int l = (int)threadIdx.x % LANES;
-    const long long row = (long long)blockIdx.x * (256 / LANES) + (int)threadIdx.x / LANES;
+    const long long row = ((long long)blockIdx.z * gridDim.x + blockIdx.x) * (256 / LANES) + (int)threadIdx.x / LANES;
     const long long token = row / a.c.heads;
     const int head = (int)(row - token * a.c.heads);
     if (token >= a.tokens || 8 * l >= a.c.dim) return;
@@ -77,9 +77,11 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const CacheMoveArgs a) 
     store8<TYPE>(x + 8 * l, 8, a.wide, v);
 }
 
+constexpr long long kMostBlocks = 1 << 22;
 template <int TYPE, int LANES>
 void move_of(const CacheMoveArgs& a, bool write, hipStream_t st) {
-    const dim3 grid((unsigned)(((long long)a.tokens * a.c.heads + 256 / LANES - 1) / (256 / LANES)), 2);
+    const long long blocks = ((long long)a.tokens * a.c.heads + 256 / LANES - 1) / (256 / LANES), x = blocks < kMostBlocks ? blocks : kMostBlocks;
+    const dim3 grid((unsigned)x, 2, (unsigned)((blocks + x - 1) / x));
     KernelTimer kt(write ? KID_CACHE_WRITE : KID_CACHE_READ, st);
     if (write) launch_timed(kt, (cache_write_kernel<TYPE, LANES>), grid, dim3(256), 0, st, a);
     else launch_timed(kt, (cache_read_kernel<TYPE, LANES>), grid, dim3(256), 0, st, a);

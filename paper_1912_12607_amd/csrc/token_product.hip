@@ -490,6 +490,15 @@ hipError_t launch_few_tokens(const FewArgs& a, hipStream_t st) {
 #undef LAUNCH
 }
 
+bool product_fits(int M, int N, int Kp) {
+    static const int kRows[4] = {256, 128, 128, 64};
+    for (const bool scratch : {false, true}) {
+        const ProductPlan p = product_plan(M, N, Kp, scratch);
+        const unsigned long long blocks = ((unsigned long long)M + kRows[p.tile] - 1) / kRows[p.tile] * (((unsigned long long)N + kRows[p.tile] - 1) / kRows[p.tile]) * p.splits;
+        if ((blocks + 8) * (p.tile == 0 ? 512 : 256) >= 1ull << 32) return false;
+    }
+    return true;
+}
 size_t product_scratch(int M, int N, int Kp) {
     const ProductPlan p = product_plan(M, N, Kp, true);
     return p.splits > 1 ? (size_t)p.splits * M * ((N + 3) & ~3) * sizeof(int32_t) : 0;

@@ -77,6 +77,7 @@ struct RowsArgs {            // codes of rows x cols values, a scale for each ro
     float* scale;            // rows
 };
 constexpr int kLongSpan = 32768;         // values of a row that a block holds; longer rows are passed in steps of so many: at most 2^31 - kLongSpan columns
+constexpr int kMostRows = (1 << 26) - 4;  // a launch has fewer than 2^32 threads, a row 64 at least
 // with b (as many columns, the same type and rounding to nearest in both): two matrices in one launch
 hipError_t launch_quantize_rows(const RowsArgs& a, hipStream_t st, const RowsArgs* b = nullptr);
 
@@ -129,6 +130,7 @@ struct FewArgs {             // the same from x itself, codes made on the way: f
 };
 bool few_tokens(int M, int Kp);
 hipError_t launch_few_tokens(const FewArgs& a, hipStream_t st);
+bool product_fits(int M, int N, int Kp);      // its blocks fit a launch
 size_t product_scratch(int M, int N, int Kp);
 hipError_t launch_product(ProductArgs a, size_t scratch_bytes, hipStream_t st);
 // Two products, in one launch where both take the same tiles whole.  They share the scratch.

@@ -18,3 +18,19 @@ NULL, SHAPE, ARG, WORKSPACE = 1, 2, 3, 4
 @pytest.mark.parametrize("cols", [(1 << 31) - 32767, (1 << 31) - 16])
 def test_rows_that_a_loop_cannot_count(cols):
     assert B.lib.int8t_quantize_rows(FAKE, B.BF16, 1, cols, cols, None, 0, 0, FAKE, FAKE, None) == SHAPE
+
+
+def linear(M, K, N, w=None, xq=None, ws=FAKE):
+    b = B.LinearBuffers(x=FAKE, w=w, x_pitch=K, w_pitch=K, y_pitch=N, xq=xq, wq=FAKE, sx=xq, sw=FAKE, y=FAKE, ws=ws, ws_bytes=BIG)
+    return B.lib.int8t_linear_fwd(C.byref(B.LinearDesc(M, K, N, B.BF16, B.BF16)), C.byref(b), None)
+
+
+# 2^32 threads and more in a launch: 64 at least for a row, 256 for a tile of 64 x 64 results
+def test_launches_of_too_many_threads():
+    most = (1 << 26) - 4
+    assert B.lib.int8t_quantize_rows(FAKE, B.BF16, most + 1, 16, 16, None, 0, 0, FAKE, FAKE, None) == SHAPE
+    assert linear(most + 1, 16, 5) == SHAPE                                 # served
+    assert linear(most + 1, 16, 5, w=FAKE, xq=FAKE) == SHAPE                # kept for a backward pass
+    assert linear(5, 16, most + 1, w=FAKE, xq=FAKE) == SHAPE                # as many output channels
+    for M, N in ((1 << 26, 1 << 26), (1 << 20, 1 << 25)):
+        assert B.lib.int8t_product(FAKE, FAKE, FAKE, FAKE, M, N, 16, None, FAKE, B.BF16, N, None, 0, None) == SHAPE
