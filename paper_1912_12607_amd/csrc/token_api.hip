@@ -114,7 +114,7 @@ int8t_status attend_ok(const int8t_cache* c, const int8t_attend_desc* d) {
     if ((unsigned long long)d->tokens * (unsigned long long)c->heads * (unsigned long long)d->group > 0x7fffffffull) return INT8T_ERR_SHAPE;
     if ((unsigned long long)d->tokens * (unsigned long long)d->group / 16 + (unsigned long long)d->requests > 0x7fffffull) return INT8T_ERR_SHAPE;
     if (((unsigned long long)d->tokens * (unsigned long long)d->group / 16 + (unsigned long long)d->requests) * (unsigned long long)c->heads > 0x7fffffffull) return INT8T_ERR_SHAPE;
-    if ((long long)d->table_width * c->page_size > 0x7fffffffll || d->table_pitch < (size_t)d->table_width) return INT8T_ERR_SHAPE;
+    if ((long long)d->table_width * c->page_size > kMostKeys || d->table_pitch < (size_t)d->table_width) return INT8T_ERR_SHAPE;
     return INT8T_OK;
 }
 AttendArgs attend_args(const int8t_cache* c, const int8t_attend_desc* d) {

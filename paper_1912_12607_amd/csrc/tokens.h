@@ -156,6 +156,8 @@ hipError_t launch_cache_write(const CacheMoveArgs& a, hipStream_t st);
 hipError_t launch_cache_read(const CacheMoveArgs& a, hipStream_t st);
 
 // ---- token_attend.hip, token_attend_chunk.hip --------------------------------------------------------------------------
+// Keys that a table may have: the kernels look at the pages of tiles ahead, some 300 keys behind the last, and round lengths up to a share of 2048, in an int.
+constexpr long long kMostKeys = 0x7fffffffll - 4096;
 struct AttendArgs {
     CacheArgs c;
     const void* q;

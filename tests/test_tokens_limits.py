@@ -34,3 +34,15 @@ def test_launches_of_too_many_threads():
     assert linear(5, 16, most + 1, w=FAKE, xq=FAKE) == SHAPE                # as many output channels
     for M, N in ((1 << 26, 1 << 26), (1 << 20, 1 << 25)):
         assert B.lib.int8t_product(FAKE, FAKE, FAKE, FAKE, M, N, 16, None, FAKE, B.BF16, N, None, 0, None) == SHAPE
+
+
+# pages of tiles ahead are looked up by places counted in an int: a table whose places nearly fill one is refused
+@pytest.mark.parametrize("width,page,status", [((1 << 31) - 1, 1, SHAPE), ((1 << 27) - 1, 16, SHAPE), ((1 << 21) - 1, 1024, SHAPE),
+                                               ((1 << 31) - 4096, 1, SHAPE), ((1 << 31) - 4097, 1, WORKSPACE)])
+@pytest.mark.parametrize("tokens_", [1, 4000])
+def test_tables_that_an_int_cannot_count(width, page, status, tokens_):
+    c = B.Cache(FAKE, FAKE, FAKE, FAKE, 1, page, 1, 16)
+    d = B.AttendDesc(tokens_, 1, 1, width, 0, B.BF16, 1, 0.25, 16, 16, width)
+    need = B.int8t_cache_attend_workspace_bytes(c, d)
+    assert (need > 0) == (status != SHAPE)
+    assert B.lib.int8t_cache_attend(C.byref(c), C.byref(d), FAKE, FAKE, FAKE, FAKE, FAKE, None, FAKE, max(need, 1) - 1, None) == status
