@@ -95,20 +95,52 @@ __device__ __forceinline__ float halves_sum(float x) { const Pair p = halves(x);
 __device__ __forceinline__ float rows16_max(float x) { const Pair p = rows16(x); return fmaxf(p.a, p.b); }
 __device__ __forceinline__ float rows16_sum(float x) { const Pair p = rows16(x); return p.a + p.b; }
 
-// The power of two that p carries: p times a value scale is held in fp16, and 2^up times the largest scale seen so far lies between 2^14 and
-// 2^15, so that it fits, with room below (p may pass 1 by a factor below 2).
-struct ValueUnit {
-    float up = 0.0f, ref = -1.0f;            // ref: the largest scale that up allows
-    // `largest`, of all of the wave's rows: the change of up
-    __device__ __forceinline__ float raise(float largest) {
-        if (!(largest > ref)) return 0.0f;
-        const int e = max((int)((__float_as_uint(largest) >> 23) & 255u), 27);
-        const float before = up;
-        up = (float)(14 + 127 - e);
-        ref = __uint_as_float(((uint32_t)(e + 1) << 23) - 1u);
-        return up - before;
+// What a row's p carries, as a power of two: p_j = 2^(s_j + c), s_j its scores times log2(e), so that l = sum p and the weights w_j = p_j vs_j that the
+// products take in fp16 share it.  c brings the largest weight that the row has seen to 2^14 .. 2^15, where fp16 has 11 bits down to 2^-28 of it and steps
+// of 2^-38 below; a larger weight lowers c.  It goes by the row's own weights: by the tile's largest scale and score, a key that the row does not see, or
+// sees at 2^-40, would take the bits of the others.
+struct RowUnit {
+    static constexpr float kMostWeight = 63000.0f, kMostSum = 0x1p120f;     // (p alone stays in range where the scales are tiny or zero)
+    float c = 0.0f;
+    float room = kNone;          // p and p vs are finite up to this score; -infinity: nothing seen yet
+    float vs = 0.0f;             // the largest value scale so far, of all rows of the wave
+    static __device__ __forceinline__ float log_of(float scale) { return fminf(__builtin_amdgcn_logf(fabsf(scale)), 128.0f); }
+    // Before p of a tile is formed, where a score may pass `room` or a value scale (each in some lane) vs: whether the size of some row's weights has to be
+    // found out; `top`: its largest score.
+    __device__ __forceinline__ bool unknown(float top, float scale) {
+        vs = fmaxf(vs, wave_max(fabsf(scale)));
+        if (room != kNone) room = limit();
+        return __any(top > room);
     }
+    // then, 2^weight the row's largest: what to multiply l and o with.  (Rows that have seen keys: only as far as p and p vs are finite, so that c
+    // does not depend on what made the wave look.)
+    __device__ __forceinline__ float set(float top, float weight) {
+        if (!(top > room)) return 1.0f;
+        const float before = c;
+        const bool first = room == kNone;
+        c = first ? floorf(fminf(15.0f - weight, 110.0f - top)) : fminf(c, floorf(fminf(100.0f - weight, 110.0f - top)));
+        room = limit();
+        return first ? 0.0f : __builtin_amdgcn_exp2f(c - before);
+    }
+    // after: whether weights are too large for fp16 (or l for fp32), and by how much (l, o, this tile's weights); `largest`, `sum` of the row
+    static __device__ __forceinline__ bool large(float largest, float sum) { return __any(largest > kMostWeight || sum > kMostSum); }
+    __device__ __forceinline__ float lower(float largest, float sum) {
+        const int d = max(max(largest > kMostWeight ? __builtin_amdgcn_frexp_expf(largest) - 15 : 0, sum > kMostSum ? __builtin_amdgcn_frexp_expf(sum) - 105 : 0), 0);
+        c -= (float)d;
+        room += (float)d;
+        return __builtin_ldexpf(1.0f, -d);
+    }
+   private:
+    __device__ __forceinline__ float limit() const { return fminf(112.0f, 126.0f - log_of(vs)) - c; }
 };
+// l to 1/2 .. 1: the shares of a row are joined by m = log2 of what l and o are in units of, and l;  *down: what o is to be multiplied with
+__device__ __forceinline__ float normalised(float c, float* l, float* down) {
+    const int e = __builtin_amdgcn_frexp_expf(*l);
+    *down = __builtin_ldexpf(1.0f, -e);
+    const float m = *l == 0.0f ? kNone : (float)e - c;
+    *l *= *down;
+    return m;
+}
 
 // w in two fp16 pieces.  The product that w is must be rounded to fp32 before it is split: left to itself the compiler forms the first
 // piece from the unrounded product and the rest from the rounded one, which differ by a step of the first now and then.

@@ -10,7 +10,7 @@ namespace {
 // out in shares of `share` to blocks and in each to RW waves, which run on their own, 32 keys at a time, the next 32 on their way
 // meanwhile, and join their sums in LDS.
 //   scores   S^T[key][row] = K Q^T (16 x 16 x 32 products): a lane loads 16 bytes of a key, codes become fp16 exactly;
-//   softmax  a lane's eight scores belong to one row; running maximum shared by a row's four lanes, raised when some lane needs it;
+//   softmax  a lane's eight scores belong to one row; its unit (RowUnit) is shared by the row's four lanes and changes when some lane needs it;
 //   values   O^T[dim][row] = V^T P^T: S^T's layout is P^T's operand layout if the keys of a 32 are numbered (lane group, tile, i), so
 //            nothing is exchanged; a lane loads DIM / 16 bytes of eight keys and turns them in registers.
 // PARTS = 2 (fp32): q and p in two fp16 pieces each.  UNI: the page size is a multiple of 16, whole tiles of 16 keys lie on a page and their
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
     const int row = r0 + n16;
     const bool have = row < nrows;
     const int token = div_by(have ? row : r0, a.by_group), gh = (have ? row : r0) - token * a.group;
-    const int limit = !have ? 0 : a.causal ? min(rq.length, behind + token + 1) : rq.length;
+    const int limit = a.causal ? min(rq.length, behind + token + 1) : rq.length;
 
     // this wave's keys: whole 32s of the block's share
     const int steps = (end - from + 31) >> 5;
@@ -172,8 +172,8 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
             }
     }
 
-    ValueUnit unit;
-    float m = kNone, l = 0.0f;                   // maximum that p goes by; sum of this lane's p (times 2^up)
+    RowUnit unit;
+    float l = 0.0f;                              // sum of this lane's p
     tk_f4 o[CB];
 #pragma unroll
     for (int c = 0; c < CB; ++c) o[c] = tk_f4{0.f, 0.f, 0.f, 0.f};
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
             fetch(s + 1);
             page_ids(s + 2);
         }
-        float x[8], top = kNone;
+        float x[8], top = kNone, scale = 0.0f;
 #pragma unroll
         for (int u = 0; u < 8; ++u) x[u] = sc[u >> 2][u & 3] * kc[u];
         if (j0 + 32 > all || __any(in != 255u)) {            // some keys are not there, or not for all rows
@@ -223,34 +223,50 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
                 x[u] = there && j0 + 16 * (u >> 2) + 4 * kg + (u & 3) < limit ? x[u] : kNone;
             }
         }
-        float vmax = vsc[0];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             top = fmaxf(top, x[u]);
-            vmax = fmaxf(vmax, vsc[u]);
+            scale = fmaxf(scale, fabsf(vsc[u]));
         }
         top *= qscale;
-        if (__any(top > m + 0.99f || vmax > unit.ref)) {
+        if (__any(top > unit.room || scale > unit.vs)) {
             top = halves_max(rows16_max(top));
-            const float m1 = fmaxf(m, top), grown = unit.raise(wave_max(vmax));
-            const float by = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - m1) + grown);
+            if (unit.unknown(top, scale)) {
+                float weight = kNone;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) weight = fmaxf(weight, x[u] * qscale + RowUnit::log_of(vsc[u]));
+                const float by = unit.set(top, halves_max(rows16_max(weight)));
+                l *= by;
+#pragma unroll
+                for (int d = 0; d < CB; ++d)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[d][r] *= by;
+            }
+        }
+        float largest = 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u], qscale, unit.c));
+            l += p;
+            x[u] = p * vsc[u];
+            largest = fmaxf(largest, fabsf(x[u]));
+        }
+        if (RowUnit::large(largest, l)) {
+            const float by = unit.lower(halves_max(rows16_max(largest)), halves_max(rows16_max(l)));
             l *= by;
 #pragma unroll
-            for (int c = 0; c < CB; ++c)
+            for (int u = 0; u < 8; ++u) x[u] *= by;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[c][r] *= by;
-            m = m1;
+            for (int d = 0; d < CB; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[d][r] *= by;
         }
-        const float base = m == kNone ? 0.0f : unit.up - m;
         tk_h8 pf[PARTS];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u], qscale, base));
-            l += p;
-            const float w = p * vsc[u];
-            _Float16 first = (_Float16)w, rest;
+            _Float16 first = (_Float16)x[u], rest;
             if (PARTS == 2) {
-                two_pieces(w, &first, &rest);
+                two_pieces(x[u], &first, &rest);
                 pf[PARTS - 1][u] = rest;
             }
             pf[0][u] = first;
@@ -276,7 +292,8 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
         }
     }
     l = halves_sum(rows16_sum(l));
-    const float down = __builtin_amdgcn_exp2f(-unit.up);
+    float down;
+    const float m = normalised(unit.c, &l, &down);
 
     // the waves' sums, in LDS: [wave][row][DIM + 4], in units of the values.  A lane has CB neighbouring dims of its row for each r.
     float* const sm = lds;
@@ -285,7 +302,7 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
     constexpr int PITCH = DIM + 4;
     if (kg == 0) {
         sm[wave * 16 + n16] = m;
-        sl[wave * 16 + n16] = l * down;
+        sl[wave * 16 + n16] = l;
     }
     if (have) {
 #pragma unroll

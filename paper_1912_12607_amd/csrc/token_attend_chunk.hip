@@ -4,7 +4,7 @@
 // A block has 32 NW rows (tokens times heads of a group, in order) of one request and head of the cache, a wave 32 of them; the keys pass
 // by in tiles of 64.  While one tile is multiplied, the next one's codes, which were loaded a tile ahead, become fp16 (exactly) in LDS,
 // once for all waves, and the one after it is loaded.
-//   scores   S^T[key][row] = K Q^T in products of 32 x 32 x 16: a lane's 16 scores of 32 keys belong to one row, so maximum and sum need
+//   scores   S^T[key][row] = K Q^T in products of 32 x 32 x 16: a lane's 16 scores of 32 keys belong to one row, so its unit (RowUnit) needs
 //            one exchange between the halves of the wave;
 //   values   O^T[dim][row] = V^T P^T: the scores' layout is P^T's operand layout with the keys in the order that the transposing LDS read
 //            of V (rows of keys, as they came) delivers: p never leaves its lane.
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
     const bool have = row < nrows;
     const int token = div_by(have ? row : r0, a.by_group), gh = (have ? row : r0) - token * a.group;
     const int behind = rq.length - rq.new_tokens;               // keys before the new tokens
-    const int limit = !have ? 0 : a.causal ? min(rq.length, behind + token + 1) : rq.length;
+    const int limit = a.causal ? min(rq.length, behind + token + 1) : rq.length;
     // keys that the block's last row sees, and those that all of its rows see
     const int last_token = div_by(min(r0 + ROWS - 1, nrows - 1), a.by_group);
     const int end = max(0, a.causal ? min(rq.length, behind + last_token + 1) : rq.length);
@@ -168,8 +168,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
         }
     };
 
-    ValueUnit unit;
-    float m = kNone, l = 0.0f;                   // maximum (times qscale) that p goes by; sum of this lane's p (times 2^up)
+    RowUnit unit;
+    float l = 0.0f;                              // sum of this lane's p
     tk_f16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -230,11 +230,14 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    // (dims up to 256 leave no registers for operands that are read ahead: without 13 of them are spilled, and chunks take 4 % longer)
+    const auto packed = []() __attribute__((always_inline)) {
+        if constexpr (DIM == 256) __builtin_amdgcn_sched_barrier(0);
+    };
     const auto softmax = [&](int t, int sslot) __attribute__((always_inline)) {
         const float* const s = sc + sslot * 3 * TK;
         // times the keys' scales; the tile's last keys and those behind a row's own
         const bool masked = (t + 1) * TK > all || __any(s[2 * TK + lane] != 0.0f);
-        float top = kNone;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -255,24 +258,33 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
                         if (none[i] != 0.0f || kt * 32 + 8 * q + i >= left) x[kt][4 * q + i] = kNone;
                 }
         }
+        float top = kNone;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int v = 0; v < 16; ++v) top = fmaxf(top, x[kt][v]);
         top = halves_max(top) * qscale;
-        // (half of the raised maxima are within the factor of 2 that p may pass 1 by)
-        const float vsl = s[TK + lane];
-        if (__any(vsl > unit.ref || top > m + 0.99f)) {
-            const float m1 = fmaxf(m, top), grown = unit.raise(wave_max(vsl));
-            const float by = m == kNone ? 0.0f : __builtin_amdgcn_exp2f((m - m1) + grown);
+        const float scale = s[TK + lane];
+        if (__any(top > unit.room || fabsf(scale) > unit.vs) && unit.unknown(top, scale)) {
+            float weight = kNone;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const tk_f4 vs = *reinterpret_cast<const tk_f4*>(s + TK + kt * 32 + 8 * q + 4 * half);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) weight = fmaxf(weight, x[kt][4 * q + i] * qscale + RowUnit::log_of(vs[i]));
+                    packed();
+                }
+            const float by = unit.set(top, halves_max(weight));
             l *= by;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) o[d][v] *= by;
-            m = m1;
         }
-        const float base = m == kNone ? 0.0f : unit.up - m;
+        packed();
+        float largest = 0.0f;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -280,16 +292,41 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
                 const tk_f4 vs = *reinterpret_cast<const tk_f4*>(s + TK + kt * 32 + 8 * q + 4 * half);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kt][4 * q + i], qscale, base));
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kt][4 * q + i], qscale, unit.c));
                     l += p;
-                    const float w = p * vs[i];
-                    _Float16 first = (_Float16)w, rest;
-                    if (PARTS == 2) {
-                        two_pieces(w, &first, &rest);
-                        pf[kt][PARTS - 1][q >> 1][4 * (q & 1) + i] = rest;
-                    }
-                    pf[kt][0][q >> 1][4 * (q & 1) + i] = first;
+                    x[kt][4 * q + i] = p * vs[i];
+                    if (DIM < 256) largest = fmaxf(largest, fabsf(x[kt][4 * q + i]));
                 }
+                if (q & 1) packed();
+            }
+        if (DIM == 256) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) largest = fmaxf(largest, fabsf(x[kt][v]));
+        }
+        if (RowUnit::large(largest, l)) {
+            const float by = unit.lower(halves_max(largest), halves_max(l));
+            l *= by;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) x[kt][v] *= by;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[d][v] *= by;
+        }
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                _Float16 first = (_Float16)x[kt][v], rest;
+                if (PARTS == 2) {
+                    two_pieces(x[kt][v], &first, &rest);
+                    pf[kt][PARTS - 1][v >> 3][v & 7] = rest;
+                }
+                pf[kt][0][v >> 3][v & 7] = first;
             }
     };
 
@@ -346,10 +383,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
     if (!have) return;
     const int heads = a.c.heads * a.group;
     const size_t out_row = (size_t)(rq.token0 + token) * heads + head * a.group + gh;
-    const float down = __builtin_amdgcn_exp2f(-unit.up);
     if (a.splits == 1) {
         const float by = l > 0.0f ? 1.0f / l : 0.0f;
-        if (a.lse && half == 0) a.lse[out_row] = l > 0.0f ? (m + __log2f(l * down)) * (1.0f / kLog2e) : kNone;
+        if (a.lse && half == 0) a.lse[out_row] = l > 0.0f ? (__log2f(l) - unit.c) * (1.0f / kLog2e) : kNone;
         T* const out = static_cast<T*>(a.out) + out_row * D;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -366,9 +402,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
             }
     } else {
         const size_t part_row = (size_t)split * a.tokens * heads + out_row;
+        float down;
+        const float m = normalised(unit.c, &l, &down);
         if (half == 0) {
             a.part_ml[2 * part_row] = m;
-            a.part_ml[2 * part_row + 1] = l * down;
+            a.part_ml[2 * part_row + 1] = l;
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d)
