@@ -133,6 +133,9 @@ struct RowUnit {
    private:
     __device__ __forceinline__ float limit() const { return fminf(112.0f, 126.0f - log_of(vs)) - c; }
 };
+// p vs, and 0 where p is, whatever the scale: the place of a key that a row does not see may not have been written yet.
+extern "C" __device__ __attribute__((const)) float multiply_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");       // 0 times anything is 0
+__device__ __forceinline__ float weight_of(float p, float vs) { return multiply_legacy(p, vs); }
 // l to 1/2 .. 1: the shares of a row are joined by m = log2 of what l and o are in units of, and l;  *down: what o is to be multiplied with
 __device__ __forceinline__ float normalised(float c, float* l, float* down) {
     const int e = __builtin_amdgcn_frexp_expf(*l);

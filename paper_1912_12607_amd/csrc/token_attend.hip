@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
         for (int u = 0; u < 8; ++u) {
             const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u], qscale, unit.c));
             l += p;
-            x[u] = p * vsc[u];
+            x[u] = weight_of(p, vsc[u]);
             largest = fmaxf(largest, fabsf(x[u]));
         }
         if (RowUnit::large(largest, l)) {

@@ -294,7 +294,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
                 for (int i = 0; i < 4; ++i) {
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kt][4 * q + i], qscale, unit.c));
                     l += p;
-                    x[kt][4 * q + i] = p * vs[i];
+                    x[kt][4 * q + i] = weight_of(p, vs[i]);
                     if (DIM < 256) largest = fmaxf(largest, fabsf(x[kt][4 * q + i]));
                 }
                 if (q & 1) packed();

@@ -116,7 +116,7 @@ FORMS = [(1, 4, 64, 16, [20, 9], [90, 300]), (2, 2, 80, 24, [3, 17], [40, 5000])
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("heads,group,dim,page,new,lengths", FORMS)
-@pytest.mark.parametrize("poison", [1e10, 1e30])
+@pytest.mark.parametrize("poison", [1e10, 1e30, float("inf"), float("nan")])
 def test_keys_behind_a_row_do_not_reach_it(dtype, heads, group, dim, page, new, lengths, poison):
     """The causal limit hides a token's later neighbours, whose places may hold anything: rows before them are what they are without."""
     cache, table = cache_of(lengths, heads, dim, page, 1)
