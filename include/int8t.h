@@ -636,6 +636,7 @@ int8t_status int8t_cache_read(const int8t_cache *cache, const int64_t *slots_dev
  *   longest      no length is larger (a guide for the division of the work, by which sums are ordered; keys behind it are seen all the same); 0: unknown
  *   out_dev      out: [tokens][heads * group][dim] of `type`, 16-byte aligned
  *   lse_dev      NULL, or out: [tokens][heads * group] floats, the natural logarithm of sum_j p_j
+ *   NaN in a query, or in a scale of a key that a token sees, makes that row NaN and no other; places that no row sees, or not yet, may hold anything
  *   ws_dev       int8t_cache_attend_workspace_bytes(cache, desc) bytes, 16-byte aligned; may be NULL where that is 0
  * Products run on fp16 with sums in fp32: codes are exact, each q is scaled by a power of two, and p_j times the value scale is rounded to 11 bits for bf16
  * and fp16 tensors (one fp16) and 22 bits for fp32 ones (two pieces, as q's), with steps of 2^-38 of the row's largest at least: of its own, keys that a row does

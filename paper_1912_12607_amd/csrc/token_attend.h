@@ -136,6 +136,9 @@ struct RowUnit {
 // p vs, and 0 where p is, whatever the scale: the place of a key that a row does not see may not have been written yet.
 extern "C" __device__ __attribute__((const)) float multiply_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");       // 0 times anything is 0
 __device__ __forceinline__ float weight_of(float p, float vs) { return multiply_legacy(p, vs); }
+// What o of a row is multiplied with, and the row's natural logarithm, from its sum l in units of 2^m.  Only a sum of zero is one of no keys: NaN shows.
+__device__ __forceinline__ float per_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ float log_of_sum(float m, float l) { return l == 0.0f ? kNone : (m + __log2f(l)) * (1.0f / kLog2e); }
 // l to 1/2 .. 1: the shares of a row are joined by m = log2 of what l and o are in units of, and l;  *down: what o is to be multiplied with
 __device__ __forceinline__ float normalised(float c, float* l, float* down) {
     const int e = __builtin_amdgcn_frexp_expf(*l);

@@ -329,10 +329,10 @@ __global__ __launch_bounds__(64 * RW, 2) void attend_rows_kernel(const AttendArg
     const size_t out_row = (size_t)(rq.token0 + jt) * heads + head * a.group + jg;
     const bool whole = a.splits == 1;
     const size_t part_row = (size_t)split * a.tokens * heads + out_row;
-    const float by = !whole ? 1.0f : total > 0.0f ? 1.0f / total : 0.0f;
+    const float by = whole ? per_sum(total) : 1.0f;
     if (jl == 0) {
         if (whole) {
-            if (a.lse) a.lse[out_row] = total > 0.0f ? (mm + __log2f(total)) * (1.0f / kLog2e) : kNone;
+            if (a.lse) a.lse[out_row] = log_of_sum(mm, total);
         } else {
             a.part_ml[2 * part_row] = mm;
             a.part_ml[2 * part_row + 1] = total;
@@ -382,11 +382,12 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     for (int o = 1; o < 16; o *= 2) {
         const float m2 = __shfl_xor(m, o, kWave), t2 = __shfl_xor(total, o, kWave), m1 = fmaxf(m, m2);
         if (m1 != kNone) total = total * __builtin_amdgcn_exp2f(m - m1) + t2 * __builtin_amdgcn_exp2f(m2 - m1);
+        else total += t2;                        // (nothing, or NaN)
         m = m1;
     }
     if (!have) return;
-    const float by = total > 0.0f ? 1.0f / total : 0.0f;
-    if (l == 0 && a.lse) a.lse[row] = total > 0.0f ? (m + __log2f(total)) * (1.0f / kLog2e) : kNone;
+    const float by = per_sum(total);
+    if (l == 0 && a.lse) a.lse[row] = log_of_sum(m, total);
     for (int d = l * 8; d < D; d += 128) {
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4

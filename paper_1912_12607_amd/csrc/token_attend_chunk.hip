@@ -384,8 +384,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
     const int heads = a.c.heads * a.group;
     const size_t out_row = (size_t)(rq.token0 + token) * heads + head * a.group + gh;
     if (a.splits == 1) {
-        const float by = l > 0.0f ? 1.0f / l : 0.0f;
-        if (a.lse && half == 0) a.lse[out_row] = l > 0.0f ? (__log2f(l) - unit.c) * (1.0f / kLog2e) : kNone;
+        const float by = per_sum(l);
+        if (a.lse && half == 0) a.lse[out_row] = log_of_sum(-unit.c, l);
         T* const out = static_cast<T*>(a.out) + out_row * D;
 #pragma unroll
         for (int d = 0; d < DT; ++d)

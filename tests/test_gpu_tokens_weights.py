@@ -170,3 +170,33 @@ def test_sums_over_many_keys(dtype, dim, group, new, scale):
     assert bool(((lse.double() - math.log(L)).abs() <= 2.0**-18).all())
     want = cache.vq[0, 0, 0].double() * cache.vs[0, 0, 0].double()
     assert bool(((got.double() - want).abs() <= (E_P[dtype] + E_OUT[dtype] + L / 16 * 2.0**-24) * want.abs()).all())
+
+
+SHARED = [(2, 4, 64, 16, [1, 1], [9000, 40]), (1, 3, 256, 24, [1, 2], [40, 6000]), (1, 2, 128, 7, [20], [5000])] + FORMS
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,group,dim,page,new,lengths", SHARED)
+def test_nan_shows_in_rows_that_meet_it(dtype, heads, group, dim, page, new, lengths):
+    """A query of NaN, a key's or a value's scale of NaN: NaN for the rows that they belong to (a value's: not in the sum's logarithm), nothing for the others."""
+    starts = starts_of(new)
+    T, longest = sum(new), lengths.index(max(lengths))
+    for where in ("q", "k", "v"):
+        cache, table = cache_of(lengths, heads, dim, page, 7)
+        q = queries(T, heads * group, dim, dtype, 8)
+        want = in_64_bits(cache, q, starts, lengths, table)
+        hit = torch.zeros(T, heads * group, dtype=torch.bool, device=DEV)
+        if where == "q":
+            t = starts[longest + 1] - 1
+            q[t, 0, dim - 1] = float("nan")
+            hit[t, 0] = True
+        else:
+            n, L = new[longest], lengths[longest]
+            at = L - max(1, n // 2)                                       # a key that the request's last tokens see
+            p, r = places(table, longest, [at], page)
+            (cache.ks if where == "k" else cache.vs)[p, heads - 1, r] = float("nan")
+            hit[starts[longest + 1] - (L - at):starts[longest + 1], (heads - 1) * group:] = True
+        got, lse = cache.attend(q, *ints(starts, lengths), table, return_lse=True)
+        assert bool(got[hit].isnan().all()), where
+        assert bool(lse[hit].isnan().all()) == (where != "v"), where
+        compare([t[~hit] for t in (got, lse)], [t[~hit] for t in want], max(lengths))
