@@ -524,6 +524,8 @@ double int8t_dclr_scale(double d_c, double alpha, double beta);
  * linear layers and the attention of transformers, whose tokens differ in size.  Floating tensors are of an int8t_dtype; a result is
  * formed in fp32 and rounded once.  `pitch` arguments are in elements; rows themselves are contiguous.  Any alignment of an element is
  * served; rows that start on 16 bytes are faster.  fp32 vectors (scales, factors, biases) and codes lie on 16 bytes.
+ * A row or column (token, channel, head of a cached token) that holds NaN or an infinity gets codes of 0 and that as its scale, so what is computed from it is NaN:
+ * a training program sees the overflow of a gradient in fp16.
  * Codes of `rows` x `cols`: INT8T_ACT codes of dims {rows, cols, 1, 1}, i.e. [rows][cols rounded up to 16], zero beyond cols.
  * Sums of products are exact: at most INT8T_MAX_REDUCTION products (16129 each at most) go into one int32.
  */

@@ -43,6 +43,14 @@ __device__ __forceinline__ float wave_max(float v) {
     v = fmaxf(v, dpp_of<kDppRor8>(v));
     return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
 }
+// (keeps NaN)
+__device__ __forceinline__ float wave_maximum(float v) {
+    v = __builtin_elementwise_maximum(v, dpp_of<kDppSwap1>(v));
+    v = __builtin_elementwise_maximum(v, dpp_of<kDppSwap2>(v));
+    v = __builtin_elementwise_maximum(v, dpp_of<kDppRor4>(v));
+    v = __builtin_elementwise_maximum(v, dpp_of<kDppRor8>(v));
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(lane_of(v, 0), lane_of(v, 16)), __builtin_elementwise_maximum(lane_of(v, 32), lane_of(v, 48)));
+}
 __device__ __forceinline__ double wave_sum(double v) {
     v += dpp_of<kDppSwap1>(v);
     v += dpp_of<kDppSwap2>(v);

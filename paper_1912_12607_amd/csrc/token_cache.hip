@@ -38,13 +38,13 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const CacheMoveArgs a)
     }
     float m = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
+    for (int i = 0; i < 8; ++i) m = most(m, fabsf(v[i]));
 #pragma unroll
-    for (int o = 1; o < LANES; o *= 2) m = fmaxf(m, __shfl_xor(m, o, kWave));
+    for (int o = 1; o < LANES; o *= 2) m = most(m, __shfl_xor(m, o, kWave));
     if (!live) return;
     const float inv = inv_scale_of(m);
     const size_t place = (page * a.c.heads + head) * a.c.page_size + at;
-    if (l == 0) (values ? a.c.vs : a.c.ks)[place] = scale_of(m);
+    if (l == 0) (values ? a.c.vs : a.c.ks)[place] = token_scale_of(m);
     if (8 * l < a.c.dim) {
         int c[8];
 #pragma unroll

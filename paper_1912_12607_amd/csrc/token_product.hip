@@ -299,16 +299,16 @@ __global__ __launch_bounds__(64 * FW, 4) void few_tokens_kernel(const FewArgs a)
 #pragma unroll
                 for (int u = 0; u < CH; ++u)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) top[r] = fmaxf(top[r], fabsf(v[r][u][i]));
+                    for (int i = 0; i < 8; ++i) top[r] = most(top[r], fabsf(v[r][u][i]));
         }
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) top[r] = wave_max(top[r]);
+        for (int r = 0; r < ROWS; ++r) top[r] = wave_maximum(top[r]);
         if (WPR > 1) {
             if (lane == 0) part[wave] = top[0];
             __syncthreads();
             top[0] = part[m0 * WPR];
 #pragma unroll
-            for (int i = 1; i < WPR; ++i) top[0] = fmaxf(top[0], part[m0 * WPR + i]);
+            for (int i = 1; i < WPR; ++i) top[0] = most(top[0], part[m0 * WPR + i]);
         }
         for (int base = 0; base < a.Kp; base += SPAN) {
             if (a.K > SPAN) values(base);
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(64 * FW, 4) void few_tokens_kernel(const FewArgs a)
                 const int m = m0 + FW / WPR * r;
                 const float inv = inv_scale_of(top[r]);
                 if (m >= a.M) continue;
-                if (t8 == 0 && base == 0) scales[m] = scale_of(top[r]);
+                if (t8 == 0 && base == 0) scales[m] = token_scale_of(top[r]);
 #pragma unroll
                 for (int u = 0; u < CH; ++u) {
                     const int c = base + u * 512 * WPR + t8;

@@ -63,18 +63,18 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a, const int block, co
 #pragma unroll
         for (int u = 0; u < CH; ++u)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[u][i]));
+            for (int i = 0; i < 8; ++i) m = most(m, fabsf(v[u][i]));
     }
-    m = wave_max(m);
+    m = wave_maximum(m);
     if constexpr (TPR > 64) {
         __shared__ float lds[TPR / 64];
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
         __syncthreads();
         m = lds[0];
 #pragma unroll
-        for (int i = 1; i < TPR / 64; ++i) m = fmaxf(m, lds[i]);
+        for (int i = 1; i < TPR / 64; ++i) m = most(m, lds[i]);
     }
-    float inv = inv_scale_of(m), sc = scale_of(m);
+    float inv = inv_scale_of(m), sc = token_scale_of(m);
     if (live && t == 0) a.scale[row] = sc;
     if (STOCH) inv = __fmul_rn(inv, kTwo24);
     int8_t* __restrict__ q = a.q + (size_t)(live ? row : 0) * Kp;
@@ -151,7 +151,7 @@ __device__ __forceinline__ void cols_max_body(const ColsArgs& a, const int bx, c
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             s[i] += v[i];
-            m[i] = fmaxf(m[i], fabsf(__fmul_rn(v[i], f)));
+            m[i] = most(m[i], fabsf(__fmul_rn(v[i], f)));
         }
     }
     const int c = bx * 256 + (int)threadIdx.x;
@@ -161,7 +161,7 @@ __device__ __forceinline__ void cols_max_body(const ColsArgs& a, const int bx, c
     if (c < a.cols) {
         float t = lds[0][threadIdx.x];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) t = fmaxf(t, lds[i][threadIdx.x]);
+        for (int i = 1; i < 8; ++i) t = most(t, lds[i][threadIdx.x]);
         a.part_max[(size_t)part * a.cols + c] = t;
     }
     if (!a.sum) return;
@@ -221,15 +221,15 @@ __device__ __forceinline__ void cols_codes_body(uint32_t* const tile, const Cols
         const float* const part = a.part_max + (col0 + c < a.cols ? col0 + c : 0);
         float m = 0.0f;
 #pragma unroll 8
-        for (int p = p0; p < a.parts; p += 4) m = fmaxf(m, part[(size_t)p * a.cols]);
+        for (int p = p0; p < a.parts; p += 4) m = most(m, part[(size_t)p * a.cols]);
         tops[p0][c] = m;
     }
     __syncthreads();
     if (threadIdx.x < CT_C) {
         const int c = col0 + (int)threadIdx.x;
-        const float m = fmaxf(fmaxf(tops[0][threadIdx.x], tops[1][threadIdx.x]), fmaxf(tops[2][threadIdx.x], tops[3][threadIdx.x]));
+        const float m = most(most(tops[0][threadIdx.x], tops[1][threadIdx.x]), most(tops[2][threadIdx.x], tops[3][threadIdx.x]));
         if (by == 0 && c < a.cols) {
-            a.scale[c] = scale_of(m);
+            a.scale[c] = token_scale_of(m);
             if (a.sum) {
                 double s = 0.0;
 #pragma unroll 8

@@ -65,6 +65,11 @@ __device__ __forceinline__ void store8(typename ElemOf<TYPE>::type* __restrict__
     }
 }
 
+// Maxima that keep NaN (v_maximum3_f32, as fast as the other), and the scale that belongs to one: a token, channel or column that holds NaN gets codes of 0 and a
+// scale of NaN, one that holds an infinity codes of 0 and an infinite scale, so that what is computed from either is NaN.
+__device__ __forceinline__ float most(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float token_scale_of(float c) { return c > 0.0f ? __fdiv_rn(c, 127.0f) : c; }
+
 // ---- token_quantize.hip ------------------------------------------------------------------------
 struct RowsArgs {            // codes of rows x cols values, a scale for each row
     const void* x;

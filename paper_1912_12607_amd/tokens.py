@@ -2,7 +2,8 @@
 paged cache of keys and values in 8 bits, and attention of new tokens over it.
 
 Plumbing only, as in ``autograd``: every arithmetic step is one of the library's entry points; torch supplies device memory, the current
-stream and the autograd graph.  CUDA(ROCm) tensors in fp32, bf16 or fp16.
+stream and the autograd graph.  CUDA(ROCm) tensors in fp32, bf16 or fp16.  NaN and infinities make what is computed from their token, channel or
+cached row NaN.
 
     layer = ServedLinear.of(weight, bias)               # codes and scales, laid out once
     cache = PagedCache.empty(pages, page_size, heads, dim, device)
