@@ -15,6 +15,14 @@ __device__ __forceinline__ void pin8(float v[8]) {
     asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7]));
 }
 
+// Stochastic codes of values below 2^-93 go by 2^40 times the values, and by inv in units that much smaller: inv 2^24 would pass fp32's range.
+__device__ __forceinline__ bool tiny_values(float inv) { return inv > 0x1p100f; }
+__device__ __forceinline__ float stochastic_inv(float inv) { return __fmul_rn(inv, tiny_values(inv) ? 0x1p-16f : kTwo24); }
+__device__ __forceinline__ void raise8(float v[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], 0x1p40f);
+}
+
 // Codes of eight neighbouring values.  STOCH: in the round-down mode, inv times 2^24 (see stoch_fixed()).
 template <bool STOCH>
 __device__ __forceinline__ uint2 codes8(const float v[8], float inv, uint32_t kx, uint32_t ka, uint32_t index, uint32_t step) {
@@ -76,10 +84,15 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a, const int block, co
     }
     float inv = inv_scale_of(m), sc = token_scale_of(m);
     if (live && t == 0) a.scale[row] = sc;
-    if (STOCH) inv = __fmul_rn(inv, kTwo24);
+    const bool tiny = STOCH && tiny_values(inv);
+    if (STOCH) inv = stochastic_inv(inv);
     int8_t* __restrict__ q = a.q + (size_t)(live ? row : 0) * Kp;
     for (int base = 0; base < (LONG ? a.cols : 1); base += SPAN) {
         if (LONG) fetch(base);
+        if (tiny) {
+#pragma unroll
+            for (int u = 0; u < CH; ++u) raise8(v[u]);
+        }
 #pragma unroll
         for (int u = 0; u < CH; ++u) pin8(v[u]);
         if (STOCH) fp32_round_down_mode(inv, sc);
@@ -238,7 +251,7 @@ __device__ __forceinline__ void cols_codes_body(uint32_t* const tile, const Cols
             }
         }
         const float inv = inv_scale_of(m);
-        invs[threadIdx.x] = STOCH ? __fmul_rn(inv, kTwo24) : inv;
+        invs[threadIdx.x] = inv;
     }
     __syncthreads();
 #pragma unroll
@@ -249,6 +262,23 @@ __device__ __forceinline__ void cols_codes_body(uint32_t* const tile, const Cols
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) inv[i] = invs[cg * 8 + i];
+    if (STOCH) {
+        float highest = inv[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) highest = fmaxf(highest, inv[i]);
+        if (__any(tiny_values(highest))) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float up = tiny_values(inv[i]) ? 0x1p40f : 1.0f;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u][i] = __fmul_rn(v[u][i], up);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) pin8(v[u]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) inv[i] = stochastic_inv(inv[i]);
+    }
     float dummy = 0.0f;
     if (STOCH) {
         pin8(inv);
