@@ -371,9 +371,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     const bool have = row < rows;                       // (all lanes stay for the exchanges)
     const size_t r = have ? row : 0;
     float m = kNone, total = 0.0f;
+    int end = 0;                                        // behind the last share that saw keys
     for (int s = l; s < a.splits; s += 16) {
         const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (s * rows + r));
         if (ml.x == kNone) continue;
+        end = s + 1;
         const float m1 = fmaxf(m, ml.x);
         total = total * __builtin_amdgcn_exp2f(m - m1) + __builtin_amdgcn_exp2f(ml.x - m1) * ml.y;      // (m = -infinity: total is 0)
         m = m1;
@@ -384,6 +386,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
         if (m1 != kNone) total = total * __builtin_amdgcn_exp2f(m - m1) + t2 * __builtin_amdgcn_exp2f(m2 - m1);
         else total += t2;                        // (nothing, or NaN)
         m = m1;
+        end = max(end, __shfl_xor(end, o, kWave));
     }
     if (!have) return;
     const float by = per_sum(total);
@@ -391,9 +394,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     for (int d = l * 8; d < D; d += 128) {
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int s = 0; s < a.splits; ++s) {
+        for (int s = 0; s < end; ++s) {
             const float ms = a.part_ml[2 * (s * rows + row)];
-            // (a share of which nothing was seen may have written no sums: they are read -- the memory is there -- and not used)
+            // (a share between others of which nothing was seen may have written no sums: they are read -- the memory is there -- and not used)
             float p[8];
             load8<kF32>(a.part_o + (s * rows + row) * D + d, 8, true, p);
             const float w = __builtin_amdgcn_exp2f(ms - m) * by;
@@ -482,9 +485,12 @@ void attend_plan(AttendArgs* a, int longest) {
         a->share = blocks >= 512 || (blocks >= 128 && blocks <= 256) ? 2048 : 1024;
         a->splits = (longest + a->share - 1) / a->share;
         a->waves = tiles * a->splits <= 256 ? 8 : 4;
-        if (a->splits > 256) {
-            a->splits = 256;
-            a->share = ((longest + 255) / 256 + 31) & ~31;
+        // At most 256 of them, and at most 2^14 blocks with theirs (a block leaves 16 rows of sums in the scratch, 2^20 times dim bytes together): the length may be
+        // a table's, many times the requests'.
+        const long long most = (1 << 14) / tiles < 1 ? 1 : (1 << 14) / tiles < 256 ? (1 << 14) / tiles : 256;
+        if (a->splits > most) {
+            a->splits = (int)most;
+            a->share = (int)((longest + most - 1) / most + 31) & ~31;
         }
         if (a->splits < 1) a->splits = 1;
         return;

@@ -200,3 +200,14 @@ def test_nan_shows_in_rows_that_meet_it(dtype, heads, group, dim, page, new, len
         assert bool(got[hit].isnan().all()), where
         assert bool(lse[hit].isnan().all()) == (where != "v"), where
         compare([t[~hit] for t in (got, lse)], [t[~hit] for t in want], max(lengths))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,group,dim,page,new,lengths", [(8, 4, 128, 16, [1] * 12, [1500, 1, 40, 2049, 0, 700, 3, 1024, 1025, 90, 33, 5000]), (2, 1, 64, 24, [13, 2], [20, 4000]),
+                                                              (1, 2, 256, 7, [1], [3]), (64, 1, 64, 16, [14] * 20, [1500] * 19 + [3])])
+def test_tables_much_longer_than_the_requests(dtype, heads, group, dim, page, new, lengths):
+    """The division of the keys goes by the table where `longest` is not given: most shares have none, or all keys lie in the first."""
+    cache, table = cache_of(lengths, heads, dim, page, 9)
+    wide = torch.full((len(new), 300000 // page), 0x7FFFFFF0, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    check(cache, queries(sum(new), heads * group, dim, dtype, 10), starts_of(new), lengths, wide)

@@ -46,3 +46,18 @@ def test_tables_that_an_int_cannot_count(width, page, status, tokens_):
     need = B.int8t_cache_attend_workspace_bytes(c, d)
     assert (need > 0) == (status != SHAPE)
     assert B.lib.int8t_cache_attend(C.byref(c), C.byref(d), FAKE, FAKE, FAKE, FAKE, FAKE, None, FAKE, max(need, 1) - 1, None) == status
+
+
+# shares of the keys go by a table's length, which may be many times the requests': what they leave for the joining pass stays within 2^14 blocks of 16 rows of dim
+# sums, a maximum and a sum (2^20 (dim + 2) bytes), and blocks that fill the chip many times over are not divided at all
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("kind", [B.F32, B.BF16])
+@pytest.mark.parametrize("requests,new,heads,group", [(1, 1, 8, 4), (64, 1, 8, 4), (64, 95, 8, 4), (1, 12, 64, 1), (300, 1, 8, 8), (2000, 1, 8, 1), (5, 20, 32, 1)])
+@pytest.mark.parametrize("width", [1, 100, 8192, 65536, 1 << 23])
+def test_scratch_of_attention(requests, new, heads, group, dim, kind, width):
+    c = B.Cache(FAKE, FAKE, FAKE, FAKE, 1 << 20, 16, heads, dim)
+    need = [B.int8t_cache_attend_workspace_bytes(c, B.AttendDesc(requests * new, requests, group, width, longest, kind, 1, 0.125, dim, dim, width))
+            for longest in (0, 1, 16 * width)]
+    assert need[0] == need[2] and max(need) <= ((dim + 2) << 20) + 512
+    if requests * new * group * heads >= 1 << 18:
+        assert max(need) == 0
