@@ -580,8 +580,8 @@ int8t_status int8t_product(const int8_t *a_dev, const float *sa_dev, const int8_
  *             db[n] = sum_m dy[m][n]
  *             (the scale that changes along the summed axis is in the values before their codes are made)
  * int8t_linear_fwd: w NULL takes the codes at wq, sw (laid out before) as they are; xq NULL keeps no codes of x (nobody's backward
- * pass comes for them).  M may be 0 there.  int8t_linear_bwd: dx, dw, db NULL: not wanted (one of dx, dw at least); reads xq, sx,
- * wq, sw of the forward pass.  ws: int8t_linear_workspace_bytes() bytes, 16-byte aligned; may be NULL where that is 0.
+ * pass comes for them).  M may be 0 there.  int8t_linear_bwd: dx, dw, db NULL: not wanted (one of them at least); reads xq, sx
+ * (for dw), wq, sw (for dx) of the forward pass.  ws: int8t_linear_workspace_bytes() bytes, 16-byte aligned; may be NULL where that is 0.
  */
 typedef struct int8t_linear_desc {
     int M, K, N;

@@ -237,8 +237,8 @@ extern "C" int8t_status int8t_linear_fwd(const int8t_linear_desc* d, const int8t
 extern "C" int8t_status int8t_linear_bwd(const int8t_linear_desc* d, const int8t_linear_buffers* b, uint64_t seed, void* stream) {
     const int8t_status ok = linear_ok(d, true);
     if (ok != INT8T_OK) return ok;
-    if (!b || !b->dy || !b->ws || (!b->dx && !b->dw)) return INT8T_ERR_NULL;
-    if ((b->dx && (!b->wq || !b->sw)) || (b->dw && (!b->xq || !b->sx)) || (b->db && !b->sx)) return INT8T_ERR_NULL;
+    if (!b || !b->dy || !b->ws || (!b->dx && !b->dw && !b->db)) return INT8T_ERR_NULL;
+    if ((b->dx && (!b->wq || !b->sw)) || (b->dw && (!b->xq || !b->sx))) return INT8T_ERR_NULL;
     if (b->dy_pitch < (size_t)d->N) return INT8T_ERR_SHAPE;
     if (!aligned(b->dy, bytes_of(d->type)) || !aligned(b->dx, bytes_of(d->type)) || !aligned(b->dw, bytes_of(d->wtype)) || !aligned(b->db, 4) ||
         !aligned16(b->wq) || !aligned16(b->sw) || !aligned16(b->xq) || !aligned16(b->sx) || !aligned16(b->ws))
@@ -247,7 +247,7 @@ extern "C" int8t_status int8t_linear_bwd(const int8t_linear_desc* d, const int8t
     if (b->ws_bytes < s.bytes) return INT8T_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
     const RowsArgs g{b->dy, b->dy_pitch, d->type, d->M, d->N, b->sw, 1, seed, s.gq, s.sg};
-    const ColsArgs h = cols_args(b->dy, d->type, d->M, d->N, b->dy_pitch, b->sx, 1, seed ^ (1ull << 63), s.hq, s.sh, b->db, s.cols);
+    const ColsArgs h = cols_args(b->dy, d->type, d->M, d->N, b->dy_pitch, b->dw ? b->sx : nullptr, 1, seed ^ (1ull << 63), b->dw ? s.hq : nullptr, s.sh, b->db, s.cols);
     ProductArgs px{}, pw{};
     px.part = pw.part = static_cast<int32_t*>(s.product);
     px.a = s.gq; px.sa = s.sg; px.b = s.wqt;

@@ -190,9 +190,22 @@ __device__ __forceinline__ void cols_max_body(const ColsArgs& a, const int bx, c
     }
 }
 
+__device__ __forceinline__ float parts_sum(const ColsArgs& a, const int c) {
+    double s = 0.0;
+#pragma unroll 8
+    for (int p = 0; p < a.parts; ++p) s += (double)a.part_sum[(size_t)p * a.cols + c];
+    return (float)s;
+}
+
 template <int TYPE>
 __global__ __launch_bounds__(256) void cols_max_kernel(const ColsArgs a, const int wide) {
     cols_max_body<TYPE>(a, (int)blockIdx.x, (int)blockIdx.y, wide);
+}
+
+// Sums alone (a bias without its weights): those of the parts, as the second pass forms them.
+__global__ __launch_bounds__(256) void cols_sum_kernel(const ColsArgs a) {
+    const int c = (int)(blockIdx.x * 256 + threadIdx.x);
+    if (c < a.cols) a.sum[c] = parts_sum(a, c);
 }
 
 // Tiles of 128 rows, turned in LDS: the codes of four neighbouring rows of a column are one word, 32 words a column, and leave in runs of 128
@@ -243,12 +256,7 @@ __device__ __forceinline__ void cols_codes_body(uint32_t* const tile, const Cols
         const float m = most(most(tops[0][threadIdx.x], tops[1][threadIdx.x]), most(tops[2][threadIdx.x], tops[3][threadIdx.x]));
         if (by == 0 && c < a.cols) {
             a.scale[c] = token_scale_of(m);
-            if (a.sum) {
-                double s = 0.0;
-#pragma unroll 8
-                for (int p = 0; p < a.parts; ++p) s += (double)a.part_sum[(size_t)p * a.cols + c];
-                a.sum[c] = (float)s;
-            }
+            if (a.sum) a.sum[c] = parts_sum(a, c);
         }
         const float inv = inv_scale_of(m);
         invs[threadIdx.x] = inv;
@@ -309,6 +317,10 @@ void cols_of(const ColsArgs& a, int wide, hipStream_t st) {
         launch_timed(kt, cols_max_kernel<TYPE>, dim3((a.cols + 255) / 256, a.parts), dim3(256), 0, st, a, wide);
     }
     KernelTimer kt(KID_TOKEN_COLS, st);
+    if (!a.q) {
+        launch_timed(kt, cols_sum_kernel, dim3((a.cols + 255) / 256), dim3(256), 0, st, a);
+        return;
+    }
     const dim3 grid((a.cols + CT_C - 1) / CT_C, (a.rows + CT_R - 1) / CT_R);
     const uint32_t kx = seed_key_x(a.seed), ka = seed_key_a(a.seed);
     if (a.stochastic) launch_timed(kt, (cols_codes_kernel<TYPE, true>), grid, dim3(256), 0, st, a, wide, kx, ka);

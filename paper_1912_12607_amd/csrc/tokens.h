@@ -93,7 +93,7 @@ struct ColsArgs {            // ... a scale for each column, codes transposed
     const float* factor;     // rows, or null
     int stochastic;
     uint64_t seed;
-    int8_t* q;               // [cols][pad16(rows)]
+    int8_t* q;               // [cols][pad16(rows)]; null: sums alone
     float* scale;            // cols
     float* sum;              // cols, or null: sums of x (without the factor)
     float *part_max, *part_sum;   // [parts][cols]

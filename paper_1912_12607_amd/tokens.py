@@ -173,11 +173,6 @@ class _LinearFn(torch.autograd.Function):
             return (dx, torch.zeros(N, K, dtype=ctx.w_dtype, device=dev) if want_w else None,
                     torch.zeros(N, dtype=torch.float32, device=dev) if want_b else None, None)
         g, pitch = _rows(dy, N)
-        db = None
-        if want_b and not want_w:                # (with the weights' gradient the sums come out of its pass over dy)
-            db = g.sum(0, dtype=torch.float32)
-            if not want_x:
-                return None, None, db, None
         kept, = ctx.saved_tensors
         b = B.LinearBuffers()
         at, places = kept.data_ptr(), ctx.places
@@ -185,13 +180,13 @@ class _LinearFn(torch.autograd.Function):
         b.dy, b.dy_pitch = g.data_ptr(), pitch
         if want_x:
             b.dx = dx.data_ptr()
-        dw = None
+        dw = db = None
         if want_w:
             dw = torch.empty(N, K, dtype=ctx.w_dtype, device=dev)
             b.dw = dw.data_ptr()
-            if want_b:
-                db = torch.empty(N, dtype=torch.float32, device=dev)
-                b.db = db.data_ptr()
+        if want_b:
+            db = torch.empty(N, dtype=torch.float32, device=dev)
+            b.db = db.data_ptr()
         need = ctx.need
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
         b.ws, b.ws_bytes = ws.data_ptr(), need
