@@ -656,6 +656,16 @@ int8t_status int8t_cache_attend(const int8t_cache *cache, const int8t_attend_des
                                 const int *lengths_dev, const int *table_dev, void *out_dev, float *lse_dev, void *ws_dev,
                                 size_t ws_bytes, void *stream);
 
+/*
+ * How a call of these sizes is divided (on the host, nothing is launched): rows of a block -- of its results' columns too, in products --, its waves, stages of
+ * operands that it holds in LDS (products), and into how many shares the reduction (the keys) goes.  ws_bytes: as the call will have it.
+ */
+typedef struct int8t_division {
+    int rows, waves, stages, shares;
+} int8t_division;
+int8t_status int8t_product_division(int M, int N, int K, size_t ws_bytes, int8t_division *out);
+int8t_status int8t_cache_attend_division(const int8t_cache *cache, const int8t_attend_desc *desc, int8t_division *out);
+
 #ifdef __cplusplus
 }
 #endif

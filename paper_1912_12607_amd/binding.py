@@ -36,6 +36,7 @@ EXPORTS = ["int8t_status_string", "int8t_code_bytes", "int8t_unpack_codes", "int
            "int8t_quantize_rows", "int8t_quantize_cols_workspace_bytes", "int8t_quantize_cols", "int8t_transpose_codes",
            "int8t_product_workspace_bytes", "int8t_product", "int8t_linear_workspace_bytes", "int8t_linear_fwd", "int8t_linear_bwd",
            "int8t_cache_write", "int8t_cache_read", "int8t_cache_attend_workspace_bytes", "int8t_cache_attend",
+           "int8t_product_division", "int8t_cache_attend_division",
            "int8t_profile_start", "int8t_profile_start_sampled", "int8t_profile_stop", "int8t_profile_mfma_ceiling"]
 
 
@@ -81,6 +82,11 @@ class Cache(C.Structure):
 class AttendDesc(C.Structure):
     _fields_ = ([(n, C.c_int) for n in ("tokens", "requests", "group", "table_width", "longest", "type", "causal")]
                 + [("scale", C.c_float)] + [(n, C.c_size_t) for n in ("q_token_pitch", "q_head_pitch", "table_pitch")])
+
+
+class Division(C.Structure):
+    """int8t_division: how a call is divided among blocks."""
+    _fields_ = [(n, C.c_int) for n in ("rows", "waves", "stages", "shares")]
 
 
 class ConvDesc(C.Structure):
@@ -174,6 +180,10 @@ def _load():
     L.int8t_cache_attend_workspace_bytes.argtypes = [C.POINTER(Cache), C.POINTER(AttendDesc)]
     L.int8t_cache_attend.restype = i32
     L.int8t_cache_attend.argtypes = [C.POINTER(Cache), C.POINTER(AttendDesc), vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.int8t_product_division.restype = i32
+    L.int8t_product_division.argtypes = [i32, i32, i32, sz, C.POINTER(Division)]
+    L.int8t_cache_attend_division.restype = i32
+    L.int8t_cache_attend_division.argtypes = [C.POINTER(Cache), C.POINTER(AttendDesc), C.POINTER(Division)]
     L.int8t_dclr_scale.restype = C.c_double
     L.int8t_dclr_scale.argtypes = [C.c_double, C.c_double, C.c_double]
     L.int8t_profile_start.restype = i32
@@ -448,6 +458,18 @@ def int8t_cache_attend_workspace_bytes(cache: Cache, desc: AttendDesc) -> int:
 def int8t_cache_attend(cache: Cache, desc: AttendDesc, q, starts, lengths, table, out, lse=None, ws=None, stream=None):
     _check(lib.int8t_cache_attend(C.byref(cache), C.byref(desc), _ptr(q), _ptr(starts), _ptr(lengths), _ptr(table), _ptr(out), _ptr(lse), _ptr(ws),
                                   _nbytes(ws), _stream(stream)))
+
+
+def int8t_product_division(M: int, N: int, K: int, ws_bytes: int = 0) -> Division:
+    out = Division()
+    _check(lib.int8t_product_division(M, N, K, ws_bytes, C.byref(out)))
+    return out
+
+
+def int8t_cache_attend_division(cache: Cache, desc: AttendDesc) -> Division:
+    out = Division()
+    _check(lib.int8t_cache_attend_division(C.byref(cache), C.byref(desc), C.byref(out)))
+    return out
 
 
 def int8t_dclr_scale(d_c: float, alpha: float = 20.0, beta: float = 0.1) -> float:

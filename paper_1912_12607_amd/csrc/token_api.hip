@@ -335,3 +335,20 @@ extern "C" int8t_status int8t_cache_attend(const int8t_cache* cache, const int8t
     a.part_ml = a.part_o ? a.part_o + align256((size_t)a.splits * a.tokens * a.c.heads * a.group * a.c.dim * sizeof(float)) / sizeof(float) : nullptr;
     return launched(launch_attend(a, (hipStream_t)stream));
 }
+
+extern "C" int8t_status int8t_product_division(int M, int N, int K, size_t ws_bytes, int8t_division* out) {
+    if (!out) return INT8T_ERR_NULL;
+    if (!codes_ok(M, K) || !codes_ok(N, K) || K > INT8T_MAX_REDUCTION || !product_fits(M, N, pad16(K))) return INT8T_ERR_SHAPE;
+    product_division(M, N, pad16(K), ws_bytes, &out->rows, &out->waves, &out->stages, &out->shares);
+    return INT8T_OK;
+}
+
+extern "C" int8t_status int8t_cache_attend_division(const int8t_cache* cache, const int8t_attend_desc* desc, int8t_division* out) {
+    const int8t_status ok = attend_ok(cache, desc);
+    if (ok != INT8T_OK) return ok;
+    if (!out) return INT8T_ERR_NULL;
+    if (desc->tokens == 0 || desc->requests == 0) return INT8T_ERR_SHAPE;
+    const AttendArgs a = attend_args(cache, desc);
+    *out = int8t_division{a.rows, a.waves, 0, a.splits};
+    return INT8T_OK;
+}

@@ -495,6 +495,7 @@ void attend_plan(AttendArgs* a, int longest) {
         if (a->splits < 1) a->splits = 1;
         return;
     }
+    a->waves = a->rows / 32;
     const long long blocks = (each + a->rows - 1) / a->rows * a->requests * a->c.heads;
     long long s = (a->rows == 128 ? 512 : 256) / blocks;
     const int least = a->rows == 128 ? 256 : 1024;

@@ -490,14 +490,25 @@ hipError_t launch_few_tokens(const FewArgs& a, hipStream_t st) {
 #undef LAUNCH
 }
 
+constexpr int kTileRows[4] = {256, 128, 128, 64}, kTileWaves[4] = {8, 4, 4, 4}, kTileStages[4] = {2, 2, 3, 4};
 bool product_fits(int M, int N, int Kp) {
-    static const int kRows[4] = {256, 128, 128, 64};
     for (const bool scratch : {false, true}) {
         const ProductPlan p = product_plan(M, N, Kp, scratch);
-        const unsigned long long blocks = ((unsigned long long)M + kRows[p.tile] - 1) / kRows[p.tile] * (((unsigned long long)N + kRows[p.tile] - 1) / kRows[p.tile]) * p.splits;
-        if ((blocks + 8) * (p.tile == 0 ? 512 : 256) >= 1ull << 32) return false;
+        const int rows = kTileRows[p.tile];
+        const unsigned long long blocks = ((unsigned long long)M + rows - 1) / rows * (((unsigned long long)N + rows - 1) / rows) * p.splits;
+        if ((blocks + 8) * 64 * kTileWaves[p.tile] >= 1ull << 32) return false;
     }
     return true;
+}
+void product_division(int M, int N, int Kp, size_t scratch_bytes, int* rows, int* waves, int* stages, int* shares) {
+    ProductArgs a{};
+    int32_t there = 0;
+    a.M = M; a.N = N; a.Kp = Kp; a.part = scratch_bytes ? &there : nullptr;
+    const int tile = planned(&a, scratch_bytes);
+    *rows = kTileRows[tile];
+    *waves = kTileWaves[tile];
+    *stages = kTileStages[tile];
+    *shares = a.splits;
 }
 size_t product_scratch(int M, int N, int Kp) {
     const ProductPlan p = product_plan(M, N, Kp, true);

@@ -136,6 +136,7 @@ struct FewArgs {             // the same from x itself, codes made on the way: f
 bool few_tokens(int M, int Kp);
 hipError_t launch_few_tokens(const FewArgs& a, hipStream_t st);
 bool product_fits(int M, int N, int Kp);      // its blocks fit a launch
+void product_division(int M, int N, int Kp, size_t scratch_bytes, int* rows, int* waves, int* stages, int* shares);
 size_t product_scratch(int M, int N, int Kp);
 hipError_t launch_product(ProductArgs a, size_t scratch_bytes, hipStream_t st);
 // Two products, in one launch where both take the same tiles whole.  They share the scratch.
@@ -174,7 +175,7 @@ struct AttendArgs {
     float scale;
     void* out;               // [tokens][heads * group][dim]
     float* lse;              // [tokens][heads * group], or null
-    int rows, waves;         // of a block (waves: blocks of 16 rows): attend_plan()
+    int rows, waves;         // of a block: attend_plan()
     int splits;              // blocks per row tile; blocks of 16 rows: the last one has what is left
     int share;               // keys of one, blocks of 16 rows (a multiple of 32)
     float *part_o, *part_ml; // [splits][tokens * heads * group][dim], [..][2]

@@ -61,3 +61,18 @@ def test_scratch_of_attention(requests, new, heads, group, dim, kind, width):
     assert need[0] == need[2] and max(need) <= ((dim + 2) << 20) + 512
     if requests * new * group * heads >= 1 << 18:
         assert max(need) == 0
+
+
+def test_divisions_are_asked_for_with_sizes_that_a_call_takes():
+    out = B.Division()
+    assert B.lib.int8t_product_division(8, 8, 8, 0, None) == NULL
+    for bad in ((0, 8, 8), (8, 0, 8), (8, 8, 0), (8, 8, B.MAX_REDUCTION + 1), (1 << 26, 1 << 26, 16)):
+        assert B.lib.int8t_product_division(*bad, 0, C.byref(out)) == SHAPE
+    assert B.int8t_product_division(8, 8, 100000).shares == 1                # (no scratch)
+    c, d = B.Cache(FAKE, FAKE, FAKE, FAKE, 10, 16, 2, 64), B.AttendDesc(4, 2, 3, 8, 0, 0, 1, 0.125, 384, 64, 8)
+    assert B.lib.int8t_cache_attend_division(C.byref(c), C.byref(d), None) == NULL
+    assert B.int8t_cache_attend_division(c, d).rows == 16
+    d.tokens = 0
+    assert B.lib.int8t_cache_attend_division(C.byref(c), C.byref(d), C.byref(out)) == SHAPE
+    d.tokens, c.dim = 4, 65
+    assert B.lib.int8t_cache_attend_division(C.byref(c), C.byref(d), C.byref(out)) == SHAPE
