@@ -121,9 +121,10 @@ def test_attention_by_16_rows(dtype, dim, page, rows, waves, divided, heads, gro
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("divided,group,new,lengths", [(False, 4, [300, 290], [301, 500]), (True, 4, [330, 320], [3000, 2500])])
 def test_attention_by_many_rows(dtype, dim, page, causal, divided, group, new, lengths):
-    cache, table = cache_of(lengths, 1, dim, page, 3)
+    heads = 8
+    cache, table = cache_of(lengths, heads, dim, page, 3)
     longest = max(lengths) if divided else 1
     d = division(cache, sum(new), len(new), group, table.shape[1], dtype, longest)
     want = 256 if dim == 128 and dtype is not F32 else 128
     assert (d.rows, d.waves, d.shares > 1) == (want, want // 32, divided)
-    check(cache, queries(sum(new), group, dim, dtype, 4), starts_of(new), lengths, table, causal, longest=longest)
+    check(cache, queries(sum(new), heads * group, dim, dtype, 4), starts_of(new), lengths, table, causal, longest=longest)
