@@ -451,27 +451,27 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
 // of a request on average that their rows are filled, and from so many of all requests and heads that a block is there for a third of the compute units at least
 // (us with 16 rows / with 128, dim 128 in bf16: 256; equal requests, all keys seen:
 //   rows, requests, heads, keys    66,9,12,1500  200,2,32,6000  264,8,8,2048  256,4,8,2048  400,4,8,3000  2048,1,8,8192  64,64,8,1024  400,64,4,1024  512,2,4,2000  384,1,2,16000  96,4,2,700
-//   pages of 16, dim  64 bf16     27/39          95/68         50/50         33/37         56/44          145/88        46/68          125/83        24/27          34/59        10/20   
-//   pages of 16, dim  64 fp32     31/45          114/84        62/61         38/44         64/53         174/110        55/85         154/107        26/31          36/63        10/23   
-//   pages of 16, dim 128 bf16     42/68          169/85        82/62         35/60         92/82         253/109        80/98         234/158        26/92          47/68        11/35   
-//   pages of 16, dim 128 fp32     48/92         186/200        95/140        42/81        107/114        296/256        93/192        280/267        30/40          55/91        14/34   
-//   pages of 16, dim 256 bf16    112/130        386/276       200/192        80/110       201/156        582/356       213/271        530/368        53/53         104/145       20/45   
-//   pages of 16, dim 256 fp32    171/220        636/516       321/335       123/181       311/271        948/617       332/528        902/703        74/80         147/205       29/71   
-//   pages of 24, dim  64 bf16     38/39          126/68        64/50         41/38         66/44          183/88        60/67          166/84        27/26          38/58        10/20   
-//   pages of 24, dim  64 fp32     41/45          137/85        72/62         46/44         74/54         204/111        66/84         184/107        30/31          42/63        11/23   
-//   pages of 24, dim 128 bf16     49/68          200/85        104/63        58/60         103/83        289/108        96/99         259/157        38/92          49/68        13/36   
-//   pages of 24, dim 128 fp32     74/92         255/199       131/140        53/81        141/114        384/257       125/192        367/267        36/40          69/90        16/34   
-//   pages of 24, dim 256 bf16     97/129        342/277       172/193        73/111       187/156        517/356       185/270        478/368        49/53          95/144       19/46   
-//   pages of 24, dim 256 fp32    130/220        494/545       243/337       101/181       258/270        744/615       259/528        705/732        63/81         125/204       28/71   
-//   pages of  7, dim  64 bf16     62/38          210/68        104/50        60/38         98/44          291/88        93/68          265/85        36/26          48/58        13/20   
-//   pages of  7, dim  64 fp32     64/45          219/85        114/62        64/44         108/54        307/112        99/84         281/109        39/31          51/63        14/23   
-//   pages of  7, dim 128 bf16     75/70          311/88        163/63        79/62         156/84        420/111       144/101        393/161        48/94          65/70        17/35   
-//   pages of  7, dim 128 fp32     127/92        417/197       218/138        75/81        214/113        576/253       197/189        579/264        45/40          103/91       19/33   
-//   pages of  7, dim 256 bf16    152/129        498/271       265/189       105/111       255/154        718/349       280/271        681/360        63/53         127/145       22/45   
+//   pages of 16, dim  64 bf16     27/39          95/68         50/50         33/37         56/44          145/88        46/68          125/83        24/27          34/59        10/20
+//   pages of 16, dim  64 fp32     31/45          114/84        62/61         38/44         64/53         174/110        55/85         154/107        26/31          36/63        10/23
+//   pages of 16, dim 128 bf16     42/68          169/85        82/62         35/60         92/82         253/109        80/98         234/158        26/92          47/68        11/35
+//   pages of 16, dim 128 fp32     48/92         186/200        95/140        42/81        107/114        296/256        93/192        280/267        30/40          55/91        14/34
+//   pages of 16, dim 256 bf16    112/130        386/276       200/192        80/110       201/156        582/356       213/271        530/368        53/53         104/145       20/45
+//   pages of 16, dim 256 fp32    171/220        636/516       321/335       123/181       311/271        948/617       332/528        902/703        74/80         147/205       29/71
+//   pages of 24, dim  64 bf16     38/39          126/68        64/50         41/38         66/44          183/88        60/67          166/84        27/26          38/58        10/20
+//   pages of 24, dim  64 fp32     41/45          137/85        72/62         46/44         74/54         204/111        66/84         184/107        30/31          42/63        11/23
+//   pages of 24, dim 128 bf16     49/68          200/85        104/63        58/60         103/83        289/108        96/99         259/157        38/92          49/68        13/36
+//   pages of 24, dim 128 fp32     74/92         255/199       131/140        53/81        141/114        384/257       125/192        367/267        36/40          69/90        16/34
+//   pages of 24, dim 256 bf16     97/129        342/277       172/193        73/111       187/156        517/356       185/270        478/368        49/53          95/144       19/46
+//   pages of 24, dim 256 fp32    130/220        494/545       243/337       101/181       258/270        744/615       259/528        705/732        63/81         125/204       28/71
+//   pages of  7, dim  64 bf16     62/38          210/68        104/50        60/38         98/44          291/88        93/68          265/85        36/26          48/58        13/20
+//   pages of  7, dim  64 fp32     64/45          219/85        114/62        64/44         108/54        307/112        99/84         281/109        39/31          51/63        14/23
+//   pages of  7, dim 128 bf16     75/70          311/88        163/63        79/62         156/84        420/111       144/101        393/161        48/94          65/70        17/35
+//   pages of  7, dim 128 fp32     127/92        417/197       218/138        75/81        214/113        576/253       197/189        579/264        45/40          103/91       19/33
+//   pages of  7, dim 256 bf16    152/129        498/271       265/189       105/111       255/154        718/349       280/271        681/360        63/53         127/145       22/45
 //   pages of  7, dim 256 fp32    181/258        666/674       325/390       130/208       316/311        946/722       350/677        914/890        78/92         151/226       31/76).
-// Over those and 150 other calls (ragged and equal, causal and not, dims from 48 to 256, pages from 1 to 64) the rule costs 1.3 and 1.5 % over the faster of the two, by
-// rows of a request alone 7.7 and 9.1 %.
-// Shares of the keys of larger blocks: up to a block for each compute unit (two of 128 rows, which 64 KiB of LDS let run together), of 256 keys at least (us with 256, 512, 1024 keys at
+// Over 1210 calls (those and drawn ones: ragged and equal, causal and not, dims from 48 to 256, pages from 1 to 64) the rule costs 2.6 % over the faster of the two, the
+// best pair of limits for each dim, type and kind of page 2.0, rows of a request alone 7.9.
+// Shares of the keys of larger blocks: up to a block for each compute unit (two of 128 rows), of 256 keys at least (us with 256, 512, 1024 keys at
 // least: 256 rows of 5 requests and 8 heads over 1500 keys, dim 64 bf16 30, 33, 48, fp32 36, 39, 60, dim 128 59, 53, 74 and 66, 62, 95, dim 256 86, 82, 132 and
 // 144, 138, 232; 300 rows of 4 and 12 over 1000: 31, 34, 34 | 36, 42, 42 | 44, 55, 56 | 67, 69, 69 | 92, 94, 94 | 155, 165, 166; 256 rows of 12 and 4 over 2500: 36, 37, 57 |
 // 42, 46, 70 | 82, 88, 74 | 86, 98, 89 | 120, 137, 123 | 226, 251, 238).
@@ -483,9 +483,10 @@ void attend_plan(AttendArgs* a, int longest) {
     // smaller pages: blocks of 16 rows look the table up for four keys at a time, or for each; larger ones look less often
     if (a->c.page_size % 4 != 0) {
         many = dim <= 128 ? 24 : fp32 ? 300 : 64;
-        all = 4000;
+        all = dim == 64 ? 2500 : dim == 128 ? 5000 : 8000;
     } else if (a->c.page_size % 16 != 0) {
         many = dim == 64 || (dim == 128 && !fp32) ? 72 : dim == 256 && fp32 ? 600 : 160;
+        all = dim == 256 ? 10000 : 8000;
     }
     a->rows = each < many || rows * a->c.heads < all ? 16 : dim == 128 && !fp32 ? 256 : 128;
     const long long tiles = (rows / a->rows + a->requests) * a->c.heads;
