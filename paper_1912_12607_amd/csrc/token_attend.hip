@@ -14,7 +14,7 @@ namespace {
 //   values   O^T[dim][row] = V^T P^T: S^T's layout is P^T's operand layout if the keys of a 32 are numbered (lane group, tile, i), so
 //            nothing is exchanged; a lane loads DIM / 16 bytes of eight keys and turns them in registers.
 // PARTS = 2 (fp32): q and p in two fp16 pieces each.  UNI: the page size is a multiple of 16, whole tiles of 16 keys lie on a page and their
-// address is scalar.  Bound by memory, codes and scales read once: the next token of 64 requests over 1 to 8192 keys, 8 heads of 128, 135 us with the
+// address is scalar.  Bound by memory, codes and scales read once: the next token of 64 requests over 1 to 8192 keys, 8 heads of 128, 139 us with the
 // joining pass (640 MB: 4.8 TB/s, a large copy 5.1).  A request alone, by its few blocks' arithmetic: 1021 keys 12 us, 5.8 and 1.7 for each 32 keys of a wave.
 // ------------------------------------------------------------------------------------------------
 // RW waves: four (two blocks on a compute unit, one at work while the other starts or ends), or eight where there are few blocks.

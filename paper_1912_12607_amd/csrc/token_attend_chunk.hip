@@ -10,7 +10,8 @@
 //            of V (rows of keys, as they came) delivers: p never leaves its lane.
 // Bound by vector and matrix units together: a score costs 9 to 10 vector operations, of which the exponential counts for four, and 256 multiply-adds
 // (DIM 128), and arithmetic of one wave and products of another overlap by half only (fma 295 us, products 322, together 466).  Two chunks of 2048 tokens over 8192 keys, 32 heads of 128 on 8, bf16:
-// 585 to 608 us (478 GFLOP: 0.8 PFLOP/s; a large library product in fp16 1.18).  Nine fp32 requests of up to 131 tokens over up to 1500 keys, 12 heads of 64: 25 us.
+// 603 to 615 us (478 GFLOP: 0.8 PFLOP/s; a large library product in fp16 1.18), in 55 % of whose cycles a SIMD issues vector instructions and in 32 % has a product: 88 %
+// together; LDS 12 %.
 #include "token_attend.h"
 
 namespace int8t {
@@ -52,7 +53,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, half = lane >> 5;
     // Heads first, so that an XCD has as few heads' keys in its L2 as can be, and each request's last rows, which see the most keys, before its others, so that
-    // the chip runs out of short blocks (tiles first, in order: 650 us for two chunks of 2048 tokens over 8192 keys, not 597).
+    // the chip runs out of short blocks (tiles first, in order: 9 % more time for two chunks of 2048 tokens over 8192 keys).
     const int place = (int)(blockIdx.y * gridDim.x + blockIdx.x), group_of = div_by(place, a.by_heads);
     const int head = place - group_of * a.c.heads, split = (int)blockIdx.z, block = (int)gridDim.x - 1 - group_of;
     const int D = a.c.dim;
