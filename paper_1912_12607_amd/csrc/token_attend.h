@@ -99,6 +99,9 @@ __device__ __forceinline__ float rows16_sum(float x) { const Pair p = rows16(x);
 // products take in fp16 share it.  c brings the largest weight that the row has seen to 2^14 .. 2^15, where fp16 has 11 bits down to 2^-28 of it and steps
 // of 2^-38 below; a larger weight lowers c.  It goes by the row's own weights: by the tile's largest scale and score, a key that the row does not see, or
 // sees at 2^-40, would take the bits of the others.
+// bf16 and fp16 tensors have a weight in one piece, off by 2^-12 of itself at most and to either side: errors against 64 bits are 1.6e-3 to 1.7e-3 of bf16 results, as
+// with weights in fp32, and 2.8e-4 of fp16 ones, where those have 2.1e-4.  A second piece costs a chunk 60 % more time (two of 2048 tokens over 8192 keys 610 -> 994 us,
+// dim 64 477 -> 570, dim 256 583 -> 659), single tokens 1 to 6 %.
 struct RowUnit {
     static constexpr float kMostWeight = 63000.0f, kMostSum = 0x1p120f;     // (p alone stays in range where the scales are tiny or zero)
     float c = 0.0f;
