@@ -264,9 +264,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int v = 0; v < 16; ++v) top = fmaxf(top, x[kt][v]);
-        top = halves_max(top) * qscale;
+        top *= qscale;
         const float scale = s[TK + lane];
-        if (__any(top > unit.room || fabsf(scale) > unit.vs) && unit.unknown(top, scale)) {
+        if (__any(top > unit.room || fabsf(scale) > unit.vs) && unit.unknown(top = halves_max(top), scale)) {
             float weight = kNone;
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
