@@ -478,7 +478,8 @@ int8t_variant int8t_conv_selected_variant(int8t_op op, const int8t_conv_desc *de
  *            "deviation_finish_kernel", "igemm_kernel", "igemm_dma_kernel", "igemm_fused_kernel", "igemm_reduce_kernel",
  *            "band_kernel", "band_reg_kernel", "wgrad_kernel", "wgrad_lines_kernel", "wgrad_reduce_kernel", "s2d_repack_kernel",
  *            "conv_trio_kernel", "quantize_rows_kernel", "quantize_cols_kernel" (both passes), "transpose_codes_kernel", "product_kernel",
- *            "product_reduce_kernel", "few_tokens_kernel", "cache_write_kernel", "cache_read_kernel", "attend_kernel", "attend_join_kernel", "dw_conv_kernel" (every depthwise forward / backward-data variant),
+ *            "product_reduce_kernel", "few_tokens_kernel", "cache_write_kernel", "cache_read_kernel", "attend_kernel", "attend_join_kernel", "mx4_quantize_kernel" (all passes), "mx4_product_kernel",
+ *            "mx4_reduce_kernel", "mx4_few_kernel", "mx4_cache_write_kernel", "mx4_cache_read_kernel", "mx4_attend_kernel", "rotate_kernel", "pages_kernel", "dw_conv_kernel" (every depthwise forward / backward-data variant),
  *            "dw_wgrad_kernel" (every depthwise backward-weight variant), "dw_wgrad_reduce_kernel", "dw_trio_kernel", "infer_1x1_kernel");
  *            "conv_trio_kernel" and "dw_trio_kernel" are all the launches that several passes share: strided layers' and the one that
  *            quantizes depthwise tensors too;
@@ -665,6 +666,147 @@ typedef struct int8t_division {
 } int8t_division;
 int8t_status int8t_product_division(int M, int N, int K, size_t ws_bytes, int8t_division *out);
 int8t_status int8t_cache_attend_division(const int8t_cache *cache, const int8t_attend_desc *desc, int8t_division *out);
+
+/*
+ * ---- Microscaled 4-bit tokens ---------------------------------------------------------------------------------------------
+ * Codes of four bits: a sign (the highest bit) over 0, .5, 1, 1.5, 2, 3, 4, 6.  A block of 32 values along the axis that a product sums over shares a power of
+ * two 2^e, held as the byte e + 127; e is the least integer of [-127, 127] for which the block's largest magnitude is at most 6 * 2^e, so that no value is
+ * clipped.  Nearest: ties to the even code.  Stochastic: with a = |v| 2^-e, F = floor(a 2^23) for a < 1 and (the bits of a) - (the bits of 0.5) above counts 2^-22 of
+ * a step, and the magnitude's code is (F + u) >> 22 with u the upper 22 of the 24 bits drawn for (seed, row * cols + col): unbiased.
+ * A block that holds NaN or an infinity has the byte 255 (NaN) and codes of 0.
+ *   codes    [rows][16 * blocks] bytes, blocks = cols / 32 rounded up: value c is the low (c even) or high half of byte c / 2; zero beyond cols
+ *   scales   [panels][rows][8] bytes, panels = blocks / 8 rounded up: block b of row r is at ((b / 8) * rows + r) * 8 + b % 8; zero beyond the last block
+ *            (products read scales 16 bytes at a time: 8 bytes behind an odd number of rows and panels have to be there, and are not used)
+ * Sums of products are in fp32.  Pointers to codes and scales lie on 16 bytes.
+ */
+
+/*
+ * Codes of rows x cols values with blocks along the columns (q, s) and, transposed, of cols x rows with blocks along the rows (qt, st), of one matrix.
+ *   x_dev         rows x cols elements of `type`, rows `pitch` apart;  rows, cols at most INT8T_MAX_REDUCTION where they are the blocks' axis
+ *   q_dev, s_dev  NULL, or out: codes and scales of rows x cols;   draws of `seed`
+ *   qt_dev, st_dev   NULL, or out: codes and scales of cols x rows;   draws of `seed` with its highest bit flipped, of the same index
+ *   sum_dev       NULL, or out: cols floats, the columns' sums
+ *   ws_dev        with sum_dev: int8t_mx4_quantize_workspace_bytes(rows, cols) bytes, 16-byte aligned; else unused
+ */
+size_t int8t_mx4_quantize_workspace_bytes(int rows, int cols);
+int8t_status int8t_mx4_quantize(const void *x_dev, int8t_dtype type, int rows, int cols, size_t pitch, int8t_round mode, uint64_t seed,
+                                uint8_t *q_dev, uint8_t *s_dev, uint8_t *qt_dev, uint8_t *st_dev, float *sum_dev, void *ws_dev,
+                                size_t ws_bytes, void *stream);
+
+/*
+ * y[m][n] = sum_k a[m][k] b[n][k] + bias[n] of what codes and scales of M x K and N x K stand for
+ *   bias_dev   NULL, or N floats;   y_dev  out: M x N of `type`, rows `pitch` apart
+ *   ws_dev     NULL, or int8t_mx4_product_workspace_bytes(M, N, K) bytes, 16-byte aligned: products with few results split their reduction with it (the order of
+ *              the sums goes by M, N, K and whether it is there, nothing else)
+ */
+size_t int8t_mx4_product_workspace_bytes(int M, int N, int K);
+int8t_status int8t_mx4_product(const uint8_t *a_dev, const uint8_t *sa_dev, const uint8_t *b_dev, const uint8_t *sb_dev, int M, int N, int K,
+                               const float *bias_dev, void *y_dev, int8t_dtype type, size_t pitch, void *ws_dev, size_t ws_bytes,
+                               void *stream);
+
+/*
+ * A linear layer of M tokens, y = x W^T + b: every product's operands have their blocks along its summed axis.
+ *   forward   y  = Q(x) Q(W)^T + b           blocks along K, nearest
+ *   backward  dx = S(dy) Q'(W)               blocks along N;  S: stochastic, draws of `seed`
+ *             dw = S'(dy)^T Q'(x)            blocks along M;  S': draws of `seed` with its highest bit flipped
+ *             db = sum_m dy[m]
+ * int8t_mx4_linear_fwd: w NULL takes wq, sw (codes of N x K, laid out before).  With w: they are written where given (else in scratch), and so are wt, swt (codes
+ * of K x N, for dx).  xt, sxt: codes of K x M of x, for dw; NULL: not kept.  M may be 0.
+ * int8t_mx4_linear_bwd: dx, dw, db NULL: not wanted (one of them at least); dx reads wt, swt, dw reads xt, sxt of the forward pass.
+ * ws: int8t_mx4_linear_workspace_bytes() bytes, 16-byte aligned; may be NULL where that is 0.
+ */
+typedef struct int8t_mx4_linear_buffers {
+    const void *x, *w, *dy;
+    size_t x_pitch, w_pitch, y_pitch, dy_pitch;
+    uint8_t *wq, *sw, *wt, *swt, *xt, *sxt;
+    const float *bias;
+    void *y, *dx, *dw;             /* dx, dw: rows of K elements, dense */
+    float *db;
+    void *ws;
+    size_t ws_bytes;
+} int8t_mx4_linear_buffers;
+/* direction: 0 forward, 1 backward, 2 forward with w NULL that keeps nothing */
+size_t int8t_mx4_linear_workspace_bytes(const int8t_linear_desc *desc, int direction);
+int8t_status int8t_mx4_linear_fwd(const int8t_linear_desc *desc, const int8t_mx4_linear_buffers *b, void *stream);
+int8t_status int8t_mx4_linear_bwd(const int8t_linear_desc *desc, const int8t_mx4_linear_buffers *b, uint64_t seed, void *stream);
+
+/*
+ * A paged cache of keys and values in these codes, blocks along a head's dims: places, slots and limits as int8t_cache.  dim: a multiple of 16, at most 256.
+ * int8t_mx4_cache_write, _read, _attend: as int8t_cache_write, _read, _attend with k, v what codes and scales stand for.
+ * attend: q . k_j exact products in fp32 sums (blocks of 16 rows; larger ones as the 8-bit cache's, with fp16 codes relative to the largest scale of a key's row:
+ * blocks 2^36 below it lose bits); p_j is rounded to 16 bits for bf16 and fp16 tensors and 24 for fp32 ones (larger blocks: 11 and 22).  A key or value with a block
+ * of scale 255 (values, in blocks of 16 rows: 253 and more, whose products pass fp32) makes the rows that see it NaN, all of their dims, and no others.
+ */
+typedef struct int8t_mx4_cache {
+    uint8_t *kq, *vq;              /* [pages][heads][page_size][16 * blocks], blocks = dim / 32 rounded up */
+    uint8_t *ks, *vs;              /* [pages][heads][page_size][blocks] */
+    int pages, page_size, heads, dim;
+} int8t_mx4_cache;
+int8t_status int8t_mx4_cache_write(const int8t_mx4_cache *cache, const void *k_dev, const void *v_dev, int8t_dtype type, int tokens,
+                                   size_t k_token_pitch, size_t k_head_pitch, size_t v_token_pitch, size_t v_head_pitch,
+                                   const int64_t *slots_dev, void *stream);
+int8t_status int8t_mx4_cache_read(const int8t_mx4_cache *cache, const int64_t *slots_dev, int tokens, void *k_dev, void *v_dev,
+                                  int8t_dtype type, void *stream);
+size_t int8t_mx4_cache_attend_workspace_bytes(const int8t_mx4_cache *cache, const int8t_attend_desc *desc);
+int8t_status int8t_mx4_cache_attend(const int8t_mx4_cache *cache, const int8t_attend_desc *desc, const void *q_dev, const int *starts_dev,
+                                    const int *lengths_dev, const int *table_dev, void *out_dev, float *lse_dev, void *ws_dev,
+                                    size_t ws_bytes, void *stream);
+
+int8t_status int8t_mx4_product_division(int M, int N, int K, size_t ws_bytes, int8t_division *out);
+int8t_status int8t_mx4_cache_attend_division(const int8t_mx4_cache *cache, const int8t_attend_desc *desc, int8t_division *out);
+
+/*
+ * ---- Positions -------------------------------------------------------------------------------------------------------------
+ * Rotary positions: pair i of a head's first `rot` values, (a, b), of a token at position p becomes
+ *   amplitude * (a cos t - b sin t, a sin t + b cos t),   t = 2 pi p turns[i],
+ * and with back = 1 the same with -t (the gradient: of the result's gradient the argument's).  Pairs are values (i, i + rot / 2), or (2 i, 2 i + 1) with interleaved = 1.
+ * Values from `rot` on are copied.  p turns[i] is formed in 64 bits; results in fp32, rounded once.
+ *   x, y            element (token, head, d) at token * token_pitch + head * head_pitch + d;  y may be x (the same pitches then), and overlaps it in no other way
+ *   second          heads of a second tensor of the same tokens (keys beside queries), 0: none
+ *   positions_dev   tokens ints;   turns_dev  rot / 2 doubles
+ */
+typedef struct int8t_rotate_tensor {
+    const void *x;
+    void *y;
+    size_t x_token_pitch, x_head_pitch, y_token_pitch, y_head_pitch;
+    int heads;
+} int8t_rotate_tensor;
+typedef struct int8t_rotate_desc {
+    int tokens, dim, rot;
+    int8t_dtype type;
+    int interleaved, back;
+    float amplitude;
+} int8t_rotate_desc;
+int8t_status int8t_rotate(const int8t_rotate_desc *desc, const int8t_rotate_tensor *first, const int8t_rotate_tensor *second,
+                          const int *positions_dev, const double *turns_dev, void *stream);
+
+/*
+ * Pages of the new tokens of a batch, found on the GPU: what int8t_cache_write (slots), int8t_rotate (positions) and int8t_cache_attend (starts, lengths, table) take.
+ * Request b has have[b] tokens on the first have[b] / page_size (rounded up) pages of table[b], and add[b] new ones (below 0: none).  Free pages are a stack,
+ * free[0 .. available - 1], taken from its end in the order of the requests and of their pages.  A request gets no pages where its tokens end behind `tokens`, where its
+ * row of the table is too short, or where the pages that it and all before it need are more than there are: its new tokens have no slots, its length stays.
+ *   table_dev      [requests][width], rows table_pitch apart; entries of new pages are written
+ *   lengths_dev    out: requests ints, have + add, or have where there were no pages
+ *   left_dev       out: 1 int, pages that are still free
+ *   starts_dev     out: requests + 1 ints, sums of the new tokens
+ *   slots_dev      out: `tokens` 64-bit integers, page * page_size + row; -1: no place, or behind the last request's tokens
+ *   positions_dev  out: `tokens` ints, 0 without a place
+ *   without_dev    out: 1 int, requests that got none (without a new token too, where its length is beyond its table's row)
+ * No output is an input (but table).  width * page_size < 2^31.  `pages`: the length of free.
+ */
+typedef struct int8t_pages_desc {
+    int requests, width, page_size, pages, tokens;
+    size_t table_pitch;
+} int8t_pages_desc;
+int8t_status int8t_pages_extend(const int8t_pages_desc *desc, const int *have_dev, const int *add_dev, int *table_dev, const int *free_dev,
+                                const int *available_dev, int *lengths_dev, int *left_dev, int *starts_dev, int64_t *slots_dev,
+                                int *positions_dev, int *without_dev, void *stream);
+/*
+ * Only the first stay[b] tokens of each request stay (0: it has ended; more than it has: all): lengths_dev, in and out; pages behind them go back onto the stack free_dev,
+ * in the order of the requests, and available_dev, in and out, counts them.  `tokens` of the descriptor is not used.
+ */
+int8t_status int8t_pages_shrink(const int8t_pages_desc *desc, const int *stay_dev, int *lengths_dev, const int *table_dev, int *free_dev,
+                                int *available_dev, void *stream);
 
 #ifdef __cplusplus
 }

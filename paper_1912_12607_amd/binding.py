@@ -37,6 +37,10 @@ EXPORTS = ["int8t_status_string", "int8t_code_bytes", "int8t_unpack_codes", "int
            "int8t_product_workspace_bytes", "int8t_product", "int8t_linear_workspace_bytes", "int8t_linear_fwd", "int8t_linear_bwd",
            "int8t_cache_write", "int8t_cache_read", "int8t_cache_attend_workspace_bytes", "int8t_cache_attend",
            "int8t_product_division", "int8t_cache_attend_division",
+           "int8t_mx4_quantize_workspace_bytes", "int8t_mx4_quantize", "int8t_mx4_product_workspace_bytes", "int8t_mx4_product",
+           "int8t_mx4_linear_workspace_bytes", "int8t_mx4_linear_fwd", "int8t_mx4_linear_bwd", "int8t_mx4_cache_write", "int8t_mx4_cache_read",
+           "int8t_mx4_cache_attend_workspace_bytes", "int8t_mx4_cache_attend", "int8t_mx4_product_division", "int8t_mx4_cache_attend_division",
+           "int8t_rotate", "int8t_pages_extend", "int8t_pages_shrink",
            "int8t_profile_start", "int8t_profile_start_sampled", "int8t_profile_stop", "int8t_profile_mfma_ceiling"]
 
 
@@ -77,6 +81,29 @@ class LinearBuffers(C.Structure):
 
 class Cache(C.Structure):
     _fields_ = ([(n, C.c_void_p) for n in ("kq", "vq", "ks", "vs")] + [(n, C.c_int) for n in ("pages", "page_size", "heads", "dim")])
+
+
+class Mx4LinearBuffers(C.Structure):
+    """int8t_mx4_linear_buffers: field names are the header's."""
+    _fields_ = ([(n, C.c_void_p) for n in ("x", "w", "dy")] + [(n, C.c_size_t) for n in ("x_pitch", "w_pitch", "y_pitch", "dy_pitch")]
+                + [(n, C.c_void_p) for n in ("wq", "sw", "wt", "swt", "xt", "sxt", "bias", "y", "dx", "dw", "db", "ws")] + [("ws_bytes", C.c_size_t)])
+
+
+class Mx4Cache(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("kq", "vq", "ks", "vs")] + [(n, C.c_int) for n in ("pages", "page_size", "heads", "dim")])
+
+
+class RotateTensor(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("x", "y")] + [(n, C.c_size_t) for n in ("x_token_pitch", "x_head_pitch", "y_token_pitch", "y_head_pitch")]
+                + [("heads", C.c_int)])
+
+
+class RotateDesc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("tokens", "dim", "rot", "type", "interleaved", "back")] + [("amplitude", C.c_float)]
+
+
+class PagesDesc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("requests", "width", "page_size", "pages", "tokens")] + [("table_pitch", C.c_size_t)]
 
 
 class AttendDesc(C.Structure):
@@ -184,6 +211,38 @@ def _load():
     L.int8t_product_division.argtypes = [i32, i32, i32, sz, C.POINTER(Division)]
     L.int8t_cache_attend_division.restype = i32
     L.int8t_cache_attend_division.argtypes = [C.POINTER(Cache), C.POINTER(AttendDesc), C.POINTER(Division)]
+    L.int8t_mx4_quantize_workspace_bytes.restype = sz
+    L.int8t_mx4_quantize_workspace_bytes.argtypes = [i32, i32]
+    L.int8t_mx4_quantize.restype = i32
+    L.int8t_mx4_quantize.argtypes = [vp, i32, i32, i32, sz, i32, u64, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.int8t_mx4_product_workspace_bytes.restype = sz
+    L.int8t_mx4_product_workspace_bytes.argtypes = [i32, i32, i32]
+    L.int8t_mx4_product.restype = i32
+    L.int8t_mx4_product.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, i32, sz, vp, sz, vp]
+    L.int8t_mx4_linear_workspace_bytes.restype = sz
+    L.int8t_mx4_linear_workspace_bytes.argtypes = [C.POINTER(LinearDesc), i32]
+    L.int8t_mx4_linear_fwd.restype = i32
+    L.int8t_mx4_linear_fwd.argtypes = [C.POINTER(LinearDesc), C.POINTER(Mx4LinearBuffers), vp]
+    L.int8t_mx4_linear_bwd.restype = i32
+    L.int8t_mx4_linear_bwd.argtypes = [C.POINTER(LinearDesc), C.POINTER(Mx4LinearBuffers), u64, vp]
+    L.int8t_mx4_cache_write.restype = i32
+    L.int8t_mx4_cache_write.argtypes = [C.POINTER(Mx4Cache), vp, vp, i32, i32, sz, sz, sz, sz, vp, vp]
+    L.int8t_mx4_cache_read.restype = i32
+    L.int8t_mx4_cache_read.argtypes = [C.POINTER(Mx4Cache), vp, i32, vp, vp, i32, vp]
+    L.int8t_mx4_cache_attend_workspace_bytes.restype = sz
+    L.int8t_mx4_cache_attend_workspace_bytes.argtypes = [C.POINTER(Mx4Cache), C.POINTER(AttendDesc)]
+    L.int8t_mx4_cache_attend.restype = i32
+    L.int8t_mx4_cache_attend.argtypes = [C.POINTER(Mx4Cache), C.POINTER(AttendDesc), vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.int8t_mx4_product_division.restype = i32
+    L.int8t_mx4_product_division.argtypes = [i32, i32, i32, sz, C.POINTER(Division)]
+    L.int8t_mx4_cache_attend_division.restype = i32
+    L.int8t_mx4_cache_attend_division.argtypes = [C.POINTER(Mx4Cache), C.POINTER(AttendDesc), C.POINTER(Division)]
+    L.int8t_rotate.restype = i32
+    L.int8t_rotate.argtypes = [C.POINTER(RotateDesc), C.POINTER(RotateTensor), C.POINTER(RotateTensor), vp, vp, vp]
+    L.int8t_pages_extend.restype = i32
+    L.int8t_pages_extend.argtypes = [C.POINTER(PagesDesc)] + [vp] * 12
+    L.int8t_pages_shrink.restype = i32
+    L.int8t_pages_shrink.argtypes = [C.POINTER(PagesDesc)] + [vp] * 6
     L.int8t_dclr_scale.restype = C.c_double
     L.int8t_dclr_scale.argtypes = [C.c_double, C.c_double, C.c_double]
     L.int8t_profile_start.restype = i32
@@ -470,6 +529,78 @@ def int8t_cache_attend_division(cache: Cache, desc: AttendDesc) -> Division:
     out = Division()
     _check(lib.int8t_cache_attend_division(C.byref(cache), C.byref(desc), C.byref(out)))
     return out
+
+
+def int8t_mx4_quantize_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib.int8t_mx4_quantize_workspace_bytes(rows, cols))
+
+
+def int8t_mx4_quantize(x, rows, cols, pitch, mode, seed, q=None, s=None, qt=None, st=None, sums=None, ws=None, type=F32, stream=None):
+    _check(lib.int8t_mx4_quantize(_ptr(x), type, rows, cols, pitch, mode, seed, _ptr(q), _ptr(s), _ptr(qt), _ptr(st), _ptr(sums), _ptr(ws), _nbytes(ws),
+                                  _stream(stream)))
+
+
+def int8t_mx4_product_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib.int8t_mx4_product_workspace_bytes(M, N, K))
+
+
+def int8t_mx4_product(a, sa, b, sb, M, N, K, bias, y, pitch, type=F32, ws=None, stream=None):
+    _check(lib.int8t_mx4_product(_ptr(a), _ptr(sa), _ptr(b), _ptr(sb), M, N, K, _ptr(bias), _ptr(y), type, pitch, _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def int8t_mx4_linear_workspace_bytes(desc: LinearDesc, direction: int) -> int:
+    return int(lib.int8t_mx4_linear_workspace_bytes(C.byref(desc), direction))
+
+
+def int8t_mx4_linear_fwd(desc: LinearDesc, buffers: Mx4LinearBuffers, stream=None):
+    _check(lib.int8t_mx4_linear_fwd(C.byref(desc), C.byref(buffers), _stream(stream)))
+
+
+def int8t_mx4_linear_bwd(desc: LinearDesc, buffers: Mx4LinearBuffers, seed: int = 0, stream=None):
+    _check(lib.int8t_mx4_linear_bwd(C.byref(desc), C.byref(buffers), seed, _stream(stream)))
+
+
+def int8t_mx4_cache_write(cache: Mx4Cache, k, v, type, tokens, k_token_pitch, k_head_pitch, v_token_pitch, v_head_pitch, slots, stream=None):
+    _check(lib.int8t_mx4_cache_write(C.byref(cache), _ptr(k), _ptr(v), type, tokens, k_token_pitch, k_head_pitch, v_token_pitch, v_head_pitch, _ptr(slots),
+                                     _stream(stream)))
+
+
+def int8t_mx4_cache_read(cache: Mx4Cache, slots, tokens, k, v, type, stream=None):
+    _check(lib.int8t_mx4_cache_read(C.byref(cache), _ptr(slots), tokens, _ptr(k), _ptr(v), type, _stream(stream)))
+
+
+def int8t_mx4_cache_attend_workspace_bytes(cache: Mx4Cache, desc: AttendDesc) -> int:
+    return int(lib.int8t_mx4_cache_attend_workspace_bytes(C.byref(cache), C.byref(desc)))
+
+
+def int8t_mx4_cache_attend(cache: Mx4Cache, desc: AttendDesc, q, starts, lengths, table, out, lse=None, ws=None, stream=None):
+    _check(lib.int8t_mx4_cache_attend(C.byref(cache), C.byref(desc), _ptr(q), _ptr(starts), _ptr(lengths), _ptr(table), _ptr(out), _ptr(lse), _ptr(ws),
+                                      _nbytes(ws), _stream(stream)))
+
+
+def int8t_mx4_product_division(M: int, N: int, K: int, ws_bytes: int = 0) -> Division:
+    out = Division()
+    _check(lib.int8t_mx4_product_division(M, N, K, ws_bytes, C.byref(out)))
+    return out
+
+
+def int8t_mx4_cache_attend_division(cache: Mx4Cache, desc: AttendDesc) -> Division:
+    out = Division()
+    _check(lib.int8t_mx4_cache_attend_division(C.byref(cache), C.byref(desc), C.byref(out)))
+    return out
+
+
+def int8t_rotate(desc: RotateDesc, first: RotateTensor, second, positions, turns, stream=None):
+    _check(lib.int8t_rotate(C.byref(desc), C.byref(first), None if second is None else C.byref(second), _ptr(positions), _ptr(turns), _stream(stream)))
+
+
+def int8t_pages_extend(desc: PagesDesc, have, add, table, free, available, lengths, left, starts, slots, positions, without, stream=None):
+    _check(lib.int8t_pages_extend(C.byref(desc), *(_ptr(t) for t in (have, add, table, free, available, lengths, left, starts, slots, positions, without)),
+                                  _stream(stream)))
+
+
+def int8t_pages_shrink(desc: PagesDesc, stay, lengths, table, free, available, stream=None):
+    _check(lib.int8t_pages_shrink(C.byref(desc), *(_ptr(t) for t in (stay, lengths, table, free, available)), _stream(stream)))
 
 
 def int8t_dclr_scale(d_c: float, alpha: float = 20.0, beta: float = 0.1) -> float:

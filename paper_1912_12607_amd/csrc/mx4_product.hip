@@ -1,0 +1,504 @@
+// Products of microscaled 4-bit codes:  y[m][n] = sum_k (a[m][k] 2^ea) (b[n][k] 2^eb) + bias[n], sums in fp32.
+#include <type_traits>
+
+#include "lds_dma.h"
+#include "mx4.h"
+
+namespace int8t {
+namespace {
+
+typedef int mp_v4i __attribute__((ext_vector_type(4)));
+typedef int mp_v8i __attribute__((ext_vector_type(8)));
+constexpr int kMxFewBytes = 32768;       // codes of few tokens, see mx_few_tokens()
+
+// 32 x 32 sums of 64 products each: a lane has a block of a row (16 bytes), the lanes of the wave's other half another one; byte S of `sa`, `sb` is its scale.
+template <int S>
+__device__ __forceinline__ tk_f16 product32(const mp_v4i& a, const mp_v4i& b, const tk_f16& c, uint32_t sa, uint32_t sb) {
+    const mp_v8i wa = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wb = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wa, wb, c, 4, 4, S, (int)sa, S, (int)sb);
+}
+__device__ __forceinline__ tk_f16 product32_at(int s, const mp_v4i& a, const mp_v4i& b, const tk_f16& c, uint32_t sa, uint32_t sb) {
+    return s == 0 ? product32<0>(a, b, c, sa, sb) : s == 1 ? product32<1>(a, b, c, sa, sb) : s == 2 ? product32<2>(a, b, c, sa, sb) : product32<3>(a, b, c, sa, sb);
+}
+// 16 x 16 sums of 128 products: a quarter of the wave's lanes has a block each
+template <int S>
+__device__ __forceinline__ tk_f4 product16(const uint4& a, const uint4& b, const tk_f4& c, uint32_t sa, uint32_t sb) {
+    const mp_v8i wa = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, wb = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, c, 4, 4, S, (int)sa, S, (int)sb);
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// Output tile of WM x WN waves, each MI x NJ products of 32 x 32; stages of 256 values (128 bytes of a row, whole lines, and a panel of eight scales), NS of them
+// in LDS: while one is multiplied, the next ones are on their way (buffer loads into LDS, rows beyond the operand and bytes beyond the reduction read as zeros).
+// A lane's blocks of a stage are four neighbours (4 half + kk for product kk), so that one word has their scales.
+// SPLIT: the block has a share of the reduction and leaves its sums for mx_reduce_kernel.
+template <int TYPE, int WM, int WN, int MI, int NJ, int NS, bool SPLIT>
+__device__ __forceinline__ void product_body(const MxProductArgs& a, const int mtiles, const int ntiles, const int block) {
+    typedef typename ElemOf<TYPE>::type T;
+    constexpr int KG = 8, NW = WM * WN, BM = WM * MI * 32, BN = WN * NJ * 32, CODES = (BM + BN) * KG, STAGE = CODES + (BM + BN) / 2;      // (in pieces of 16 bytes)
+    constexpr int NLA = BM * KG / 64 / NW, NLB = BN * KG / 64 / NW, NL = NLA + NLB;
+    constexpr int SL = (BM + BN) / 2 / NW;                 // lanes of a wave that load scales, 16 bytes each: the first half of the waves a's, the others b's
+    static_assert((NW & 1) == 0 && BM == BN && SL <= 64, "the swizzle below needs an even wave count, the scales' loads as many rows as columns");
+    extern __shared__ __attribute__((aligned(1024))) uint4 ring[];
+    __shared__ __attribute__((aligned(16))) float cbias[BN];
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wm = wave % WM, wn = wave / WM;
+
+    // Workgroup b runs on XCD b % 8: an XCD takes a run of tiles, four tiles of rows by one of columns at a time, so that the operands that its tiles share
+    // meet in its L2.  SPLIT: the shares of a tile's reduction are tiles of their own.
+    const int total = mtiles * ntiles * (SPLIT ? a.splits : 1), per = (total + 7) >> 3;
+    int tile = (block & 7) * per + (block >> 3), share = 0;
+    if ((block >> 3) >= per || tile >= total) return;
+    if (SPLIT) {
+        share = tile / (mtiles * ntiles);
+        tile -= share * (mtiles * ntiles);
+    }
+    const int group = tile / (4 * ntiles), first = group * 4, height = mtiles - first < 4 ? mtiles - first : 4;
+    const int in = tile - group * 4 * ntiles;
+    const int row0 = (first + in % height) * BM, col0 = (in / height) * BN;
+
+    const int rows = a.M - row0 < BM ? a.M - row0 : BM, cols = a.N - col0 < BN ? a.N - col0 : BN;
+    const int all_steps = (a.Kb + KG * 16 - 1) / (KG * 16);
+    const lds_dma_v4i ra = igd_rsrc(a.a + (size_t)row0 * a.Kb, (uint32_t)rows * (uint32_t)a.Kb);
+    const lds_dma_v4i rb = igd_rsrc(a.b + (size_t)col0 * a.Kb, (uint32_t)cols * (uint32_t)a.Kb);
+    // (two rows a lane; one behind the last is read with it, and not stored)
+    const bool scales_a = wave < NW / 2;
+    const int lines = scales_a ? a.M : a.N, line0 = scales_a ? row0 : col0;
+    const lds_dma_v4i rs = igd_rsrc((scales_a ? a.sa : a.sb) + (size_t)line0 * 8, (uint32_t)(((size_t)all_steps * lines - line0 + 1) * 8));
+    const uint32_t lds_a = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(size_t)(ring + 64 * wave));
+    const uint32_t lds_b = lds_a + BM * KG * 16;
+    const uint32_t lds_s = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(size_t)(ring + CODES + SL * wave));
+    const int sline = ((wave % (NW / 2)) * SL + lane) * 2;
+    const uint32_t sv = line0 + sline < lines ? (uint32_t)sline * 8u : IGD_OOB;
+    // load i of this wave covers RL tile rows from RL (wave + NW i); the lane's granule is the inverse of igd_slot<KG>()
+    constexpr int RL = 64 / KG;
+    const int lrow = lane / KG;
+    const int gran = (lane & 7) ^ (((lrow >> 1) & 3) | ((wave & 1) << 2));
+    const uint32_t voff = (uint32_t)(RL * wave + lrow) * (uint32_t)a.Kb + (uint32_t)gran * 16u;
+    const uint32_t vstep = (uint32_t)(RL * NW) * (uint32_t)a.Kb;
+    const int first_step = SPLIT ? (int)((long long)all_steps * share / a.splits) : 0, nsteps = SPLIT ? (int)((long long)all_steps * (share + 1) / a.splits) - first_step : all_steps;
+    auto load = [&](int buf, int step, int u) __attribute__((always_inline)) {      // the u-th of this wave's NL loads of a stage, with the first its scales
+        const uint32_t boff = (uint32_t)buf * (STAGE * 16u);
+        const int at = (first_step + step) * (KG * 16);
+        const uint32_t past = at + gran * 16 < a.Kb ? 0u : IGD_OOB;      // beyond the reduction
+        const uint32_t k = (uint32_t)__builtin_amdgcn_readfirstlane(at);
+        if (u == 0 && lane < SL) igd_load_lds(rs, lds_s + boff, sv, (uint32_t)__builtin_amdgcn_readfirstlane((first_step + step) * lines * 8));
+        if (u < NLA) igd_load_lds(ra, lds_a + boff + (uint32_t)u * (NW * 1024), (voff + (uint32_t)u * vstep) | past, k);
+        else igd_load_lds(rb, lds_b + boff + (uint32_t)(u - NLA) * (NW * 1024), (voff + (uint32_t)(u - NLA) * vstep) | past, k);
+    };
+
+    for (int c = (int)threadIdx.x; c < BN; c += 64 * NW) cbias[c] = c < cols && a.bias ? a.bias[col0 + c] : 0.0f;
+    tk_f16 acc[MI][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+
+    // Operands of 64 values are read while the 64 before them are multiplied, across the stages too: before a stage's last products every wave has all of the
+    // stage's operands in registers, so behind the barrier that stands there the next stage can be read and this one's place filled again.
+    mp_v4i fa[2][MI], fb[2][NJ];
+    uint32_t ea[NS][MI], eb[NS][NJ];
+    const int half = lane >> 5, l32 = lane & 31;
+    const auto read = [&](const auto slot, int kk) __attribute__((always_inline)) {
+        constexpr int BUF = decltype(slot)::value;
+        const uint4* __restrict__ sA = ring + BUF * STAGE;
+        const uint4* __restrict__ sB = sA + BM * KG;
+        const uint32_t* __restrict__ sS = reinterpret_cast<const uint32_t*>(sA + CODES);
+        const int g = 4 * half + kk;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const int r = (wm * MI + i) * 32 + l32;
+            const uint4 t = sA[igd_slot<KG>(r, g)];
+            fa[kk & 1][i] = mp_v4i{(int)t.x, (int)t.y, (int)t.z, (int)t.w};
+            if (kk == 0) ea[BUF][i] = sS[2 * r + half];
+        }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const int c = (wn * NJ + j) * 32 + l32;
+            const uint4 t = sB[igd_slot<KG>(c, g)];
+            fb[kk & 1][j] = mp_v4i{(int)t.x, (int)t.y, (int)t.z, (int)t.w};
+            if (kk == 0) eb[BUF][j] = sS[2 * (BM + c) + half];
+        }
+    };
+    // (more: the loads of the NS - 2 stages behind the next one are still under way)
+    const auto turn = [&](bool more) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (NS > 2 && more) wait_loads<NS == 2 ? 0 : (NS - 2) * (NL + 1)>();
+        else wait_loads<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // The loads of a stage are dealt out between the products from the barrier on that frees their place, NQ products to a load, so that they
+    // are under way at least a step before they are waited for.
+    constexpr int NP = MI * NJ, NQ = NP * (NS > 2 ? KG / 2 : KG / 2 - 1) / NL > 0 ? NP * (NS > 2 ? KG / 2 : KG / 2 - 1) / NL : 1;
+    static_assert((NL - 1) * NQ < NP * (KG / 2), "all loads of a stage are issued before the next barrier");
+#pragma unroll
+    for (int p = 0; p < NS - 1; ++p)
+#pragma unroll
+        for (int u = 0; u < NL; ++u)
+            if (p < nsteps) load(p, p, u);
+    turn(nsteps >= NS);
+#pragma unroll
+    for (int u = 0; u < NL; ++u)
+        if (u * NQ < NP && NS - 1 < nsteps) load(NS - 1, NS - 1, u);
+    read(std::integral_constant<int, 0>(), 0);
+    const auto stage = [&](const auto slot, int step) __attribute__((always_inline)) {
+        constexpr int BUF = decltype(slot)::value;
+#pragma unroll
+        for (int kk = 0; kk < KG / 2; ++kk) {
+            // from the last group on the loads of NS stages ahead go into this stage's place; they go on through the next stage's other groups
+            const bool last = kk + 1 == KG / 2;
+            if (!last) {
+                read(slot, kk + 1);
+            } else if (step + 1 < nsteps) {
+                turn(step + NS - 1 < nsteps);
+                read(std::integral_constant<int, (BUF + 1) % NS>(), 0);
+            }
+            const int into = last ? BUF : (BUF + NS - 1) % NS, which = last ? step + NS : step + NS - 1;
+            const int done = last ? 0 : (kk + 1) * NP;                      // products since the barrier
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int q = 0; q < NP; ++q) {
+                const int i = q / NJ, j = q % NJ;
+                if ((done + q) % NQ == 0 && (done + q) / NQ < NL && which < nsteps) load(into, which, (done + q) / NQ);
+                acc[i][j] = product32_at(kk, fb[kk & 1][j], fa[kk & 1][i], acc[i][j], eb[BUF][j], ea[BUF][i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    for (int step = 0; step < nsteps; step += NS) {
+        stage(std::integral_constant<int, 0>(), step);
+        if (step + 1 < nsteps) stage(std::integral_constant<int, 1>(), step + 1);
+        if constexpr (NS > 2) {
+            if (step + 2 < nsteps) stage(std::integral_constant<int, 2 % NS>(), step + 2);
+        }
+        if constexpr (NS > 3) {
+            if (step + 3 < nsteps) stage(std::integral_constant<int, 3 % NS>(), step + 3);
+        }
+    }
+
+    if constexpr (SPLIT) {
+        // [share][row][column], columns padded to four
+        const int np = (a.N + 3) & ~3;
+        float* const part = a.part + (size_t)share * a.M * np;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const int m = row0 + (wm * MI + i) * 32 + l32;
+            if (m >= a.M) continue;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = col0 + (wn * NJ + j) * 32 + 8 * q + 4 * half;
+                    if (n < a.N) *reinterpret_cast<float4*>(part + (size_t)m * np + n) = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                }
+        }
+        return;
+    }
+
+    // Results: a lane has four neighbouring columns of a row at a time (the products' rows are b's).  They go through LDS, 32 rows of the
+    // wave at a time in a place of its own, and leave in pieces of 16 bytes, whole cache lines of a row together.
+    __syncthreads();                 // the ring has been read by all
+    constexpr int CW = NJ * 32, ES = (int)sizeof(T), RP = CW * ES + 16, VE = 16 / ES, LPR = CW / VE, RPI = 64 / LPR;
+    static_assert(NW * 32 * RP <= NS * STAGE * 16, "the staged rows fit the ring");
+    unsigned char* const stg = reinterpret_cast<unsigned char*>(ring) + wave * 32 * RP;
+    const int n0 = col0 + wn * CW;
+    const bool wide = ((uintptr_t)a.y & 15) == 0 && (a.pitch * ES & 15) == 0;
+    T* const y = static_cast<T*>(a.y);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int m0 = row0 + (wm * MI + i) * 32;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = j * 32 + 8 * q + 4 * half;
+                typedef T V4 __attribute__((ext_vector_type(4)));
+                V4 o;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) o[u] = (T)__fadd_rn(acc[i][j][4 * q + u], cbias[wn * CW + c + u]);
+                *reinterpret_cast<V4*>(stg + l32 * RP + c * ES) = o;
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the wave's own place: no other wave reads or writes it)
+        const int pc = lane % LPR * VE, pr = lane / LPR;
+#pragma unroll
+        for (int p = 0; p < 32 / RPI; ++p) {
+            const int r = m0 + p * RPI + pr, n = n0 + pc;
+            typedef T VE_ __attribute__((ext_vector_type(VE)));
+            const VE_ t = *reinterpret_cast<const VE_*>(stg + (p * RPI + pr) * RP + pc * ES);
+            if (r >= a.M) continue;
+            T* const to = y + (size_t)r * a.pitch + n;
+            if (wide && n + VE <= a.N) {
+                *reinterpret_cast<VE_*>(to) = t;
+            } else {
+#pragma unroll
+                for (int u = 0; u < VE; ++u)
+                    if (n + u < a.N) to[u] = t[u];
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+}
+
+// One product, or two whose blocks from `first` (a multiple of eight) on have the second one's tiles.
+template <int TYPE, int WM, int WN, int MI, int NJ, int NS, bool SPLIT>
+__global__ __launch_bounds__(64 * WM * WN) void mx_product_kernel(const MxProductArgs a, const MxProductArgs b, const int first) {
+    constexpr int BM = WM * MI * 32, BN = WN * NJ * 32;
+    const bool second = (int)blockIdx.x >= first;
+    const MxProductArgs p = second ? b : a;
+    product_body<TYPE, WM, WN, MI, NJ, NS, SPLIT>(p, (p.M + BM - 1) / BM, (p.N + BN - 1) / BN, (int)blockIdx.x - (second ? first : 0));
+}
+
+// ------------------------------------------------------------------------------------------------
+// Few tokens (at most 16) through weights that are laid out: one launch, codes of the tokens included.  Every block makes them for itself in LDS -- the tokens are
+// small and come from the caches -- and multiplies them with 16 channels at a time: a wave has an eighth of the reduction's panels, loads two blocks of 16 weight
+// rows per lane straight into the products' operands (16 x 16 x 128), and the eight sums meet in LDS.  The first channels' weights are on their way while the
+// codes are made.
+// ------------------------------------------------------------------------------------------------
+constexpr int XW = 8;            // waves
+constexpr int XL = 4;            // panels of a lane's weights in flight
+__host__ __device__ constexpr int few_pitch(int Kb) { return ((Kb + 127) & ~127) + 16; }       // rows of codes 16 bytes apart modulo the banks
+__host__ __device__ constexpr int few_lds(int M, int Kb) { return M * few_pitch(Kb) + M * ((Kb + 127) / 128 * 8); }
+template <int TYPE>
+__global__ __launch_bounds__(64 * XW, 4) void mx_few_kernel(const MxFewArgs a) {
+    typedef typename ElemOf<TYPE>::type T;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t codes[];      // [M][few_pitch], scales [M][8 panels]
+    __shared__ __attribute__((aligned(16))) float sums[XW][4][64];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n16 = lane & 15, kg = lane >> 4;
+    const int pitch = few_pitch(a.Kb), panels = (a.Kb + 127) >> 7, spitch = panels * 8;
+    uint8_t* const scales = codes + a.M * pitch;
+    // this wave's part of the reduction: whole panels
+    const int p_from = panels * wave / XW, p_to = panels * (wave + 1) / XW;
+    const int tiles = (a.N + 15) >> 4;
+
+    uint4 w[XL][2];
+    uint32_t sw[XL];
+    auto fetch = [&](int tile, int p0) __attribute__((always_inline)) {
+        const int n = min(tile * 16 + n16, a.N - 1);
+        const uint8_t* const row = a.wq + (size_t)n * a.Kb;
+#pragma unroll
+        for (int i = 0; i < XL; ++i) {
+            sw[i] = 0u;
+            if (p0 + i < p_to) sw[i] = *reinterpret_cast<const uint16_t*>(a.sw + ((size_t)(p0 + i) * a.N + n) * 8 + 2 * kg);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = (p0 + i) * 128 + kg * 32 + h * 16;
+                w[i][h] = make_uint4(0u, 0u, 0u, 0u);
+                if (p0 + i < p_to && k < a.Kb) w[i][h] = *reinterpret_cast<const uint4*>(row + k);
+            }
+        }
+    };
+    int tile = (int)blockIdx.x;
+    fetch(tile, p_from);
+
+    // the tokens' codes: four neighbouring lanes a block, in whole panels
+    {
+        const T* const x = static_cast<const T*>(a.x);
+        const int groups = panels * 32, all = a.M * groups;
+        for (int t = tid; t < all; t += 64 * XW) {          // (groups, and with it each step's end, are multiples of four lanes)
+            const int m = t / groups, g = t - m * groups;
+            float v[8];
+            load8<TYPE>(x + (size_t)m * a.x_pitch + 8 * g, a.K - 8 * g, a.wide, v);
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = most(top, fabsf(v[i]));
+            top = most(top, dpp_of<kDppSwap1>(top));
+            top = most(top, dpp_of<kDppSwap2>(top));
+            const uint32_t byte = mx_byte_of(top);
+            *reinterpret_cast<uint32_t*>(codes + m * pitch + 4 * g) = byte < 255u ? mx_codes8(v, mx_power(byte)) : 0u;
+            if ((g & 3) == 0) scales[m * spitch + (g >> 2)] = (uint8_t)byte;
+        }
+    }
+    __syncthreads();
+
+    // (columns of tokens that there are not: not stored)
+    const uint8_t* const mine = codes + (n16 < a.M ? n16 : 0) * pitch + kg * 32;
+    const uint8_t* const mine_s = scales + (n16 < a.M ? n16 : 0) * spitch + 2 * kg;
+    for (;;) {
+        tk_f4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int p0 = p_from; p0 < p_to; p0 += XL) {
+            if (p0 > p_from) fetch(tile, p0);
+#pragma unroll
+            for (int i = 0; i < XL; ++i) {
+                if (p0 + i >= p_to) break;
+                const int p = p0 + i;
+                const uint32_t sx = *reinterpret_cast<const uint16_t*>(mine_s + p * 8);
+                const uint4 t0 = *reinterpret_cast<const uint4*>(mine + p * 128), t1 = *reinterpret_cast<const uint4*>(mine + p * 128 + 16);
+                acc = product16<0>(w[i][0], t0, acc, sw[i], sx);
+                acc = product16<1>(w[i][1], t1, acc, sw[i], sx);
+            }
+        }
+        const int next = tile + (int)gridDim.x;
+        if (next < tiles) fetch(next, p_from);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[wave][r][lane] = acc[r];
+        __syncthreads();
+        if (tid < 256) {
+            // channel 4 (lane / 16) + r of token lane % 16: neighbouring threads take neighbouring channels
+            const int n = tile * 16 + (tid & 15), m = tid >> 4, at = ((tid & 15) >> 2) * 16 + m, r = tid & 3;
+            float s = sums[0][r][at];
+#pragma unroll
+            for (int i = 1; i < XW; ++i) s += sums[i][r][at];
+            if (n < a.N && m < a.M) {
+                if (a.bias) s = __fadd_rn(s, a.bias[n]);
+                static_cast<T*>(a.y)[(size_t)m * a.y_pitch + n] = (T)s;
+            }
+        }
+        if (next >= tiles) break;
+        tile = next;
+        __syncthreads();
+    }
+}
+
+// Sums of the shares, bias: four neighbouring results a lane
+template <int TYPE>
+__global__ __launch_bounds__(256) void mx_reduce_kernel(const MxProductArgs a) {
+    typedef typename ElemOf<TYPE>::type T;
+    const int np = (a.N + 3) & ~3, quads = np >> 2;
+    const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= (size_t)a.M * quads) return;
+    const int m = (int)(at / quads), n = (int)(at - (size_t)m * quads) * 4;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < a.splits; ++p) {
+        const float4 t = *reinterpret_cast<const float4*>(a.part + ((size_t)p * a.M + m) * np + n);
+        v[0] += t.x;
+        v[1] += t.y;
+        v[2] += t.z;
+        v[3] += t.w;
+    }
+    T* const y = static_cast<T*>(a.y) + (size_t)m * a.pitch;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        if (n + u < a.N) y[n + u] = (T)(a.bias ? __fadd_rn(v[u], a.bias[n + u]) : v[u]);
+}
+
+template <int TYPE, int WM, int WN, int MI, int NJ, int NS, bool SPLIT>
+hipError_t product_split(const MxProductArgs& a, const MxProductArgs* b, hipStream_t st) {
+    constexpr int BM = WM * MI * 32, BN = WN * NJ * 32, LDS = NS * (BM + BN) * (128 + 8);
+    static std::atomic<unsigned long long> done{0};
+    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&mx_product_kernel<TYPE, WM, WN, MI, NJ, NS, SPLIT>), LDS, done);
+    if (e != hipSuccess) return e;
+    const auto blocks = [](const MxProductArgs& p) {
+        return (unsigned)((((size_t)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * (SPLIT ? p.splits : 1) + 7) / 8) * 8);
+    };
+    const unsigned first = blocks(a);
+    {
+        KernelTimer kt(KID_MX_PRODUCT, st);
+        launch_timed(kt, (mx_product_kernel<TYPE, WM, WN, MI, NJ, NS, SPLIT>), dim3(first + (b ? blocks(*b) : 0u)), dim3(64 * WM * WN), LDS, st, a, b ? *b : a, (int)first);
+    }
+    if (SPLIT) {
+        KernelTimer kt(KID_MX_REDUCE, st);
+        launch_timed(kt, mx_reduce_kernel<TYPE>, dim3((unsigned)(((size_t)a.M * ((a.N + 3) / 4) + 255) / 256)), dim3(256), 0, st, a);
+    }
+    return hipGetLastError();
+}
+template <int TYPE, int WM, int WN, int MI, int NJ, int NS>
+hipError_t product_of(const MxProductArgs& a, const MxProductArgs* b, hipStream_t st) {
+    return a.splits > 1 ? product_split<TYPE, WM, WN, MI, NJ, NS, true>(a, nullptr, st) : product_split<TYPE, WM, WN, MI, NJ, NS, false>(a, b, st);
+}
+
+// Tiles and shares of the reduction by an estimate, us: rounds of blocks times stages of 256 values, plus what a block and the joining pass cost.  occ: blocks on
+// a compute unit; busy: of its matrix units per stage; least: a stage of a block alone.
+struct ProductPlan {
+    int tile, splits;          // 0: 256 x 256, 1: 128 x 128, 2: the same with three stages, 3: 64 x 64 with four
+};
+ProductPlan product_plan(int M, int N, int Kb, bool scratch) {
+    static const struct { int bm, occ; double busy, least, fixed; } kTiles[4] = {{256, 1, 1.63, 1.63, 10.0}, {128, 2, 0.57, 0.85, 4.0}, {128, 1, 0.66, 0.66, 4.5}, {64, 2, 0.22, 0.26, 2.5}};
+    const int steps = (Kb + 127) >> 7;
+    ProductPlan best{0, 1};
+    double least = 1e30;
+    for (int t = 0; t < 4; ++t) {
+        const long long tiles = (long long)((M + kTiles[t].bm - 1) / kTiles[t].bm) * ((N + kTiles[t].bm - 1) / kTiles[t].bm);
+        for (int s = 1; s <= (scratch ? 16 : 1) && s <= steps; s *= 2) {
+            const long long blocks = tiles * s, slots = 256ll * kTiles[t].occ;
+            if (s > 1 && (tiles * s > 1024 || (size_t)M * N * s > (1u << 26))) break;
+            const double together = blocks >= slots ? kTiles[t].occ : (double)((blocks + 255) / 256);
+            const double stage = together * kTiles[t].busy > kTiles[t].least ? together * kTiles[t].busy : kTiles[t].least;
+            double us = (double)((blocks + slots - 1) / slots) * ((steps + s - 1) / s * stage + kTiles[t].fixed);
+            if (s > 1) us += 3.5 + 8e-6 * (double)s * M * N / 4;
+            if (us < least) {
+                least = us;
+                best = ProductPlan{t, s};
+            }
+        }
+    }
+    return best;
+}
+
+template <int TYPE>
+hipError_t product_type(const MxProductArgs& a, const MxProductArgs* b, int tile, hipStream_t st) {
+    return tile == 0 ? product_of<TYPE, 2, 4, 4, 2, 2>(a, b, st) : tile == 1 ? product_of<TYPE, 2, 2, 2, 2, 2>(a, b, st)
+           : tile == 2 ? product_of<TYPE, 2, 2, 2, 2, 3>(a, b, st) : product_of<TYPE, 2, 2, 1, 1, 4>(a, b, st);
+}
+hipError_t product_launch(const MxProductArgs& a, const MxProductArgs* b, int tile, hipStream_t st) {
+    if (a.type == kF32) return product_type<kF32>(a, b, tile, st);
+    if (a.type == kBF16) return product_type<kBF16>(a, b, tile, st);
+    return product_type<kF16>(a, b, tile, st);
+}
+// the plan of a product, with shares only where their scratch is there
+int planned(MxProductArgs* a, size_t scratch_bytes) {
+    const size_t need = mx_product_scratch(a->M, a->N, a->Kb);
+    const ProductPlan p = product_plan(a->M, a->N, a->Kb, need > 0 && a->part && scratch_bytes >= need);
+    a->splits = p.splits;
+    return p.tile;
+}
+
+template <int TYPE>
+hipError_t few_of(const MxFewArgs& a, hipStream_t st) {
+    static_assert(kMxFewBytes + 16 * (127 + 16) + (kMxFewBytes + 16 * 127) / 16 + 8 * 1024 <= 64 * 1024, "the codes fit what a launch may ask for");
+    const int tiles = (a.N + 15) / 16;
+    KernelTimer kt(KID_MX_FEW, st);
+    launch_timed(kt, mx_few_kernel<TYPE>, dim3(tiles < 512 ? tiles : 512), dim3(64 * XW), (size_t)few_lds(a.M, a.Kb), st, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Up to so many codes every block makes them for itself: a launch less.
+bool mx_few_tokens(int M, int Kb) { return M <= 16 && M * (long long)Kb <= kMxFewBytes; }
+hipError_t launch_mx_few_tokens(const MxFewArgs& a, hipStream_t st) {
+    if (a.type == kF32) return few_of<kF32>(a, st);
+    if (a.type == kBF16) return few_of<kBF16>(a, st);
+    return few_of<kF16>(a, st);
+}
+
+constexpr int kTileRows[4] = {256, 128, 128, 64}, kTileWaves[4] = {8, 4, 4, 4}, kTileStages[4] = {2, 2, 3, 4};
+bool mx_product_fits(int M, int N, int Kb) {
+    for (const bool scratch : {false, true}) {
+        const ProductPlan p = product_plan(M, N, Kb, scratch);
+        const int rows = kTileRows[p.tile];
+        const unsigned long long blocks = ((unsigned long long)M + rows - 1) / rows * (((unsigned long long)N + rows - 1) / rows) * p.splits;
+        if ((blocks + 8) * 64 * kTileWaves[p.tile] >= 1ull << 32) return false;
+    }
+    return true;
+}
+void mx_product_division(int M, int N, int Kb, size_t scratch_bytes, int* rows, int* waves, int* stages, int* shares) {
+    MxProductArgs a{};
+    float there = 0;
+    a.M = M; a.N = N; a.Kb = Kb; a.part = scratch_bytes ? &there : nullptr;
+    const int tile = planned(&a, scratch_bytes);
+    *rows = kTileRows[tile];
+    *waves = kTileWaves[tile];
+    *stages = kTileStages[tile];
+    *shares = a.splits;
+}
+size_t mx_product_scratch(int M, int N, int Kb) {
+    const ProductPlan p = product_plan(M, N, Kb, true);
+    return p.splits > 1 ? (size_t)p.splits * M * ((N + 3) & ~3) * sizeof(float) : 0;
+}
+hipError_t launch_mx_product(MxProductArgs a, size_t scratch_bytes, hipStream_t st) {
+    const int tile = planned(&a, scratch_bytes);
+    return product_launch(a, nullptr, tile, st);
+}
+hipError_t launch_mx_products(MxProductArgs a, MxProductArgs b, size_t scratch_bytes, hipStream_t st) {
+    const int ta = planned(&a, scratch_bytes), tb = planned(&b, scratch_bytes);
+    if (ta == tb && a.type == b.type && a.splits == 1 && b.splits == 1) return product_launch(a, &b, ta, st);
+    const hipError_t e = product_launch(a, nullptr, ta, st);
+    return e != hipSuccess ? e : product_launch(b, nullptr, tb, st);
+}
+
+}  // namespace int8t

@@ -48,6 +48,15 @@ enum KernelId : int {
     KID_CACHE_READ,
     KID_ATTEND,
     KID_ATTEND_JOIN,
+    KID_MX_QUANTIZE,
+    KID_MX_PRODUCT,
+    KID_MX_REDUCE,
+    KID_MX_FEW,
+    KID_MX_CACHE_WRITE,
+    KID_MX_CACHE_READ,
+    KID_MX_ATTEND,
+    KID_ROTATE,
+    KID_PAGES,
     KID_COUNT
 };
 

@@ -29,7 +29,8 @@ const char* const kNames[KID_COUNT] = {
     "band_kernel",         "band_reg_kernel",     "wgrad_kernel",        "wgrad_lines_kernel", "wgrad_reduce_kernel",    "s2d_repack_kernel", "conv_trio_kernel", "dw_conv_kernel",
     "dw_wgrad_kernel",     "dw_wgrad_reduce_kernel", "dw_trio_kernel", "infer_1x1_kernel", "conv_band_trio_kernel",
     "quantize_rows_kernel", "quantize_cols_kernel", "transpose_codes_kernel", "product_kernel", "product_reduce_kernel", "few_tokens_kernel", "cache_write_kernel",
-    "cache_read_kernel",   "attend_kernel",       "attend_join_kernel"};
+    "cache_read_kernel",   "attend_kernel",       "attend_join_kernel",  "mx4_quantize_kernel", "mx4_product_kernel",  "mx4_reduce_kernel",   "mx4_few_kernel",   "mx4_cache_write_kernel",
+    "mx4_cache_read_kernel", "mx4_attend_kernel", "rotate_kernel",       "pages_kernel"};
 
 void drop_all() {
     for (Rec& r : g_recs) {

@@ -1,5 +1,6 @@
 // C ABI of the token operators (see include/int8t.h): argument checks, scratch, the order of the launches.
 #include "../../include/int8t.h"
+#include "token_api.h"
 #include "tokens.h"
 
 using namespace int8t;
@@ -107,19 +108,28 @@ CacheArgs cache_args(const int8t_cache* c) {
 
 int8t_status attend_ok(const int8t_cache* c, const int8t_attend_desc* d) {
     const int8t_status s = cache_ok(c);
-    if (s != INT8T_OK) return s;
+    return s != INT8T_OK ? s : attend_desc_ok(d, c->heads, c->page_size);
+}
+
+}  // namespace
+
+// ---- attention over either cache -----------------------------------------------------------------
+namespace int8t {
+
+int8t_status attend_desc_ok(const int8t_attend_desc* d, int heads, int page_size) {
     if (!d) return INT8T_ERR_NULL;
     if (!type_ok(d->type) || (d->causal != 0 && d->causal != 1) || !(d->scale - d->scale == 0.0f)) return INT8T_ERR_ARG;
     if (d->tokens < 0 || d->requests < 0 || d->group <= 0 || d->table_width < 0 || d->longest < 0) return INT8T_ERR_SHAPE;
-    if ((unsigned long long)d->tokens * (unsigned long long)c->heads * (unsigned long long)d->group > 0x7fffffffull) return INT8T_ERR_SHAPE;
+    if ((unsigned long long)d->tokens * (unsigned long long)heads * (unsigned long long)d->group > 0x7fffffffull) return INT8T_ERR_SHAPE;
     if ((unsigned long long)d->tokens * (unsigned long long)d->group / 16 + (unsigned long long)d->requests > 0x7fffffull) return INT8T_ERR_SHAPE;
-    if (((unsigned long long)d->tokens * (unsigned long long)d->group / 16 + (unsigned long long)d->requests) * (unsigned long long)c->heads > 0x7fffffffull) return INT8T_ERR_SHAPE;
-    if ((long long)d->table_width * c->page_size > kMostKeys || d->table_pitch < (size_t)d->table_width) return INT8T_ERR_SHAPE;
+    if (((unsigned long long)d->tokens * (unsigned long long)d->group / 16 + (unsigned long long)d->requests) * (unsigned long long)heads > 0x7fffffffull) return INT8T_ERR_SHAPE;
+    if ((long long)d->table_width * page_size > kMostKeys || d->table_pitch < (size_t)d->table_width) return INT8T_ERR_SHAPE;
     return INT8T_OK;
 }
-AttendArgs attend_args(const int8t_cache* c, const int8t_attend_desc* d) {
+AttendArgs attend_args(const CacheArgs& c, const int8t_attend_desc* d, int mx) {
     AttendArgs a{};
-    a.c = cache_args(c);
+    a.c = c;
+    a.mx = mx;
     a.q_token = d->q_token_pitch;
     a.q_head = d->q_head_pitch;
     a.table_pitch = d->table_pitch;
@@ -127,12 +137,12 @@ AttendArgs attend_args(const int8t_cache* c, const int8t_attend_desc* d) {
     a.requests = d->requests;
     a.group = d->group;
     a.by_group = fast_div((unsigned)d->group);
-    a.by_heads = fast_div((unsigned)c->heads);
+    a.by_heads = fast_div((unsigned)c.heads);
     a.width = d->table_width;
     a.type = d->type;
     a.causal = d->causal;
     a.scale = d->scale;
-    const int most = d->table_width * c->page_size;
+    const int most = d->table_width * c.page_size;
     a.splits = 1;
     if (d->tokens && d->requests) attend_plan(&a, d->longest > 0 && d->longest < most ? d->longest : most);
     return a;
@@ -143,7 +153,31 @@ size_t attend_bytes(const AttendArgs& a) {
     return align256(rows * a.c.dim * sizeof(float)) + align256(2 * rows * sizeof(float));
 }
 
-}  // namespace
+int8t_status attend_call(AttendArgs a, const int8t_attend_desc* desc, const void* q_dev, const int* starts_dev, const int* lengths_dev, const int* table_dev, void* out_dev,
+                         float* lse_dev, void* ws_dev, size_t ws_bytes, void* stream) {
+    if (desc->tokens == 0) return INT8T_OK;
+    if (desc->requests == 0) return INT8T_ERR_SHAPE;
+    if (!q_dev || !starts_dev || !lengths_dev || (!table_dev && desc->table_width > 0) || !out_dev) return INT8T_ERR_NULL;
+    const size_t e = bytes_of(desc->type);
+    if (!aligned(q_dev, e) || !aligned(starts_dev, 4) || !aligned(lengths_dev, 4) || !aligned(table_dev, 4) || !aligned16(out_dev) || !aligned(lse_dev, 4) ||
+        !aligned16(ws_dev))
+        return INT8T_ERR_ARG;
+    const size_t need = attend_bytes(a);
+    if (need > 0 && !ws_dev) return INT8T_ERR_NULL;
+    if (ws_bytes < need) return INT8T_ERR_WORKSPACE;
+    a.q = q_dev;
+    a.starts = starts_dev;
+    a.lengths = lengths_dev;
+    a.table = table_dev;
+    a.out = out_dev;
+    a.lse = lse_dev;
+    a.wide_q = (((uintptr_t)q_dev | (desc->q_token_pitch | desc->q_head_pitch) * e) & 15) == 0;
+    a.part_o = static_cast<float*>(ws_dev);
+    a.part_ml = a.part_o ? a.part_o + align256((size_t)a.splits * a.tokens * a.c.heads * a.group * a.c.dim * sizeof(float)) / sizeof(float) : nullptr;
+    return launched(launch_attend(a, (hipStream_t)stream));
+}
+
+}  // namespace int8t
 
 extern "C" int8t_status int8t_quantize_rows(const void* x_dev, int8t_dtype type, int rows, int cols, size_t pitch, const float* factor_dev, int8t_round mode,
                                             uint64_t seed, int8_t* q_dev, float* scale_dev, void* stream) {
@@ -305,7 +339,7 @@ extern "C" int8t_status int8t_cache_read(const int8t_cache* cache, const int64_t
 }
 
 extern "C" size_t int8t_cache_attend_workspace_bytes(const int8t_cache* cache, const int8t_attend_desc* desc) {
-    return attend_ok(cache, desc) == INT8T_OK ? attend_bytes(attend_args(cache, desc)) : 0;
+    return attend_ok(cache, desc) == INT8T_OK ? attend_bytes(attend_args(cache_args(cache), desc, 0)) : 0;
 }
 
 extern "C" int8t_status int8t_cache_attend(const int8t_cache* cache, const int8t_attend_desc* desc, const void* q_dev, const int* starts_dev,
@@ -313,27 +347,7 @@ extern "C" int8t_status int8t_cache_attend(const int8t_cache* cache, const int8t
                                            void* stream) {
     const int8t_status ok = attend_ok(cache, desc);
     if (ok != INT8T_OK) return ok;
-    if (desc->tokens == 0) return INT8T_OK;
-    if (desc->requests == 0) return INT8T_ERR_SHAPE;
-    if (!q_dev || !starts_dev || !lengths_dev || (!table_dev && desc->table_width > 0) || !out_dev) return INT8T_ERR_NULL;
-    const size_t e = bytes_of(desc->type);
-    if (!aligned(q_dev, e) || !aligned(starts_dev, 4) || !aligned(lengths_dev, 4) || !aligned(table_dev, 4) || !aligned16(out_dev) || !aligned(lse_dev, 4) ||
-        !aligned16(ws_dev))
-        return INT8T_ERR_ARG;
-    AttendArgs a = attend_args(cache, desc);
-    const size_t need = attend_bytes(a);
-    if (need > 0 && !ws_dev) return INT8T_ERR_NULL;
-    if (ws_bytes < need) return INT8T_ERR_WORKSPACE;
-    a.q = q_dev;
-    a.starts = starts_dev;
-    a.lengths = lengths_dev;
-    a.table = table_dev;
-    a.out = out_dev;
-    a.lse = lse_dev;
-    a.wide_q = (((uintptr_t)q_dev | (desc->q_token_pitch | desc->q_head_pitch) * e) & 15) == 0;
-    a.part_o = static_cast<float*>(ws_dev);
-    a.part_ml = a.part_o ? a.part_o + align256((size_t)a.splits * a.tokens * a.c.heads * a.group * a.c.dim * sizeof(float)) / sizeof(float) : nullptr;
-    return launched(launch_attend(a, (hipStream_t)stream));
+    return attend_call(attend_args(cache_args(cache), desc, 0), desc, q_dev, starts_dev, lengths_dev, table_dev, out_dev, lse_dev, ws_dev, ws_bytes, stream);
 }
 
 extern "C" int8t_status int8t_product_division(int M, int N, int K, size_t ws_bytes, int8t_division* out) {
@@ -348,7 +362,7 @@ extern "C" int8t_status int8t_cache_attend_division(const int8t_cache* cache, co
     if (ok != INT8T_OK) return ok;
     if (!out) return INT8T_ERR_NULL;
     if (desc->tokens == 0 || desc->requests == 0) return INT8T_ERR_SHAPE;
-    const AttendArgs a = attend_args(cache, desc);
+    const AttendArgs a = attend_args(cache_args(cache), desc, 0);
     *out = int8t_division{a.rows, a.waves, 0, a.splits};
     return INT8T_OK;
 }

@@ -430,6 +430,9 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
     if (a.rows > 16) {
         const hipError_t e = launch_attend_chunk(a, st);
         if (e != hipSuccess) return e;
+    } else if (a.mx) {
+        const hipError_t e = launch_mx_attend_rows(a, st);
+        if (e != hipSuccess) return e;
     } else {
         const bool uni = a.c.page_size % 16 == 0;
         const hipError_t e = a.waves == 8 ? (uni ? rows_of<TYPE, true, 8>(a, st) : rows_of<TYPE, false, 8>(a, st))

@@ -12,6 +12,7 @@
 // (DIM 128), and arithmetic of one wave and products of another overlap by half only (fma 295 us, products 322, together 466).  Two chunks of 2048 tokens over 8192 keys, 32 heads of 128 on 8, bf16:
 // 603 to 615 us (478 GFLOP: 0.8 PFLOP/s; a large library product in fp16 1.18), in 55 % of whose cycles a SIMD issues vector instructions and in 32 % has a product: 88 %
 // together; LDS 12 %.
+#include "mx4.h"
 #include "token_attend.h"
 
 namespace int8t {
@@ -34,8 +35,23 @@ constexpr int key_tiles(int NW) { return takes_turns(NW) ? 3 : 2; }
 constexpr int value_tiles(int DIM, int NW) { return takes_turns(NW) ? 4 : DIM == 256 ? 2 : 3; }
 constexpr int chunk_lds(int DIM, int NW) { return (key_tiles(NW) + value_tiles(DIM, NW)) * TK * DIM * 2 + 3 * 3 * TK * 4; }
 
+// MX: keys and values are microscaled 4-bit codes (mx4.h).  A block's codes become fp16 times a power of two relative to its row's largest scale, which is then
+// the row's: what is above stays as it is.  Blocks 2^36 below the row's largest lose bits, 2^39 below they are zeros.
+template <bool MX> struct Piece { typedef uint4 codes; typedef float scale; };
+template <> struct Piece<true> { typedef uint2 codes; typedef uint32_t scale; };
+constexpr int kMxUp = 13;       // 6 2^13 is in fp16's range
+// The largest of the DIM / 16 neighbouring lanes that have a key
+template <int DIM>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+    v = max(v, (uint32_t)dpp_word<kDppSwap1>((int)v));
+    v = max(v, (uint32_t)dpp_word<kDppSwap2>((int)v));
+    if (DIM >= 128) v = max(v, (uint32_t)dpp_word<0x141>((int)v));      // (row_half_mirror: the quads of eight lanes)
+    if (DIM >= 256) v = max(v, (uint32_t)dpp_word<kDppRor8>((int)v));
+    return v;
+}
+
 // UNI: the keys whose pieces a wave loads at a time lie on one page (its size is a multiple of 1024 / DIM): addresses are scalar.
-template <int TYPE, int DIM, int NW, bool UNI>
+template <int TYPE, int DIM, int NW, bool UNI, bool MX>
 __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && TYPE == kF32)) ? 1 : 2) void attend_chunk_kernel(const AttendArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int PARTS = TYPE == kF32 ? 2 : 1, NT = 64 * NW, ROWS = 32 * NW;
@@ -110,8 +126,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
 
     // ---- loader: this thread's pieces, piece p is 16 dims of a key; a wave's are those of KW neighbouring keys
     constexpr int KW = 1024 / DIM;
-    uint4 rk[NP], rv[NP];
-    float rks[NP], rvs[NP];
+    typename Piece<MX>::codes rk[NP], rv[NP];
+    typename Piece<MX>::scale rks[NP], rvs[NP];
     bool rok[NP];
     int ids[NP], ins[NP];                                      // pages, and places on them, of the keys that are loaded next
     const int d16 = (tid % (DIM / 16)) * 16, dc = d16 < D ? d16 : 0;              // (beyond D: q is zero there, and nothing is stored)
@@ -126,7 +142,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
         }
     };
     const size_t page_rows = (size_t)a.c.heads * a.c.page_size, head_rows = (size_t)head * a.c.page_size;
-    const uint32_t code_at = UNI ? (uint32_t)((key0 - wkey0) * D + dc) : (uint32_t)dc, scale_at = UNI ? (uint32_t)(key0 - wkey0) : 0u;      // from a wave's (a key's) place on
+    const int row_scales = MX ? mx_blocks(D) : 1, row_bytes = MX ? 16 * row_scales : D;      // of a key
+    const uint32_t code_at = (uint32_t)(MX ? dc / 2 : dc) + (UNI ? (uint32_t)((key0 - wkey0) * row_bytes) : 0u);                  // from a wave's (a key's) place on
+    const uint32_t scale_at = (uint32_t)(MX ? dc / 32 : 0) + (UNI ? (uint32_t)((key0 - wkey0) * row_scales) : 0u);
+    typedef typename Piece<MX>::codes Codes;
     auto fetch = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
@@ -136,18 +155,35 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
                 id = __builtin_amdgcn_readfirstlane(id);
                 in = __builtin_amdgcn_readfirstlane(in);
             }
-            const size_t place = (size_t)id * page_rows + (head_rows + in), codes = place * D;
+            const size_t place = (size_t)id * page_rows + (head_rows + in), codes = place * row_bytes;
             rok[p] = ok && t * TK + key_of(p) < end;
-            rk[p] = *reinterpret_cast<const uint4*>(a.c.kq + codes + code_at);
-            rks[p] = (a.c.ks + place)[scale_at];
-            rv[p] = *reinterpret_cast<const uint4*>(a.c.vq + codes + code_at);
-            rvs[p] = (a.c.vs + place)[scale_at];
+            rk[p] = *reinterpret_cast<const Codes*>(a.c.kq + codes + code_at);
+            rv[p] = *reinterpret_cast<const Codes*>(a.c.vq + codes + code_at);
+            if constexpr (MX) {
+                rks[p] = (reinterpret_cast<const uint8_t*>(a.c.ks) + place * row_scales)[scale_at];
+                rvs[p] = (reinterpret_cast<const uint8_t*>(a.c.vs) + place * row_scales)[scale_at];
+            } else {
+                rks[p] = (a.c.ks + place)[scale_at];
+                rvs[p] = (a.c.vs + place)[scale_at];
+            }
         }
     };
-    auto expand = [](const uint4& c, uint4* lo, uint4* hi) __attribute__((always_inline)) {
-        const uint32_t w[4] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u, c.z ^ 0x80808080u, c.w ^ 0x80808080u};
-        *lo = make_uint4(codes_f16<kLowPair>(w[0]), codes_f16<kHighPair>(w[0]), codes_f16<kLowPair>(w[1]), codes_f16<kHighPair>(w[1]));
-        *hi = make_uint4(codes_f16<kLowPair>(w[2]), codes_f16<kHighPair>(w[2]), codes_f16<kLowPair>(w[3]), codes_f16<kHighPair>(w[3]));
+    // 16 codes as fp16; `row`: the row's scale
+    auto expand = [](const auto& c, const auto& scale, uint4* lo, uint4* hi, float* row) __attribute__((always_inline)) {
+        if constexpr (MX) {
+            const uint32_t top = lanes_max<DIM>(scale);
+            const float up = __uint_as_float((uint32_t)max(127 + kMxUp - (int)(top - scale), 0) << 23);
+            *row = top == 255u ? NAN : __uint_as_float((uint32_t)max((int)top - kMxUp, 0) << 23);
+            const auto pair = [up](uint32_t w, auto sel) __attribute__((always_inline)) { return as_u32(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, up, decltype(sel)::value)); };
+            typedef std::integral_constant<int, 0> B0; typedef std::integral_constant<int, 1> B1; typedef std::integral_constant<int, 2> B2; typedef std::integral_constant<int, 3> B3;
+            *lo = make_uint4(pair(c.x, B0()), pair(c.x, B1()), pair(c.x, B2()), pair(c.x, B3()));
+            *hi = make_uint4(pair(c.y, B0()), pair(c.y, B1()), pair(c.y, B2()), pair(c.y, B3()));
+        } else {
+            *row = scale;
+            const uint32_t w[4] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u, c.z ^ 0x80808080u, c.w ^ 0x80808080u};
+            *lo = make_uint4(codes_f16<kLowPair>(w[0]), codes_f16<kHighPair>(w[0]), codes_f16<kLowPair>(w[1]), codes_f16<kHighPair>(w[1]));
+            *hi = make_uint4(codes_f16<kLowPair>(w[2]), codes_f16<kHighPair>(w[2]), codes_f16<kLowPair>(w[3]), codes_f16<kHighPair>(w[3]));
+        }
     };
     auto stage = [&](int kslot, int vslot, int sslot) __attribute__((always_inline)) {
 #pragma unroll
@@ -155,15 +191,16 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
             const int key = key_of(p), g = d16 >> 3;
             uint4 lo, hi;
             float* const s = sc + sslot * 3 * TK;
-            expand(rk[p], &lo, &hi);
+            float ks, vs;
+            expand(rk[p], rks[p], &lo, &hi, &ks);
             sk[kslot * TILE + k_slot<DIM>(key, g)] = lo;
             sk[kslot * TILE + k_slot<DIM>(key, g + 1)] = hi;
-            expand(rv[p], &lo, &hi);
+            expand(rv[p], rvs[p], &lo, &hi, &vs);
             sv[vslot * TILE + v_slot<DIM>(key, g)] = lo;
             sv[vslot * TILE + v_slot<DIM>(key, g + 1)] = hi;
             if (g == 0) {
-                s[key] = rok[p] ? rks[p] : 0.0f;
-                s[TK + key] = rok[p] ? rvs[p] : 0.0f;
+                s[key] = rok[p] ? ks : 0.0f;
+                s[TK + key] = rok[p] ? vs : 0.0f;
                 s[2 * TK + key] = rok[p] ? 0.0f : kNone;
             }
         }
@@ -421,33 +458,35 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
     }
 }
 
-template <int TYPE, int DIM, int NW, bool UNI>
+template <int TYPE, int DIM, int NW, bool UNI, bool MX>
 hipError_t chunk_pages(const AttendArgs& a, hipStream_t st) {
     static std::atomic<unsigned long long> done{0};
-    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&attend_chunk_kernel<TYPE, DIM, NW, UNI>), chunk_lds(DIM, NW), done);
+    const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(&attend_chunk_kernel<TYPE, DIM, NW, UNI, MX>), chunk_lds(DIM, NW), done);
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)((long long)a.tokens * a.group / (32 * NW) + a.requests), (unsigned)a.c.heads, (unsigned)a.splits);
-    KernelTimer kt(KID_ATTEND, st);
-    launch_timed(kt, (attend_chunk_kernel<TYPE, DIM, NW, UNI>), grid, dim3(64 * NW), chunk_lds(DIM, NW), st, a);
+    KernelTimer kt(MX ? KID_MX_ATTEND : KID_ATTEND, st);
+    launch_timed(kt, (attend_chunk_kernel<TYPE, DIM, NW, UNI, MX>), grid, dim3(64 * NW), chunk_lds(DIM, NW), st, a);
     return hipGetLastError();
 }
-template <int TYPE, int DIM, int NW>
+template <int TYPE, int DIM, int NW, bool MX>
 hipError_t chunk_of(const AttendArgs& a, hipStream_t st) {
-    return a.c.page_size % (1024 / DIM) == 0 ? chunk_pages<TYPE, DIM, NW, true>(a, st) : chunk_pages<TYPE, DIM, NW, false>(a, st);
+    return a.c.page_size % (1024 / DIM) == 0 ? chunk_pages<TYPE, DIM, NW, true, MX>(a, st) : chunk_pages<TYPE, DIM, NW, false, MX>(a, st);
 }
-template <int TYPE>
+template <int TYPE, bool MX>
 hipError_t chunk_type(const AttendArgs& a, hipStream_t st) {
-    if (a.c.dim <= 64) return chunk_of<TYPE, 64, 4>(a, st);
-    if (a.c.dim <= 128) return chunk_of<TYPE, 128, TYPE == kF32 ? 4 : 8>(a, st);
-    return chunk_of<TYPE, 256, 4>(a, st);
+    if (a.c.dim <= 64) return chunk_of<TYPE, 64, 4, MX>(a, st);
+    if (a.c.dim <= 128) return chunk_of<TYPE, 128, TYPE == kF32 ? 4 : 8, MX>(a, st);
+    return chunk_of<TYPE, 256, 4, MX>(a, st);
+}
+template <bool MX>
+hipError_t chunk_any(const AttendArgs& a, hipStream_t st) {
+    if (a.type == kF32) return chunk_type<kF32, MX>(a, st);
+    if (a.type == kBF16) return chunk_type<kBF16, MX>(a, st);
+    return chunk_type<kF16, MX>(a, st);
 }
 
 }  // namespace
 
-hipError_t launch_attend_chunk(const AttendArgs& a, hipStream_t st) {
-    if (a.type == kF32) return chunk_type<kF32>(a, st);
-    if (a.type == kBF16) return chunk_type<kBF16>(a, st);
-    return chunk_type<kF16>(a, st);
-}
+hipError_t launch_attend_chunk(const AttendArgs& a, hipStream_t st) { return a.mx ? chunk_any<true>(a, st) : chunk_any<false>(a, st); }
 
 }  // namespace int8t

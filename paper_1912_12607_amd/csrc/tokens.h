@@ -180,9 +180,11 @@ struct AttendArgs {
     int share;               // keys of one, blocks of 16 rows (a multiple of 32)
     float *part_o, *part_ml; // [splits][tokens * heads * group][dim], [..][2]
     int wide_q;
+    int mx;                  // the cache holds microscaled 4-bit codes (mx4.h)
 };
 void attend_plan(AttendArgs* a, int longest);       // rows, splits
 hipError_t launch_attend_chunk(const AttendArgs& a, hipStream_t st);      // (blocks of 128 or 256 rows; does not join)
+hipError_t launch_mx_attend_rows(const AttendArgs& a, hipStream_t st);    // (blocks of 16 rows; does not join)
 hipError_t launch_attend(const AttendArgs& a, hipStream_t st);
 
 }  // namespace int8t

@@ -229,18 +229,23 @@ class PagedCache:
 
     kq, vq: (pages, heads, page_size, dim) int8;  ks, vs: (pages, heads, page_size) float32"""
 
+    _calls = B.lib.int8t_cache_write, B.lib.int8t_cache_read, B.lib.int8t_cache_attend_workspace_bytes, B.lib.int8t_cache_attend
+
     def __init__(self, kq, ks, vq, vs):
         if kq.dim() != 4 or kq.shape != vq.shape or ks.shape != kq.shape[:3] or vs.shape != ks.shape:
             raise RuntimeError(f"cache of codes {tuple(kq.shape)}, {tuple(vq.shape)} and scales {tuple(ks.shape)}, {tuple(vs.shape)}")
         for t, kind, name in ((kq, torch.int8, "kq"), (vq, torch.int8, "vq"), (ks, torch.float32, "ks"), (vs, torch.float32, "vs")):
             if t.dtype is not kind or not t.is_cuda or not t.is_contiguous() or t.device != kq.device:
                 raise RuntimeError(f"{name}: contiguous {kind} on {kq.device}")
+        self._keep(B.Cache, kq, ks, vq, vs, kq.shape[3])
+
+    def _keep(self, struct, kq, ks, vq, vs, dim):
         self._tensors = kq, ks, vq, vs
-        self.pages, self.heads, self.page_size, self.dim = kq.shape
+        (self.pages, self.heads, self.page_size), self.dim = kq.shape[:3], dim
         if self.dim % 16 or not 0 < self.dim <= 256:
             raise RuntimeError(f"head dimension {self.dim}: a multiple of 16, at most 256")
         self._index = kq.get_device()
-        self._c = B.Cache(kq.data_ptr(), vq.data_ptr(), ks.data_ptr(), vs.data_ptr(), self.pages, self.page_size, self.heads, self.dim)
+        self._c = struct(kq.data_ptr(), vq.data_ptr(), ks.data_ptr(), vs.data_ptr(), self.pages, self.page_size, self.heads, self.dim)
 
     # (not to be replaced: their addresses are taken once)
     kq = property(lambda self: self._tensors[0])
@@ -277,7 +282,7 @@ class PagedCache:
         if vd != 1:
             v = v.contiguous()
             vt, vh, _ = v.stride()
-        _call(self._index, B.lib.int8t_cache_write, self._c, k.data_ptr(), v.data_ptr(), kind, shape[0], kt, kh, vt, vh, slots.data_ptr())
+        _call(self._index, self._calls[0], self._c, k.data_ptr(), v.data_ptr(), kind, shape[0], kt, kh, vt, vh, slots.data_ptr())
 
     def read(self, slots: torch.Tensor, dtype=torch.float32):
         """(k, v), each (len(slots), heads, dim), as the cache holds them; zeros for slots outside it."""
@@ -288,7 +293,7 @@ class PagedCache:
         n = slots.shape[0]
         k = torch.empty((n, self.heads, self.dim), dtype=dtype, device=slots.device)
         v = torch.empty_like(k)
-        _call(self._index, B.lib.int8t_cache_read, self._c, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(), kind)
+        _call(self._index, self._calls[1], self._c, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(), kind)
         return k, v
 
     def attend(self, q: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, causal: bool = True,
@@ -325,8 +330,8 @@ class PagedCache:
         if T:
             d = B.AttendDesc(T, n, heads // self.heads, wide[1], 0 if longest is None else max(1, int(longest)), kind, 1 if causal else 0,
                              dim ** -0.5 if scale is None else scale, token, head, max(pitch, wide[1]))
-            need = B.lib.int8t_cache_attend_workspace_bytes(self._c, d)
+            need = self._calls[2](self._c, d)
             ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-            _call(index, B.lib.int8t_cache_attend, self._c, d, q.data_ptr(), starts.data_ptr(), lengths.data_ptr(), table.data_ptr(), out.data_ptr(),
+            _call(index, self._calls[3], self._c, d, q.data_ptr(), starts.data_ptr(), lengths.data_ptr(), table.data_ptr(), out.data_ptr(),
                   None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), need)
         return (out, lse) if return_lse else out
