@@ -676,7 +676,6 @@ int8t_status int8t_cache_attend_division(const int8t_cache *cache, const int8t_a
  * A block that holds NaN or an infinity has the byte 255 (NaN) and codes of 0.
  *   codes    [rows][16 * blocks] bytes, blocks = cols / 32 rounded up: value c is the low (c even) or high half of byte c / 2; zero beyond cols
  *   scales   [panels][rows][8] bytes, panels = blocks / 8 rounded up: block b of row r is at ((b / 8) * rows + r) * 8 + b % 8; zero beyond the last block
- *            (products read scales 16 bytes at a time: 8 bytes behind an odd number of rows and panels have to be there, and are not used)
  * Sums of products are in fp32.  Pointers to codes and scales lie on 16 bytes.
  */
 

@@ -20,7 +20,7 @@ inline bool codes_ok(int rows, int cols) {
     return rows > 0 && cols > 0 && cols <= INT8T_MAX_REDUCTION && (unsigned long long)rows * (unsigned long long)mx_panels(cols) * 256 < (1ull << 31);
 }
 inline size_t code_bytes(int rows, int cols) { return align256((size_t)rows * mx_row_bytes(cols)); }
-inline size_t scale_bytes(int rows, int cols) { return align256((size_t)mx_panels(cols) * rows * 8 + 8); }
+inline size_t scale_bytes(int rows, int cols) { return align256((size_t)mx_panels(cols) * rows * 8); }
 inline size_t part_bytes(int rows, int cols) { return align256((size_t)mx_sum_parts(rows) * cols * sizeof(float)); }
 
 int8t_status linear_ok(const int8t_linear_desc* d, bool backward) {

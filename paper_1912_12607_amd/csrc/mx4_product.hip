@@ -26,6 +26,10 @@ __device__ __forceinline__ tk_f4 product16(const uint4& a, const uint4& b, const
     const mp_v8i wa = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, wb = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, c, 4, 4, S, (int)sa, S, (int)sb);
 }
+// One wave-wide 4-byte-per-lane buffer load into LDS: lane l's word lands at lds_base + 4 l (see igd_load_lds()).
+__device__ __forceinline__ void load_words_lds(const lds_dma_v4i& rsrc, uint32_t lds_base_uniform, uint32_t voff, uint32_t soff) {
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds_base_uniform), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
@@ -38,8 +42,8 @@ __device__ __forceinline__ void product_body(const MxProductArgs& a, const int m
     typedef typename ElemOf<TYPE>::type T;
     constexpr int KG = 8, NW = WM * WN, BM = WM * MI * 32, BN = WN * NJ * 32, CODES = (BM + BN) * KG, STAGE = CODES + (BM + BN) / 2;      // (in pieces of 16 bytes)
     constexpr int NLA = BM * KG / 64 / NW, NLB = BN * KG / 64 / NW, NL = NLA + NLB;
-    constexpr int SL = (BM + BN) / 2 / NW;                 // lanes of a wave that load scales, 16 bytes each: the first half of the waves a's, the others b's
-    static_assert((NW & 1) == 0 && BM == BN && SL <= 64, "the swizzle below needs an even wave count, the scales' loads as many rows as columns");
+    constexpr int SD = (BM + BN) * 8 / 256 / NW;           // loads of scales, 32 rows each: the first half of the waves a's, the others b's
+    static_assert((NW & 1) == 0 && BM == BN && SD * 256 * NW == (BM + BN) * 8, "the swizzle below needs an even wave count, the scales' loads as many rows as columns");
     extern __shared__ __attribute__((aligned(1024))) uint4 ring[];
     __shared__ __attribute__((aligned(16))) float cbias[BN];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -62,15 +66,14 @@ __device__ __forceinline__ void product_body(const MxProductArgs& a, const int m
     const int all_steps = (a.Kb + KG * 16 - 1) / (KG * 16);
     const lds_dma_v4i ra = igd_rsrc(a.a + (size_t)row0 * a.Kb, (uint32_t)rows * (uint32_t)a.Kb);
     const lds_dma_v4i rb = igd_rsrc(a.b + (size_t)col0 * a.Kb, (uint32_t)cols * (uint32_t)a.Kb);
-    // (two rows a lane; one behind the last is read with it, and not stored)
     const bool scales_a = wave < NW / 2;
     const int lines = scales_a ? a.M : a.N, line0 = scales_a ? row0 : col0;
-    const lds_dma_v4i rs = igd_rsrc((scales_a ? a.sa : a.sb) + (size_t)line0 * 8, (uint32_t)(((size_t)all_steps * lines - line0 + 1) * 8));
+    const lds_dma_v4i rs = igd_rsrc((scales_a ? a.sa : a.sb) + (size_t)line0 * 8, (uint32_t)(((size_t)all_steps * lines - line0) * 8));
     const uint32_t lds_a = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(size_t)(ring + 64 * wave));
     const uint32_t lds_b = lds_a + BM * KG * 16;
-    const uint32_t lds_s = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(size_t)(ring + CODES + SL * wave));
-    const int sline = ((wave % (NW / 2)) * SL + lane) * 2;
-    const uint32_t sv = line0 + sline < lines ? (uint32_t)sline * 8u : IGD_OOB;
+    const uint32_t lds_s = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(size_t)(ring + CODES + SD * 16 * wave));
+    const int sline = (wave % (NW / 2)) * (SD * 32) + (lane >> 1);
+    const uint32_t sv = (uint32_t)(sline * 8 + (lane & 1) * 4);
     // load i of this wave covers RL tile rows from RL (wave + NW i); the lane's granule is the inverse of igd_slot<KG>()
     constexpr int RL = 64 / KG;
     const int lrow = lane / KG;
@@ -78,12 +81,18 @@ __device__ __forceinline__ void product_body(const MxProductArgs& a, const int m
     const uint32_t voff = (uint32_t)(RL * wave + lrow) * (uint32_t)a.Kb + (uint32_t)gran * 16u;
     const uint32_t vstep = (uint32_t)(RL * NW) * (uint32_t)a.Kb;
     const int first_step = SPLIT ? (int)((long long)all_steps * share / a.splits) : 0, nsteps = SPLIT ? (int)((long long)all_steps * (share + 1) / a.splits) - first_step : all_steps;
-    auto load = [&](int buf, int step, int u) __attribute__((always_inline)) {      // the u-th of this wave's NL loads of a stage, with the first its scales
+    // The u-th of this wave's NL loads of codes of a stage, scales with the first ones.  Stages behind the last are loaded too, as zeros: no branch stands between the
+    // products, which the compiler would move behind it, operands and all (registers spilled, 16384 x 4096 -> 4096 1080 us).
+    auto load = [&](int buf, int step, int u) __attribute__((always_inline)) {
         const uint32_t boff = (uint32_t)buf * (STAGE * 16u);
         const int at = (first_step + step) * (KG * 16);
-        const uint32_t past = at + gran * 16 < a.Kb ? 0u : IGD_OOB;      // beyond the reduction
+        const uint32_t end = step < nsteps ? 0u : IGD_OOB;
+        const uint32_t past = at + gran * 16 < a.Kb ? end : IGD_OOB;      // beyond the reduction
         const uint32_t k = (uint32_t)__builtin_amdgcn_readfirstlane(at);
-        if (u == 0 && lane < SL) igd_load_lds(rs, lds_s + boff, sv, (uint32_t)__builtin_amdgcn_readfirstlane((first_step + step) * lines * 8));
+        if (u < SD) {
+            const uint32_t behind = line0 + sline + u * 32 < lines ? end : IGD_OOB;
+            load_words_lds(rs, lds_s + boff + (uint32_t)u * 256u, (sv + (uint32_t)u * 256u) | behind, (uint32_t)__builtin_amdgcn_readfirstlane((first_step + step) * lines * 8));
+        }
         if (u < NLA) igd_load_lds(ra, lds_a + boff + (uint32_t)u * (NW * 1024), (voff + (uint32_t)u * vstep) | past, k);
         else igd_load_lds(rb, lds_b + boff + (uint32_t)(u - NLA) * (NW * 1024), (voff + (uint32_t)(u - NLA) * vstep) | past, k);
     };
@@ -123,11 +132,10 @@ __device__ __forceinline__ void product_body(const MxProductArgs& a, const int m
             if (kk == 0) eb[BUF][j] = sS[2 * (BM + c) + half];
         }
     };
-    // (more: the loads of the NS - 2 stages behind the next one are still under way)
-    const auto turn = [&](bool more) __attribute__((always_inline)) {
+    // (the loads of the NS - 2 stages behind the next one are still under way)
+    const auto turn = []() __attribute__((always_inline)) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (NS > 2 && more) wait_loads<NS == 2 ? 0 : (NS - 2) * (NL + 1)>();
-        else wait_loads<0>();
+        wait_loads<(NS - 2) * (NL + SD)>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -139,11 +147,11 @@ __device__ __forceinline__ void product_body(const MxProductArgs& a, const int m
     for (int p = 0; p < NS - 1; ++p)
 #pragma unroll
         for (int u = 0; u < NL; ++u)
-            if (p < nsteps) load(p, p, u);
-    turn(nsteps >= NS);
+            load(p, p, u);
+    turn();
 #pragma unroll
     for (int u = 0; u < NL; ++u)
-        if (u * NQ < NP && NS - 1 < nsteps) load(NS - 1, NS - 1, u);
+        if (u * NQ < NP) load(NS - 1, NS - 1, u);
     read(std::integral_constant<int, 0>(), 0);
     const auto stage = [&](const auto slot, int step) __attribute__((always_inline)) {
         constexpr int BUF = decltype(slot)::value;
@@ -153,8 +161,8 @@ __device__ __forceinline__ void product_body(const MxProductArgs& a, const int m
             const bool last = kk + 1 == KG / 2;
             if (!last) {
                 read(slot, kk + 1);
-            } else if (step + 1 < nsteps) {
-                turn(step + NS - 1 < nsteps);
+            } else {
+                turn();
                 read(std::integral_constant<int, (BUF + 1) % NS>(), 0);
             }
             const int into = last ? BUF : (BUF + NS - 1) % NS, which = last ? step + NS : step + NS - 1;
@@ -163,7 +171,7 @@ __device__ __forceinline__ void product_body(const MxProductArgs& a, const int m
 #pragma unroll
             for (int q = 0; q < NP; ++q) {
                 const int i = q / NJ, j = q % NJ;
-                if ((done + q) % NQ == 0 && (done + q) / NQ < NL && which < nsteps) load(into, which, (done + q) / NQ);
+                if ((done + q) % NQ == 0 && (done + q) / NQ < NL) load(into, which, (done + q) / NQ);
                 acc[i][j] = product32_at(kk, fb[kk & 1][j], fa[kk & 1][i], acc[i][j], eb[BUF][j], ea[BUF][i]);
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -180,6 +188,7 @@ __device__ __forceinline__ void product_body(const MxProductArgs& a, const int m
         }
     }
 
+    wait_loads<0>();                 // (of the zeros behind the last stage)
     if constexpr (SPLIT) {
         // [share][row][column], columns padded to four
         const int np = (a.N + 3) & ~3;

@@ -34,7 +34,7 @@ def _plan(M: int, K: int, N: int, kind: int, wkind: int):
     desc = B.LinearDesc(M, K, N, kind, wkind)
     need = tuple(B.lib.int8t_mx4_linear_workspace_bytes(desc, i) for i in range(3))
     at, places = 0, []
-    for n in (K * 16 * _blocks(M), K * 8 * _panels(M) + 8, K * 16 * _blocks(N), K * 8 * _panels(N) + 8):
+    for n in (K * 16 * _blocks(M), K * 8 * _panels(M), K * 16 * _blocks(N), K * 8 * _panels(N)):
         places.append(at)
         at += (n + 255) & ~255
     return desc, need, tuple(places), at
@@ -54,17 +54,9 @@ class ServedLinear4:
         out, index = codes.shape[0], codes.get_device()
         if scales.dtype is not torch.uint8 or scales.dim() != 2 or scales.shape[0] != out or scales.shape[1] < blocks or scales.get_device() != index:
             raise RuntimeError(f"scales: uint8 ({out}, {blocks}) on {codes.device}, not {tuple(scales.shape)} of {scales.dtype} on {scales.device}")
-        panel = self._panels_of(n, out, codes.device)
         whole = torch.zeros(out, 8 * panels, dtype=torch.uint8, device=codes.device)
         whole[:, :blocks] = scales[:, :blocks]
-        panel.copy_(whole.view(out, panels, 8).transpose(0, 1))
-        self._set(codes, panel, n, bias)
-
-    @staticmethod
-    def _panels_of(n, out, device):
-        """Room for scales in panels of eight blocks, a row's eight bytes together (and the eight bytes behind them that products read)."""
-        size = _panels(n) * out * 8
-        return torch.zeros(size + 8, dtype=torch.uint8, device=device)[:size].view(_panels(n), out, 8)
+        self._set(codes, whole.view(out, panels, 8).transpose(0, 1).contiguous(), n, bias)
 
     def _set(self, codes, panels, n, bias):
         self.in_features, self.out_features = n, codes.shape[0]
@@ -90,7 +82,7 @@ class ServedLinear4:
         N, K = weight.shape
         w, pitch = _rows(weight.detach(), K)
         codes = torch.empty(N, 16 * _blocks(K), dtype=torch.uint8, device=w.device)
-        panels = cls._panels_of(K, N, w.device)
+        panels = torch.empty(_panels(K), N, 8, dtype=torch.uint8, device=w.device)
         _call(w.get_device(), B.lib.int8t_mx4_quantize, w.data_ptr(), kind, N, K, pitch, B.ROUND_NEAREST_EVEN, 0, codes.data_ptr(), panels.data_ptr(), None, None, None, None, 0)
         layer = cls.__new__(cls)
         layer._set(codes, panels, K, bias)

@@ -151,10 +151,7 @@ def operand(rows, K, seed, spread):
 
 
 def on_device(code, byte, K):
-    panels = R.in_panels(byte, K)
-    flat = torch.zeros(panels.size + 8, dtype=torch.uint8)
-    flat[:panels.size] = torch.from_numpy(panels.reshape(-1))
-    return torch.from_numpy(R.packed(code)).to(DEV), flat.to(DEV)
+    return torch.from_numpy(R.packed(code)).to(DEV), torch.from_numpy(R.in_panels(byte, K)).to(DEV)
 
 
 def product(M, N, K, dtype, bias, scratch, spread, seed=1, extra=0):
