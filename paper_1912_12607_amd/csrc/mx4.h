@@ -63,10 +63,11 @@ struct MxArgs {              // codes of rows x cols values
     uint8_t *q, *s;          // blocks along the columns: [rows][mx_row_bytes(cols)], [mx_panels(cols)][rows][8]; or null
     uint8_t *qt, *st;        // blocks along the rows: [cols][mx_row_bytes(rows)], [mx_panels(rows)][cols][8]; or null
     float* sum;              // cols, or null: sums of the columns
-    float* part;             // [parts][cols], with sum
+    float* part;             // [parts][cols], with sum (one part: not used)
 };
 int mx_sum_parts(int rows);
-hipError_t launch_mx_quantize(const MxArgs& a, hipStream_t st);
+// with b (the same type and rounding to nearest in both): two matrices in one launch
+hipError_t launch_mx_quantize(const MxArgs& a, hipStream_t st, const MxArgs* b = nullptr);
 
 // ---- mx4_product.hip --------------------------------------------------------------------------------------------------
 struct MxProductArgs {       // y[m][n] = sum_k a[m][k] b[n][k] + bias[n]

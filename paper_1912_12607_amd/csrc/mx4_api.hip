@@ -170,10 +170,12 @@ extern "C" int8t_status int8t_mx4_linear_fwd(const int8t_linear_desc* d, const i
         return launched(launch_mx_few_tokens(MxFewArgs{b->x, b->x_pitch, d->type, d->M, d->K, mx_row_bytes(d->K), d->N, wide, b->wq, b->sw, b->bias, b->y, b->y_pitch}, st));
     }
     uint8_t *const wq = b->wq ? b->wq : s.wq, *const sw = b->wq ? b->sw : s.sw;
-    hipError_t e = hipSuccess;
-    if (b->w) e = launch_mx_quantize(MxArgs{b->w, b->w_pitch, d->wtype, d->N, d->K, 0, 0, wq, sw, b->wt, b->swt, nullptr, nullptr}, st);
-    if (d->M == 0 || e != hipSuccess) return launched(e);
-    e = launch_mx_quantize(MxArgs{b->x, b->x_pitch, d->type, d->M, d->K, 0, 0, s.xq, s.sx, b->xt, b->sxt, nullptr, nullptr}, st);
+    const MxArgs w{b->w, b->w_pitch, d->wtype, d->N, d->K, 0, 0, wq, sw, b->wt, b->swt, nullptr, nullptr};
+    const MxArgs x{b->x, b->x_pitch, d->type, d->M, d->K, 0, 0, s.xq, s.sx, b->xt, b->sxt, nullptr, nullptr};
+    if (d->M == 0) return b->w ? launched(launch_mx_quantize(w, st)) : INT8T_OK;
+    const bool together = b->w && d->wtype == d->type;
+    hipError_t e = b->w && !together ? launch_mx_quantize(w, st) : hipSuccess;
+    if (e == hipSuccess) e = launch_mx_quantize(x, st, together ? &w : nullptr);
     if (e != hipSuccess) return INT8T_ERR_RUNTIME;
     MxProductArgs a{};
     a.a = s.xq; a.sa = s.sx; a.b = wq; a.sb = sw; a.bias = b->bias;

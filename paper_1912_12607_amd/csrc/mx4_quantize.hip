@@ -40,70 +40,140 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(const MxArgs a, const Fast
     *reinterpret_cast<uint32_t*>(a.q + (size_t)row * (16 * blocks) + 4 * g) = w;
 }
 
-// Blocks along the rows' axis: a lane has 16 bytes of 32 neighbouring rows in registers, RB blocks of rows and 64 / RB groups of columns a wave.
-template <int TYPE, bool STOCH, int RB>
-__global__ __launch_bounds__(256) void mx_cols_kernel(const MxArgs a, const int wide, const uint32_t kx, const uint32_t ka) {
+// Both directions from one pass: tiles of 256 rows by 128 bytes (64 columns, 32 of fp32), a lane has eight rows of 16 bytes, four lanes above each other a block of
+// rows, four or eight side by side one of columns; the largest goes round by lane exchanges.  Codes along the rows' axis are turned in registers -- the eight rows
+// of a lane's column are a word -- and go through LDS, so that a column's 256 rows leave as one line.  An XCD takes a run of tiles side by side: what two of them
+// write of a line meets in its L2.
+constexpr int QT_R = 256, QT_PITCH = QT_R / 2 + 16;
+template <int TYPE, bool STOCH>
+__device__ __forceinline__ void tile_body(const MxArgs& a, const int block, const int total, const int wide, const uint32_t kx, const uint32_t ka, const uint32_t tx, const uint32_t ta) {
     typedef typename ElemOf<TYPE>::type T;
-    constexpr int C = 16 / (int)sizeof(T), CG = 64 / RB;               // columns of a lane, groups of a wave
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const int col = (((int)blockIdx.x * 4 + wave) * CG + lane % CG) * C, block = (int)blockIdx.y * RB + lane / CG;
-    const int blocks = mx_blocks(a.rows), row0 = block * 32;
-    if (col >= a.cols) return;
-    if (block >= blocks) {
-        if (a.qt && block < (blocks + 7) / 8 * 8)
+    constexpr int C = 16 / (int)sizeof(T), TC = 8 * C;
+    __shared__ __attribute__((aligned(16))) uint8_t turned[TC * QT_PITCH], turned_s[TC * 8];
+    __shared__ float sums[4][TC];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, cg = lane & 7, rg = tid >> 3;
+    const int tiles_c = ((a.q ? mx_panels(a.cols) * 256 : a.cols) + TC - 1) / TC, per = (total + 7) >> 3, tile = (block & 7) * per + (block >> 3);
+    if ((block >> 3) >= per || tile >= total) return;
+    const int row0 = tile / tiles_c * QT_R, col0 = (tile - tile / tiles_c * tiles_c) * TC;
+    const int row = row0 + 8 * rg, col = col0 + cg * C;
+    T v[8][C];
+    {
+        const T* const x = static_cast<const T*>(a.x);
+        const bool whole = wide && col + C <= a.cols;
 #pragma unroll
-            for (int j = 0; j < C; ++j)
-                if (col + j < a.cols) a.st[((size_t)(block >> 3) * a.cols + col + j) * 8 + (block & 7)] = 0;
-        return;
-    }
-    T v[32][C];
-    const bool whole = wide && col + C <= a.cols;
-    const T* const x = static_cast<const T*>(a.x) + (size_t)row0 * a.pitch + col;
+        for (int r = 0; r < 8; ++r) {
+            const bool in = row + r < a.rows;
+            const T* const at = x + (size_t)(in ? row + r : 0) * a.pitch + col;
+            if (whole) {
+                typedef T V __attribute__((ext_vector_type(C)));
+                const V t = *reinterpret_cast<const V*>(at);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        const bool in = row0 + i < a.rows;
-        if (whole) {
-            typedef T V __attribute__((ext_vector_type(C)));
-            V t = *reinterpret_cast<const V*>(x + (in ? (size_t)i * a.pitch : 0));
+                for (int j = 0; j < C; ++j) v[r][j] = in ? t[j] : (T)0.0f;
+            } else {
 #pragma unroll
-            for (int j = 0; j < C; ++j) v[i][j] = in ? t[j] : (T)0.0f;
-        } else {
-#pragma unroll
-            for (int j = 0; j < C; ++j) v[i][j] = in && col + j < a.cols ? x[(size_t)i * a.pitch + j] : (T)0.0f;
+                for (int j = 0; j < C; ++j) v[r][j] = in && col + j < a.cols ? at[j] : (T)0.0f;
+            }
         }
     }
+    if (a.q) {
+        const int block_c = col >> 5, blocks = mx_blocks(a.cols);
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-        if (col + j >= a.cols) break;
-        float m = 0.0f, sum = 0.0f;
+        for (int r = 0; r < 8; ++r) {
+            float m = 0.0f, f[8];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            m = most(m, fabsf((float)v[i][j]));
-            sum += (float)v[i][j];
-        }
-        if (a.sum) a.part[(size_t)block * a.cols + col + j] = sum;
-        if (!a.qt) continue;
-        const uint32_t byte = mx_byte_of(m);
-        a.st[((size_t)(block >> 3) * a.cols + col + j) * 8 + (block & 7)] = (uint8_t)byte;
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
-        if (byte < 255u) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                float f[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = (float)v[8 * u + i][j];
+            for (int j = 0; j < C; ++j) {
+                f[j] = (float)v[r][j];
+                m = most(m, fabsf(f[j]));
+            }
+            m = most(m, dpp_of<kDppSwap1>(m));
+            m = most(m, dpp_of<kDppSwap2>(m));
+            if (C == 4) m = most(m, dpp_of<0x141>(m));             // (row_half_mirror: the quads of eight lanes)
+            const uint32_t byte = mx_byte_of(m);
+            uint32_t w = 0;
+            if (byte < 255u) {
                 if (STOCH) {
                     const float inv = mx_inverse(byte);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        w[u] |= mx_drawn(f[i], inv, rng24(kx, ka, (uint32_t)(row0 + 8 * u + i) * (uint32_t)a.cols + (uint32_t)(col + j))) << (4 * i);
+                    for (int j = 0; j < C; ++j) w |= mx_drawn(f[j], inv, rng24(kx, ka, (uint32_t)(row + r) * (uint32_t)a.cols + (uint32_t)(col + j))) << (4 * j);
                 } else {
-                    w[u] = mx_codes8(f, mx_power(byte));
+#pragma unroll
+                    for (int j = C; j < 8; ++j) f[j] = 0.0f;
+                    w = mx_codes8(f, mx_power(byte));
                 }
             }
+            if (row + r < a.rows && block_c < blocks) {
+                uint8_t* const q = a.q + (size_t)(row + r) * (16 * blocks) + col / 2;
+                if (C == 8) *reinterpret_cast<uint32_t*>(q) = w;
+                else *reinterpret_cast<uint16_t*>(q) = (uint16_t)w;
+                if ((col & 31) == 0) a.s[((size_t)(block_c >> 3) * a.rows + row + r) * 8 + (block_c & 7)] = (uint8_t)byte;
+            }
+            // (behind the last block, the rest of its panel)
+            if (row + r < a.rows && block_c >= blocks && block_c < ((blocks + 7) & ~7) && (col & 31) == 0) a.s[((size_t)(block_c >> 3) * a.rows + row + r) * 8 + (block_c & 7)] = 0;
         }
-        *reinterpret_cast<uint4*>(a.qt + ((size_t)(col + j) * blocks + block) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
     }
+    if (a.qt || a.sum) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            float m = 0.0f, sum = 0.0f, f[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                f[r] = (float)v[r][j];
+                m = most(m, fabsf(f[r]));
+                sum += f[r];
+            }
+            if (a.sum) {
+                sum += dpp_of<kDppRor8>(sum);
+                const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+                sum = __uint_as_float(b[0]) + __uint_as_float(b[1]);
+                const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+                sum = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+                if (lane < 8) sums[wave][cg * C + j] = sum;
+            }
+            if (!a.qt) continue;
+            m = most(m, dpp_of<kDppRor8>(m));
+            const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+            m = most(__uint_as_float(b[0]), __uint_as_float(b[1]));
+            const uint32_t byte = mx_byte_of(m);
+            uint32_t w = 0;
+            if (byte < 255u) {
+                if (STOCH) {
+                    const float inv = mx_inverse(byte);
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) w |= mx_drawn(f[r], inv, rng24(tx, ta, (uint32_t)(row + r) * (uint32_t)a.cols + (uint32_t)(col + j))) << (4 * r);
+                } else {
+                    w = mx_codes8(f, mx_power(byte));
+                }
+            }
+            *reinterpret_cast<uint32_t*>(turned + (cg * C + j) * QT_PITCH + 4 * rg) = w;
+            if ((rg & 3) == 0) turned_s[(cg * C + j) * 8 + (rg >> 2)] = (uint8_t)byte;
+        }
+        __syncthreads();
+        if (a.qt) {
+            const int blocks = mx_blocks(a.rows), b0 = row0 >> 5;
+#pragma unroll
+            for (int u = 0; u < TC * 8 / 256; ++u) {
+                const int c = (tid >> 3) + 32 * u, b = tid & 7;
+                if (col0 + c < a.cols && b0 + b < blocks)
+                    *reinterpret_cast<uint4*>(a.qt + ((size_t)(col0 + c) * blocks + b0 + b) * 16) = *reinterpret_cast<const uint4*>(turned + c * QT_PITCH + 16 * b);
+            }
+            // (a tile's rows are a panel; blocks behind the last have largest values of zero, and bytes of zero)
+            if (tid < TC && col0 + tid < a.cols)
+                *reinterpret_cast<uint2*>(a.st + ((size_t)(b0 >> 3) * a.cols + col0 + tid) * 8) = *reinterpret_cast<const uint2*>(turned_s + tid * 8);
+        }
+        if (a.sum && tid < TC && col0 + tid < a.cols) {
+            const float s = (sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid]);
+            if (a.rows <= QT_R) a.sum[col0 + tid] = s;
+            else a.part[(size_t)(row0 / QT_R) * a.cols + col0 + tid] = s;
+        }
+    }
+}
+// Two matrices in one launch: blocks from `first` (a multiple of eight) on have the second's tiles.
+template <int TYPE, bool STOCH>
+__global__ __launch_bounds__(256) void mx_tiles_kernel(const MxArgs a, const MxArgs b, const int first, const int total_a, const int total_b, const int wide_a, const int wide_b,
+                                                       const uint32_t kx, const uint32_t ka, const uint32_t tx, const uint32_t ta) {
+    const bool second = (int)blockIdx.x >= first;
+    const MxArgs m = second ? b : a;
+    tile_body<TYPE, STOCH>(m, (int)blockIdx.x - (second ? first : 0), second ? total_b : total_a, second ? wide_b : wide_a, kx, ka, tx, ta);
 }
 
 // Sums of columns from those of the blocks of rows
@@ -116,39 +186,44 @@ __global__ __launch_bounds__(256) void mx_sum_kernel(const MxArgs a, const int p
     a.sum[c] = (float)s;
 }
 
+inline int wide_rows(const MxArgs& a) { return (((uintptr_t)a.x | (a.pitch * (a.type == kF32 ? 4 : 2))) & 15) == 0; }
+inline long long tiles_of(const MxArgs& a) {
+    const int tc = a.type == kF32 ? 32 : 64, cols = a.q ? mx_panels(a.cols) * 256 : a.cols;      // (whole panels: the scales behind the last block are written)
+    return (long long)((a.rows + QT_R - 1) / QT_R) * ((cols + tc - 1) / tc);
+}
+
 template <int TYPE, bool STOCH>
-hipError_t quantize_of(const MxArgs& a, hipStream_t st) {
-    const int wide = (((uintptr_t)a.x | (a.pitch * (TYPE == kF32 ? 4 : 2))) & 15) == 0;
-    if (a.q) {
+hipError_t quantize_of(const MxArgs& a, const MxArgs* b, hipStream_t st) {
+    const uint64_t turned = a.seed ^ (1ull << 63);
+    if (!a.qt && !a.sum && !b) {
         const int groups = mx_panels(a.cols) * 32;
         KernelTimer kt(KID_MX_QUANTIZE, st);
-        launch_timed(kt, (mx_rows_kernel<TYPE, STOCH>), dim3((unsigned)(((long long)a.rows * groups + 255) / 256)), dim3(256), 0, st, a, fast_div((unsigned)groups), groups, wide,
-                     seed_key_x(a.seed), seed_key_a(a.seed));
+        launch_timed(kt, (mx_rows_kernel<TYPE, STOCH>), dim3((unsigned)(((long long)a.rows * groups + 255) / 256)), dim3(256), 0, st, a, fast_div((unsigned)groups), groups,
+                     wide_rows(a), seed_key_x(a.seed), seed_key_a(a.seed));
+        return hipGetLastError();
     }
-    if (a.qt || a.sum) {
-        constexpr int C = TYPE == kF32 ? 4 : 8;
-        const uint64_t seed = a.seed ^ (1ull << 63);
-        const int blocks = mx_panels(a.rows) * 8;
+    {
+        const int ta = (int)tiles_of(a), tb = b ? (int)tiles_of(*b) : 0, first = (ta + 7) & ~7;
         KernelTimer kt(KID_MX_QUANTIZE, st);
-        launch_timed(kt, (mx_cols_kernel<TYPE, STOCH, 8>), dim3((unsigned)((a.cols + 32 * C - 1) / (32 * C)), (unsigned)(blocks / 8)), dim3(256), 0, st, a, wide, seed_key_x(seed),
-                     seed_key_a(seed));
+        launch_timed(kt, (mx_tiles_kernel<TYPE, STOCH>), dim3((unsigned)(first + ((tb + 7) & ~7))), dim3(256), 0, st, a, b ? *b : a, first, ta, tb, wide_rows(a), b ? wide_rows(*b) : 0,
+                     seed_key_x(a.seed), seed_key_a(a.seed), seed_key_x(turned), seed_key_a(turned));
     }
-    if (a.sum) {
+    if (a.sum && a.rows > QT_R) {
         KernelTimer kt(KID_MX_QUANTIZE, st);
         launch_timed(kt, mx_sum_kernel, dim3((unsigned)((a.cols + 255) / 256)), dim3(256), 0, st, a, mx_sum_parts(a.rows));
     }
     return hipGetLastError();
 }
 template <int TYPE>
-hipError_t quantize_type(const MxArgs& a, hipStream_t st) { return a.stochastic ? quantize_of<TYPE, true>(a, st) : quantize_of<TYPE, false>(a, st); }
+hipError_t quantize_type(const MxArgs& a, const MxArgs* b, hipStream_t st) { return a.stochastic ? quantize_of<TYPE, true>(a, b, st) : quantize_of<TYPE, false>(a, b, st); }
 
 }  // namespace
 
-int mx_sum_parts(int rows) { return mx_blocks(rows); }
-hipError_t launch_mx_quantize(const MxArgs& a, hipStream_t st) {
-    if (a.type == kF32) return quantize_type<kF32>(a, st);
-    if (a.type == kBF16) return quantize_type<kBF16>(a, st);
-    return quantize_type<kF16>(a, st);
+int mx_sum_parts(int rows) { return (rows + QT_R - 1) / QT_R; }
+hipError_t launch_mx_quantize(const MxArgs& a, hipStream_t st, const MxArgs* b) {
+    if (a.type == kF32) return quantize_type<kF32>(a, b, st);
+    if (a.type == kBF16) return quantize_type<kBF16>(a, b, st);
+    return quantize_type<kF16>(a, b, st);
 }
 
 }  // namespace int8t
