@@ -492,7 +492,22 @@ void attend_plan(AttendArgs* a, int longest) {
         all = dim == 256 ? 10000 : 8000;
     }
     a->rows = each < many || rows * a->c.heads < all ? 16 : dim == 128 && !fp32 ? 256 : 128;
-    const long long tiles = (rows / a->rows + a->requests) * a->c.heads;
+    // Caches in 4 bits: blocks of 16 rows spend less on a key (mx4_attend.hip), so that larger ones are faster only for dims up to 64 and, in bf16 and fp16, up to 128, where their rows
+    // are filled to three quarters (us with 16 rows / with larger ones, pages of 16; rows, requests, heads, keys as above:
+    //                 66,9,12,1500  200,2,32,6000  264,8,8,2048  400,4,8,3000  2048,1,8,8192  64,64,8,1024  400,64,4,1024  512,2,4,2000  1024,4,8,4096  600,16,8,2000
+    //   dim  64 bf16     26/36         90/95          45/56         50/49         131/119        41/48         110/90         21/38         132/120        143/113
+    //   dim  64 fp32     27/47         97/91          52/62         57/54         147/114        46/89         127/111        25/32         155/116        168/169
+    //   dim 128 bf16     28/82        107/86          57/63         62/57         166/112        50/100        147/158        25/36         179/113        194/192
+    //   dim 128 fp32     37/94        139/203         75/140        80/115        219/265        65/199        190/275        32/40         234/267        248/375
+    //   dim 256 bf16     48/130       191/282         95/196       110/161        309/366        88/272        280/380        33/55         324/377        348/523;
+    // pages of 24 and 7: within 15 % of these).
+    if (a->mx) {
+        const int tall = dim == 128 ? 256 : 128;
+        const bool larger = (dim == 64 || (dim == 128 && !fp32)) && each >= (dim == 64 ? 320 : 200) && 4 * each >= 3 * ((each + tall - 1) / tall * tall) && rows * a->c.heads >= 10000;
+        a->rows = larger ? tall : 16;
+    }
+    // (4 bits: blocks that have rows, where these are dealt out evenly)
+    const long long tiles = a->mx && a->rows == 16 ? (each > 16 ? (each + 15) / 16 : 1) * a->requests * a->c.heads : (rows / a->rows + a->requests) * a->c.heads;
     if (a->rows == 16) {
         // Shares of a fixed number of keys, so that long requests among short ones have more blocks: 2048, or 1024 where those are too few (below 128), or
         // too many for one block of eight waves on each compute unit and too few for two of four (us, shares of 1024 / 2048: single tokens of 1 request over

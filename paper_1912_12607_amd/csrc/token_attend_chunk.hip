@@ -45,8 +45,7 @@ template <int DIM>
 __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
     v = max(v, (uint32_t)dpp_word<kDppSwap1>((int)v));
     v = max(v, (uint32_t)dpp_word<kDppSwap2>((int)v));
-    if (DIM >= 128) v = max(v, (uint32_t)dpp_word<0x141>((int)v));      // (row_half_mirror: the quads of eight lanes)
-    if (DIM >= 256) v = max(v, (uint32_t)dpp_word<kDppRor8>((int)v));
+    if (DIM == 128) v = max(v, (uint32_t)dpp_word<0x141>((int)v));      // (row_half_mirror: the quads of eight lanes)
     return v;
 }
 
@@ -475,8 +474,13 @@ hipError_t chunk_of(const AttendArgs& a, hipStream_t st) {
 template <int TYPE, bool MX>
 hipError_t chunk_type(const AttendArgs& a, hipStream_t st) {
     if (a.c.dim <= 64) return chunk_of<TYPE, 64, 4, MX>(a, st);
-    if (a.c.dim <= 128) return chunk_of<TYPE, 128, TYPE == kF32 ? 4 : 8, MX>(a, st);
-    return chunk_of<TYPE, 256, 4, MX>(a, st);
+    if constexpr (MX) {          // (others have blocks of 16 rows: attend_plan())
+        if constexpr (TYPE != kF32) return chunk_of<TYPE, 128, 8, MX>(a, st);
+        return hipErrorInvalidValue;
+    } else {
+        if (a.c.dim <= 128) return chunk_of<TYPE, 128, TYPE == kF32 ? 4 : 8, MX>(a, st);
+        return chunk_of<TYPE, 256, 4, MX>(a, st);
+    }
 }
 template <bool MX>
 hipError_t chunk_any(const AttendArgs& a, hipStream_t st) {

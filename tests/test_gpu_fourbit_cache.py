@@ -207,9 +207,11 @@ def test_attend_of_larger_blocks(dtype, causal, heads, group, dim, page, new, le
 
 
 def test_larger_blocks_are_used_by_those_calls():
-    for heads, group, dim, page, new, lengths in LARGE[:2] + LARGE[4:5]:
+    for heads, group, dim, page, new, lengths in LARGE:
         cache, table = make_cache(lengths, heads, dim, page)
-        assert division(cache, queries(sum(new), heads * group, dim, BF16), len(new), max(len(t) for t in table), True).rows > 16
+        for dtype in (BF16, F32):
+            rows = division(cache, queries(sum(new), heads * group, dim, dtype), len(new), max(len(t) for t in table), True).rows
+            assert rows == (16 if dim > 128 or (dim > 64 and dtype is F32) else 128 if dim <= 64 else 256)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
