@@ -26,7 +26,7 @@ class _RotateFn(torch.autograd.Function):
         ctx.rotary, ctx.two = rotary, k is not None
         ctx.save_for_backward(positions)
         ctx.set_materialize_grads(False)
-        out = rotary._turn(q, k, positions, False)
+        out = rotary._turn(q, k, positions, 0)
         return out if ctx.two else out[0]
 
     @staticmethod
@@ -38,7 +38,7 @@ class _RotateFn(torch.autograd.Function):
         there = [g for g in want if g is not None]
         if not there:
             return None, None, None, None
-        turned = iter(ctx.rotary._turn(there[0], there[1] if len(there) > 1 else None, positions, True))
+        turned = iter(ctx.rotary._turn(there[0], there[1] if len(there) > 1 else None, positions, 1))
         out = [next(turned) if g is not None else None for g in want]
         return (None, None, out[0], out[1] if ctx.two else None)
 
@@ -75,6 +75,7 @@ class Rotary:
         self.rot, self.layout, self.amplitude = int(rot), layout, float(amplitude)
         self.frequencies = f.clone()
         self._turns = {}                     # device -> turns per position
+        self._plans = {}                     # shapes and type -> descriptors
 
     def _on(self, device):
         t = self._turns.get(device)
@@ -88,67 +89,87 @@ class Rotary:
         self._on(torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device)
         return self
 
-    def _tensor(self, x, y):
-        if x.dim() == 3:
-            return B.RotateTensor(x.data_ptr(), y.data_ptr(), x.stride(0), x.stride(1), y.stride(0), y.stride(1), x.shape[1])
-        heads, dim = x.shape[-2:]
-        return B.RotateTensor(x.data_ptr(), y.data_ptr(), heads * dim, dim, heads * dim, dim, heads)
-
     def _check(self, q, k, positions):
-        kind = _type(q, "q")
-        for t, name in ((q, "q"), (k, "k")):
-            if t is None:
-                continue
-            if t.dim() < 3 or t.dtype is not q.dtype or t.device != q.device or t.shape[:-2] != q.shape[:-2] or t.shape[-1] != q.shape[-1] or t.shape[-2] == 0:
-                raise RuntimeError(f"{name} {tuple(t.shape)} of {t.dtype} on {t.device}: (.., heads, dim) as q, {tuple(q.shape)} of {q.dtype} on {q.device}")
-        if self.rot > q.shape[-1]:
-            raise RuntimeError(f"heads of {q.shape[-1]} values, {self.rot} of them turned")
-        if positions.dtype is not torch.int32 or positions.shape != q.shape[:-2] or positions.device != q.device:
-            raise RuntimeError(f"positions {tuple(positions.shape)} of {positions.dtype} on {positions.device}: int32 {tuple(q.shape[:-2])} on {q.device}")
-        return kind
+        """What calls of these shapes have in common: (descriptor, tokens, pitches and heads of each tensor), looked up after the first."""
+        shape, device = q.shape, q.device
+        if positions.dtype is not torch.int32 or positions.shape != shape[:-2] or positions.device != device:
+            _type(q, "q")
+            raise RuntimeError(f"positions {tuple(positions.shape)} of {positions.dtype} on {positions.device}: int32 {tuple(shape[:-2])} on {device}")
+        kind = q.dtype
+        if k is None:
+            key = shape, kind
+        else:
+            key = shape, kind, k.shape
+            if k.dtype is not kind or k.device != device:
+                raise RuntimeError(f"k of {k.dtype} on {k.device}, q of {kind} on {device}")
+        plan = self._plans.get(key)
+        if plan is None:
+            code = _type(q, "q")
+            for t, name in ((q, "q"), (k, "k")):
+                if t is not None and (t.dim() < 3 or t.shape[:-2] != shape[:-2] or t.shape[-1] != shape[-1] or t.shape[-2] == 0):
+                    raise RuntimeError(f"{name} {tuple(t.shape)}: (.., heads, dim) as q, {tuple(shape)}")
+            if self.rot > shape[-1]:
+                raise RuntimeError(f"heads of {shape[-1]} values, {self.rot} of them turned")
+            tokens = positions.numel()
+            descs = tuple(B.RotateDesc(tokens, shape[-1], self.rot, code, 1 if self.layout == "interleaved" else 0, back, self.amplitude) for back in (0, 1))
+            if len(self._plans) >= 1024:
+                self._plans.clear()
+            plan = self._plans[key] = descs, tokens
+        elif not q.is_cuda:
+            _type(q, "q")
+        return plan
 
-    def _launch(self, kind, pairs, positions, back):
-        first = pairs[0][0]
-        tokens = positions.numel()
-        if tokens == 0:
+    @staticmethod
+    def _tensor(x, y):
+        heads, dim = x.shape[-2:]
+        row = heads * dim
+        if x.dim() == 3:
+            token, head, _ = x.stride()
+            return B.RotateTensor(x.data_ptr(), y.data_ptr(), token, head, *((token, head) if y is x else (row, dim)), heads)
+        return B.RotateTensor(x.data_ptr(), y.data_ptr(), row, dim, row, dim, heads)
+
+    def _launch(self, plan, first, second, positions, back):
+        """first, second: (source, result) each, or None."""
+        if plan[1] == 0:
             return
-        d = B.RotateDesc(tokens, first.shape[-1], self.rot, kind, 1 if self.layout == "interleaved" else 0, 1 if back else 0, self.amplitude)
-        ts = [self._tensor(x, y) for x, y in pairs]
-        _call(first.get_device(), B.lib.int8t_rotate, d, ts[0], ts[1] if len(ts) > 1 else None, positions.contiguous().data_ptr(), self._on(first.device).data_ptr())
+        if not positions.is_contiguous():
+            positions = positions.contiguous()
+        x = first[0]
+        _call(x.get_device(), B.lib.int8t_rotate, plan[0][back], self._tensor(*first), None if second is None else self._tensor(*second), positions.data_ptr(),
+              self._on(x.device).data_ptr())
 
     def _turn(self, q, k, positions, back):
-        kind = self._check(q, k, positions)
-        pairs = []
-        for x in (q, k):
-            if x is not None:
-                if x.stride(-1) != 1 or (x.dim() != 3 and not x.is_contiguous()):
-                    x = x.contiguous()
-                pairs.append((x, torch.empty(x.shape, dtype=x.dtype, device=x.device)))
-        self._launch(kind, pairs, positions, back)
-        return tuple(y for _, y in pairs)
+        plan = self._check(q, k, positions)
+        yq, yk = torch.empty(q.shape, dtype=q.dtype, device=q.device), None
+        if q.stride(-1) != 1 or (q.dim() != 3 and not q.is_contiguous()):
+            q = q.contiguous()
+        if k is not None:
+            if k.stride(-1) != 1 or (k.dim() != 3 and not k.is_contiguous()):
+                k = k.contiguous()
+            yk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        self._launch(plan, (q, yq), None if k is None else (k, yk), positions, back)
+        return (yq,) if k is None else (yq, yk)
 
     def __call__(self, q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor):
         """(q, k) turned, or q alone where k is None: (.., heads, dim) of one type, int32 positions (..).  Differentiable (once)."""
         if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad)):
             return _RotateFn.apply(self, positions, q, k)
-        out = self._turn(q, k, positions, False)
+        out = self._turn(q, k, positions, 0)
         return out if k is not None else out[0]
 
     def turn_(self, q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor) -> None:
         """The same in place, without gradients: q and k (tokens, heads, dim) in any strides whose heads are contiguous, or contiguous (.., heads, dim)."""
-        kind = self._check(q, k, positions)
-        pairs = []
+        plan = self._check(q, k, positions)
         for x in (q, k):
             if x is None:
                 continue
             if x.requires_grad and torch.is_grad_enabled():
                 raise RuntimeError("turn_ has no gradients")
-            if x.stride(-1) != 1 or (x.dim() != 3 and not x.is_contiguous()) or _overlaps(x):
+            if not x.is_contiguous() and (x.stride(-1) != 1 or x.dim() != 3 or _overlaps(x)):
                 raise RuntimeError(f"in place with strides {x.stride()} of {tuple(x.shape)}")
-            pairs.append((x, x))
-        if len(pairs) == 2 and _share(q, k):
+        if k is not None and _share(q, k):
             raise RuntimeError("q and k share memory")
-        self._launch(kind, pairs, positions, False)
+        self._launch(plan, (q, q), None if k is None else (k, k), positions, 0)
 
 
 def _overlaps(x):
@@ -204,6 +225,8 @@ class PageTable:
                 raise RuntimeError(f"{name}: contiguous int32 on {table.device}, not {t.dtype} on {t.device}")
         self._tensors = table, lengths, free, available
         self.page_size, self._index = int(page_size), index
+        self._descs = {}
+        self._at = lengths.data_ptr(), table.data_ptr(), free.data_ptr(), available.data_ptr()
         self.requests, self.width = table.shape
         if self.width * self.page_size > 0x7FFFFFFF:
             raise RuntimeError(f"{self.width} pages of {self.page_size}: fewer than 2^31 tokens")
@@ -220,7 +243,7 @@ class PageTable:
         return cls(torch.full((requests, width), -1, **ints), torch.zeros(requests, **ints), torch.arange(pages - 1, -1, -1, **ints), torch.full((1,), pages, **ints), page_size)
 
     def _desc(self, tokens):
-        return B.PagesDesc(self.requests, self.width, self.page_size, self.free.shape[0], tokens, self.width)
+        return B.PagesDesc(self.requests, self.width, self.page_size, self._tensors[2].shape[0], tokens, self.width)
 
     def _ints(self, t, name):
         if t.dtype is not torch.int32 or t.shape != (self.requests,) or t.get_device() != self._index:
@@ -232,15 +255,23 @@ class PageTable:
         there, whose row of the table is full or whose tokens pass the batch gets none.  Entries of new pages are written into the table; lengths and free pages stay as
         they are until the step is accepted (tokens that are only tried need no more)."""
         new = self._ints(new, "new")
-        tokens = int(tokens)
+        n, tokens = self.requests, int(tokens)
         if tokens < 0:
             raise RuntimeError(f"{tokens} tokens")
-        n = self.requests
-        ints = torch.empty(2 * n + 3 + tokens, dtype=torch.int32, device=self.table.device)
-        lengths, starts, available, without, positions = ints.split([n, n + 1, 1, 1, tokens])
-        slots = torch.empty(tokens, dtype=torch.int64, device=self.table.device)
-        _call(self._index, B.lib.int8t_pages_extend, self._desc(tokens), self.lengths.data_ptr(), new.data_ptr(), self.table.data_ptr(), self.free.data_ptr(),
-              self.available.data_ptr(), lengths.data_ptr(), available.data_ptr(), starts.data_ptr(), slots.data_ptr(), positions.data_ptr(), without.data_ptr())
+        device = new.device
+        ints = torch.empty(3 * tokens + 2 * n + 3, dtype=torch.int32, device=device)          # (slots take two each)
+        slots, positions, lengths, starts, available, without = ints.split((2 * tokens, tokens, n, n + 1, 1, 1))
+        at = ints.data_ptr()
+        first = at + 12 * tokens
+        desc = self._descs.get(tokens)
+        if desc is None:
+            if len(self._descs) >= 1024:
+                self._descs.clear()
+            desc = self._descs[tokens] = self._desc(tokens)
+        lengths_at, table_at, free_at, available_at = self._at
+        _call(self._index, B.lib.int8t_pages_extend, desc, lengths_at, new.data_ptr(), table_at, free_at, available_at, first, first + 8 * n + 4, first + 4 * n, at, at + 8 * tokens,
+              first + 8 * n + 8)
+        slots = slots.view(torch.int64)
         return PageStep(lengths, available, starts, slots, positions, without)
 
     def accept(self, step: PageStep) -> None:
