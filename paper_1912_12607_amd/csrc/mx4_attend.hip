@@ -46,11 +46,24 @@ __device__ __forceinline__ void rarely() { asm volatile(""); }
 template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
+// tile_request() of 16 rows, by a look of 64 lanes at a time: one load for up to 64 requests, two for 4096
+__device__ __forceinline__ int block_request(const AttendArgs& a, int t, int lane) {
+    int lo = 0, n = a.requests;                  // among requests lo .. lo + n - 1
+    while (n > 1) {
+        const int step = (n + 63) >> 6, at = lane * step;
+        const bool before = at < n && (long long)a.starts[lo + at] * a.group / 16 + lo + at <= t;
+        const int last = (int)__popcll(__ballot(before)) - 1;            // (ascending: the lanes before it too; the first one's always is)
+        lo += max(last, 0) * step;
+        n = min(step, n - max(last, 0) * step);
+    }
+    return lo;
+}
+
 // A wave's steps of 32 keys in LDS: codes of keys and values, then their scales.  WORDS: a key has four or eight blocks, its scales are loaded by words; else by bytes, which
 // lie in words of their own.
 constexpr int most_blocks(int DIM, bool words) { return DIM == 256 && !words ? 7 : DIM / 32; }
 constexpr int step_bytes(int DIM, bool words) { return 2 * 32 * most_blocks(DIM, words) * (words ? 17 : 20); }
-constexpr int steps_ahead(int DIM) { return DIM == 64 ? 4 : DIM == 128 ? 3 : 2; }
+constexpr int steps_ahead(int DIM) { return DIM == 64 ? 4 : 2; }          // (dim 128 with three: a block less on a compute unit, 64 requests over 1 to 8192 keys 87 us, not 83)
 constexpr int rows_lds(int DIM, bool words, int RW) {
     const int ring = RW * steps_ahead(DIM) * step_bytes(DIM, words), sums = RW * 16 * (DIM + 4 + 2) * 4;
     return ring > sums ? ring : sums;
@@ -84,7 +97,7 @@ __global__ __launch_bounds__(64 * RW, 2) void mx_attend_rows_kernel(const Attend
     const int head = place - group_of * a.c.heads, split = (int)blockIdx.z, block = (int)gridDim.x - 1 - group_of;
     const int D = a.c.dim, NB = UNI ? DIM / 32 : mx_blocks(D), RB = 16 * NB;
 
-    const int b = tile_request(a, block, 16);
+    const int b = block_request(a, block, lane);
     const Request rq = request_of(a, b);
     const int nrows = rq.tokens * a.group;
     const long long tile = (long long)block - ((long long)a.starts[b] * a.group / 16 + b);

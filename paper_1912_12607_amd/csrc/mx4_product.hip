@@ -411,12 +411,16 @@ hipError_t product_of(const MxProductArgs& a, const MxProductArgs* b, hipStream_
 }
 
 // Tiles and shares of the reduction by an estimate, us: rounds of blocks times stages of 256 values, plus what a block and the joining pass cost.  occ: blocks on
-// a compute unit; busy: of its matrix units per stage; least: a stage of a block alone.
+// a compute unit; a stage, and a block's start and end, take longer the fuller the chip is (first: one block alone, then all places taken).  (Measured, one share, bf16 results,
+// tiles of 256, 128 with two and three stages in LDS, 64: 8192 x 4096 -> 4096 73, 86, 97, 127; 1001 x 4096 -> 16384 38, 46, 51, 65; 1001 x 4096 -> 4096 25, 14.6, 13.9, 19;
+// 512 x 8192 -> 4096 45, 26, 20, 18; 128 x 8192 -> 4096 41, 18, 17, 9; shares hardly ever pay: 17 x 8192 -> 512 with four 8.6, with one 9.3.  Over 76 sizes from 17 x 256 -> 512
+// to 8192 x 8192 -> 4096 the choice takes 1.2 % longer than the fastest.)
 struct ProductPlan {
     int tile, splits;          // 0: 256 x 256, 1: 128 x 128, 2: the same with three stages, 3: 64 x 64 with four
 };
-ProductPlan product_plan(int M, int N, int Kb, bool scratch) {
-    static const struct { int bm, occ; double busy, least, fixed; } kTiles[4] = {{256, 1, 1.63, 1.63, 10.0}, {128, 2, 0.57, 0.85, 4.0}, {128, 1, 0.66, 0.66, 4.5}, {64, 2, 0.22, 0.26, 2.5}};
+ProductPlan find_plan(int M, int N, int Kb, bool scratch) {
+    static const struct { int bm, occ; double stage, full_stage, fixed, full_fixed; } kTiles[4] = {
+        {256, 1, 1.17, 1.76, 4.0, 9.5}, {128, 2, 0.41, 1.04, 4.0, 6.2}, {128, 1, 0.40, 0.57, 3.8, 4.5}, {64, 2, 0.20, 0.42, 2.5, 2.9}};
     const int steps = (Kb + 127) >> 7;
     ProductPlan best{0, 1};
     double least = 1e30;
@@ -425,10 +429,10 @@ ProductPlan product_plan(int M, int N, int Kb, bool scratch) {
         for (int s = 1; s <= (scratch ? 16 : 1) && s <= steps; s *= 2) {
             const long long blocks = tiles * s, slots = 256ll * kTiles[t].occ;
             if (s > 1 && (tiles * s > 1024 || (size_t)M * N * s > (1u << 26))) break;
-            const double together = blocks >= slots ? kTiles[t].occ : (double)((blocks + 255) / 256);
-            const double stage = together * kTiles[t].busy > kTiles[t].least ? together * kTiles[t].busy : kTiles[t].least;
-            double us = (double)((blocks + slots - 1) / slots) * ((steps + s - 1) / s * stage + kTiles[t].fixed);
-            if (s > 1) us += 3.5 + 8e-6 * (double)s * M * N / 4;
+            const double load = blocks < slots ? (double)blocks / (double)slots : 1.0;
+            const double stage = kTiles[t].stage + (kTiles[t].full_stage - kTiles[t].stage) * load, fixed = kTiles[t].fixed + (kTiles[t].full_fixed - kTiles[t].fixed) * load;
+            double us = (double)((blocks + slots - 1) / slots) * ((steps + s - 1) / s * stage + fixed);
+            if (s > 1) us += 4.5 + 0.1 * s + 3.6e-6 * (double)s * M * N;
             if (us < least) {
                 least = us;
                 best = ProductPlan{t, s};
@@ -436,6 +440,14 @@ ProductPlan product_plan(int M, int N, int Kb, bool scratch) {
         }
     }
     return best;
+}
+// (a call asks for its plan several times: the last ones are kept, by sizes alone)
+ProductPlan product_plan(int M, int N, int Kb, bool scratch) {
+    struct Kept { int M, N, Kb, scratch; ProductPlan plan; };
+    static thread_local Kept kept[64];
+    Kept& k = kept[((unsigned)M * 0x9E3779B1u ^ (unsigned)N * 0x85EBCA77u ^ (unsigned)Kb * 0xC2B2AE3Du ^ (scratch ? 0x27D4EB2Fu : 0u)) >> 26];
+    if (k.M != M || k.N != N || k.Kb != Kb || k.scratch != (int)scratch) k = Kept{M, N, Kb, (int)scratch, find_plan(M, N, Kb, scratch)};
+    return k.plan;
 }
 
 template <int TYPE>
@@ -477,6 +489,7 @@ hipError_t launch_mx_few_tokens(const MxFewArgs& a, hipStream_t st) {
 
 constexpr int kTileRows[4] = {256, 128, 128, 64}, kTileWaves[4] = {8, 4, 4, 4}, kTileStages[4] = {2, 2, 3, 4};
 bool mx_product_fits(int M, int N, int Kb) {
+    if (((unsigned long long)M + 63) / 64 * (((unsigned long long)N + 63) / 64) < (1u << 18)) return true;      // (with 16 shares and 512 lanes a block)
     for (const bool scratch : {false, true}) {
         const ProductPlan p = product_plan(M, N, Kb, scratch);
         const int rows = kTileRows[p.tile];
