@@ -724,7 +724,7 @@ typedef struct int8t_mx4_linear_buffers {
     void *ws;
     size_t ws_bytes;
 } int8t_mx4_linear_buffers;
-/* direction: 0 forward, 1 backward, 2 forward with w NULL that keeps nothing */
+/* direction: 0 forward, 1 backward, 2 forward with w and xt NULL */
 size_t int8t_mx4_linear_workspace_bytes(const int8t_linear_desc *desc, int direction);
 int8t_status int8t_mx4_linear_fwd(const int8t_linear_desc *desc, const int8t_mx4_linear_buffers *b, void *stream);
 int8t_status int8t_mx4_linear_bwd(const int8t_linear_desc *desc, const int8t_mx4_linear_buffers *b, uint64_t seed, void *stream);

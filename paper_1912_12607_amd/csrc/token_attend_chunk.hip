@@ -49,11 +49,17 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
     return v;
 }
 
+// bf16 tensors' keys keep their scales -- bf16 has the range, and q is exact in it --, so that scores need no factor of a key (two chunks of 2048 tokens over 8192 keys
+// 600 -> 579 us); values, whose weights need more bits than bf16's, are fp16 in either case.
+constexpr bool whole_keys(int type, bool mx) { return mx && type == kBF16; }
+typedef __bf16 tc_b8 __attribute__((ext_vector_type(8)));
+
 // UNI: the keys whose pieces a wave loads at a time lie on one page (its size is a multiple of 1024 / DIM): addresses are scalar.
 template <int TYPE, int DIM, int NW, bool UNI, bool MX>
 __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && TYPE == kF32)) ? 1 : 2) void attend_chunk_kernel(const AttendArgs a) {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int PARTS = TYPE == kF32 ? 2 : 1, NT = 64 * NW, ROWS = 32 * NW;
+    constexpr bool WHOLE = whole_keys(TYPE, MX);               // keys in LDS are bf16 with their scales, and q as it is
     constexpr int QS = DIM / 16, DT = DIM / 32;                // steps of the scores' products; tiles of dims
     constexpr int CH = 4 * DIM;                                // 16-byte pieces of a tile of codes
     constexpr int NP = CH / NT;                                // pieces of either tensor per thread
@@ -106,14 +112,18 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
             for (int u = 0; u < 8; ++u) m = fmaxf(m, fabsf(v[i][u]));
         }
         m = halves_max(m);
-        float back;
-        float up = row_scale(m, &back);
+        float back = 1.0f;
+        float up = WHOLE ? 1.0f : row_scale(m, &back);
         qscale = score_scale(a.scale, back, &up);
 #pragma unroll
         for (int i = 0; i < QS; ++i)
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const float t = v[i][u] * up;
+                if constexpr (WHOLE) {           // (bf16's bits, in the same registers)
+                    qf[0][i][u] = __builtin_bit_cast(_Float16, (__bf16)t);
+                    continue;
+                }
                 _Float16 first = (_Float16)t, rest;
                 if (PARTS == 2) {
                     two_pieces(t, &first, &rest);
@@ -184,6 +194,20 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
             *hi = make_uint4(codes_f16<kLowPair>(w[2]), codes_f16<kHighPair>(w[2]), codes_f16<kLowPair>(w[3]), codes_f16<kHighPair>(w[3]));
         }
     };
+    auto expand_key = [&](const auto& c, const auto& scale, uint4* lo, uint4* hi, float* row) __attribute__((always_inline)) {
+        if constexpr (WHOLE) {
+            const float up = mx_power(scale);
+            const auto pair = [up](uint32_t w, auto sel) __attribute__((always_inline)) {
+                return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, up, decltype(sel)::value));
+            };
+            typedef std::integral_constant<int, 0> B0; typedef std::integral_constant<int, 1> B1; typedef std::integral_constant<int, 2> B2; typedef std::integral_constant<int, 3> B3;
+            *lo = make_uint4(pair(c.x, B0()), pair(c.x, B1()), pair(c.x, B2()), pair(c.x, B3()));
+            *hi = make_uint4(pair(c.y, B0()), pair(c.y, B1()), pair(c.y, B2()), pair(c.y, B3()));
+            *row = 1.0f;
+        } else {
+            expand(c, scale, lo, hi, row);
+        }
+    };
     auto stage = [&](int kslot, int vslot, int sslot) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
@@ -191,14 +215,14 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
             uint4 lo, hi;
             float* const s = sc + sslot * 3 * TK;
             float ks, vs;
-            expand(rk[p], rks[p], &lo, &hi, &ks);
+            expand_key(rk[p], rks[p], &lo, &hi, &ks);
             sk[kslot * TILE + k_slot<DIM>(key, g)] = lo;
             sk[kslot * TILE + k_slot<DIM>(key, g + 1)] = hi;
             expand(rv[p], rvs[p], &lo, &hi, &vs);
             sv[vslot * TILE + v_slot<DIM>(key, g)] = lo;
             sv[vslot * TILE + v_slot<DIM>(key, g + 1)] = hi;
             if (g == 0) {
-                s[key] = rok[p] ? ks : 0.0f;
+                if (!WHOLE) s[key] = rok[p] ? ks : 0.0f;
                 s[TK + key] = rok[p] ? vs : 0.0f;
                 s[2 * TK + key] = rok[p] ? 0.0f : kNone;
             }
@@ -260,7 +284,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
 #pragma unroll
             for (int i = 0; i < QS; ++i) {
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p) x[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[i], qf[p][i], x[kt], 0, 0, 0);
+                for (int p = 0; p < PARTS; ++p) {
+                    if constexpr (WHOLE) x[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(tc_b8, kf[i]), __builtin_bit_cast(tc_b8, qf[p][i]), x[kt], 0, 0, 0);
+                    else x[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[i], qf[p][i], x[kt], 0, 0, 0);
+                }
                 if (kt == 0) kf[i] = keys_at(kslot, 1, i);
             }
             if (kt == 0 && PARTS == 1) first_values(vslot);
@@ -275,14 +302,16 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
         const float* const s = sc + sslot * 3 * TK;
         // times the keys' scales; the tile's last keys and those behind a row's own
         const bool masked = (t + 1) * TK > all || __any(s[2 * TK + lane] != 0.0f);
+        if constexpr (!WHOLE) {
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+            for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const tk_f4 ks = *reinterpret_cast<const tk_f4*>(s + kt * 32 + 8 * q + 4 * half);
+                for (int q = 0; q < 4; ++q) {
+                    const tk_f4 ks = *reinterpret_cast<const tk_f4*>(s + kt * 32 + 8 * q + 4 * half);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[kt][4 * q + i] *= ks[i];
-            }
+                    for (int i = 0; i < 4; ++i) x[kt][4 * q + i] *= ks[i];
+                }
+        }
         if (masked) {
             const int left = limit - t * TK - 4 * half;
 #pragma unroll

@@ -126,7 +126,9 @@ class _Linear4Fn(torch.autograd.Function):
         kept = None
         if M:
             b = B.Mx4LinearBuffers()
-            want_x, want_w = ctx.needs_input_grad[:2]
+            want_x, want_w, want_b = ctx.needs_input_grad[:3]
+            if (want_x or want_w or want_b) and not later:
+                raise RuntimeError(f"{M} tokens, {K} inputs, {N} outputs: a backward pass of that size is not served")
             if want_x or want_w:
                 kept = torch.empty(size, dtype=torch.uint8, device=dev)
                 at = kept.data_ptr()

@@ -170,6 +170,9 @@ class Rotary:
         if k is not None and _share(q, k):
             raise RuntimeError("q and k share memory")
         self._launch(plan, (q, q), None if k is None else (k, k), positions, 0)
+        for x in (q, k):                         # (a graph that has kept one of them for its backward pass will notice)
+            if x is not None:
+                torch.autograd.graph.increment_version(x)
 
 
 def _overlaps(x):

@@ -183,6 +183,35 @@ def test_linear_of_no_tokens_single_gradients_and_broadcast_ones():
     assert torch.equal(torch.autograd.grad(y, w)[0], parts[0] + parts[1])
 
 
+@pytest.mark.parametrize("M", [1, 3, 40])
+def test_weights_laid_out_and_tokens_kept(M):
+    """Through the binding: codes of W that are there, codes of x kept for dw (few tokens too)."""
+    K, N = 70, 50
+    (x, x64), (w, w64), (g, g64) = values((M, K), 1), values((N, K), 2), values((M, N), 3)
+    layer = fourbit.ServedLinear4.of(w.to(DEV))
+    xd, gd = x.to(DEV), g.to(DEV)
+    xt, sxt = torch.zeros(K, 16 * R.blocks_of(M), dtype=torch.uint8, device=DEV), torch.zeros(R.panels_of(M), K, 8, dtype=torch.uint8, device=DEV)
+    y, dw = torch.empty(M, N, device=DEV), torch.empty(N, K, device=DEV)
+    d = B.LinearDesc(M, K, N, B.F32, B.F32)
+    b = B.Mx4LinearBuffers.from_buffer_copy(layer._b)
+    b.x, b.x_pitch, b.y, b.y_pitch, b.xt, b.sxt, b.dy, b.dy_pitch, b.dw = xd.data_ptr(), K, y.data_ptr(), N, xt.data_ptr(), sxt.data_ptr(), gd.data_ptr(), N, dw.data_ptr()
+    ws = torch.empty(max(B.int8t_mx4_linear_workspace_bytes(d, i) for i in (0, 1)), dtype=torch.uint8, device=DEV)
+    b.ws, b.ws_bytes = ws.data_ptr(), ws.numel()
+    B.int8t_mx4_linear_fwd(d, b)
+    B.int8t_mx4_linear_bwd(d, b, 9)
+    near(y, R.rounded(x64), R.rounded(w64), F32)
+    near(dw, _drawn(g64, 9)[1], R.rounded(x64.T), F32)
+
+
+def test_more_tokens_than_a_backward_pass_takes_are_refused_before_it():
+    x, w = torch.zeros(131073, 1, device=DEV), torch.zeros(1, 1, device=DEV)
+    b = torch.zeros(1, device=DEV)
+    assert fourbit.linear4(x, w, b).shape == (131073, 1)
+    for args in ((x, w.clone().requires_grad_(True), b), (x, w, b.clone().requires_grad_(True))):
+        with pytest.raises(RuntimeError, match="not served"):
+            fourbit.linear4(*args)
+
+
 def test_gradients_of_what_is_not_finite():
     """NaN in the gradient of one token: its dx, and dw and db of its output; in fp16 training a program sees the overflow."""
     (x, _), (w, _), (g, _) = values((40, 50), 1), values((30, 50), 2), values((40, 30), 3)

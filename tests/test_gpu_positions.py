@@ -153,6 +153,16 @@ def test_rotary_of_strides_dimensions_and_nothing():
     assert y.shape == (0, 3, 64) and torch.autograd.grad(y, none, torch.zeros_like(y))[0].shape == (0, 3, 64)
 
 
+def test_turning_in_place_what_a_graph_has_kept_is_noticed():
+    x = normal((3, 2, 16), 1, F32).requires_grad_(True)
+    h = x * 2.0
+    y = h * h                                            # keeps h
+    with torch.no_grad():
+        Rotary(16).turn_(h, None, torch.arange(3, dtype=torch.int32, device=DEV))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+
+
 def test_rotary_of_what_is_not_finite():
     q = normal((3, 2, 16), 1, F32)
     q[1, 1, 2] = float("nan")
