@@ -24,6 +24,8 @@ __device__ __forceinline__ uint32_t mx_byte_of(float m) {
 __device__ __forceinline__ float mx_power(uint32_t byte) {
     return __uint_as_float(byte == 255u ? 0x7fc00000u : byte == 0u ? 0x00400000u : byte << 23);
 }
+// The same of 0 .. 254, in two operations (254 itself is not a quantiser's)
+__device__ __forceinline__ float mx_scale(uint32_t byte) { return __uint_as_float(max(byte << 23, 0x00400000u)); }
 // Two values as codes in byte SEL of `into`, to the nearest (ties to even): x / scale, scale 2^e
 template <int SEL>
 __device__ __forceinline__ uint32_t mx_pair(uint32_t into, float x0, float x1, float scale) {
@@ -44,11 +46,18 @@ __device__ __forceinline__ void mx_values8(uint32_t w, float v[8]) {
     v[4] = c[0]; v[5] = c[1]; v[6] = d[0]; v[7] = d[1];
 }
 // One code drawn: the magnitude in units of 2^-22 of a step -- below 1 steps are .5, from there on a float's bits count them, two steps to each power of
-// two -- plus 22 bits of the draw.  inv: 2^-e; |x| inv <= 6 exactly.
-__device__ __forceinline__ uint32_t mx_drawn(float x, float inv, uint32_t draw24) {
+// two -- plus the upper 22 bits of a word drawn.  |x| inv <= 6 exactly, inv 2^-e.  The bits of a + max(a, 1) are the count in either range, if the sum is rounded toward zero:
+// draws_begin() switches the wave to that, and gives the 1 that keeps the sums behind it.
+__device__ __forceinline__ float draws_begin() {
+    float one = 1.0f;
+    asm volatile("s_setreg_imm32_b32 hwreg(HW_REG_MODE, 0, 2), 3\n\ts_nop 3" : "+v"(one)::"memory");
+    return one;
+}
+__device__ __forceinline__ void draws_end() { asm volatile("s_setreg_imm32_b32 hwreg(HW_REG_MODE, 0, 2), 0\n\ts_nop 3" ::: "memory"); }
+__device__ __forceinline__ uint32_t mx_drawn(float x, float inv, float one, uint32_t draw32) {
     const float a = __fmul_rn(fabsf(x), inv);
-    const uint32_t fixed = a < 1.0f ? (uint32_t)__fmul_rn(a, 8388608.0f) : __float_as_uint(a) - (126u << 23);
-    return (fixed + (draw24 >> 2)) >> 22 | (__float_as_uint(x) >> 28 & 8u);
+    const uint32_t count = __float_as_uint(a + fmaxf(a, one)) + (draw32 >> 10) - (127u << 23);
+    return count >> 22 | (__float_as_uint(x) >> 28 & 8u);
 }
 // 2^-e from 2^e's byte (0 .. 253)
 __device__ __forceinline__ float mx_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }

@@ -1,8 +1,13 @@
 // Microscaled 4-bit codes of matrices: blocks along the rows' values, or along the columns' with the codes transposed, or both from one pass.
+#include <type_traits>
+
 #include "mx4.h"
 
 namespace int8t {
 namespace {
+
+// The word whose upper 24 bits are rng24()
+__device__ __forceinline__ uint32_t draw32(uint32_t key_x, uint32_t key_a, uint32_t index) { return rng_mix32((index ^ key_x) + key_a); }
 
 // Four neighbouring lanes have a block, eight values each; their largest goes round by lane exchanges of a quad.  Rows are lanes in whole panels (256
 // values), so that the scales behind the last block are written (zeros).
@@ -26,18 +31,16 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(const MxArgs a, const Fast
     if ((g & 3) == 0) a.s[((size_t)(block >> 3) * a.rows + row) * 8 + (block & 7)] = block < blocks ? (uint8_t)byte : (uint8_t)0;
     if (block >= blocks) return;
     uint32_t w = 0;
-    if (byte < 255u) {
-        if (STOCH) {
-            const float inv = mx_inverse(byte);
-            const uint32_t index = (uint32_t)row * (uint32_t)a.cols + (uint32_t)c;
+    if (STOCH) {
+        const float inv = mx_inverse(byte), one = draws_begin();
+        const uint32_t index = (uint32_t)row * (uint32_t)a.cols + (uint32_t)c;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w |= mx_drawn(v[i], inv, rng24(kx, ka, index + (uint32_t)i)) << (4 * i);
-            // (values behind the row are zero and stay zero: a draw alone does not reach a step)
-        } else {
-            w = mx_codes8(v, mx_power(byte));
-        }
+        for (int i = 0; i < 8; ++i) w |= mx_drawn(v[i], inv, one, draw32(kx, ka, index + (uint32_t)i)) << (4 * i);
+        // (values behind the row are zero and stay zero: a draw alone does not reach a step)
+    } else {
+        w = mx_codes8(v, mx_scale(byte));
     }
-    *reinterpret_cast<uint32_t*>(a.q + (size_t)row * (16 * blocks) + 4 * g) = w;
+    *reinterpret_cast<uint32_t*>(a.q + (size_t)row * (16 * blocks) + 4 * g) = byte < 255u ? w : 0u;
 }
 
 // Both directions from one pass: tiles of 256 rows by 128 bytes (64 columns, 32 of fp32), a lane has eight rows of 16 bytes, four lanes above each other a block of
@@ -56,13 +59,15 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const int block, cons
     if ((block >> 3) >= per || tile >= total) return;
     const int row0 = tile / tiles_c * QT_R, col0 = (tile - tile / tiles_c * tiles_c) * TC;
     const int row = row0 + 8 * rg, col = col0 + cg * C;
-    T v[8][C];
-    {
+    // (a tile inside of the matrix needs no look at its ends)
+    const auto tile_of = [&](auto inside) __attribute__((always_inline)) {
+        constexpr bool IN = decltype(inside)::value;
+        T v[8][C];
         const T* const x = static_cast<const T*>(a.x);
-        const bool whole = wide && col + C <= a.cols;
+        const bool whole = IN || (wide && col + C <= a.cols);
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-            const bool in = row + r < a.rows;
+            const bool in = IN || row + r < a.rows;
             const T* const at = x + (size_t)(in ? row + r : 0) * a.pitch + col;
             if (whole) {
                 typedef T V __attribute__((ext_vector_type(C)));
@@ -74,54 +79,12 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const int block, cons
                 for (int j = 0; j < C; ++j) v[r][j] = in && col + j < a.cols ? at[j] : (T)0.0f;
             }
         }
-    }
-    if (a.q) {
-        const int block_c = col >> 5, blocks = mx_blocks(a.cols);
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            float m = 0.0f, f[8];
+        if (a.sum) {
 #pragma unroll
             for (int j = 0; j < C; ++j) {
-                f[j] = (float)v[r][j];
-                m = most(m, fabsf(f[j]));
-            }
-            m = most(m, dpp_of<kDppSwap1>(m));
-            m = most(m, dpp_of<kDppSwap2>(m));
-            if (C == 4) m = most(m, dpp_of<0x141>(m));             // (row_half_mirror: the quads of eight lanes)
-            const uint32_t byte = mx_byte_of(m);
-            uint32_t w = 0;
-            if (byte < 255u) {
-                if (STOCH) {
-                    const float inv = mx_inverse(byte);
+                float sum = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < C; ++j) w |= mx_drawn(f[j], inv, rng24(kx, ka, (uint32_t)(row + r) * (uint32_t)a.cols + (uint32_t)(col + j))) << (4 * j);
-                } else {
-#pragma unroll
-                    for (int j = C; j < 8; ++j) f[j] = 0.0f;
-                    w = mx_codes8(f, mx_power(byte));
-                }
-            }
-            if (row + r < a.rows && block_c < blocks) {
-                uint8_t* const q = a.q + (size_t)(row + r) * (16 * blocks) + col / 2;
-                if (C == 8) *reinterpret_cast<uint32_t*>(q) = w;
-                else *reinterpret_cast<uint16_t*>(q) = (uint16_t)w;
-                if ((col & 31) == 0) a.s[((size_t)(block_c >> 3) * a.rows + row + r) * 8 + (block_c & 7)] = (uint8_t)byte;
-            }
-            // (behind the last block, the rest of its panel)
-            if (row + r < a.rows && block_c >= blocks && block_c < ((blocks + 7) & ~7) && (col & 31) == 0) a.s[((size_t)(block_c >> 3) * a.rows + row + r) * 8 + (block_c & 7)] = 0;
-        }
-    }
-    if (a.qt || a.sum) {
-#pragma unroll
-        for (int j = 0; j < C; ++j) {
-            float m = 0.0f, sum = 0.0f, f[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                f[r] = (float)v[r][j];
-                m = most(m, fabsf(f[r]));
-                sum += f[r];
-            }
-            if (a.sum) {
+                for (int r = 0; r < 8; ++r) sum += (float)v[r][j];
                 sum += dpp_of<kDppRor8>(sum);
                 const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
                 sum = __uint_as_float(b[0]) + __uint_as_float(b[1]);
@@ -129,24 +92,75 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const int block, cons
                 sum = __uint_as_float(h[0]) + __uint_as_float(h[1]);
                 if (lane < 8) sums[wave][cg * C + j] = sum;
             }
-            if (!a.qt) continue;
-            m = most(m, dpp_of<kDppRor8>(m));
-            const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-            m = most(__uint_as_float(b[0]), __uint_as_float(b[1]));
-            const uint32_t byte = mx_byte_of(m);
-            uint32_t w = 0;
-            if (byte < 255u) {
+        }
+        float one = 1.0f;
+        if (STOCH) one = draws_begin();
+        if (a.q) {
+            const int block_c = col >> 5, blocks = mx_blocks(a.cols);
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                float m = 0.0f, f[8];
+#pragma unroll
+                for (int j = 0; j < C; ++j) {
+                    f[j] = (float)v[r][j];
+                    m = most(m, fabsf(f[j]));
+                }
+                m = most(m, dpp_of<kDppSwap1>(m));
+                m = most(m, dpp_of<kDppSwap2>(m));
+                if (C == 4) m = most(m, dpp_of<0x141>(m));             // (row_half_mirror: the quads of eight lanes)
+                const uint32_t byte = mx_byte_of(m);
+                uint32_t w = 0;
                 if (STOCH) {
                     const float inv = mx_inverse(byte);
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) w |= mx_drawn(f[r], inv, rng24(tx, ta, (uint32_t)(row + r) * (uint32_t)a.cols + (uint32_t)(col + j))) << (4 * r);
+                    for (int j = 0; j < C; ++j) w |= mx_drawn(f[j], inv, one, draw32(kx, ka, (uint32_t)(row + r) * (uint32_t)a.cols + (uint32_t)(col + j))) << (4 * j);
                 } else {
-                    w = mx_codes8(f, mx_power(byte));
+#pragma unroll
+                    for (int j = C; j < 8; ++j) f[j] = 0.0f;
+                    w = mx_codes8(f, mx_scale(byte));
                 }
+                w = byte < 255u ? w : 0u;
+                if (IN || (row + r < a.rows && block_c < blocks)) {
+                    uint8_t* const q = a.q + (size_t)(row + r) * (16 * blocks) + col / 2;
+                    if (C == 8) *reinterpret_cast<uint32_t*>(q) = w;
+                    else *reinterpret_cast<uint16_t*>(q) = (uint16_t)w;
+                    if ((col & 31) == 0) a.s[((size_t)(block_c >> 3) * a.rows + row + r) * 8 + (block_c & 7)] = (uint8_t)byte;
+                }
+                // (behind the last block, the rest of its panel)
+                if (!IN && row + r < a.rows && block_c >= blocks && block_c < ((blocks + 7) & ~7) && (col & 31) == 0)
+                    a.s[((size_t)(block_c >> 3) * a.rows + row + r) * 8 + (block_c & 7)] = 0;
             }
-            *reinterpret_cast<uint32_t*>(turned + (cg * C + j) * QT_PITCH + 4 * rg) = w;
-            if ((rg & 3) == 0) turned_s[(cg * C + j) * 8 + (rg >> 2)] = (uint8_t)byte;
         }
+        if (a.qt) {
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                float m = 0.0f, f[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    f[r] = (float)v[r][j];
+                    m = most(m, fabsf(f[r]));
+                }
+                m = most(m, dpp_of<kDppRor8>(m));
+                const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+                m = most(__uint_as_float(b[0]), __uint_as_float(b[1]));
+                const uint32_t byte = mx_byte_of(m);
+                uint32_t w = 0;
+                if (STOCH) {
+                    const float inv = mx_inverse(byte);
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) w |= mx_drawn(f[r], inv, one, draw32(tx, ta, (uint32_t)(row + r) * (uint32_t)a.cols + (uint32_t)(col + j))) << (4 * r);
+                } else {
+                    w = mx_codes8(f, mx_scale(byte));
+                }
+                *reinterpret_cast<uint32_t*>(turned + (cg * C + j) * QT_PITCH + 4 * rg) = byte < 255u ? w : 0u;
+                if ((rg & 3) == 0) turned_s[(cg * C + j) * 8 + (rg >> 2)] = (uint8_t)byte;
+            }
+        }
+        if (STOCH) draws_end();
+    };
+    if (wide && row0 + QT_R <= a.rows && col0 + TC <= a.cols) tile_of(std::true_type());
+    else tile_of(std::false_type());
+    if (a.qt || a.sum) {
         __syncthreads();
         if (a.qt) {
             const int blocks = mx_blocks(a.rows), b0 = row0 >> 5;
