@@ -45,19 +45,22 @@ __device__ __forceinline__ void mx_values8(uint32_t w, float v[8]) {
     v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1];
     v[4] = c[0]; v[5] = c[1]; v[6] = d[0]; v[7] = d[1];
 }
-// One code drawn: the magnitude in units of 2^-22 of a step -- below 1 steps are .5, from there on a float's bits count them, two steps to each power of
-// two -- plus the upper 22 bits of a word drawn.  |x| inv <= 6 exactly, inv 2^-e.  The bits of a + max(a, 1) are the count in either range, if the sum is rounded toward zero:
-// draws_begin() switches the wave to that, and gives the 1 that keeps the sums behind it.
+// Codes drawn: a magnitude counts 2^-22 of a step -- below 1 steps are .5, from there on a float's bits count them, two steps to each power of two --, the upper 22
+// bits of a word drawn are added, and what is whole is the code.  |x| inv <= 6 exactly, inv 2^-e.  The bits of a + max(a, 1) are that count in either range, if the sum is
+// rounded toward zero: draws_begin() switches the wave to that, and gives the 1 that keeps the sums behind it.
 __device__ __forceinline__ float draws_begin() {
     float one = 1.0f;
     asm volatile("s_setreg_imm32_b32 hwreg(HW_REG_MODE, 0, 2), 3\n\ts_nop 3" : "+v"(one)::"memory");
     return one;
 }
 __device__ __forceinline__ void draws_end() { asm volatile("s_setreg_imm32_b32 hwreg(HW_REG_MODE, 0, 2), 0\n\ts_nop 3" ::: "memory"); }
-__device__ __forceinline__ uint32_t mx_drawn(float x, float inv, float one, uint32_t draw32) {
+// w shifted up by one code, and x's below: the count 64 times in a word, where the draw's lower bits reach nothing, and 127's bits by the 2 above the draw
+__device__ __forceinline__ uint32_t mx_drawn(uint32_t w, float x, float inv, float one, uint32_t draw32) {
     const float a = __fmul_rn(fabsf(x), inv);
-    const uint32_t count = __float_as_uint(a + fmaxf(a, one)) + (draw32 >> 10) - (127u << 23);
-    return count >> 22 | (__float_as_uint(x) >> 28 & 8u);
+    const uint32_t count = (__float_as_uint(a + fmaxf(a, one)) << 6) + __builtin_amdgcn_alignbit(2u, draw32, 4);
+    uint32_t top;
+    asm("v_bfi_b32 %0, %1, %2, %3" : "=v"(top) : "s"(0x7fffffffu), "v"(count), "v"(x));      // (left to itself, the compiler masks both)
+    return __builtin_amdgcn_alignbit(w, top, 28);
 }
 // 2^-e from 2^e's byte (0 .. 253)
 __device__ __forceinline__ float mx_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }

@@ -7,7 +7,11 @@ namespace int8t {
 namespace {
 
 // The word whose upper 24 bits are rng24()
-__device__ __forceinline__ uint32_t draw32(uint32_t key_x, uint32_t key_a, uint32_t index) { return rng_mix32((index ^ key_x) + key_a); }
+__device__ __forceinline__ uint32_t draw32(uint32_t key_x, uint32_t key_a, uint32_t index) {
+    uint32_t at;
+    asm("v_xad_u32 %0, %1, %2, %3" : "=v"(at) : "v"(index), "v"(key_x), "s"(key_a));
+    return rng_mix32(at);
+}
 
 // Four neighbouring lanes have a block, eight values each; their largest goes round by lane exchanges of a quad.  Rows are lanes in whole panels (256
 // values), so that the scales behind the last block are written (zeros).
@@ -35,7 +39,7 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(const MxArgs a, const Fast
         const float inv = mx_inverse(byte), one = draws_begin();
         const uint32_t index = (uint32_t)row * (uint32_t)a.cols + (uint32_t)c;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w |= mx_drawn(v[i], inv, one, draw32(kx, ka, index + (uint32_t)i)) << (4 * i);
+        for (int i = 7; i >= 0; --i) w = mx_drawn(w, v[i], inv, one, draw32(kx, ka, index + (uint32_t)i));
         // (values behind the row are zero and stay zero: a draw alone does not reach a step)
     } else {
         w = mx_codes8(v, mx_scale(byte));
@@ -113,7 +117,7 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const int block, cons
                 if (STOCH) {
                     const float inv = mx_inverse(byte);
 #pragma unroll
-                    for (int j = 0; j < C; ++j) w |= mx_drawn(f[j], inv, one, draw32(kx, ka, (uint32_t)(row + r) * (uint32_t)a.cols + (uint32_t)(col + j))) << (4 * j);
+                    for (int j = C - 1; j >= 0; --j) w = mx_drawn(w, f[j], inv, one, draw32(kx, ka, (uint32_t)(row + r) * (uint32_t)a.cols + (uint32_t)(col + j)));
                 } else {
 #pragma unroll
                     for (int j = C; j < 8; ++j) f[j] = 0.0f;
@@ -148,7 +152,7 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const int block, cons
                 if (STOCH) {
                     const float inv = mx_inverse(byte);
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) w |= mx_drawn(f[r], inv, one, draw32(tx, ta, (uint32_t)(row + r) * (uint32_t)a.cols + (uint32_t)(col + j))) << (4 * r);
+                    for (int r = 7; r >= 0; --r) w = mx_drawn(w, f[r], inv, one, draw32(tx, ta, (uint32_t)(row + r) * (uint32_t)a.cols + (uint32_t)(col + j)));
                 } else {
                     w = mx_codes8(f, mx_scale(byte));
                 }
