@@ -329,3 +329,21 @@ def test_pages_refusals():
             call()
     with pytest.raises(B.Int8tError):
         pt.extend(ints([1, 2, 3]), 2**31 - 1)
+
+
+@pytest.mark.parametrize("requests,width,pages,page", [(1, 3000, 3000, 4), (40, 700, 20000, 16), (1025, 9, 5000, 8), (2500, 300, 20000, 1)])
+def test_many_pages_go_back(requests, width, pages, page):
+    """Requests of many pages and many requests: some end, some keep a part, and then their pages are used again."""
+    r = np.random.default_rng(pages)
+    plain, pt = Plain(requests, width, pages, page), PageTable.empty(requests, width, pages, page)
+    for _ in range(3):
+        new = [int(min(n, max(0, width * page - h))) for n, h in zip(r.integers(0, 2 * pages * page // requests + 1, requests), plain.lengths)]
+        want, step = plain.extend(new, sum(new)), pt.extend(ints(new), sum(new))
+        same(step, want)
+        pt.accept(step)
+        plain.accept(want)
+        stay = [int(r.integers(0, n + 1)) if r.random() < 0.3 else n if r.random() < 0.2 else 0 for n in plain.lengths]
+        pt.shrink(ints(stay))
+        plain.shrink(stay)
+        n = int(pt.available)
+        assert n == len(plain.free) and pt.free.cpu().tolist()[:n] == plain.free and pt.lengths.cpu().tolist() == plain.lengths
