@@ -93,7 +93,7 @@ struct MxProductArgs {       // y[m][n] = sum_k a[m][k] b[n][k] + bias[n]
     float* part;             // partial sums of a split reduction, or null
     int splits;
 };
-struct MxFewArgs {           // the same from x itself, codes made on the way: mx_few_tokens(M, Kb)
+struct MxFewArgs {           // the same from x itself, codes made on the way: mx_few_tokens(M, N, Kb)
     const void* x;
     size_t x_pitch;
     int type, M, K, Kb, N, wide;
@@ -102,7 +102,7 @@ struct MxFewArgs {           // the same from x itself, codes made on the way: m
     void* y;
     size_t y_pitch;
 };
-bool mx_few_tokens(int M, int Kb);
+bool mx_few_tokens(int M, int N, int Kb);
 hipError_t launch_mx_few_tokens(const MxFewArgs& a, hipStream_t st);
 bool mx_product_fits(int M, int N, int Kb);
 void mx_product_division(int M, int N, int Kb, size_t scratch_bytes, int* rows, int* waves, int* stages, int* shares);

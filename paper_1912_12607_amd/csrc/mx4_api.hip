@@ -143,7 +143,7 @@ extern "C" int8t_status int8t_mx4_product(const uint8_t* a_dev, const uint8_t* s
 
 extern "C" size_t int8t_mx4_linear_workspace_bytes(const int8t_linear_desc* d, int direction) {
     if (direction < 0 || direction > 2 || linear_ok(d, direction == 1) != INT8T_OK) return 0;
-    return direction == 1 ? bwd_scratch(d, nullptr).bytes : fwd_scratch(d, direction == 2, direction == 2 && mx_few_tokens(d->M, mx_row_bytes(d->K)), nullptr).bytes;
+    return direction == 1 ? bwd_scratch(d, nullptr).bytes : fwd_scratch(d, direction == 2, direction == 2 && mx_few_tokens(d->M, d->N, mx_row_bytes(d->K)), nullptr).bytes;
 }
 
 extern "C" int8t_status int8t_mx4_linear_fwd(const int8t_linear_desc* d, const int8t_mx4_linear_buffers* b, void* stream) {
@@ -152,7 +152,7 @@ extern "C" int8t_status int8t_mx4_linear_fwd(const int8t_linear_desc* d, const i
     if (!b || !b->wq != !b->sw || !b->wt != !b->swt || !b->xt != !b->sxt || (!b->w && (!b->wq || b->wt))) return INT8T_ERR_NULL;
     if ((b->w && b->w_pitch < (size_t)d->K) || (b->wt && !codes_ok(d->K, d->N))) return INT8T_ERR_SHAPE;
     if (!aligned16(b->wq) || !aligned16(b->sw) || !aligned16(b->wt) || !aligned16(b->swt) || !aligned(b->w, bytes_of(d->wtype)) || !aligned(b->bias, 4)) return INT8T_ERR_ARG;
-    const bool few = !b->w && !b->xt && mx_few_tokens(d->M, mx_row_bytes(d->K));
+    const bool few = !b->w && !b->xt && mx_few_tokens(d->M, d->N, mx_row_bytes(d->K));
     const FwdScratch s = fwd_scratch(d, !b->w, few, b->ws);
     const size_t need = few || (d->M == 0 && (!b->w || b->wq)) ? 0 : s.bytes;
     if (need > 0 && !b->ws) return INT8T_ERR_NULL;

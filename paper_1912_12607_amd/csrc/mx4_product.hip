@@ -9,7 +9,7 @@ namespace {
 
 typedef int mp_v4i __attribute__((ext_vector_type(4)));
 typedef int mp_v8i __attribute__((ext_vector_type(8)));
-constexpr int kMxFewBytes = 32768;       // codes of few tokens, see mx_few_tokens()
+constexpr int kMxFewBytes = 24576;       // codes of few tokens, see mx_few_tokens()
 
 // 32 x 32 sums of 64 products each: a lane has a block of a row (16 bytes), the lanes of the wave's other half another one; byte S of `sa`, `sb` is its scale.
 template <int S>
@@ -484,8 +484,10 @@ hipError_t few_of(const MxFewArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Up to so many codes every block makes them for itself: a launch less.
-bool mx_few_tokens(int M, int Kb) { return M <= 16 && M * (long long)Kb <= kMxFewBytes; }
+// Up to so many codes every block makes them for itself: a launch less, 4 us of the host's time or of a graph's, against 0.17 us for each 1024 bytes of codes, twice that where
+// compute units have two blocks of 16 channels (bf16, us of one launch / two, by the host and in a graph: 16 x 2048 -> 1000 7.9/12 and 5.8/6.5, 8 x 4096 -> 4096 7.3/11.4 and
+// 6.3/7.8, 16 x 4096 -> 4096 9.6/11.4 and 9.5/7.8, 8 x 4096 -> 16384 12.4/11.3 and 12.4/8.8, 16 x 4096 -> 16384 18/11.3 and 18/8.8, 8 x 8192 -> 8192 16.5/11.5 and 16.4/11.5).
+bool mx_few_tokens(int M, int N, int Kb) { return M <= 16 && M * (long long)Kb * (N > 16 * 256 ? 2 : 1) <= kMxFewBytes; }
 hipError_t launch_mx_few_tokens(const MxFewArgs& a, hipStream_t st) {
     if (a.type == kF32) return few_of<kF32>(a, st);
     if (a.type == kBF16) return few_of<kBF16>(a, st);
