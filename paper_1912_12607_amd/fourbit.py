@@ -94,7 +94,7 @@ class ServedLinear4:
         if kind is None or x.get_device() != self._index or not shape or shape[-1] != self.in_features:
             _type(x, "x")
             raise RuntimeError(f"input of {tuple(shape)} on {x.device} in a layer of {self.in_features} on {self.codes.device}")
-        y = torch.empty(shape[:-1] + (self.out_features,), dtype=x.dtype, device=x.device)
+        y = x.new_empty(shape[:-1] + (self.out_features,))
         if y.numel() == 0:
             return y
         rows, pitch = _rows(x, self.in_features)
@@ -120,7 +120,7 @@ class _Linear4Fn(torch.autograd.Function):
         bias = _vector(bias, N, "bias", index)
         (rows, pitch), (wr, w_pitch) = _rows(x, K), _rows(w, K)
         M = rows.shape[0]
-        y = torch.empty(shape[:-1] + (N,), dtype=x.dtype, device=dev)
+        y = x.new_empty(shape[:-1] + (N,))
         # codes and scales of x and W by columns, in one piece of memory: the backward pass reads them
         desc, (need, later, _), places, size = _plan(M, K, N, kind, wkind)
         kept = None
@@ -153,7 +153,7 @@ class _Linear4Fn(torch.autograd.Function):
         want_x, want_w, want_b = ctx.needs_input_grad[:3]
         desc, dev = ctx.desc, dy.device
         M, K, N = desc.M, desc.K, desc.N
-        dx = torch.empty(ctx.x_shape, dtype=dy.dtype, device=dev) if want_x else None
+        dx = dy.new_empty(ctx.x_shape) if want_x else None
         if M == 0:
             return (dx, torch.zeros(N, K, dtype=ctx.w_dtype, device=dev) if want_w else None,
                     torch.zeros(N, dtype=torch.float32, device=dev) if want_b else None, None)

@@ -23,10 +23,10 @@ from .tokens import _call, _type
 class _RotateFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, rotary, positions, q, k):
-        ctx.rotary, ctx.two = rotary, k is not None
+        ctx.rotary, ctx.two, ctx.plan = rotary, k is not None, rotary._check(q, k, positions)
         ctx.save_for_backward(positions)
         ctx.set_materialize_grads(False)
-        out = rotary._turn(q, k, positions, 0)
+        out = rotary._turn(ctx.plan, q, k, positions, 0)
         return out if ctx.two else out[0]
 
     @staticmethod
@@ -34,11 +34,13 @@ class _RotateFn(torch.autograd.Function):
         if torch.is_grad_enabled():
             raise RuntimeError("a Rotary is differentiable once")
         positions, = ctx.saved_tensors
+        if ctx.two and grads[0] is not None and grads[1] is not None and ctx.needs_input_grad[2] and ctx.needs_input_grad[3]:
+            return None, None, *ctx.rotary._turn(ctx.plan, *grads, positions, 1)
         want = [g if n else None for g, n in zip(grads, ctx.needs_input_grad[2:])]
         there = [g for g in want if g is not None]
         if not there:
             return None, None, None, None
-        turned = iter(ctx.rotary._turn(there[0], there[1] if len(there) > 1 else None, positions, 1))
+        turned = iter(ctx.rotary._turn(ctx.rotary._check(there[0], None, positions), there[0], None, positions, 1))
         out = [next(turned) if g is not None else None for g in want]
         return (None, None, out[0], out[1] if ctx.two else None)
 
@@ -90,7 +92,7 @@ class Rotary:
         return self
 
     def _check(self, q, k, positions):
-        """What calls of these shapes have in common: (descriptor, tokens, pitches and heads of each tensor), looked up after the first."""
+        """What calls of these shapes have in common: (descriptors, tokens, heads of q and k, dim), looked up after the first."""
         shape, device = q.shape, q.device
         if positions.dtype is not torch.int32 or positions.shape != shape[:-2] or positions.device != device:
             _type(q, "q")
@@ -114,19 +116,18 @@ class Rotary:
             descs = tuple(B.RotateDesc(tokens, shape[-1], self.rot, code, 1 if self.layout == "interleaved" else 0, back, self.amplitude) for back in (0, 1))
             if len(self._plans) >= 1024:
                 self._plans.clear()
-            plan = self._plans[key] = descs, tokens
+            plan = self._plans[key] = descs, tokens, (shape[-2], 0 if k is None else k.shape[-2]), shape[-1]
         elif not q.is_cuda:
             _type(q, "q")
         return plan
 
     @staticmethod
-    def _tensor(x, y):
-        heads, dim = x.shape[-2:]
+    def _tensor(x, y, heads, dim):
         row = heads * dim
-        if x.dim() == 3:
-            token, head, _ = x.stride()
-            return B.RotateTensor(x.data_ptr(), y.data_ptr(), token, head, *((token, head) if y is x else (row, dim)), heads)
-        return B.RotateTensor(x.data_ptr(), y.data_ptr(), row, dim, row, dim, heads)
+        if x.is_contiguous():
+            return B.RotateTensor(x.data_ptr(), y.data_ptr(), row, dim, row, dim, heads)
+        token, head, _ = x.stride()
+        return B.RotateTensor(x.data_ptr(), y.data_ptr(), token, head, *((token, head) if y is x else (row, dim)), heads)
 
     def _launch(self, plan, first, second, positions, back):
         """first, second: (source, result) each, or None."""
@@ -135,18 +136,24 @@ class Rotary:
         if not positions.is_contiguous():
             positions = positions.contiguous()
         x = first[0]
-        _call(x.get_device(), B.lib.int8t_rotate, plan[0][back], self._tensor(*first), None if second is None else self._tensor(*second), positions.data_ptr(),
-              self._on(x.device).data_ptr())
+        heads, dim = plan[2:]
+        _call(x.get_device(), B.lib.int8t_rotate, plan[0][back], self._tensor(*first, heads[0], dim), None if second is None else self._tensor(*second, heads[1], dim),
+              positions.data_ptr(), self._on(x.device).data_ptr())
 
-    def _turn(self, q, k, positions, back):
-        plan = self._check(q, k, positions)
-        yq, yk = torch.empty(q.shape, dtype=q.dtype, device=q.device), None
-        if q.stride(-1) != 1 or (q.dim() != 3 and not q.is_contiguous()):
-            q = q.contiguous()
+    @staticmethod
+    def _result(x):
+        """(source, result): contiguous, the source a tensor that _tensor() takes."""
+        if x.is_contiguous():
+            return x, torch.empty_like(x)
+        if x.stride(-1) != 1 or x.dim() != 3:
+            x = x.contiguous()
+        return x, x.new_empty(x.shape)
+
+    def _turn(self, plan, q, k, positions, back):
+        q, yq = self._result(q)
+        yk = None
         if k is not None:
-            if k.stride(-1) != 1 or (k.dim() != 3 and not k.is_contiguous()):
-                k = k.contiguous()
-            yk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            k, yk = self._result(k)
         self._launch(plan, (q, yq), None if k is None else (k, yk), positions, back)
         return (yq,) if k is None else (yq, yk)
 
@@ -154,7 +161,7 @@ class Rotary:
         """(q, k) turned, or q alone where k is None: (.., heads, dim) of one type, int32 positions (..).  Differentiable (once)."""
         if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad)):
             return _RotateFn.apply(self, positions, q, k)
-        out = self._turn(q, k, positions, 0)
+        out = self._turn(self._check(q, k, positions), q, k, positions, 0)
         return out if k is not None else out[0]
 
     def turn_(self, q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor) -> None:
@@ -261,8 +268,7 @@ class PageTable:
         n, tokens = self.requests, int(tokens)
         if tokens < 0:
             raise RuntimeError(f"{tokens} tokens")
-        device = new.device
-        ints = torch.empty(3 * tokens + 2 * n + 3, dtype=torch.int32, device=device)          # (slots take two each)
+        ints = new.new_empty(3 * tokens + 2 * n + 3)                                           # (slots take two each)
         slots, positions, lengths, starts, available, without = ints.split((2 * tokens, tokens, n, n + 1, 1, 1))
         at = ints.data_ptr()
         first = at + 12 * tokens

@@ -325,7 +325,7 @@ class PagedCache:
             pitch = wide[1]
         if not (starts.is_contiguous() and lengths.is_contiguous()):
             starts, lengths = starts.contiguous(), lengths.contiguous()
-        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape)
         lse = torch.empty((T, heads), dtype=torch.float32, device=q.device) if return_lse else None
         if T:
             d = B.AttendDesc(T, n, heads // self.heads, wide[1], 0 if longest is None else max(1, int(longest)), kind, 1 if causal else 0,
