@@ -76,6 +76,7 @@ struct MxArgs {              // codes of rows x cols values
     uint8_t *qt, *st;        // blocks along the rows: [cols][mx_row_bytes(rows)], [mx_panels(rows)][cols][8]; or null
     float* sum;              // cols, or null: sums of the columns
     float* part;             // [parts][cols], with sum (one part: not used)
+    bool parts_only = false; // parts are left for the product that follows (MxProductArgs)
 };
 int mx_sum_parts(int rows);
 // with b (the same type and rounding to nearest in both): two matrices in one launch
@@ -92,7 +93,17 @@ struct MxProductArgs {       // y[m][n] = sum_k a[m][k] b[n][k] + bias[n]
     int type;
     float* part;             // partial sums of a split reduction, or null
     int splits;
+    const float* sum_part;   // [sum_parts][M] sums to join beside the product, in sum; or null
+    float* sum;
+    int sum_parts;
 };
+// Parts in their order, in 64 bits
+__device__ __forceinline__ float mx_join(const float* part, int parts, size_t pitch) {
+    double s = 0.0;
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) s += (double)part[(size_t)p * pitch];
+    return (float)s;
+}
 struct MxFewArgs {           // the same from x itself, codes made on the way: mx_few_tokens(M, N, Kb)
     const void* x;
     size_t x_pitch;

@@ -195,7 +195,7 @@ extern "C" int8t_status int8t_mx4_linear_bwd(const int8t_linear_desc* d, const i
     const BwdScratch s = bwd_scratch(d, b->ws);
     if (b->ws_bytes < s.bytes) return INT8T_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
-    const MxArgs g{b->dy, b->dy_pitch, d->type, d->M, d->N, 1, seed, b->dx ? s.gq : nullptr, s.sg, b->dw ? s.hq : nullptr, s.sh, b->db, s.part};
+    const MxArgs g{b->dy, b->dy_pitch, d->type, d->M, d->N, 1, seed, b->dx ? s.gq : nullptr, s.sg, b->dw ? s.hq : nullptr, s.sh, b->db, s.part, b->dw != nullptr};
     hipError_t e = launch_mx_quantize(g, st);
     if (e != hipSuccess) return INT8T_ERR_RUNTIME;
     MxProductArgs px{}, pw{};
@@ -204,6 +204,9 @@ extern "C" int8t_status int8t_mx4_linear_bwd(const int8t_linear_desc* d, const i
     px.M = d->M; px.N = d->K; px.Kb = mx_row_bytes(d->N); px.y = b->dx; px.pitch = (size_t)d->K; px.type = d->type;
     pw.a = s.hq; pw.sa = s.sh; pw.b = b->xt; pw.sb = b->sxt;
     pw.M = d->N; pw.N = d->K; pw.Kb = mx_row_bytes(d->M); pw.y = b->dw; pw.pitch = (size_t)d->K; pw.type = d->wtype;
+    if (b->db && b->dw && mx_sum_parts(d->M) > 1) {
+        pw.sum_part = s.part; pw.sum = b->db; pw.sum_parts = mx_sum_parts(d->M);
+    }
     if (b->dx && b->dw) e = launch_mx_products(px, pw, s.product_bytes, st);
     else if (b->dx) e = launch_mx_product(px, s.product_bytes, st);
     else if (b->dw) e = launch_mx_product(pw, s.product_bytes, st);

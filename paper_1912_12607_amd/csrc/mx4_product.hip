@@ -261,7 +261,12 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_product_kernel(const MxProduc
     constexpr int BM = WM * MI * 32, BN = WN * NJ * 32;
     const bool second = (int)blockIdx.x >= first;
     const MxProductArgs p = second ? b : a;
-    product_body<TYPE, WM, WN, MI, NJ, NS, SPLIT>(p, (p.M + BM - 1) / BM, (p.N + BN - 1) / BN, (int)blockIdx.x - (second ? first : 0));
+    const int block = (int)blockIdx.x - (second ? first : 0);
+    product_body<TYPE, WM, WN, MI, NJ, NS, SPLIT>(p, (p.M + BM - 1) / BM, (p.N + BN - 1) / BN, block);
+    // (a launch of 4 us less; the first blocks have as many lanes as the product has rows)
+    static_assert(64 * WM * WN >= BM, "a lane for each row");
+    const long long m = (long long)block * (64 * WM * WN) + (int)threadIdx.x;
+    if (p.sum && m < p.M) p.sum[m] = mx_join(p.sum_part + m, p.sum_parts, (size_t)p.M);
 }
 
 // ------------------------------------------------------------------------------------------------

@@ -197,14 +197,11 @@ __global__ __launch_bounds__(256) void mx_tiles_kernel(const MxArgs a, const MxA
     tile_body<TYPE, STOCH>(m, (int)blockIdx.x - (second ? first : 0), second ? total_b : total_a, second ? wide_b : wide_a, kx, ka, tx, ta);
 }
 
-// Sums of columns from those of the blocks of rows
+// Sums of columns from those of the blocks of rows (where no product follows)
 __global__ __launch_bounds__(256) void mx_sum_kernel(const MxArgs a, const int parts) {
     const int c = (int)(blockIdx.x * 256 + threadIdx.x);
     if (c >= a.cols) return;
-    double s = 0.0;
-#pragma unroll 8
-    for (int p = 0; p < parts; ++p) s += (double)a.part[(size_t)p * a.cols + c];
-    a.sum[c] = (float)s;
+    a.sum[c] = mx_join(a.part + c, parts, (size_t)a.cols);
 }
 
 inline int wide_rows(const MxArgs& a) { return (((uintptr_t)a.x | (a.pitch * (a.type == kF32 ? 4 : 2))) & 15) == 0; }
@@ -229,7 +226,7 @@ hipError_t quantize_of(const MxArgs& a, const MxArgs* b, hipStream_t st) {
         launch_timed(kt, (mx_tiles_kernel<TYPE, STOCH>), dim3((unsigned)(first + ((tb + 7) & ~7))), dim3(256), 0, st, a, b ? *b : a, first, ta, tb, wide_rows(a), b ? wide_rows(*b) : 0,
                      seed_key_x(a.seed), seed_key_a(a.seed), seed_key_x(turned), seed_key_a(turned));
     }
-    if (a.sum && a.rows > QT_R) {
+    if (a.sum && a.rows > QT_R && !a.parts_only) {
         KernelTimer kt(KID_MX_QUANTIZE, st);
         launch_timed(kt, mx_sum_kernel, dim3((unsigned)((a.cols + 255) / 256)), dim3(256), 0, st, a, mx_sum_parts(a.rows));
     }
