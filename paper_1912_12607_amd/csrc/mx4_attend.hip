@@ -96,17 +96,26 @@ __global__ __launch_bounds__(64 * RW, 2) void mx_attend_rows_kernel(const Attend
     extern __shared__ __attribute__((aligned(1024))) float lds[];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n16 = lane & 15, kg = lane >> 4;
-    // Heads first: an XCD has as few heads' keys in its L2 as can be, and blocks without rows, a few for each request, lie together.
-    const int place = (int)(blockIdx.y * gridDim.x + blockIdx.x), group_of = div_by(place, a.by_heads);
-    const int head = place - group_of * a.c.heads, split = (int)blockIdx.z, block = (int)gridDim.x - 1 - group_of;
+    // Heads first: an XCD has as few heads' keys in its L2 as can be.
+    const int place = (int)((a.close ? blockIdx.z * gridDim.y * gridDim.x : 0u) + blockIdx.y * gridDim.x + blockIdx.x), group_of = div_by(place, a.by_heads);
+    const int head = place - group_of * a.c.heads;
     const int D = a.c.dim, NB = UNI ? DIM / 32 : mx_blocks(D), RB = 16 * NB;
 
-    const int b = block_request(a, block, lane);
-    const Request rq = request_of(a, b);
-    const int nrows = rq.tokens * a.group;
-    const long long tile = (long long)block - ((long long)a.starts[b] * a.group / 16 + b);
-    if (tile < 0 || tile * 16 >= nrows) return;
-    const int r0 = (int)tile * 16;
+    Unit unit_;
+    if (a.close) {
+        if (!unit_of(a, group_of, 16, true, lane, &unit_)) return;
+    } else {
+        const int block = (int)gridDim.x - 1 - group_of;
+        const int b = block_request(a, block, lane);
+        unit_.rq = request_of(a, b);
+        unit_.tile = (int)((long long)block - ((long long)a.starts[b] * a.group / 16 + b));
+        unit_.share = (int)blockIdx.z;
+        unit_.shares = shares_of(a, unit_.rq.length);
+    }
+    const Request& rq = unit_.rq;
+    const int nrows = rq.tokens * a.group, tile = unit_.tile, split = unit_.share, shares = unit_.shares;
+    if (tile < 0 || (long long)tile * 16 >= nrows) return;
+    const int r0 = tile * 16;
     const int heads = a.c.heads * a.group;
 
     // the block's keys: of those that its last row sees
@@ -114,13 +123,18 @@ __global__ __launch_bounds__(64 * RW, 2) void mx_attend_rows_kernel(const Attend
     const int behind = rq.length - rq.new_tokens;               // keys before the new tokens
     const int seen_end = max(0, a.causal ? min(rq.length, behind + last_token + 1) : rq.length);
     const int all = max(0, a.causal ? min(rq.length, behind + div_by(r0, a.by_group) + 1) : rq.length);      // keys that all of its rows see
-    const int from = (int)min((long long)split * a.share, (long long)seen_end), end = split + 1 == a.splits ? seen_end : min(from + a.share, seen_end);
-    if (a.splits > 1 && from >= end && !(split == 0)) {              // nothing here: the joining pass looks at m alone
-        if ((int)threadIdx.x < 16 && r0 + (int)threadIdx.x < nrows) {
-            const int r = r0 + (int)threadIdx.x, t = div_by(r, a.by_group);
-            a.part_ml[2 * ((size_t)split * a.tokens * heads + (size_t)(rq.token0 + t) * heads + head * a.group + (r - t * a.group))] = kNone;
+    const int all_steps = (seen_end + 31) >> 5;
+    const int from = split < shares ? 32 * (int)((long long)all_steps * split / shares) : seen_end;
+    const int end = split < shares ? min(32 * (int)((long long)all_steps * (split + 1) / shares), seen_end) : seen_end;
+    if (a.splits > 1) {
+        // nothing here, or in the shares behind the request's last (which have blocks of their own where those are not close): the joining pass looks at m alone
+        const bool none = from >= end && split != 0;
+        const int lo = none ? split : shares, hi = none ? split + 1 : a.close && split == 0 ? a.splits : 0;
+        for (int i = (int)threadIdx.x; i < 16 * (hi - lo); i += 64 * RW) {
+            const int r = r0 + (i & 15), t = div_by(r, a.by_group);
+            if (r < nrows) a.part_ml[2 * ((size_t)(lo + (i >> 4)) * a.tokens * heads + (size_t)(rq.token0 + t) * heads + head * a.group + (r - t * a.group))] = kNone;
         }
-        return;
+        if (none) return;
     }
 
     // this lane's row

@@ -40,18 +40,57 @@ struct Request {
     int new_tokens;          // (as the starts say: the causal limit goes by it)
     const int* pages;
 };
-__device__ __forceinline__ Request request_of(const AttendArgs& a, int b) {
+__device__ __forceinline__ Request request_of(const AttendArgs& a, int b, int s0, int s1, int len) {
     Request r;
-    const int s0 = a.starts[b], s1 = a.starts[b + 1];
     r.new_tokens = s1 - s0;
     r.token0 = s0 < 0 ? 0 : s0;
     const int end = s1 < a.tokens ? s1 : a.tokens;
     r.tokens = end > r.token0 && s0 >= 0 ? end - r.token0 : 0;
     const long long most = (long long)a.width * a.c.page_size;
-    const int len = a.lengths[b];
     r.length = len < 0 ? 0 : (long long)len < most ? len : (int)most;
     r.pages = a.table + (size_t)b * a.table_pitch;
     return r;
+}
+__device__ __forceinline__ Request request_of(const AttendArgs& a, int b) { return request_of(a, b, a.starts[b], a.starts[b + 1], a.lengths[b]); }
+
+// Inclusive sums over a wave's lanes
+__device__ __forceinline__ int wave_sums(int n) {
+    n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xf, 0xf, false);      // (row_shr: rows of 16 lanes)
+    n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xa, 0xf, false);      // (the last lane of the row before)
+    n += __builtin_amdgcn_update_dpp(0, n, 0x143, 0xc, 0xf, false);      // (of the half before)
+    return n;
+}
+// The shares that a request of `length` keys is dealt out in: as many of `share` keys as it has, `splits` at most
+__device__ __forceinline__ int shares_of(const AttendArgs& a, int length) { return a.splits == 1 ? 1 : max(1, min(a.splits, (int)(((long long)length + a.share - 1) / a.share))); }
+
+// What request, which tile of `rows` rows of it and which share the u-th block (of a head) has, counted over those that there are: false behind the last one.  A request's last rows,
+// which see the most keys, come first.  Workgroups are dealt out to an XCD's groups of compute units in turn, whatever these have to do: where every other one ends
+// at once, half of the chip has two rounds of work and the other none (256 blocks of 256 rows with 500 keys 69 us, not 34).
+struct Unit { Request rq; int tile, share, shares; };
+__device__ __forceinline__ bool unit_of(const AttendArgs& a, int u, int rows, bool by_length, int lane, Unit* out) {
+    const long long most = (long long)a.width * a.c.page_size;
+    int before = 0;
+    for (int r0 = 0; r0 < a.requests; r0 += 64) {
+        const int r = min(r0 + lane, a.requests - 1), s0 = a.starts[r], s1 = a.starts[r + 1], len = a.lengths[r], end = min(s1, a.tokens);
+        const int n = r0 + lane < a.requests && s0 >= 0 && end > s0 ? end - s0 : 0;
+        const int tiles = (int)(((long long)n * a.group + rows - 1) / rows), shares = by_length ? shares_of(a, (int)min((long long)max(0, len), most)) : a.splits;
+        const int units = tiles * shares, upto = before + wave_sums(units);
+        const unsigned long long behind = __ballot(upto > u);
+        if (behind) {
+            const int l = __builtin_ctzll(behind);
+            const int all = __builtin_amdgcn_readlane(tiles, l), in = u - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(units, l));
+            out->rq = request_of(a, r0 + l, __builtin_amdgcn_readlane(s0, l), __builtin_amdgcn_readlane(s1, l), __builtin_amdgcn_readlane(len, l));
+            out->shares = __builtin_amdgcn_readlane(shares, l);
+            out->share = in / max(all, 1);
+            out->tile = all - 1 - (in - out->share * all);
+            return true;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
 }
 
 // Where key j of a request lies (its row of the cache's codes and scales); false: nowhere -- beyond `end`, or on a page that there is not.

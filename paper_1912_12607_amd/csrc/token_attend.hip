@@ -505,6 +505,7 @@ void attend_plan(AttendArgs* a, int longest) {
         const int tall = dim == 128 ? 256 : 128;
         const bool larger = (dim == 64 || (dim == 128 && !fp32)) && each >= (dim == 64 ? 320 : 200) && 4 * each >= 3 * ((each + tall - 1) / tall * tall) && rows * a->c.heads >= 10000;
         a->rows = larger ? tall : 16;
+        a->close = a->requests <= 512;           // (more of them take a block longer to look through than its neighbours wait)
     }
     // (4 bits: blocks that have rows, where these are dealt out evenly)
     const long long tiles = a->mx && a->rows == 16 ? (each > 16 ? (each + 15) / 16 : 1) * a->requests * a->c.heads : (rows / a->rows + a->requests) * a->c.heads;

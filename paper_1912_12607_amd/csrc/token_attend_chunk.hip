@@ -76,15 +76,25 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
     const int n32 = lane & 31, half = lane >> 5;
     // Heads first, so that an XCD has as few heads' keys in its L2 as can be, and each request's last rows, which see the most keys, before its others, so that
     // the chip runs out of short blocks (tiles first, in order: 9 % more time for two chunks of 2048 tokens over 8192 keys).
-    const int place = (int)(blockIdx.y * gridDim.x + blockIdx.x), group_of = div_by(place, a.by_heads);
-    const int head = place - group_of * a.c.heads, split = (int)blockIdx.z, block = (int)gridDim.x - 1 - group_of;
+    const bool close = MX && a.close;
+    const int place = (int)((close ? blockIdx.z * gridDim.y * gridDim.x : 0u) + blockIdx.y * gridDim.x + blockIdx.x), group_of = div_by(place, a.by_heads);
+    const int head = place - group_of * a.c.heads, block = (int)gridDim.x - 1 - group_of;
     const int D = a.c.dim;
 
-    const int b = tile_request(a, block, ROWS);
-    const Request rq = request_of(a, b);
+    Unit u_;
+    if (close) {
+        if (!unit_of(a, group_of, ROWS, false, lane, &u_)) return;
+    } else {
+        const int b = tile_request(a, block, ROWS);
+        u_.rq = request_of(a, b);
+        u_.tile = (int)((long long)block - ((long long)a.starts[b] * a.group / ROWS + b));
+        u_.share = (int)blockIdx.z;
+    }
+    const int split = u_.share;
+    const Request& rq = u_.rq;
     const int nrows = rq.tokens * a.group;
-    const long long tile = (long long)block - ((long long)a.starts[b] * a.group / ROWS + b);
-    if (tile < 0 || tile * ROWS >= nrows) return;
+    const int tile = u_.tile;
+    if (tile < 0 || (long long)tile * ROWS >= nrows) return;
     const int r0 = (int)tile * ROWS;
     const int row = r0 + 32 * wave + n32;
     const bool have = row < nrows;

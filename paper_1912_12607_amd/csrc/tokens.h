@@ -181,6 +181,7 @@ struct AttendArgs {
     float *part_o, *part_ml; // [splits][tokens * heads * group][dim], [..][2]
     int wide_q;
     int mx;                  // the cache holds microscaled 4-bit codes (mx4.h)
+    int close;               // ... and blocks that have rows come first (unit_of())
 };
 void attend_plan(AttendArgs* a, int longest);       // rows, splits
 hipError_t launch_attend_chunk(const AttendArgs& a, hipStream_t st);      // (blocks of 128 or 256 rows; does not join)
