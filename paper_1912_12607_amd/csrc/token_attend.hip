@@ -450,6 +450,16 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// Shares of the keys of larger blocks: up to a block for each compute unit (two of 128 rows), of 256 keys at least (us with 256, 512, 1024 keys at
+// least: 256 rows of 5 requests and 8 heads over 1500 keys, dim 64 bf16 30, 33, 48, fp32 36, 39, 60, dim 128 59, 53, 74 and 66, 62, 95, dim 256 86, 82, 132 and
+// 144, 138, 232; 300 rows of 4 and 12 over 1000: 31, 34, 34 | 36, 42, 42 | 44, 55, 56 | 67, 69, 69 | 92, 94, 94 | 155, 165, 166; 256 rows of 12 and 4 over 2500: 36, 37, 57 |
+// 42, 46, 70 | 82, 88, 74 | 86, 98, 89 | 120, 137, 123 | 226, 251, 238).
+static int chunk_shares(int rows, long long blocks, int longest) {
+    long long s = (rows == 128 ? 512 : 256) / (blocks > 0 ? blocks : 1);
+    if (s > longest / 256) s = longest / 256;
+    return s < 1 ? 1 : (int)s;
+}
+
 // Rows of a block and shares of the keys.  Blocks of 16 rows stream the cache; the larger ones of token_attend_chunk.hip multiply it.  These are faster from so many rows
 // of a request on average that their rows are filled, and from so many of all requests and heads that a block is there for a third of the compute units at least
 // (us with 16 rows / with 128, dim 128 in bf16: 256; equal requests, all keys seen:
@@ -474,10 +484,6 @@ hipError_t attend_type(const AttendArgs& a, hipStream_t st) {
 //   pages of  7, dim 256 fp32    181/258        666/674       325/390       130/208       316/311        946/722       350/677        914/890        78/92         151/226       31/76).
 // Over 1210 calls (those and drawn ones: ragged and equal, causal and not, dims from 48 to 256, pages from 1 to 64) the rule costs 2.6 % over the faster of the two, the
 // best pair of limits for each dim, type and kind of page 2.0, rows of a request alone 7.9.
-// Shares of the keys of larger blocks: up to a block for each compute unit (two of 128 rows), of 256 keys at least (us with 256, 512, 1024 keys at
-// least: 256 rows of 5 requests and 8 heads over 1500 keys, dim 64 bf16 30, 33, 48, fp32 36, 39, 60, dim 128 59, 53, 74 and 66, 62, 95, dim 256 86, 82, 132 and
-// 144, 138, 232; 300 rows of 4 and 12 over 1000: 31, 34, 34 | 36, 42, 42 | 44, 55, 56 | 67, 69, 69 | 92, 94, 94 | 155, 165, 166; 256 rows of 12 and 4 over 2500: 36, 37, 57 |
-// 42, 46, 70 | 82, 88, 74 | 86, 98, 89 | 120, 137, 123 | 226, 251, 238).
 void attend_plan(AttendArgs* a, int longest) {
     const long long rows = (long long)a->tokens * a->group, each = rows / a->requests;
     const bool fp32 = a->type == kF32;
@@ -493,17 +499,19 @@ void attend_plan(AttendArgs* a, int longest) {
     }
     a->rows = each < many || rows * a->c.heads < all ? 16 : dim == 128 && !fp32 ? 256 : 128;
     // Caches in 4 bits: blocks of 16 rows spend less on a key (mx4_attend.hip), so that larger ones are faster only for dims up to 64 and, in bf16 and fp16, up to 128, where their rows
-    // are filled to three quarters (us with 16 rows / with larger ones, pages of 16; rows, requests, heads, keys as above:
-    //                 66,9,12,1500  200,2,32,6000  264,8,8,2048  400,4,8,3000  2048,1,8,8192  64,64,8,1024  400,64,4,1024  512,2,4,2000  1024,4,8,4096  600,16,8,2000
-    //   dim  64 bf16     26/36         90/95          45/56         50/49         131/119        41/48         110/90         21/38         132/120        143/113
-    //   dim  64 fp32     27/47         97/91          52/62         57/54         147/114        46/89         127/111        25/32         155/116        168/169
-    //   dim 128 bf16     28/82        107/86          57/63         62/57         166/112        50/100        147/158        25/36         179/113        194/192
-    //   dim 128 fp32     37/94        139/203         75/140        80/115        219/265        65/199        190/275        32/40         234/267        248/375
-    //   dim 256 bf16     48/130       191/282         95/196       110/161        309/366        88/272        280/380        33/55         324/377        348/523;
-    // pages of 24 and 7: within 15 % of these).
+    // are half filled at least and the compute units have one (dim 64: two take turns on a unit) of all keys, or of 1000 of them (us with 16 rows / with larger ones, causal, pages of 16:
+    //   new tokens, requests, heads, group, keys   433,2,12,1,433  433,2,12,1,3000  1024,1,8,4,1024  256,8,8,4,256  256,16,8,1,256-1000  73,32,8,3,1-627  700,2,16,1,700-1400  512,3,8,2,2000-4000
+    //   dim  64 bf16                                   9.8/17          47/41            26/36          27/16            28/35               33/24             29/37             88/75
+    //   dim  64 fp32                                   11/21           51/50            31/44          32/22            34/44               39/34             35/48            103/104
+    //   dim  96 bf16                                   13/27           65/48            40/45          45/22            46/45               53/36             45/51            141/101
+    //   dim 128 bf16                                   11/28           57/49            34/48          38/24            38/47               45/39             38/53            124/105
+    //   dim 128 fp16                                   11/30           60/51            36/50          41/25            41/49               48/41             41/55            130/111;
+    // over 80 calls, drawn and these, the choice and its shares take some 3.5 % more than the fastest of some 25 divisions of each).
     if (a->mx) {
         const int tall = dim == 128 ? 256 : 128;
-        const bool larger = (dim == 64 || (dim == 128 && !fp32)) && each >= (dim == 64 ? 320 : 200) && 4 * each >= 3 * ((each + tall - 1) / tall * tall) && rows * a->c.heads >= 10000;
+        const long long filled = (each + tall - 1) / tall, blocks = filled * a->requests * a->c.heads, units = dim == 128 ? 160 : 320;
+        const long long shares = chunk_shares(tall, blocks, longest);
+        const bool larger = (dim == 64 || (dim == 128 && !fp32)) && each >= 128 && 2 * each >= filled * tall && (blocks >= units || (blocks * shares >= units && longest / shares >= 1000));
         a->rows = larger ? tall : 16;
         a->close = a->requests <= 512;           // (more of them take a block longer to look through than its neighbours wait)
     }
@@ -517,6 +525,14 @@ void attend_plan(AttendArgs* a, int longest) {
         // 107/116).
         const long long blocks = tiles * ((longest + 2047) / 2048);
         a->share = blocks >= 512 || (blocks >= 128 && blocks <= 256) ? 2048 : 1024;
+        if (a->mx) {
+            // As many as bring blocks to 1024, or to 256 of eight waves where tiles are few, of some 1024 keys at least; none of more than 2048, or 4096 where blocks are many already (us with shares of 1024, 2048, 4096:
+            // eight waves, single tokens of 1 request over 8192 keys 18, 21, 31, of 4 over 8192 21, 22, 31, of 8 over 1 to 8192 30, 23, 31; four waves, of 64 over 1 to 8192 79, 74, 81;
+            // 100 tokens of 6 over 1 to 3000 27, 30, 30; 64 of 9 over 1 to 1500 19, 16, 16; 20 of 20 over 100 to 2000 23, 27, 27; 512 of 4 over 3000 -, 73, 64).
+            const long long wanted = tiles <= 64 ? 256 / tiles : (1024 + tiles - 1) / tiles, most = ((long long)longest + 512) / 1024, full = tiles < 1024 ? 2048 : 4096, least = (longest + full - 1) / full;
+            const long long s = wanted < most ? wanted : most, some = s > least ? s : least, n = some > 1 ? some : 1;
+            a->share = longest > 0 ? (int)(((longest + n - 1) / n + 31) & ~31ll) : 32;
+        }
         a->splits = (longest + a->share - 1) / a->share;
         a->waves = tiles * a->splits <= 256 ? 8 : 4;
         // At most 256 of them, and at most 2^14 blocks with theirs (a block leaves 16 rows of sums in the scratch, 2^20 times dim bytes together): the length may be
@@ -530,10 +546,7 @@ void attend_plan(AttendArgs* a, int longest) {
         return;
     }
     a->waves = a->rows / 32;
-    const long long blocks = (each + a->rows - 1) / a->rows * a->requests * a->c.heads;
-    long long s = (a->rows == 128 ? 512 : 256) / blocks;
-    if (s > longest / 256) s = longest / 256;
-    a->splits = s < 1 ? 1 : (int)s;
+    a->splits = chunk_shares(a->rows, (each + a->rows - 1) / a->rows * a->requests * a->c.heads, longest);
 }
 
 hipError_t launch_attend(const AttendArgs& a, hipStream_t st) {

@@ -228,3 +228,19 @@ def test_memory_shared_by_two_tensors():
     assert not positions._share(qkv[:, :4], qkv[:, 4:6]) and positions._share(qkv[:, :5], qkv[:, 4:6]) and not positions._share(qkv[:2], qkv[2:4])
     assert positions._share(qkv[:3], qkv[2:5]) and not positions._share(qkv, torch.zeros(5, 7, 16))
     assert positions._overlaps(qkv[:, :1].expand(5, 3, 16)) and not positions._overlaps(qkv) and not positions._overlaps(qkv[:, 1::2]) and not positions._overlaps(qkv[::2])
+
+
+def test_division_of_attention_at_the_edges():
+    """Fewer tokens than requests, no pages, tables of the greatest length, blocks of every size: some division, scratch within 2^20 (dim + 2) bytes."""
+    for dim in (16, 64, 96, 128, 256):
+        for page in (1, 16, 24):
+            c = cache(dim=dim, page_size=page, heads=8)
+            for tokens in (1, 5, 63, 64, 700, 20000):
+                for requests in (1, 3, 64, 600, 5000):
+                    for group in (1, 7):
+                        for width in (0, 1, 40, (2**31 - 5000) // page):
+                            for kind, longest in ((B.F32, 0), (B.BF16, 1), (B.F16, 3000), (B.BF16, 2**31 - 1)):
+                                d = B.AttendDesc(tokens, requests, group, width, longest, kind, 1, 0.1, 8 * group * dim, dim, width)
+                                how, size = B.int8t_mx4_cache_attend_division(c, d), call("int8t_mx4_cache_attend_workspace_bytes", C.byref(c), C.byref(d))
+                                assert how.rows in (16, 128, 256) and how.waves in (4, 8) and 1 <= how.shares <= 512
+                                assert (size > 0) == (how.shares > 1) and size <= (2**20 + 4096) * (dim + 2) + 512

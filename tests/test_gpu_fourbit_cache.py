@@ -140,6 +140,8 @@ def check_attend(cache, q, starts, lengths, table, causal=True, scale=None, long
     bound = (2 * ds[..., None] + e_p + e_sum) * absolute + e_out * 1.01 * want.abs() + floor + 1e-30
     if dt is F16:
         bound = bound + 2.0**-25                                            # (smallest fp16 step, halved)
+        # (what is 65520 or more, half a step above the largest, rounds to infinity)
+        got = torch.where(torch.isinf(got) & (got.sign() == want.sign()) & (want.abs() + bound >= 65520.0), want, got)
     assert bool(((got - want).abs() <= bound).all()), ((got - want).abs() / bound).max()
     none = torch.isinf(lse)
     assert torch.equal(none, torch.isinf(glse) & (glse < 0)) and not got[none].any()
@@ -195,11 +197,14 @@ def test_attend_chunks(dtype, causal, heads, group, dim, page):
 
 LARGE = [(8, 4, 128, 16, [300, 77, 1, 130], [500, 77, 40, 131]), (8, 8, 64, 16, [170, 0, 129, 3], [300, 9, 140, 64]), (8, 8, 64, 24, [170, 129], [300, 140]),
          (8, 5, 128, 7, [210, 60], [210, 333]), (8, 6, 256, 32, [190, 100], [400, 123]), (8, 6, 224, 10, [190, 100], [400, 123]), (8, 6, 96, 64, [300, 100], [310, 700]), (10, 8, 48, 1, [180], [200])]
+# ... with heads enough for larger blocks, and few of those in shares
+LARGER = [(40, 4, 128, 16, [300, 77, 1, 130], [500, 77, 40, 131]), (16, 8, 64, 16, [170, 0, 129, 3], [300, 9, 140, 64]), (16, 8, 64, 24, [170, 129], [300, 140]),
+          (27, 5, 128, 7, [210, 60], [210, 333]), (16, 6, 96, 64, [300, 100], [310, 700]), (27, 8, 48, 1, [180], [200]), (8, 4, 128, 16, [250, 150], [4100, 2500]), (4, 8, 64, 24, [256], [8200])]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("causal", [True, False])
-@pytest.mark.parametrize("heads,group,dim,page,new,lengths", LARGE)
+@pytest.mark.parametrize("heads,group,dim,page,new,lengths", LARGE + LARGER)
 def test_attend_of_larger_blocks(dtype, causal, heads, group, dim, page, new, lengths):
     cache, table = make_cache(lengths, heads, dim, page)
     q = queries(sum(new), heads * group, dim, dtype)
@@ -207,21 +212,31 @@ def test_attend_of_larger_blocks(dtype, causal, heads, group, dim, page, new, le
 
 
 def test_larger_blocks_are_used_by_those_calls():
-    for heads, group, dim, page, new, lengths in LARGE:
+    for heads, group, dim, page, new, lengths in LARGER:
         cache, table = make_cache(lengths, heads, dim, page)
         for dtype in (BF16, F32):
-            rows = division(cache, queries(sum(new), heads * group, dim, dtype), len(new), max(len(t) for t in table), True).rows
-            assert rows == (16 if dim > 128 or (dim > 64 and dtype is F32) else 128 if dim <= 64 else 256)
+            how = division(cache, queries(sum(new), heads * group, dim, dtype), len(new), max(len(t) for t in table), True)
+            assert how.rows == (16 if dim > 128 or (dim > 64 and dtype is F32) else 128 if dim <= 64 else 256)
+            assert (how.shares > 1) == (max(lengths) > 1024)
+
+
+@pytest.mark.parametrize("dtype,new", [(BF16, [1] * 530), (F32, [i % 3 for i in range(513)]), (BF16, [32] * 514)])
+def test_attend_of_many_requests(dtype, new):
+    """More of them than blocks look through: single tokens, some without a token or a key, and whole larger blocks."""
+    lengths = [max(n, (7 * b) % 60) for b, n in enumerate(new)]
+    cache, table = make_cache(lengths, 1, 64, 16)
+    check_attend(cache, queries(sum(new), 4, 64, dtype), starts_of(new), lengths, table, rows=128 if new[0] == 32 else 16)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("new", [[3, 2, 2], [300, 2, 200]])
 def test_attend_rows_that_see_nothing(dtype, new):
     """More new tokens than keys: the first see nothing; a request whose pages are not in the cache."""
-    lengths = [1, 0, 20]
-    cache, table = make_cache(lengths, 8, 64, 16)
+    lengths, large = [1, 0, 20], sum(new) > 100
+    heads = 24 if large else 8
+    cache, table = make_cache(lengths, heads, 64, 16)
     table[2] = [cache.pages, -5]
-    got = check_attend(cache, queries(sum(new), 32, 64, dtype), starts_of(new), lengths, table)
+    got = check_attend(cache, queries(sum(new), 4 * heads, 64, dtype), starts_of(new), lengths, table, rows=128 if large else 16)
     assert not got[sum(new[:1]):].any()
 
 
@@ -241,26 +256,39 @@ def test_attend_long_context(dtype, page):
 def test_attend_scales_far_apart(dtype, new, spread):
     """Blocks of a key and of a value 2^24 and 2^40 apart, scores of hundreds: what a row sees most of is what counts.  (Blocks of larger tiles lose bits 2^36 below their row's
     largest: 2^-36 6 of it is below the bound's 2^-17.)"""
-    lengths = [200, 333]
-    cache, table = make_cache(lengths, 8, 128, 16, spread=spread)
-    check_attend(cache, queries(sum(new), 32, 128, dtype, size=2.0**-spread), starts_of(new), lengths, table, causal=False)
+    lengths, large = [200, 333], sum(new) > 100
+    heads = 24 if large else 8
+    cache, table = make_cache(lengths, heads, 128, 16, spread=spread)
+    check_attend(cache, queries(sum(new), 4 * heads, 128, dtype, size=2.0**-spread), starts_of(new), lengths, table, causal=False, rows=256 if large and dtype is not F32 else 16)
+
+
+def test_attend_without_keys_or_pages():
+    """Fewer tokens than requests, tables without a column, lengths of zero."""
+    cache, _ = make_cache([20], 2, 64, 16)
+    for width in (0, 3):
+        for new in ([1, 0, 1], [0] * 63 + [2], [40, 0, 1]):
+            q = queries(sum(new), 8, 64, BF16)
+            args = [torch.tensor(v, dtype=torch.int32, device=DEV) for v in (starts_of(new), [0] * len(new))]
+            out, lse = cache.attend(q, *args, torch.zeros(len(new), width, dtype=torch.int32, device=DEV), return_lse=True)
+            assert not out.any() and (lse == -math.inf).all()
 
 
 def test_attend_scale_of_any_sign():
     lengths = [70, 333]
-    cache, table = make_cache(lengths, 8, 64, 16)
+    cache, table = make_cache(lengths, 24, 64, 16)
     for new in ([1, 4], [200, 190]):
-        q = queries(sum(new), 32, 64, BF16)
+        q = queries(sum(new), 96, 64, BF16)
         for scale in (-0.3, 0.0, 2.0):
-            check_attend(cache, q, starts_of(new), lengths, table, scale=scale, causal=False)
+            check_attend(cache, q, starts_of(new), lengths, table, scale=scale, causal=False, rows=128 if new[0] > 1 else 16)
 
 
 @pytest.mark.parametrize("new", [[1, 2], [300, 200]])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_nan_reaches_the_rows_that_see_it_and_no_others(new, dtype):
-    lengths = [320, 260]
-    cache, table = make_cache(lengths, 8, 64, 16)
-    q = queries(sum(new), 32, 64, dtype)
+    lengths, heads = [320, 260], 24
+    cache, table = make_cache(lengths, heads, 64, 16)
+    q = queries(sum(new), 4 * heads, 64, dtype)
+    assert division(cache, q, 2, 20, True).rows == (128 if sum(new) > 100 else 16)
     starts = starts_of(new)
     args = [torch.tensor(v, dtype=torch.int32, device=DEV) for v in (starts, lengths)]
     t = torch.zeros(2, 20, dtype=torch.int32)
@@ -277,14 +305,14 @@ def test_nan_reaches_the_rows_that_see_it_and_no_others(new, dtype):
         tensor[at] = before
         rows = torch.arange(sum(new), device=DEV)
         sees = (rows < new[0]) & (rows + lengths[0] - new[0] >= j)
-        bad = torch.zeros(sum(new), 32, dtype=torch.bool, device=DEV)
+        bad = torch.zeros(sum(new), 4 * heads, dtype=torch.bool, device=DEV)
         bad[sees, 4 * head:4 * head + 4] = True
         assert torch.equal(torch.isnan(got).all(-1), bad) and torch.equal(torch.isnan(got).any(-1), bad)
         assert torch.equal(got[~bad], clean[~bad])
     q2 = q.clone()
     q2[0, 7, 20] = float("nan")
     got = cache.attend(q2, *args, t)
-    bad = torch.zeros(sum(new), 32, dtype=torch.bool, device=DEV)
+    bad = torch.zeros(sum(new), 4 * heads, dtype=torch.bool, device=DEV)
     bad[0, 7] = True
     assert torch.equal(torch.isnan(got).all(-1), bad) and torch.equal(torch.isnan(got).any(-1), bad)
 
