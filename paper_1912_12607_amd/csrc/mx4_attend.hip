@@ -80,10 +80,10 @@ constexpr int rows_lds(int DIM, bool words, int RW) {
 //            group of four, so that the lanes' reads of four groups use all banks.
 // bf16 has fp32's range, so that no scale leaves the codes; q and p are held in pieces of it: q exactly (bf16 1, fp16 2, fp32 3 pieces), p to 16 bits for bf16 and fp16
 // tensors and to 24 for fp32 ones.
-// Bound by memory where keys are many: a token each of 64 requests of 1 to 8192 keys, 8 heads of 128 with four rows each, bf16, 77 to 80 us (4.1 TB/s; equal lengths of
-// 4096 64 us, 4.45 TB/s); vector instructions are issued in 40 % of the cycles, most of them codes' way to bf16.  Values through registers, as the 8-bit cache's blocks take
+// Bound by memory where keys are many: a token each of 64 requests of 1 to 8192 keys, 8 heads of 128 with four rows each, bf16, 72 to 77 us (4.3 to 4.5 TB/s;
+// equal lengths of 4096 in 60 to 62 with the joining pass); vector instructions are issued in 40 % of the cycles, most of them codes' way to bf16.  Values through registers, as the 8-bit cache's blocks take
 // them, were 105: a wave's loads were too few to fill the way to memory.  Few requests are bound by a wave's steps in
-// sequence (nine of up to 1500 keys, fp32, dim 64: 19 to 20 us, of which the joining pass is not a part).
+// sequence (nine of up to 1500 keys, fp32, dim 64: 20 us in one share each).
 // UNI: the page size is a multiple of 16 and DIM is the heads' dim (rounded up to blocks): whole tiles of 16 keys lie on a page and their address is scalar.
 // ------------------------------------------------------------------------------------------------
 template <int TYPE, int DIM, bool UNI, bool WORDS, int RW>

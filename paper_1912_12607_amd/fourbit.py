@@ -181,7 +181,8 @@ class _Linear4Fn(torch.autograd.Function):
 
 def linear4(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None, seed: int = 0) -> torch.Tensor:
     """x W^T + b, every product in microscaled 4-bit codes with blocks along its summed axis, differentiable (once): the gradients' codes are rounded
-    stochastically with draws of `seed`.  x (.., in) and weight (out, in) fp32, bf16 or fp16; bias fp32."""
+    stochastically with draws of `seed`.  x (.., in) and weight (out, in) fp32, bf16 or fp16; bias fp32.  A pass that is captured into a CUDA graph takes leaves of which no
+    eager autograd graph lives any more (torch would join the streams of both, and ends the process)."""
     return _Linear4Fn.apply(x, weight, bias, int(seed) & 0xFFFFFFFFFFFFFFFF)
 
 

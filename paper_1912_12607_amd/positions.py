@@ -158,7 +158,8 @@ class Rotary:
         return (yq,) if k is None else (yq, yk)
 
     def __call__(self, q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor):
-        """(q, k) turned, or q alone where k is None: (.., heads, dim) of one type, int32 positions (..).  Differentiable (once)."""
+        """(q, k) turned, or q alone where k is None: (.., heads, dim) of one type, int32 positions (..).  Differentiable (once); a pass that is captured into a CUDA graph
+        takes leaves of which no eager autograd graph lives any more, as linear4()."""
         if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad)):
             return _RotateFn.apply(self, positions, q, k)
         out = self._turn(self._check(q, k, positions), q, k, positions, 0)
