@@ -270,7 +270,7 @@ class PageTable:
         if tokens < 0:
             raise RuntimeError(f"{tokens} tokens")
         ints = new.new_empty(3 * tokens + 2 * n + 3)                                           # (slots take two each)
-        slots, positions, lengths, starts, available, without = ints.split((2 * tokens, tokens, n, n + 1, 1, 1))
+        slots, positions, lengths, starts, available, without = ints.split_with_sizes((2 * tokens, tokens, n, n + 1, 1, 1))
         at = ints.data_ptr()
         first = at + 12 * tokens
         desc = self._descs.get(tokens)

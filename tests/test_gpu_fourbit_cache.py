@@ -220,10 +220,11 @@ def test_larger_blocks_are_used_by_those_calls():
             assert (how.shares > 1) == (max(lengths) > 1024)
 
 
-@pytest.mark.parametrize("dtype,new", [(BF16, [1] * 530), (F32, [i % 3 for i in range(513)]), (BF16, [32] * 514)])
+@pytest.mark.parametrize("dtype,new", [(BF16, [1] * 530), (F32, [i % 3 for i in range(513)]), (BF16, [32] * 514), (BF16, [1] * 65), (F32, [i % 3 for i in range(512)]),
+                                       (F16, [0] * 64 + [3] + [0] * 63 + [2, 1]), (F32, [0, 7] * 100), (BF16, [32] * 320)])
 def test_attend_of_many_requests(dtype, new):
-    """More of them than blocks look through: single tokens, some without a token or a key, and whole larger blocks."""
-    lengths = [max(n, (7 * b) % 60) for b, n in enumerate(new)]
+    """More of them than a wave looks at once, and than blocks look through: single tokens, some without a token or a key, and whole larger blocks."""
+    lengths = [max(n, (7 * b) % 60 if b % 50 else 2100) for b, n in enumerate(new)]          # (some in shares)
     cache, table = make_cache(lengths, 1, 64, 16)
     check_attend(cache, queries(sum(new), 4, 64, dtype), starts_of(new), lengths, table, rows=128 if new[0] == 32 else 16)
 
