@@ -244,7 +244,7 @@ class PagedCache:
         (self.pages, self.heads, self.page_size), self.dim = kq.shape[:3], dim
         if self.dim % 16 or not 0 < self.dim <= 256:
             raise RuntimeError(f"head dimension {self.dim}: a multiple of 16, at most 256")
-        self._index = kq.get_device()
+        self._index, self._plans = kq.get_device(), {}
         self._c = struct(kq.data_ptr(), vq.data_ptr(), ks.data_ptr(), vs.data_ptr(), self.pages, self.page_size, self.heads, self.dim)
 
     # (not to be replaced: their addresses are taken once)
@@ -312,9 +312,11 @@ class PagedCache:
         n, wide = lengths.numel(), table.shape
         if lengths.dim() != 1 or starts.shape != (n + 1,) or len(wide) != 2 or wide[0] != n:
             raise RuntimeError(f"starts {tuple(starts.shape)}, lengths {tuple(lengths.shape)}, table {tuple(wide)}")
-        for t in (starts, lengths, table):
-            if t.dtype is not torch.int32 or t.get_device() != index:
-                raise RuntimeError(f"starts, lengths, table: int32 on {q.device}, not {t.dtype} on {t.device}")
+        i32 = torch.int32
+        if not (starts.dtype is i32 and lengths.dtype is i32 and table.dtype is i32 and starts.get_device() == lengths.get_device() == table.get_device() == index):
+            for t in (starts, lengths, table):
+                if t.dtype is not i32 or t.get_device() != index:
+                    raise RuntimeError(f"starts, lengths, table: int32 on {q.device}, not {t.dtype} on {t.device}")
         token, head, step = q.stride()
         if step != 1:
             q = q.contiguous()
@@ -328,9 +330,15 @@ class PagedCache:
         out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape)
         lse = torch.empty((T, heads), dtype=torch.float32, device=q.device) if return_lse else None
         if T:
-            d = B.AttendDesc(T, n, heads // self.heads, wide[1], 0 if longest is None else max(1, int(longest)), kind, 1 if causal else 0,
-                             dim ** -0.5 if scale is None else scale, token, head, max(pitch, wide[1]))
-            need = self._calls[2](self._c, d)
+            # (descriptors and scratch bytes of the last calls' sizes)
+            key = T, n, heads, wide[1], 0 if longest is None else max(1, int(longest)), kind, 1 if causal else 0, dim ** -0.5 if scale is None else float(scale), token, head, pitch
+            plan = self._plans.get(key)
+            if plan is None:
+                d = B.AttendDesc(T, n, heads // self.heads, *key[3:10], max(pitch, wide[1]))
+                if len(self._plans) >= 256:
+                    self._plans.clear()
+                plan = self._plans[key] = d, self._calls[2](self._c, d)
+            d, need = plan
             ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
             _call(index, self._calls[3], self._c, d, q.data_ptr(), starts.data_ptr(), lengths.data_ptr(), table.data_ptr(), out.data_ptr(),
                   None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), need)
