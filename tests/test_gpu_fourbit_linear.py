@@ -44,7 +44,8 @@ def near(got, a, b, dtype, bias=None):
 
 
 # few tokens, tiles of each size, odd everything
-SERVED = [(1, 1, 1), (1, 4096, 4096), (2, 33, 17), (3, 300, 1000), (9, 2048, 1000), (16, 4096, 100), (17, 64, 40), (16, 8192, 33), (40, 1000, 300), (130, 520, 515), (1, 33000, 5)]
+SERVED = [(1, 1, 1), (1, 4096, 4096), (2, 33, 17), (3, 300, 1000), (9, 2048, 1000), (16, 4096, 100), (17, 64, 40), (16, 8192, 33), (40, 1000, 300), (130, 520, 515), (1, 33000, 5), (16, 2048, 100), (16, 3000, 33), (3, 2048, 5001),
+          (2, 500, 9000)]
 
 
 @pytest.mark.parametrize("M,K,N", SERVED)
@@ -181,6 +182,26 @@ def test_linear_of_no_tokens_single_gradients_and_broadcast_ones():
     one = torch.ones(33, 20, device=DEV)
     parts = [torch.autograd.grad(fourbit.linear4(xs, w, None, seed=s), w, one)[0] for s in (1, 2)]
     assert torch.equal(torch.autograd.grad(y, w)[0], parts[0] + parts[1])
+
+
+@pytest.mark.parametrize("M,K,N", [(200, 64, 48), (300, 64, 40), (1030, 130, 600), (700, 2100, 31)])
+def test_each_gradient_by_itself(M, K, N):
+    """The same numbers whichever of the gradients are wanted."""
+    x, w, b = torch.randn(M, K, device=DEV, dtype=BF16), torch.randn(N, K, device=DEV, dtype=BF16), torch.randn(N, device=DEV)
+    dy = torch.randn(M, N, device=DEV, dtype=BF16)
+
+    def grads(want):
+        leaves = [t.clone().requires_grad_(n in want) for t, n in ((x, "x"), (w, "w"), (b, "b"))]
+        fourbit.linear4(*leaves, seed=5).backward(dy)
+        return [t.grad for t in leaves]
+    all_ = grads("xwb")
+    assert torch.equal(all_[2], grads("b")[2])
+    exact = dy.double().sum(0)
+    # (a part of 256 rows: 7 sums of a lane, 3 of lanes, 2 of waves in a row; parts in 64 bits, rounded once)
+    assert ((all_[2].double() - exact).abs() <= 13.1 * 2.0**-24 * dy.double().abs().sum(0)).all()
+    for want in ("x", "w", "xw", "xb", "wb"):
+        for got, ref, name in zip(grads(want), all_, "xwb"):
+            assert (got is None) == (name not in want) and (got is None or torch.equal(got, ref)), (want, name)
 
 
 @pytest.mark.parametrize("M", [1, 3, 40])
