@@ -101,19 +101,19 @@ __global__ __launch_bounds__(64 * RW, 2) void mx_attend_rows_kernel(const Attend
     const int head = place - group_of * a.c.heads;
     const int D = a.c.dim, NB = UNI ? DIM / 32 : mx_blocks(D), RB = 16 * NB;
 
-    Unit unit_;
+    Unit job;
     if (a.close) {
-        if (!unit_of(a, group_of, 16, true, lane, &unit_)) return;
+        if (!unit_of(a, group_of, 16, true, lane, &job)) return;
     } else {
         const int block = (int)gridDim.x - 1 - group_of;
         const int b = block_request(a, block, lane);
-        unit_.rq = request_of(a, b);
-        unit_.tile = (int)((long long)block - ((long long)a.starts[b] * a.group / 16 + b));
-        unit_.share = (int)blockIdx.z;
-        unit_.shares = shares_of(a, unit_.rq.length);
+        job.rq = request_of(a, b);
+        job.tile = (int)((long long)block - ((long long)a.starts[b] * a.group / 16 + b));
+        job.share = (int)blockIdx.z;
+        job.shares = shares_of(a, job.rq.length);
     }
-    const Request& rq = unit_.rq;
-    const int nrows = rq.tokens * a.group, tile = unit_.tile, split = unit_.share, shares = unit_.shares;
+    const Request& rq = job.rq;
+    const int nrows = rq.tokens * a.group, tile = job.tile, split = job.share, shares = job.shares;
     if (tile < 0 || (long long)tile * 16 >= nrows) return;
     const int r0 = tile * 16;
     const int heads = a.c.heads * a.group;
@@ -124,8 +124,9 @@ __global__ __launch_bounds__(64 * RW, 2) void mx_attend_rows_kernel(const Attend
     const int seen_end = max(0, a.causal ? min(rq.length, behind + last_token + 1) : rq.length);
     const int all = max(0, a.causal ? min(rq.length, behind + div_by(r0, a.by_group) + 1) : rq.length);      // keys that all of its rows see
     const int all_steps = (seen_end + 31) >> 5;
-    const int from = split < shares ? 32 * (int)((long long)all_steps * split / shares) : seen_end;
-    const int end = split < shares ? min(32 * (int)((long long)all_steps * (split + 1) / shares), seen_end) : seen_end;
+    const int each = (int)((uint32_t)all_steps / (uint32_t)shares), more = all_steps - each * shares;      // (shares of `each` steps, the first ones of one more)
+    const int from = split < shares ? min(32 * (each * split + min(split, more)), seen_end) : seen_end;
+    const int end = split < shares ? min(32 * (each * (split + 1) + min(split + 1, more)), seen_end) : seen_end;
     if (a.splits > 1) {
         // nothing here, or in the shares behind the request's last (which have blocks of their own where those are not close): the joining pass looks at m alone
         const bool none = from >= end && split != 0;

@@ -64,7 +64,7 @@ __device__ __forceinline__ int wave_sums(int n) {
     return n;
 }
 // The shares that a request of `length` keys is dealt out in: as many of `share` keys as it has, `splits` at most
-__device__ __forceinline__ int shares_of(const AttendArgs& a, int length) { return a.splits == 1 ? 1 : max(1, min(a.splits, (int)(((long long)length + a.share - 1) / a.share))); }
+__device__ __forceinline__ int shares_of(const AttendArgs& a, int length) { return a.splits == 1 || length <= a.share ? 1 : min(a.splits, div_by(length - 1, a.by_share) + 1); }
 
 // What request, which tile of `rows` rows of it and which share the u-th block (of a head) has, counted over those that there are: false behind the last one.  A request's last rows,
 // which see the most keys, come first.  Workgroups are dealt out to an XCD's groups of compute units in turn, whatever these have to do: where every other one ends
@@ -84,7 +84,7 @@ __device__ __forceinline__ bool unit_of(const AttendArgs& a, int u, int rows, bo
             const int all = __builtin_amdgcn_readlane(tiles, l), in = u - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(units, l));
             out->rq = request_of(a, r0 + l, __builtin_amdgcn_readlane(s0, l), __builtin_amdgcn_readlane(s1, l), __builtin_amdgcn_readlane(len, l));
             out->shares = __builtin_amdgcn_readlane(shares, l);
-            out->share = in / max(all, 1);
+            out->share = (int)((uint32_t)in / (uint32_t)max(all, 1));
             out->tile = all - 1 - (in - out->share * all);
             return true;
         }

@@ -543,6 +543,7 @@ void attend_plan(AttendArgs* a, int longest) {
             a->share = (int)((longest + most - 1) / most + 31) & ~31;
         }
         if (a->splits < 1) a->splits = 1;
+        if (a->mx) a->by_share = fast_div((unsigned)a->share);
         return;
     }
     a->waves = a->rows / 32;

@@ -81,19 +81,19 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
     const int head = place - group_of * a.c.heads, block = (int)gridDim.x - 1 - group_of;
     const int D = a.c.dim;
 
-    Unit u_;
+    Unit job;
     if (close) {
-        if (!unit_of(a, group_of, ROWS, false, lane, &u_)) return;
+        if (!unit_of(a, group_of, ROWS, false, lane, &job)) return;
     } else {
         const int b = tile_request(a, block, ROWS);
-        u_.rq = request_of(a, b);
-        u_.tile = (int)((long long)block - ((long long)a.starts[b] * a.group / ROWS + b));
-        u_.share = (int)blockIdx.z;
+        job.rq = request_of(a, b);
+        job.tile = (int)((long long)block - ((long long)a.starts[b] * a.group / ROWS + b));
+        job.share = (int)blockIdx.z;
     }
-    const int split = u_.share;
-    const Request& rq = u_.rq;
+    const int split = job.share;
+    const Request& rq = job.rq;
     const int nrows = rq.tokens * a.group;
-    const int tile = u_.tile;
+    const int tile = job.tile;
     if (tile < 0 || (long long)tile * ROWS >= nrows) return;
     const int r0 = (int)tile * ROWS;
     const int row = r0 + 32 * wave + n32;

@@ -178,6 +178,7 @@ struct AttendArgs {
     int rows, waves;         // of a block: attend_plan()
     int splits;              // blocks per row tile; blocks of 16 rows: the last one has what is left
     int share;               // keys of one, blocks of 16 rows (a multiple of 32)
+    FastDiv by_share;        // (4 bits)
     float *part_o, *part_ml; // [splits][tokens * heads * group][dim], [..][2]
     int wide_q;
     int mx;                  // the cache holds microscaled 4-bit codes (mx4.h)
