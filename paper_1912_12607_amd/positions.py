@@ -17,32 +17,50 @@ from typing import NamedTuple
 import torch
 
 from . import binding as B
-from .tokens import _call, _type
+from .tokens import _call, _tangent, _transformed, _type
 
 
 class _RotateFn(torch.autograd.Function):
+    """back: by the negative angles.  A turn is linear: gradients are turned back, tangents as what they belong to."""
+
     @staticmethod
-    def forward(ctx, rotary, positions, q, k):
-        ctx.rotary, ctx.two, ctx.plan = rotary, k is not None, rotary._check(q, k, positions)
+    def forward(ctx, rotary, positions, q, k, back):
+        ctx.rotary, ctx.two, ctx.plan, ctx.back = rotary, k is not None, rotary._check(q, k, positions), back
+        ctx.shapes = (q.shape, k.shape) if ctx.two else (q.shape,)
         ctx.save_for_backward(positions)
+        ctx.save_for_forward(positions)
         ctx.set_materialize_grads(False)
-        out = rotary._turn(ctx.plan, q, k, positions, 0)
+        out = rotary._turn(ctx.plan, q, k, positions, back)
         return out if ctx.two else out[0]
+
+    @staticmethod
+    def jvp(ctx, _rotary, _positions, q, k, _back):
+        positions, = ctx.saved_tensors
+        tangents = (q, k) if ctx.two else (q,)
+        there = [t for t in tangents if t is not None]
+        turned = _RotateFn.apply(ctx.rotary, positions, there[0], there[1] if len(there) > 1 else None, ctx.back)
+        turned = iter(turned if len(there) > 1 else (turned,))
+        out = [next(turned) if t is not None else there[0].new_zeros(shape) for t, shape in zip(tangents, ctx.shapes)]
+        return tuple(out) if ctx.two else out[0]
 
     @staticmethod
     def backward(ctx, *grads):
         if torch.is_grad_enabled():
             raise RuntimeError("a Rotary is differentiable once")
         positions, = ctx.saved_tensors
-        if ctx.two and grads[0] is not None and grads[1] is not None and ctx.needs_input_grad[2] and ctx.needs_input_grad[3]:
-            return None, None, *ctx.rotary._turn(ctx.plan, *grads, positions, 1)
-        want = [g if n else None for g, n in zip(grads, ctx.needs_input_grad[2:])]
+        want = [g if n else None for g, n in zip(grads, ctx.needs_input_grad[2:4])]
         there = [g for g in want if g is not None]
         if not there:
-            return None, None, None, None
-        turned = iter(ctx.rotary._turn(ctx.rotary._check(there[0], None, positions), there[0], None, positions, 1))
+            return None, None, None, None, None
+        second = there[1] if len(there) > 1 else None
+        if _transformed():                       # (gradients may have tangents)
+            turned = _RotateFn.apply(ctx.rotary, positions, there[0], second, 1 - ctx.back)
+            turned = iter(turned if second is not None else (turned,))
+        else:
+            plan = ctx.plan if len(there) == 1 + ctx.two else ctx.rotary._check(there[0], None, positions)
+            turned = iter(ctx.rotary._turn(plan, there[0], second, positions, 1 - ctx.back))
         out = [next(turned) if g is not None else None for g in want]
-        return (None, None, out[0], out[1] if ctx.two else None)
+        return (None, None, out[0], out[1] if ctx.two else None, None)
 
 
 class Rotary:
@@ -158,10 +176,10 @@ class Rotary:
         return (yq,) if k is None else (yq, yk)
 
     def __call__(self, q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor):
-        """(q, k) turned, or q alone where k is None: (.., heads, dim) of one type, int32 positions (..).  Differentiable (once); a pass that is captured into a CUDA graph
-        takes leaves of which no eager autograd graph lives any more, as linear4()."""
-        if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad)):
-            return _RotateFn.apply(self, positions, q, k)
+        """(q, k) turned, or q alone where k is None: (.., heads, dim) of one type, int32 positions (..).  Differentiable (once, and in forward mode); a pass that is captured
+        into a CUDA graph takes leaves of which no eager autograd graph lives any more, as linear4()."""
+        if (torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad))) or _transformed():
+            return _RotateFn.apply(self, positions, q, k, 0)
         out = self._turn(self._check(q, k, positions), q, k, positions, 0)
         return out if k is not None else out[0]
 
@@ -171,7 +189,7 @@ class Rotary:
         for x in (q, k):
             if x is None:
                 continue
-            if x.requires_grad and torch.is_grad_enabled():
+            if (x.requires_grad and torch.is_grad_enabled()) or (_transformed() and _tangent(x)):
                 raise RuntimeError("turn_ has no gradients")
             if not x.is_contiguous() and (x.stride(-1) != 1 or x.dim() != 3 or _overlaps(x)):
                 raise RuntimeError(f"in place with strides {x.stride()} of {tuple(x.shape)}")

@@ -33,6 +33,20 @@ def _type(t: torch.Tensor, name: str) -> int:
     return B.DTYPES[t.dtype]
 
 
+_forward_ad = torch.autograd.forward_ad
+_functorch_active = getattr(torch._C, "_are_functorch_transforms_active", lambda: False)
+
+
+def _transformed() -> bool:
+    """Whether a call may see tensors that have tangents (a level of forward-mode differentiation), or that a transformation stands behind."""
+    return getattr(_forward_ad, "_current_level", -1) >= 0 or _functorch_active()
+
+
+def _tangent(t: torch.Tensor) -> bool:
+    """Whether t has a tangent at the present level of forward-mode differentiation."""
+    return _forward_ad.unpack_dual(t).tangent is not None
+
+
 def _rows(t: torch.Tensor, cols: int):
     """(t as rows of `cols` contiguous values, elements between rows); a copy where its strides do not allow it."""
     if t.dim() != 2:
