@@ -16,7 +16,7 @@ import functools
 import torch
 
 from . import binding as B
-from .tokens import PagedCache, TokenLinear, _call, _rows, _type, _vector
+from .tokens import PagedCache, TokenLinear, _call, _rows, _tangent, _transformed, _type, _vector
 
 
 def _blocks(n: int) -> int:
@@ -150,6 +150,8 @@ class _Linear4Fn(torch.autograd.Function):
     def backward(ctx, dy):
         if torch.is_grad_enabled():
             raise RuntimeError("linear4() is differentiable once")
+        if _transformed() and _tangent(dy):
+            raise RuntimeError("linear4() has no forward mode, its gradient neither")
         want_x, want_w, want_b = ctx.needs_input_grad[:3]
         desc, dev = ctx.desc, dy.device
         M, K, N = desc.M, desc.K, desc.N

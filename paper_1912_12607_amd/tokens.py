@@ -179,6 +179,8 @@ class _LinearFn(torch.autograd.Function):
     def backward(ctx, dy):
         if torch.is_grad_enabled():
             raise RuntimeError("linear() is differentiable once")
+        if _transformed() and _tangent(dy):
+            raise RuntimeError("linear() has no forward mode, its gradient neither")
         want_x, want_w, want_b = ctx.needs_input_grad[:3]
         desc, dev = ctx.desc, dy.device
         M, K, N = desc.M, desc.K, desc.N

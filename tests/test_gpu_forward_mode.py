@@ -16,6 +16,7 @@ if ROOT not in sys.path:
 
 import torch.autograd.forward_ad as forward_ad  # noqa: E402
 
+from paper_1912_12607_amd import fourbit, tokens  # noqa: E402
 from paper_1912_12607_amd.positions import Rotary  # noqa: E402
 
 DEV = torch.device("cuda:0")
@@ -56,3 +57,20 @@ def test_transformations_are_refused():
         torch.func.jvp(lambda x: rotary(x, None, at), (q,), (q,))
     with pytest.raises(RuntimeError):
         torch.func.vmap(lambda x: rotary(x, None, at))(q.expand(2, 3, 4, 16))
+
+
+@pytest.mark.parametrize("layer", [tokens.linear, fourbit.linear4])
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_linear_layers_refuse_tangents(layer, which):
+    """Of their arguments, and of the gradient that comes in (forward over reverse): none is dropped."""
+    args = [normal(5, 64), normal(32, 64, seed=1), normal(32, seed=2)]
+    with forward_ad.dual_level():
+        for grad in (True, False):
+            with torch.set_grad_enabled(grad), pytest.raises(RuntimeError):
+                layer(*(forward_ad.make_dual(a, a.clone()) if i == which else a for i, a in enumerate(args)))
+        leaves = [a.clone().requires_grad_(i == which) for i, a in enumerate(args)]
+        y = layer(*leaves)
+        g = normal(5, 32, seed=3)
+        with pytest.raises(RuntimeError, match="forward mode"):
+            torch.autograd.grad(y, leaves[which], forward_ad.make_dual(g, g.clone()))
+        assert torch.isfinite(torch.autograd.grad(layer(*leaves), leaves[which], g)[0]).all()
