@@ -108,42 +108,46 @@ class ServedLinear4:
         return y
 
 
+def _linear4(x, w, bias, want_x=False, want_w=False, want_b=False):
+    """(y, the plan, what the gradients that are wanted read: codes and scales of x and W by columns, in one piece of memory, or None)."""
+    kind, wkind = _type(x, "x"), _type(w, "weight")
+    shape = x.shape
+    if w.dim() != 2 or not shape or shape[-1] != w.shape[1] or w.device != x.device:
+        raise RuntimeError(f"input of {tuple(shape)} on {x.device}, weight of {tuple(w.shape)} on {w.device}")
+    N, K = w.shape
+    index, dev = x.get_device(), x.device
+    bias = _vector(bias, N, "bias", index)
+    (rows, pitch), (wr, w_pitch) = _rows(x, K), _rows(w, K)
+    M = rows.shape[0]
+    y = x.new_empty(shape[:-1] + (N,))
+    plan = desc, (need, later, _), places, size = _plan(M, K, N, kind, wkind)
+    kept = None
+    if M:
+        b = B.Mx4LinearBuffers()
+        if (want_x or want_w or want_b) and not later:
+            raise RuntimeError(f"{M} tokens, {K} inputs, {N} outputs: a backward pass of that size is not served")
+        if want_x or want_w:
+            kept = torch.empty(size, dtype=torch.uint8, device=dev)
+            at = kept.data_ptr()
+            if want_w:
+                b.xt, b.sxt = at, at + places[1]
+            if want_x:
+                b.wt, b.swt = at + places[2], at + places[3]
+        b.x, b.x_pitch, b.w, b.w_pitch, b.y, b.y_pitch = rows.data_ptr(), pitch, wr.data_ptr(), w_pitch, y.data_ptr(), N
+        if bias is not None:
+            b.bias = bias.data_ptr()
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        b.ws, b.ws_bytes = ws.data_ptr(), need
+        _call(index, B.lib.int8t_mx4_linear_fwd, desc, b)
+    return y, plan, kept
+
+
 class _Linear4Fn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, bias, seed):
-        kind, wkind = _type(x, "x"), _type(w, "weight")
-        shape = x.shape
-        if w.dim() != 2 or not shape or shape[-1] != w.shape[1] or w.device != x.device:
-            raise RuntimeError(f"input of {tuple(shape)} on {x.device}, weight of {tuple(w.shape)} on {w.device}")
-        N, K = w.shape
-        index, dev = x.get_device(), x.device
-        bias = _vector(bias, N, "bias", index)
-        (rows, pitch), (wr, w_pitch) = _rows(x, K), _rows(w, K)
-        M = rows.shape[0]
-        y = x.new_empty(shape[:-1] + (N,))
-        # codes and scales of x and W by columns, in one piece of memory: the backward pass reads them
-        desc, (need, later, _), places, size = _plan(M, K, N, kind, wkind)
-        kept = None
-        if M:
-            b = B.Mx4LinearBuffers()
-            want_x, want_w, want_b = ctx.needs_input_grad[:3]
-            if (want_x or want_w or want_b) and not later:
-                raise RuntimeError(f"{M} tokens, {K} inputs, {N} outputs: a backward pass of that size is not served")
-            if want_x or want_w:
-                kept = torch.empty(size, dtype=torch.uint8, device=dev)
-                at = kept.data_ptr()
-                if want_w:
-                    b.xt, b.sxt = at, at + places[1]
-                if want_x:
-                    b.wt, b.swt = at + places[2], at + places[3]
-            b.x, b.x_pitch, b.w, b.w_pitch, b.y, b.y_pitch = rows.data_ptr(), pitch, wr.data_ptr(), w_pitch, y.data_ptr(), N
-            if bias is not None:
-                b.bias = bias.data_ptr()
-            ws = torch.empty(need, dtype=torch.uint8, device=dev)
-            b.ws, b.ws_bytes = ws.data_ptr(), need
-            _call(index, B.lib.int8t_mx4_linear_fwd, desc, b)
+        y, (ctx.desc, (_, ctx.need, _), ctx.places, _), kept = _linear4(x, w, bias, *ctx.needs_input_grad[:3])
         ctx.save_for_backward(*(() if kept is None else (kept,)))
-        ctx.desc, ctx.need, ctx.places, ctx.seed, ctx.x_shape, ctx.w_dtype = desc, later, places, seed, shape, w.dtype
+        ctx.seed, ctx.x_shape, ctx.w_dtype = seed, x.shape, w.dtype
         return y
 
     @staticmethod
@@ -185,6 +189,9 @@ def linear4(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = N
     """x W^T + b, every product in microscaled 4-bit codes with blocks along its summed axis, differentiable (once): the gradients' codes are rounded
     stochastically with draws of `seed`.  x (.., in) and weight (out, in) fp32, bf16 or fp16; bias fp32.  A pass that is captured into a CUDA graph takes leaves of which no
     eager autograd graph lives any more (torch would join the streams of both, and ends the process)."""
+    # (what no graph records keeps nothing: a Function's needs_input_grad goes by the leaves alone)
+    if not _transformed() and not (torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad))):
+        return _linear4(x, weight, bias)[0]
     return _Linear4Fn.apply(x, weight, bias, int(seed) & 0xFFFFFFFFFFFFFFFF)
 
 
