@@ -633,7 +633,8 @@ int8t_status int8t_cache_read(const int8t_cache *cache, const int64_t *slots_dev
  * h * group + g goes with head h of the cache.
  *   out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale * q . k_j), sums in fp32;  zeros where a token sees nothing (its lse: -infinity)
  *   q_dev        element (t, head, d) at t * q_token_pitch + head * q_head_pitch + d
- *   starts_dev   requests + 1 ints, ascending from 0 to `tokens`;   lengths_dev  `requests` ints
+ *   starts_dev   requests + 1 ints, ascending, at most `tokens`; tokens before the first or behind the last are no request's: nothing of theirs is written
+ *   lengths_dev  `requests` ints
  *   table_dev    pages of a request in order: [requests][table_width], rows table_pitch apart; entries behind the last page that a length
  *                needs are not used; keys on a page that is not in the cache are not seen; table_width * page_size < 2^31 - 4096
  *   longest      no length is larger (a guide for the division of the work, by which sums are ordered; keys behind it are seen all the same); 0: unknown

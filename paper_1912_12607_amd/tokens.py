@@ -318,7 +318,8 @@ class PagedCache:
         starts[b] .. starts[b + 1] - 1 and see the first lengths[b] keys of pages table[b], causal: each up to its own place (the last
         new token sees all).  Query heads are a multiple of the cache's; head h goes with h // group.  `longest`: no length is larger
         (a guide for the division of the work, by which sums are ordered).  int32 starts (requests + 1), lengths (requests), table (requests, width).
-        A token that sees nothing gets zeros (logarithm of its sum: -inf).  No gradients."""
+        A token that sees nothing gets zeros (logarithm of its sum: -inf); what tokens before the first request's or behind the last one's get is not
+        defined.  No gradients."""
         kind = B.DTYPES.get(q.dtype)
         shape, index = q.shape, self._index
         if kind is None or len(shape) != 3 or shape[2] != self.dim or shape[1] % self.heads or shape[1] == 0 or q.get_device() != index:
