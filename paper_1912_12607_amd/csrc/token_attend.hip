@@ -368,12 +368,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     const size_t rows = (size_t)a.tokens * a.c.heads * a.group;
     const size_t row = ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * 16 + ((int)threadIdx.x >> 4);      // (y: a launch has fewer than 2^32 threads a dimension)
     const int l = (int)threadIdx.x & 15, D = a.c.dim;
-    const bool there = row < rows;                      // (all lanes stay for the exchanges)
-    const size_t r = there ? row : 0;
-    // Tokens before the first request's or behind the last one's have no sums, and are left as they are.
-    const size_t per = (size_t)a.c.heads * a.group;
-    const int first = a.starts[0], last = a.starts[a.requests];
-    const bool have = there && row >= (size_t)(first < 0 ? 0 : first) * per && row < (size_t)(last < 0 ? 0 : last) * per;
+    const bool have = row < rows;                       // (all lanes stay for the exchanges)
+    const size_t r = have ? row : 0;
+    // Tokens before the first request's or behind the last one's have no sums, and are left as they are: found out beside the sums, used when these are there.
+    const uint32_t per = (uint32_t)(a.c.heads * a.group), first = (uint32_t)min(max(a.starts[0], 0), a.tokens) * per, behind = (uint32_t)min(max(a.starts[a.requests], 0), a.tokens) * per;
     float m = kNone, total = 0.0f;
     int end = 0;                                        // behind the last share that saw keys
     for (int s = l; s < a.splits; s += 16) {
@@ -392,7 +390,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
         m = m1;
         end = max(end, __shfl_xor(end, o, kWave));
     }
-    if (!have) return;
+    if (!have || (uint32_t)row < first || (uint32_t)row >= behind) return;
     const float by = per_sum(total);
     if (l == 0 && a.lse) a.lse[row] = log_of_sum(m, total);
     for (int d = l * 8; d < D; d += 128) {
