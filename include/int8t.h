@@ -734,7 +734,8 @@ int8t_status int8t_mx4_linear_bwd(const int8t_linear_desc *desc, const int8t_mx4
  * A paged cache of keys and values in these codes, blocks along a head's dims: places, slots and limits as int8t_cache.  dim: a multiple of 16, at most 256.
  * int8t_mx4_cache_write, _read, _attend: as int8t_cache_write, _read, _attend with k, v what codes and scales stand for.
  * attend: blocks with the byte 0 (below 2^-124) count as zeros;  q . k_j exact products in fp32 sums (blocks of 16 rows; larger ones as the 8-bit cache's, with fp16 codes relative to the largest scale of a key's row:
- * blocks 2^36 below it lose bits, but keys of bf16 tensors, whose products stay exact); p_j is rounded to 16 bits for bf16 and fp16 tensors and 24 for fp32 ones (larger blocks: 11 and 22).  A key or value with a block
+ * blocks 2^36 below it lose bits, but keys of bf16 tensors, whose products stay exact); p_j is rounded to 16 bits for bf16 and fp16 tensors and 24 for fp32 ones (larger blocks: 11 and 22),
+ * and held down to 2^-126 of the row's largest (blocks of 16 rows; value scales beyond 2^96 shorten that by up to as much).  A key or value with a block
  * of scale 255 (values, in blocks of 16 rows: 253 and more, whose products pass fp32) makes the rows that see it NaN, all of their dims, and no others.
  */
 typedef struct int8t_mx4_cache {

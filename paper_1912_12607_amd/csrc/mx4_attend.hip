@@ -41,6 +41,13 @@ __device__ __forceinline__ void load16_lds(uint32_t lds, const void* base, uint3
 __device__ __forceinline__ void load16_lds(uint32_t lds, const void* at) { asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at) : "memory"); }
 __device__ __forceinline__ void load4_lds(uint32_t lds, const void* at) { asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(at) : "memory"); }
 __device__ __forceinline__ void load1_lds(uint32_t lds, const void* at) { asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_ubyte %1, off" ::"s"(lds), "v"(at) : "memory"); }
+// The largest of the 16 lanes that have a key's dims
+__device__ __forceinline__ uint32_t dims_max(uint32_t v) {
+    v = max(v, (uint32_t)dpp_word<kDppSwap1>((int)v));
+    v = max(v, (uint32_t)dpp_word<kDppSwap2>((int)v));
+    v = max(v, (uint32_t)dpp_word<0x141>((int)v));           // (row_half_mirror: the quads of eight lanes)
+    return max(v, (uint32_t)dpp_word<0x140>((int)v));        // (row_mirror: the eights)
+}
 // In a branch that is seldom taken: keeps the compiler from running what it holds every time and selecting.
 __device__ __forceinline__ void rarely() { asm volatile(""); }
 template <int N>
@@ -147,6 +154,8 @@ __global__ __launch_bounds__(64 * RW, 2) void mx_attend_rows_kernel(const Attend
     // this wave's keys: whole 32s of the block's share
     const int steps = (end - from + 31) >> 5;
     const int s_from = steps * wave / RW, s_to = steps * (wave + 1) / RW;
+    // Blocks of values up to this byte need no look: sums of p v with p up to 2^16, 2^16 6 2^(byte - 127) of each of the wave's keys, stay below 2^127.
+    const uint32_t calm = 235u - (32u - (uint32_t)__builtin_clz(32 * max(s_to - s_from, 1)));
 
     // ---- loader: codes of keys and values and their scales, as they are, into the wave's steps in LDS
     const uint8_t *const kq = reinterpret_cast<const uint8_t*>(a.c.kq), *const vq = reinterpret_cast<const uint8_t*>(a.c.vq);
@@ -378,6 +387,15 @@ __global__ __launch_bounds__(64 * RW, 2) void mx_attend_rows_kernel(const Attend
 #pragma unroll
         for (int u = 0; u < 8; ++u) top = fmaxf(top, x[u]);
         top *= qscale;
+        // Larger values take as much from p's range as they are beyond that: the unit goes by a key's score and this together (by 29 more at most with 32 keys).  By the row's own
+        // keys: one that it does not see, or sees at 2^-100, leaves the others their bits.
+        const bool large = __any(largest_scale > calm);
+        if (large) {
+            top = kNone;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) top = fmaxf(top, __builtin_fmaf(x[u], qscale, (float)(max(dims_max(vs[u]), calm) - calm)));
+            rarely();
+        }
         // (bf16 holds p far above 1: the unit moves rarely)
         if (__any(top > m + 16.0f)) {
             const float largest = halves_max(rows16_max(top));
@@ -397,7 +415,7 @@ __global__ __launch_bounds__(64 * RW, 2) void mx_attend_rows_kernel(const Attend
             l += x[u];
         }
         // Values that are not finite (some lane has a block of them) go into p of the rows that see them, and become zeros for the others.
-        if (__any(largest_scale >= 253u)) {
+        if (large) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const unsigned long long lanes = __ballot(vs[u] >= 253u) >> (16 * kg) & 0xffffull;
@@ -458,6 +476,8 @@ __global__ __launch_bounds__(64 * RW, 2) void mx_attend_rows_kernel(const Attend
     constexpr int LR = 4 * RW, PER = DIM / LR < 4 ? 4 : DIM / LR;      // lanes per row; dims of a lane
     const int jr = (int)threadIdx.x / LR, jl = (int)threadIdx.x % LR;
     if (r0 + jr >= nrows) return;
+    // An eighth of the waves' sums (the joining pass takes them so): together they may pass fp32 where their mean does not.
+    constexpr float kEighth = 1.0f / kRowsPartScale;
     float mm = sm[jr], total = 0.0f, w[RW];
 #pragma unroll
     for (int i = 1; i < RW; ++i) mm = fmaxf(mm, sm[16 * i + jr]);
@@ -466,12 +486,13 @@ __global__ __launch_bounds__(64 * RW, 2) void mx_attend_rows_kernel(const Attend
         const float mi = sm[16 * i + jr];
         w[i] = mi == kNone ? 0.0f : __builtin_amdgcn_exp2f(mi - mm);
         total += w[i] * sl[16 * i + jr];
+        w[i] *= kEighth;
     }
     const int jt = div_by(r0 + jr, a.by_group), jg = (r0 + jr) - jt * a.group;
     const size_t out_row = (size_t)(rq.token0 + jt) * heads + head * a.group + jg;
     const bool whole = a.splits == 1;
     const size_t part_row = (size_t)split * a.tokens * heads + out_row;
-    const float by = whole ? per_sum(total) : 1.0f;
+    const float by = whole ? per_sum(total) * kRowsPartScale : 1.0f;
     if (jl == 0) {
         if (whole) {
             if (a.lse) a.lse[out_row] = log_of_sum(mm, total);

@@ -391,7 +391,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
         end = max(end, __shfl_xor(end, o, kWave));
     }
     if (!have || (uint32_t)row < first || (uint32_t)row >= behind) return;
-    const float by = per_sum(total);
+    const float by = per_sum(total) * (a.mx && a.rows == 16 ? kRowsPartScale : 1.0f);
     if (l == 0 && a.lse) a.lse[row] = log_of_sum(m, total);
     for (int d = l * 8; d < D; d += 128) {
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
