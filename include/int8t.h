@@ -644,7 +644,7 @@ int8t_status int8t_cache_read(const int8t_cache *cache, const int64_t *slots_dev
  *   ws_dev       int8t_cache_attend_workspace_bytes(cache, desc) bytes, 16-byte aligned; may be NULL where that is 0
  * Products run on fp16 with sums in fp32: codes are exact, each q is scaled by a power of two, and p_j times the value scale is rounded to 11 bits for bf16
  * and fp16 tensors (one fp16) and 22 bits for fp32 ones (two pieces, as q's), with steps of 2^-38 of the row's largest at least: of its own, keys that a row does
- * not see do not matter.  (Value scales below 2^-95 lose bits.)
+ * not see do not matter.  (Value scales below 2^-95 and above 2^103 lose bits.)
  */
 typedef struct int8t_attend_desc {
     int tokens, requests, group, table_width, longest;
@@ -733,10 +733,11 @@ int8t_status int8t_mx4_linear_bwd(const int8t_linear_desc *desc, const int8t_mx4
 /*
  * A paged cache of keys and values in these codes, blocks along a head's dims: places, slots and limits as int8t_cache.  dim: a multiple of 16, at most 256.
  * int8t_mx4_cache_write, _read, _attend: as int8t_cache_write, _read, _attend with k, v what codes and scales stand for.
- * attend: blocks with the byte 0 (below 2^-124) count as zeros;  q . k_j exact products in fp32 sums (blocks of 16 rows; larger ones as the 8-bit cache's, with fp16 codes relative to the largest scale of a key's row:
- * blocks 2^36 below it lose bits, but keys of bf16 tensors, whose products stay exact); p_j is rounded to 16 bits for bf16 and fp16 tensors and 24 for fp32 ones (larger blocks: 11 and 22),
- * and held down to 2^-126 of the row's largest (blocks of 16 rows; value scales beyond 2^96 shorten that by up to as much).  A key or value with a block
- * of scale 255 (values, in blocks of 16 rows: 253 and more, whose products pass fp32) makes the rows that see it NaN, all of their dims, and no others.
+ * attend: blocks with the byte 0 (below 2^-124) may count as zeros;  q . k_j exact products in fp32 sums (blocks of 16 rows; larger ones as the 8-bit cache's, with fp16 codes
+ * relative to the largest scale of a key's row: blocks 2^36 below it lose bits, but keys of bf16 tensors, whose products stay exact); p_j is rounded to 16 bits for bf16 and fp16
+ * tensors and 24 for fp32 ones, and held down to 2^-126 of the row's largest (value scales beyond 2^96 shorten that by up to as much); in larger blocks to 11 and 22, with
+ * steps as the 8-bit cache's (value scales below 2^-82 and above 2^116 lose bits).  A key or value with a block of scale 255 (values, in blocks of 16 rows: 253 and more, whose products pass
+ * fp32) makes the rows that see it, with a p_j above zero in fp32, NaN, all of their dims, and no others.
  */
 typedef struct int8t_mx4_cache {
     uint8_t *kq, *vq;              /* [pages][heads][page_size][16 * blocks], blocks = dim / 32 rounded up */

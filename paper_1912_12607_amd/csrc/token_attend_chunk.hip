@@ -36,7 +36,7 @@ constexpr int value_tiles(int DIM, int NW) { return takes_turns(NW) ? 4 : DIM ==
 constexpr int chunk_lds(int DIM, int NW) { return (key_tiles(NW) + value_tiles(DIM, NW)) * TK * DIM * 2 + 3 * 3 * TK * 4; }
 
 // MX: keys and values are microscaled 4-bit codes (mx4.h).  A block's codes become fp16 times a power of two relative to its row's largest scale, which is then
-// the row's: what is above stays as it is.  Blocks 2^36 below the row's largest lose bits, 2^39 below they are zeros.  Two chunks of 2048 tokens over 8192 keys, 32 heads on 8 of
+// the row's: what is above stays as it is.  Blocks 2^36 below the row's largest lose bits, 2^41 below they are zeros.  Two chunks of 2048 tokens over 8192 keys, 32 heads on 8 of
 // 128, bf16: 578 us, 0.83 PFLOP/s; vector instructions are issued in 50 % of the cycles and products run in 33 %, hardly at once, and waves wait in 40 % of their time.
 template <bool MX> struct Piece { typedef uint4 codes; typedef float scale; };
 template <> struct Piece<true> { typedef uint2 codes; typedef uint32_t scale; };
@@ -192,8 +192,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
     auto expand = [](const auto& c, const auto& scale, uint4* lo, uint4* hi, float* row) __attribute__((always_inline)) {
         if constexpr (MX) {
             const uint32_t top = lanes_max<DIM>(scale);
-            const float up = __uint_as_float((uint32_t)max(127 + kMxUp - (int)(top - scale), 0) << 23);
-            *row = top == 255u ? NAN : __uint_as_float((uint32_t)max((int)top - kMxUp, 0) << 23);
+            const int base = max((int)top - kMxUp, 1);       // (the row's factor is not below 2^-126: small rows keep their bits in smaller codes)
+            const float up = __uint_as_float((uint32_t)max(127 + (int)scale - base, 0) << 23);
+            *row = top == 255u ? NAN : __uint_as_float((uint32_t)base << 23);
             const auto pair = [up](uint32_t w, auto sel) __attribute__((always_inline)) { return as_u32(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, up, decltype(sel)::value)); };
             typedef std::integral_constant<int, 0> B0; typedef std::integral_constant<int, 1> B1; typedef std::integral_constant<int, 2> B2; typedef std::integral_constant<int, 3> B3;
             *lo = make_uint4(pair(c.x, B0()), pair(c.x, B1()), pair(c.x, B2()), pair(c.x, B3()));

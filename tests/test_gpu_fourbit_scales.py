@@ -30,7 +30,7 @@ def rescale(scales, low, high, seed, blocks=False):
 
 
 def check(cache, q, starts, lengths, table, rows, floor):
-    """check_attend()'s bound with another floor."""
+    """check_attend()'s bound with another floor, which may go by the largest score."""
     dtype, width = q.dtype, max(len(t) for t in table)
     assert division(cache, q, len(lengths), width, True).rows == rows
     want, absolute, _, size = attend_reference(cache, q, starts, lengths, table, True, cache.dim ** -0.5)
@@ -40,7 +40,7 @@ def check(cache, q, starts, lengths, table, rows, floor):
     got = cache.attend(q, *(torch.tensor(v, dtype=torch.int32, device=DEV) for v in (starts, lengths)), t.to(DEV)).cpu().double()
     e_p = {F32: 2.0**-23, BF16: 2.0**-16}[dtype] if rows == 16 else {F32: 2.0**-20, BF16: 2.0**-11}[dtype]
     ds, e_sum = 2.0**-17 * size + 2.0**-20, (max(lengths) / 32 + 40) * 2.0**-23
-    bound = (2 * ds[..., None] + e_p + e_sum) * absolute + {F32: 2.0**-24, BF16: 2.0**-8}[dtype] * 1.01 * want.abs() + floor
+    bound = (2 * ds[..., None] + e_p + e_sum) * absolute + {F32: 2.0**-24, BF16: 2.0**-8}[dtype] * 1.01 * want.abs() + (floor(float(size.max())) if callable(floor) else floor)
     assert bool(((got - want).abs() <= bound).all()), ((got - want).abs() / bound).max()
     return got
 
@@ -106,3 +106,39 @@ def test_small_values(dtype, low, high, heads, group, dim, page, new, lengths):
     cache, table = make_cache(lengths, heads, dim, page)
     rescale(cache.vs, low, high, 3)
     check(cache, queries(sum(new), heads * group, dim, dtype), starts_of(new), lengths, table, 16, max(lengths) * 2.0**-125)
+
+
+# Larger blocks: 128 rows, 256, and keys in shares
+LARGER = [(16, 8, 64, 16, [170, 0, 129, 3], [300, 9, 140, 64], 128), (40, 4, 128, 16, [300, 77, 1, 130], [500, 77, 40, 131], 256), (4, 8, 64, 24, [256], [8200], 128)]
+
+
+@pytest.mark.parametrize("heads,group,dim,page,new,lengths,rows,dtype", [c + (t,) for c in LARGER for t in (F32, BF16) if t is BF16 or c[2] == 64])
+@pytest.mark.parametrize("low,high,blocks", [(252, 252, False), (232, 252, True)])
+def test_large_values_in_larger_blocks(dtype, low, high, blocks, heads, group, dim, page, new, lengths, rows):
+    """A row's largest weight, p times its row's factor of 2^(byte - 140) at most, is 2^14 at least, so that l is at least 2^(154 - byte); p below 2^-126 is zero, off by as much of a value for
+    each of the keys.  Steps of the weights as in check_attend()."""
+    cache, table = make_cache(lengths, heads, dim, page)
+    rescale(cache.vs, low, high, 3, blocks)
+    most, value = int(cache.vs[cache.vs < 253].max()), 6 * 2.0 ** (high - 127)
+    floor = max(lengths) * value * (2.0**-38 + 2.0 ** (-126 - (154 - most)))
+    assert torch.isfinite(check(cache, queries(sum(new), heads * group, dim, dtype), starts_of(new), lengths, table, rows, floor)).all()
+
+
+@pytest.mark.parametrize("heads,group,dim,page,new,lengths,rows", [c for c in LARGER if c[2] == 64])
+@pytest.mark.parametrize("low,high", [(1, 13), (1, 40)])
+def test_small_keys_in_larger_blocks(low, high, heads, group, dim, page, new, lengths, rows):
+    cache, table = make_cache(lengths, heads, dim, page)
+    rescale(cache.ks, low, high, 3)
+    check_attend(cache, queries(sum(new), heads * group, dim, F32) * 2.0 ** (125 - high), starts_of(new), lengths, table, rows=rows)
+
+
+@pytest.mark.parametrize("heads,group,dim,page,new,lengths,rows,dtype", [c + (t,) for c in LARGER for t in (F32, BF16) if t is BF16 or c[2] == 64])
+@pytest.mark.parametrize("low,high,blocks", [(1, 13, False), (0, 16, True), (13, 30, False)])
+def test_small_values_in_larger_blocks(dtype, low, high, blocks, heads, group, dim, page, new, lengths, rows):
+    """Positive values, and scores near each other.  p reaches 2^109 at least, so that l is at least n 2^109 e^(-2 largest score); weights p vs are rounded to steps of 2^-24, by 2^-25 at most
+    each, and multiply codes of 6 2^13 at most:  n 2^-25 6 2^13 / l.  Results below the least normal number as in check()."""
+    cache, table = make_cache(lengths, heads, dim, page)
+    rescale(cache.vs, low, high, 3, blocks)
+    cache.vq.bitwise_and_(0x77)
+    q = queries(sum(new), heads * group, dim, dtype, size=0.02)
+    check(cache, q, starts_of(new), lengths, table, rows, lambda score: 2.0**-25 * 6 * 2.0**13 * 2.0**-109 * math.exp(2 * score) + 2.0**-125)
