@@ -76,25 +76,19 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
     const int n32 = lane & 31, half = lane >> 5;
     // Heads first, so that an XCD has as few heads' keys in its L2 as can be, and each request's last rows, which see the most keys, before its others, so that
     // the chip runs out of short blocks (tiles first, in order: 9 % more time for two chunks of 2048 tokens over 8192 keys).
-    const bool close = MX && a.close;
+    const bool close = MX && a.close;                          // (4 bits: blocks that have rows come first where requests are few)
     const int place = (int)((close ? blockIdx.z * gridDim.y * gridDim.x : 0u) + blockIdx.y * gridDim.x + blockIdx.x), group_of = div_by(place, a.by_heads);
     const int head = place - group_of * a.c.heads, block = (int)gridDim.x - 1 - group_of;
     const int D = a.c.dim;
 
-    Unit job;
-    if (close) {
-        if (!unit_of(a, group_of, ROWS, false, lane, &job)) return;
-    } else {
-        const int b = tile_request(a, block, ROWS);
-        job.rq = request_of(a, b);
-        job.tile = (int)((long long)block - ((long long)a.starts[b] * a.group / ROWS + b));
-        job.share = (int)blockIdx.z;
-    }
-    const int split = job.share;
-    const Request& rq = job.rq;
+    Unit job{};
+    if (close && !unit_of(a, group_of, ROWS, false, lane, &job)) return;
+    const int split = close ? job.share : (int)blockIdx.z;
+    const int b = close ? 0 : tile_request(a, block, ROWS);
+    const Request rq = close ? job.rq : request_of(a, b);
     const int nrows = rq.tokens * a.group;
-    const int tile = job.tile;
-    if (tile < 0 || (long long)tile * ROWS >= nrows) return;
+    const long long tile = close ? job.tile : (long long)block - ((long long)a.starts[b] * a.group / ROWS + b);
+    if (tile < 0 || tile * ROWS >= nrows) return;
     const int r0 = (int)tile * ROWS;
     const int row = r0 + 32 * wave + n32;
     const bool have = row < nrows;
@@ -188,25 +182,24 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
             }
         }
     };
-    // 16 codes as fp16; `row`: the row's scale
-    auto expand = [](const auto& c, const auto& scale, uint4* lo, uint4* hi, float* row) __attribute__((always_inline)) {
+    // 16 codes as fp16; 4 bits: their block's scale becomes the row's factor (in place: handed out through a pointer of its own, the 8-bit form spilled)
+    auto expand = [](const auto& c, auto& scale, uint4* lo, uint4* hi) __attribute__((always_inline)) {
         if constexpr (MX) {
             const uint32_t top = lanes_max<DIM>(scale);
             const int base = max((int)top - kMxUp, 1);       // (the row's factor is not below 2^-126: small rows keep their bits in smaller codes)
             const float up = __uint_as_float((uint32_t)max(127 + (int)scale - base, 0) << 23);
-            *row = top == 255u ? NAN : __uint_as_float((uint32_t)base << 23);
+            scale = top == 255u ? 0x7fc00000u : (uint32_t)base << 23;
             const auto pair = [up](uint32_t w, auto sel) __attribute__((always_inline)) { return as_u32(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, up, decltype(sel)::value)); };
             typedef std::integral_constant<int, 0> B0; typedef std::integral_constant<int, 1> B1; typedef std::integral_constant<int, 2> B2; typedef std::integral_constant<int, 3> B3;
             *lo = make_uint4(pair(c.x, B0()), pair(c.x, B1()), pair(c.x, B2()), pair(c.x, B3()));
             *hi = make_uint4(pair(c.y, B0()), pair(c.y, B1()), pair(c.y, B2()), pair(c.y, B3()));
         } else {
-            *row = scale;
             const uint32_t w[4] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u, c.z ^ 0x80808080u, c.w ^ 0x80808080u};
             *lo = make_uint4(codes_f16<kLowPair>(w[0]), codes_f16<kHighPair>(w[0]), codes_f16<kLowPair>(w[1]), codes_f16<kHighPair>(w[1]));
             *hi = make_uint4(codes_f16<kLowPair>(w[2]), codes_f16<kHighPair>(w[2]), codes_f16<kLowPair>(w[3]), codes_f16<kHighPair>(w[3]));
         }
     };
-    auto expand_key = [&](const auto& c, const auto& scale, uint4* lo, uint4* hi, float* row) __attribute__((always_inline)) {
+    auto expand_key = [&](const auto& c, auto& scale, uint4* lo, uint4* hi) __attribute__((always_inline)) {
         if constexpr (WHOLE) {
             const float up = mx_power(scale);
             const auto pair = [up](uint32_t w, auto sel) __attribute__((always_inline)) {
@@ -215,27 +208,26 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && (DIM == 256 || (DIM == 128 && T
             typedef std::integral_constant<int, 0> B0; typedef std::integral_constant<int, 1> B1; typedef std::integral_constant<int, 2> B2; typedef std::integral_constant<int, 3> B3;
             *lo = make_uint4(pair(c.x, B0()), pair(c.x, B1()), pair(c.x, B2()), pair(c.x, B3()));
             *hi = make_uint4(pair(c.y, B0()), pair(c.y, B1()), pair(c.y, B2()), pair(c.y, B3()));
-            *row = 1.0f;
         } else {
-            expand(c, scale, lo, hi, row);
+            expand(c, scale, lo, hi);
         }
     };
+    const auto as_scale = [](auto s) __attribute__((always_inline)) { return __builtin_bit_cast(float, s); };
     auto stage = [&](int kslot, int vslot, int sslot) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int key = key_of(p), g = d16 >> 3;
             uint4 lo, hi;
             float* const s = sc + sslot * 3 * TK;
-            float ks, vs;
-            expand_key(rk[p], rks[p], &lo, &hi, &ks);
+            expand_key(rk[p], rks[p], &lo, &hi);
             sk[kslot * TILE + k_slot<DIM>(key, g)] = lo;
             sk[kslot * TILE + k_slot<DIM>(key, g + 1)] = hi;
-            expand(rv[p], rvs[p], &lo, &hi, &vs);
+            expand(rv[p], rvs[p], &lo, &hi);
             sv[vslot * TILE + v_slot<DIM>(key, g)] = lo;
             sv[vslot * TILE + v_slot<DIM>(key, g + 1)] = hi;
             if (g == 0) {
-                if (!WHOLE) s[key] = rok[p] ? ks : 0.0f;
-                s[TK + key] = rok[p] ? vs : 0.0f;
+                if (!WHOLE) s[key] = rok[p] ? as_scale(rks[p]) : 0.0f;
+                s[TK + key] = rok[p] ? as_scale(rvs[p]) : 0.0f;
                 s[2 * TK + key] = rok[p] ? 0.0f : kNone;
             }
         }
