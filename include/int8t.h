@@ -682,7 +682,8 @@ int8t_status int8t_cache_attend_division(const int8t_cache *cache, const int8t_a
 
 /*
  * Codes of rows x cols values with blocks along the columns (q, s) and, transposed, of cols x rows with blocks along the rows (qt, st), of one matrix.
- *   x_dev         rows x cols elements of `type`, rows `pitch` apart;  rows, cols at most INT8T_MAX_REDUCTION where they are the blocks' axis
+ *   x_dev         rows x cols elements of `type`, rows `pitch` apart;  rows, cols at most INT8T_MAX_REDUCTION where they are the blocks' axis (the 8-bit
+ *                 operators' bound, kept for sizes to be alike: sums here are in fp32 and set none)
  *   q_dev, s_dev  NULL, or out: codes and scales of rows x cols;   draws of `seed`
  *   qt_dev, st_dev   NULL, or out: codes and scales of cols x rows;   draws of `seed` with its highest bit flipped, of the same index
  *   sum_dev       NULL, or out: cols floats, the columns' sums

@@ -139,7 +139,7 @@ __device__ __forceinline__ float rows16_sum(float x) { const Pair p = rows16(x);
 // of 2^-38 below; a larger weight lowers c.  It goes by the row's own weights: by the tile's largest scale and score, a key that the row does not see, or
 // sees at 2^-40, would take the bits of the others.
 // bf16 and fp16 tensors have a weight in one piece, off by 2^-12 of itself at most and to either side: errors against 64 bits are 1.6e-3 to 1.7e-3 of bf16 results, as
-// with weights in fp32, and 2.8e-4 of fp16 ones, where those have 2.1e-4.  A second piece costs a chunk 60 % more time (two of 2048 tokens over 8192 keys 610 -> 994 us,
+// with weights in fp32, and 2.8e-4 to 2.9e-4 of fp16 ones (over 8-bit caches and over 4-bit ones), where those have 2.1e-4.  A second piece costs a chunk 60 % more time (two of 2048 tokens over 8192 keys 610 -> 994 us,
 // dim 64 477 -> 570, dim 256 583 -> 659), single tokens 1 to 6 %.
 struct RowUnit {
     static constexpr float kMostWeight = 63000.0f, kMostSum = 0x1p120f;     // (p alone stays in range where the scales are tiny or zero)

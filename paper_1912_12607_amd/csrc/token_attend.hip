@@ -508,14 +508,23 @@ void attend_plan(AttendArgs* a, int longest) {
     //   dim  96 bf16                                   13/27           65/48            40/45          45/22            46/45               53/36             45/51            141/101
     //   dim 128 bf16                                   11/28           57/49            34/48          38/24            38/47               45/39             38/53            124/105
     //   dim 128 fp16                                   11/30           60/51            36/50          41/25            41/49               48/41             41/55            130/111;
-    // over 80 calls, drawn and these, the choice and its shares take some 3.5 % more than the fastest of some 25 divisions of each).
+    // over 80 calls, drawn and these, the choice and its shares take some 3.5 % more than the fastest of some 25 divisions of each).  For other dims and types there is no larger form; with
+    // the 8-bit cache's blocks of 128 rows over these codes in its place (random codes; the last two calls 2048 tokens of 2 requests, group 4, over 8192 keys, 4 heads and 8):
+    //   dim  96 fp32                                   18/30           82/91            53/58          68/44            60/72               77/70             50/72            135/184    860/771   1704/1510
+    //   dim 128 fp32                                   15/30           67/94            42/62          50/47            48/77               59/73             43/75            110/187    671/772   1334/1519
+    //   dim 224 fp16                                   23/41          117/123           74/81          89/60            83/99              107/96             70/99            193/247   1237/1023  2466/2015
+    //   dim 256 bf16                                   18/37           90/113           56/76          70/56            63/93               82/87             52/91            146/220    934/896   1866/1766
+    //   dim 256 fp32                                   28/66          119/207           79/128        105/104           87/164             112/169            74/161           193/431   1242/1845  2490/3620.
     if (a->mx) {
         const int tall = dim == 128 ? 256 : 128;
         const long long filled = (each + tall - 1) / tall, blocks = filled * a->requests * a->c.heads, units = dim == 128 ? 160 : 320;
         const long long shares = chunk_shares(tall, blocks, longest);
         const bool larger = (dim == 64 || (dim == 128 && !fp32)) && each >= 128 && 2 * each >= filled * tall && (blocks >= units || (blocks * shares >= units && longest / shares >= 1000));
         a->rows = larger ? tall : 16;
-        a->close = a->requests <= 512;           // (more of them take a block longer to look through than its neighbours wait)
+        // More requests take a block longer to look through than its neighbours wait (us in that order / in the grid's, bf16, group 4, dim 128, a token each unless said: 300 of 8
+        // heads over 1 to 2000 keys 85/82, 513 138/133, 1000 over 1 to 1000 186/151, 2000 over 1 to 500 368/198, 4000 of 2 heads over 100 to 300 251/82; 600 of 4 tokens and 8 heads
+        // over 100 to 600 98/127, of 32 tokens and 4 heads 282/282, of 64, dim 64, 147/139; for few it is what fills the chip: 64 over 1 to 8192 75/82).
+        a->close = a->requests <= 512;
     }
     // (4 bits: blocks that have rows, where these are dealt out evenly)
     const long long tiles = a->mx && a->rows == 16 ? (each > 16 ? (each + 15) / 16 : 1) * a->requests * a->c.heads : (rows / a->rows + a->requests) * a->c.heads;

@@ -303,7 +303,7 @@ class PageTable:
         return PageStep(lengths, available, starts, slots, positions, without)
 
     def accept(self, step: PageStep) -> None:
-        """The step's tokens and pages become the requests' (its extend is the last one of this table)."""
+        """The step's tokens and pages become the requests' (no call of this table between its extend and this)."""
         self.lengths.copy_(step.lengths)
         self.available.copy_(step.available)
 
