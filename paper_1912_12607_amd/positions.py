@@ -92,15 +92,20 @@ class Rotary:
                 raise ValueError(f"frequencies of shape {tuple(f.shape)}: {rot // 2}")
         if not math.isfinite(amplitude):
             raise ValueError(f"amplitude {amplitude}")
-        self.rot, self.layout, self.amplitude = int(rot), layout, float(amplitude)
-        self.frequencies = f.clone()
+        self._parameters = int(rot), layout, float(amplitude), f.clone()
         self._turns = {}                     # device -> turns per position
         self._plans = {}                     # shapes and type -> descriptors
+
+    # (not to be replaced: calls keep what they made of them)
+    rot = property(lambda self: self._parameters[0])
+    layout = property(lambda self: self._parameters[1])
+    amplitude = property(lambda self: self._parameters[2])
+    frequencies = property(lambda self: self._parameters[3].clone())
 
     def _on(self, device):
         t = self._turns.get(device)
         if t is None:
-            t = self._turns[device] = (self.frequencies / (2.0 * math.pi)).to(device)
+            t = self._turns[device] = (self._parameters[3] / (2.0 * math.pi)).to(device)
         return t
 
     def to(self, device) -> "Rotary":
