@@ -187,7 +187,7 @@ class _Linear4Fn(torch.autograd.Function):
 
 def linear4(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None, seed: int = 0) -> torch.Tensor:
     """x W^T + b, every product in microscaled 4-bit codes with blocks along its summed axis, differentiable (once): the gradients' codes are rounded
-    stochastically with draws of `seed`.  x (.., in) and weight (out, in) fp32, bf16 or fp16; bias fp32.  A pass that is captured into a CUDA graph takes leaves of which no
+    stochastically with draws of `seed`.  Where no graph records it is the forward pass alone.  x (.., in) and weight (out, in) fp32, bf16 or fp16; bias fp32.  A pass that is captured into a CUDA graph takes leaves of which no
     eager autograd graph lives any more (torch would join the streams of both, and ends the process)."""
     # (what no graph records keeps nothing: a Function's needs_input_grad goes by the leaves alone)
     if not _transformed() and not (torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad))):
